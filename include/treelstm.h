@@ -454,6 +454,91 @@ int tl_td_generate(tl_td_ctx *ctx, int n_trees, int max_nodes, int max_depth, fl
 int tl_td_status(tl_td_ctx *ctx);
 int tl_td_destroy(tl_td_ctx *ctx);
 
+/*
+ * ---- A decoder that writes a sentence from a tree ------------------------------------------------
+ *
+ * tl_forward leaves the state of every node of every tree of a batch in node-major rows.  A decoder that
+ * produces a sentence from a tree reads those rows by cross attention and draws its words.  The
+ * three operators below need no context; they launch on the current HIP device and on hip_stream, allocate
+ * nothing, never synchronise, and may be captured in a HIP graph.  TL_OK, TL_EINVAL (see each argument;
+ * nothing is enqueued), TL_EHIP.
+ */
+enum tl_dtype { TL_DT_F32 = 0, TL_DT_BF16 = 1, TL_DT_F16 = 2 };
+
+/* Rows x heads x head_dim elements: element (r, j, d) lies at p + r * row + j * head + d (strides in elements, >= 0; p aligned to
+ * its element).  Inputs may repeat rows or heads (stride 0); an output's rows and heads must not overlap.  Where head_dim and the
+ * strides are multiples of 16 bytes and p is aligned to 16 bytes, rows are read in pieces of 16 bytes, else element by element. */
+typedef struct {
+    void *p;
+    int64_t row, head;
+} tl_rows;
+
+/*
+ * Cross attention of each tree's queries (the words of its sentence, [n_q] rows over the batch) to its nodes ([n_kv] rows):
+ *     s_ij = scale * q_i . k_j     over the nodes j of i's tree with kv_mask[j] != 0
+ *     o_i  = sum_j softmax_j(s_ij) v_j,    lse_i = log sum_j exp(s_ij)
+ * for every one of n_heads heads; query head g reads head g / (n_heads / n_kv_heads) of k and v.  A query whose tree has no node that
+ * may be read (or only scores of -infinity) gets o_i = 0 and lse_i = -infinity, and its gradients are zero.  What masked rows
+ * of k and v hold, NaN and infinities included, has no effect on any result.
+ */
+typedef struct {
+    int dtype;               /* enum tl_dtype: of q, k, v, o and their gradients.  Sums, maxima and lse are fp32; with TL_DT_F32 so are all
+                                operands, with the 16-bit types probabilities and score gradients are rounded to the type as
+                                operands of their second products.                                                       */
+    int n_trees, n_q, n_kv;  /* >= 0                                                                                       */
+    int n_heads, n_kv_heads; /* >= 1, n_heads a multiple of n_kv_heads, n_heads <= 4096                                    */
+    int head_dim;            /* 1 .. 256                                                                                   */
+    float scale;             /* finite, > 0                                                                                */
+    const int32_t *q_off;    /* [n_trees+1], from 0 to n_q, ascending (equal ones: a tree without queries)       DEVICE     */
+    const int32_t *kv_off;   /* [n_trees+1], from 0 to n_kv: tree_off of the forward                             DEVICE
+                                Offsets outside these bounds: results are unspecified, nothing outside the arrays is accessed.  */
+    const uint8_t *kv_mask;  /* [n_kv], 0: not read.  NULL: every node is read                                   DEVICE     */
+    tl_rows q, k, v;         /* [n_q, n_heads], [n_kv, n_kv_heads] twice                                         DEVICE     */
+} tl_attention;
+
+/* Bytes of DEVICE memory that tl_attend (backward == 0) or tl_attend_backward needs as workspace; depends on the counts
+ * alone, 0 where none is needed. */
+int tl_attend_workspace(const tl_attention *a, int backward, int64_t *bytes);
+
+/*
+ *   o    [n_q, n_heads] out                                              DEVICE
+ *   lse  [n_q x n_heads] fp32 out, may be NULL (tl_attend_backward needs it)   DEVICE
+ *   workspace  of at least the bytes that tl_attend_workspace names, 16-byte aligned; free once the stream has passed the call;
+ *              TL_ELIMIT if it is smaller
+ * Few queries per tree (a decoder's next token) take their own form: the nodes of a tree are divided among waves and, where
+ * rows are few, among workgroups whose results a second launch joins.  Results repeat bit for bit.
+ */
+int tl_attend(const tl_attention *a, const tl_rows *o, float *lse, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * Gradients of tl_attend: d_q, d_k, d_v from d_o = dL/do; o and lse are what tl_attend wrote for the same arguments.  Gradients
+ * of heads that share k and v are summed; rows of masked nodes and of trees without queries are zero.  No atomics: results repeat
+ * bit for bit.
+ */
+int tl_attend_backward(const tl_attention *a, const tl_rows *o, const float *lse, const tl_rows *d_o, const tl_rows *d_q,
+                       const tl_rows *d_k, const tl_rows *d_v, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * Draws one word per row of logits.  With x the row (a NaN counts as -infinity), m its largest value and T its temperature,
+ * w_j = exp((x_j - m) / T); words are ordered by x, descending, equal ones by index.
+ *     top_k   keeps the first top_k words (off where < 1 or >= vocab)
+ *     top_p   keeps, of these, every word whose mass in front of it is below top_p times the total of these; the first one always
+ *             (off where not < 1)
+ *     min_p   keeps, of these, every word with w_j >= min_p
+ *     token   the lowest kept j with sum of w over kept words up to j > u * (sum over all kept words)
+ *     logprob log of that word's share of the kept words' weights;   kept: how many words were kept
+ * T not above 0 (or NaN): the first word with the largest logit, logprob 0, kept 1.  A row without a value above -infinity: token -1,
+ * logprob -infinity, kept 0; words at -infinity are never drawn or kept.  +infinity: the words that have it share the draw.
+ * Weights are computed in 64 bits and summed as integers (multiples of 2^-52, from 1024 words on of 2^-(62 - log2 vocab)), so a result
+ * depends on no order of additions; a word lighter than that is kept but not drawn.
+ *   logits [n_rows x vocab] of dtype, `row` elements from one row to the next; 1 <= vocab <= 2^30           DEVICE, read-only
+ *   u [n_rows] in [0, 1); temperature, top_p, min_p [n_rows] fp32, top_k [n_rows] int32: NULL turns one off (T = 1)    DEVICE
+ *   token [n_rows] int32 out; logprob [n_rows] fp32, kept [n_rows] int32 out, may be NULL                    DEVICE
+ */
+int tl_sample(int dtype, int n_rows, int vocab, const void *logits, int64_t row, const float *u, const float *temperature,
+              const int32_t *top_k, const float *top_p, const float *min_p, int32_t *token, float *logprob, int32_t *kept,
+              void *hip_stream);
+
 const char *tl_strerror(int code);
 
 /* Frees the context and everything it owns.  Waits for the device. */

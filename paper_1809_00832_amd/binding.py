@@ -19,11 +19,13 @@ TL_SCHED_READY, TL_SCHED_LEVEL_DEVICE, TL_SCHED_LEVEL_HOST, TL_SCHED_READY_PRIOR
 TL_OK, TL_EINVAL, TL_ENOMEM, TL_EHIP, TL_ESTRUCT, TL_ESTALL, TL_ELIMIT = 0, -1, -2, -3, -4, -5, -6
 TL_NOALLOC_MAX_NODES = 16384
 TL_N_STAGES, TL_PROFILE_RING = 5, 128
+TL_DT_F32, TL_DT_BF16, TL_DT_F16 = 0, 1, 2
 SCHEDULERS = {"ready": TL_SCHED_READY, "level_device": TL_SCHED_LEVEL_DEVICE, "level_host": TL_SCHED_LEVEL_HOST,
               "ready_priority": TL_SCHED_READY_PRIORITY, "dataflow": TL_SCHED_DATAFLOW}
 
 EXPORTS = ("tl_create", "tl_forward", "tl_forward_noalloc", "tl_status", "tl_set_profiling", "tl_stage_ms", "tl_last_stats", "tl_backward",
-           "tl_set_keep_gates", "tl_set_async_backward", "tl_sgd_update", "tl_get_params", "tl_classify", "tl_classify_backward", "tl_td_create", "tl_td_generate", "tl_td_status", "tl_td_destroy", "tl_strerror", "tl_destroy")
+           "tl_set_keep_gates", "tl_set_async_backward", "tl_sgd_update", "tl_get_params", "tl_classify", "tl_classify_backward", "tl_td_create", "tl_td_generate", "tl_td_status", "tl_td_destroy", "tl_strerror", "tl_destroy",
+           "tl_attend", "tl_attend_backward", "tl_attend_workspace", "tl_sample")
 
 
 class tl_config(ctypes.Structure):
@@ -32,6 +34,17 @@ class tl_config(ctypes.Structure):
                 ("hidden", ctypes.c_int), ("spin_limit", ctypes.c_int),
                 ("emb", ctypes.c_void_p), ("w_leaf", ctypes.c_void_p), ("b_leaf", ctypes.c_void_p),
                 ("u", ctypes.c_void_p), ("b", ctypes.c_void_p), ("v", ctypes.c_void_p)]
+
+
+class tl_rows(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("row", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class tl_attention(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("n_trees", ctypes.c_int), ("n_q", ctypes.c_int), ("n_kv", ctypes.c_int),
+                ("n_heads", ctypes.c_int), ("n_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int), ("scale", ctypes.c_float),
+                ("q_off", ctypes.c_void_p), ("kv_off", ctypes.c_void_p), ("kv_mask", ctypes.c_void_p),
+                ("q", tl_rows), ("k", tl_rows), ("v", tl_rows)]
 
 
 _lib = None
@@ -84,6 +97,15 @@ def lib():
         L.tl_classify_backward.restype = ci
         L.tl_classify_backward.argtypes = [vp, ci, vp, vp, vp, ci] + [vp] * 7
         L.tl_strerror.argtypes = [ci]
+        attn, rows, i64 = ctypes.POINTER(tl_attention), ctypes.POINTER(tl_rows), ctypes.c_int64
+        L.tl_attend_workspace.restype = ci
+        L.tl_attend_workspace.argtypes = [attn, ci, ctypes.POINTER(i64)]
+        L.tl_attend.restype = ci
+        L.tl_attend.argtypes = [attn, rows, vp, vp, i64, vp]
+        L.tl_attend_backward.restype = ci
+        L.tl_attend_backward.argtypes = [attn, rows, vp, rows, rows, rows, rows, vp, i64, vp]
+        L.tl_sample.restype = ci
+        L.tl_sample.argtypes = [ci, ci, ci, vp, i64] + [vp] * 9
         L.tl_destroy.restype = ci
         L.tl_destroy.argtypes = [vp]
         _lib = L
@@ -300,6 +322,99 @@ def tl_td_status(ctx) -> int:
 
 def tl_td_destroy(ctx) -> None:
     _check(lib().tl_td_destroy(ctx), "tl_td_destroy")
+
+
+def _dtype(t) -> int:
+    import torch
+    code = {torch.float32: TL_DT_F32, torch.bfloat16: TL_DT_BF16, torch.float16: TL_DT_F16}.get(t.dtype)
+    assert code is not None, "float32, bfloat16 or float16"
+    return code
+
+
+def _rows(t) -> tl_rows:
+    return tl_rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _attention(q, k, v, q_off, kv_off, kv_mask, scale) -> tl_attention:
+    import torch
+    n_q, n_heads, d = q.shape
+    n_kv, n_kv_heads, _ = k.shape
+    assert q.is_cuda and k.is_cuda and v.is_cuda and k.dtype == q.dtype and v.dtype == q.dtype
+    assert k.shape == v.shape and k.shape[2] == d
+    assert d == 1 or (q.stride(2) == 1 and k.stride(2) == 1 and v.stride(2) == 1), "head_dim must be contiguous"
+    for t in (q_off, kv_off):
+        assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous()
+    assert q_off.numel() == kv_off.numel() >= 1
+    if kv_mask is not None:
+        assert kv_mask.is_cuda and kv_mask.dtype in (torch.uint8, torch.bool) and kv_mask.is_contiguous() and kv_mask.numel() == n_kv
+    return tl_attention(_dtype(q), q_off.numel() - 1, n_q, n_kv, n_heads, n_kv_heads, d, d ** -0.5 if scale is None else scale,
+                        q_off.data_ptr(), kv_off.data_ptr(), _ptr(kv_mask), _rows(q), _rows(k), _rows(v))
+
+
+def _attend_workspace(a, backward, device):
+    import torch
+    size = ctypes.c_int64()
+    _check(lib().tl_attend_workspace(ctypes.byref(a), backward, ctypes.byref(size)), "tl_attend_workspace")
+    return torch.empty(size.value, dtype=torch.uint8, device=device) if size.value else None
+
+
+def tl_attend(q, k, v, q_off, kv_off, kv_mask=None, scale=None, o=None, with_lse=False, stream=None):
+    """Cross attention of every tree's queries to its nodes.  q [n_q, heads, D], k and v [n_kv, kv_heads, D]: CUDA tensors of one type
+    (float32, bfloat16, float16) with any strides of rows and heads; q_off, kv_off [n_trees + 1] int32; kv_mask [n_kv] uint8 or bool,
+    0 for nodes that are not read; scale: 1 / sqrt(D) if None.  Returns o, or (o, lse [n_q, heads] float32)."""
+    import torch
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return tl_attend(q, k, v, q_off, kv_off, kv_mask, scale, o, with_lse)
+    a = _attention(q, k, v, q_off, kv_off, kv_mask, scale)
+    if o is None:
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    assert o.is_cuda and o.shape == q.shape and o.dtype == q.dtype and (o.shape[2] == 1 or o.stride(2) == 1)
+    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if with_lse else None
+    ws = _attend_workspace(a, 0, q.device)
+    _check(lib().tl_attend(ctypes.byref(a), ctypes.byref(_rows(o)), _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(),
+                           torch.cuda.current_stream().cuda_stream), "tl_attend")
+    return (o, lse) if with_lse else o
+
+
+def tl_attend_backward(q, k, v, o, lse, d_o, q_off, kv_off, kv_mask=None, scale=None, stream=None):
+    """Gradients of tl_attend for its arguments and what it returned; d_o like o.  Returns dict(d_q, d_k, d_v) of new tensors."""
+    import torch
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return tl_attend_backward(q, k, v, o, lse, d_o, q_off, kv_off, kv_mask, scale)
+    a = _attention(q, k, v, q_off, kv_off, kv_mask, scale)
+    for t in (o, d_o):
+        assert t.is_cuda and t.shape == q.shape and t.dtype == q.dtype and (t.shape[2] == 1 or t.stride(2) == 1)
+    assert lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:2]
+    out = {"d_q": torch.empty(q.shape, dtype=q.dtype, device=q.device), "d_k": torch.empty(k.shape, dtype=q.dtype, device=q.device),
+           "d_v": torch.empty(k.shape, dtype=q.dtype, device=q.device)}
+    ws = _attend_workspace(a, 1, q.device)
+    ref = ctypes.byref
+    _check(lib().tl_attend_backward(ref(a), ref(_rows(o)), lse.data_ptr(), ref(_rows(d_o)), ref(_rows(out["d_q"])), ref(_rows(out["d_k"])),
+                                    ref(_rows(out["d_v"])), _ptr(ws), 0 if ws is None else ws.numel(),
+                                    torch.cuda.current_stream().cuda_stream), "tl_attend_backward")
+    return out
+
+
+def tl_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+    """One word per row of logits [n, vocab] (float32, bfloat16 or float16; rows any stride apart) from the uniform numbers u [n] float32;
+    temperature, top_p, min_p [n] float32 and top_k [n] int32 CUDA tensors, None: off.  Returns dict(token int32, logprob float32,
+    kept int32) of new tensors [n]."""
+    import torch
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return tl_sample(logits, u, temperature, top_k, top_p, min_p)
+    n, vocab = logits.shape
+    assert logits.is_cuda and (vocab == 1 or logits.stride(1) == 1)
+    for t, dt in ((u, torch.float32), (temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32), (min_p, torch.float32)):
+        assert t is None or (t.is_cuda and t.dtype == dt and t.is_contiguous() and t.numel() == n)
+    out = {"token": torch.empty(n, dtype=torch.int32, device=logits.device), "logprob": torch.empty(n, dtype=torch.float32, device=logits.device),
+           "kept": torch.empty(n, dtype=torch.int32, device=logits.device)}
+    _check(lib().tl_sample(_dtype(logits), n, vocab, logits.data_ptr(), logits.stride(0), u.data_ptr(), _ptr(temperature), _ptr(top_k),
+                           _ptr(top_p), _ptr(min_p), out["token"].data_ptr(), out["logprob"].data_ptr(), out["kept"].data_ptr(),
+                           torch.cuda.current_stream().cuda_stream), "tl_sample")
+    return out
 
 
 def tl_strerror(code: int) -> str:

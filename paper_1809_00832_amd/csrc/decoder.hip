@@ -1,0 +1,209 @@
+// C entry points of the decoder's operators: cross attention, its gradients, sampling.
+#include <math.h>
+
+#include "attend_launch.hpp"
+#include "sample.hpp"
+
+using namespace tl;
+
+namespace {
+
+// Compute units of the current device (asked for once per device).
+int compute_units()
+{
+    static int known[64];
+    int dev = 0, n = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0) return 256;
+    if (dev < 64 && __atomic_load_n(&known[dev], __ATOMIC_RELAXED)) return __atomic_load_n(&known[dev], __ATOMIC_RELAXED);
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) return 256;
+    if (dev < 64) __atomic_store_n(&known[dev], n, __ATOMIC_RELAXED);
+    return n;
+}
+
+int element_size(int dtype) { return dtype == TL_DT_F32 ? 4 : 2; }
+
+bool check_rows(const tl_rows &t, int dtype, long long rows, long long heads, int D, bool out)
+{
+    if (rows == 0) return true;
+    if (!t.p || ((uintptr_t)t.p & (element_size(dtype) - 1)) || t.row < 0 || t.head < 0) return false;
+    if (!out) return true;
+    // rows of heads or heads of rows: the smaller stride spans D elements, the larger one everything the smaller one walks
+    const bool by_row = heads == 1 || (rows > 1 && t.row >= t.head);
+    const long long in_n = by_row ? heads : rows, in_s = by_row ? t.head : t.row, out_n = by_row ? rows : heads, out_s = by_row ? t.row : t.head;
+    if (in_n > 1 && in_s < D) return false;
+    return out_n <= 1 || out_s >= (in_n > 1 ? (in_n - 1) * in_s : 0) + D;
+}
+
+bool in_pieces(const tl_rows &t, int dtype, int D, int bytes)
+{
+    const int n = bytes / element_size(dtype);
+    return D % n == 0 && t.row % n == 0 && t.head % n == 0 && ((uintptr_t)t.p & (bytes - 1)) == 0;
+}
+
+bool check(const tl_attention *a)
+{
+    if (!a || a->dtype < TL_DT_F32 || a->dtype > TL_DT_F16) return false;
+    if (a->n_trees < 0 || a->n_q < 0 || a->n_kv < 0 || a->n_heads < 1 || a->n_heads > 4096 || a->n_kv_heads < 1) return false;
+    if (a->n_heads % a->n_kv_heads || a->head_dim < 1 || a->head_dim > 256) return false;
+    if (!(a->scale > 0.f) || !isfinite(a->scale)) return false;
+    if (a->n_trees == 0) return a->n_q == 0 && a->n_kv == 0;
+    if (!a->q_off || !a->kv_off) return false;
+    return check_rows(a->q, a->dtype, a->n_q, a->n_heads, a->head_dim, false) && check_rows(a->k, a->dtype, a->n_kv, a->n_kv_heads, a->head_dim, false) &&
+           check_rows(a->v, a->dtype, a->n_kv, a->n_kv_heads, a->head_dim, false);
+}
+
+// Which form a forward takes.  Up to 64 packed rows per tree on average: one tile of 32 rows, nodes divided among the waves; and where such
+// tiles do not fill the chip twice, nodes divided among workgroups too, as long as a part keeps two stages.
+AttPlan plan(const tl_attention *a)
+{
+    AttPlan p;
+    const long long rows = (long long)a->n_q * (a->n_heads / a->n_kv_heads);
+    const int dp = att_padded(a->head_dim), size = element_size(a->dtype);
+    p.wm = rows <= 64ll * a->n_trees && dp * size <= 512 ? 1 : 4;
+    p.bm = 32 * p.wm;
+    p.bn = p.wm == 1 ? 128 : dp * size <= 256 ? 64 : 32;
+    p.slots = (int)(rows / p.bm + a->n_trees);
+    p.splits = 1;
+    const long long blocks = (long long)p.slots * a->n_kv_heads, wanted = 2ll * compute_units();
+    const long long stages = a->n_kv / ((long long)p.bn * a->n_trees);
+    if (blocks < wanted && stages >= 4) {
+        const long long s = wanted / blocks < stages / 2 ? wanted / blocks : stages / 2;
+        p.splits = (int)(s < 1 ? 1 : s > 256 ? 256 : s);
+    }
+    return p;
+}
+
+long long round16(long long x) { return (x + 15) & ~15ll; }
+
+long long workspace(const tl_attention *a, const AttPlan &p, int backward)
+{
+    const long long rh = (long long)a->n_q * a->n_heads;
+    if (backward) return round16(rh * 4);
+    return p.splits > 1 ? round16(p.splits * rh * 4) + round16(p.splits * rh * a->head_dim * 4) : 0;
+}
+
+AttArgs arguments(const tl_attention *a)
+{
+    AttArgs x = {};
+    auto t = [](const tl_rows &r) { return AttTensor{r.p, r.row, r.head}; };
+    x.q = t(a->q);
+    x.k = t(a->k);
+    x.v = t(a->v);
+    x.q_off = a->q_off;
+    x.kv_off = a->kv_off;
+    x.mask = a->kv_mask;
+    x.scale = a->scale;
+    x.scale_log2 = a->scale * 1.4426950408889634f;
+    x.n_trees = a->n_trees;
+    x.n_q = a->n_q;
+    x.n_kv = a->n_kv;
+    x.Hq = a->n_heads;
+    x.Hk = a->n_kv_heads;
+    x.G = a->n_heads / a->n_kv_heads;
+    x.D = a->head_dim;
+    x.splits = 1;
+    x.vec = in_pieces(a->q, a->dtype, a->head_dim, 16) && in_pieces(a->k, a->dtype, a->head_dim, 16) && in_pieces(a->v, a->dtype, a->head_dim, 16);
+    return x;
+}
+
+bool pieces_of_4(const tl_rows &t, int dtype, int D) { return in_pieces(t, dtype, D, 4 * element_size(dtype)); }
+
+}  // namespace
+
+extern "C" {
+
+int tl_attend_workspace(const tl_attention *a, int backward, int64_t *bytes)
+{
+    if (!bytes || !check(a)) return TL_EINVAL;
+    *bytes = a->n_trees == 0 ? 0 : workspace(a, plan(a), backward);
+    return TL_OK;
+}
+
+int tl_attend(const tl_attention *a, const tl_rows *o, float *lse, void *workspace_p, int64_t workspace_bytes, void *hip_stream)
+{
+    if (!check(a) || !o || !check_rows(*o, a->dtype, a->n_q, a->n_heads, a->head_dim, true)) return TL_EINVAL;
+    if (a->n_trees == 0 || a->n_q == 0) return TL_OK;
+    const AttPlan p = plan(a);
+    if ((long long)p.slots * p.splits * a->n_kv_heads > INT32_MAX) return TL_EINVAL;
+    const long long need = workspace(a, p, 0);
+    if (need > 0 && (!workspace_p || ((uintptr_t)workspace_p & 15))) return TL_EINVAL;
+    if (need > workspace_bytes) return TL_ELIMIT;
+    AttArgs x = arguments(a);
+    x.o = AttTensor{o->p, o->row, o->head};
+    x.lse = lse;
+    x.vec_out = pieces_of_4(*o, a->dtype, a->head_dim);
+    x.slots = p.slots;
+    x.splits = p.splits;
+    if (p.splits > 1) {
+        x.part_lse = static_cast<float *>(workspace_p);
+        x.part_o = reinterpret_cast<float *>(static_cast<char *>(workspace_p) + round16((long long)p.splits * a->n_q * a->n_heads * 4));
+    }
+    const hipStream_t st = (hipStream_t)hip_stream;
+    const hipError_t e = a->dtype == TL_DT_F32 ? attend_forward<float>(x, p, st) : a->dtype == TL_DT_BF16 ? attend_forward<bf16_t>(x, p, st) : attend_forward<f16_t>(x, p, st);
+    return e == hipSuccess ? TL_OK : TL_EHIP;
+}
+
+int tl_attend_backward(const tl_attention *a, const tl_rows *o, const float *lse, const tl_rows *d_o, const tl_rows *d_q, const tl_rows *d_k,
+                       const tl_rows *d_v, void *workspace_p, int64_t workspace_bytes, void *hip_stream)
+{
+    if (!check(a) || !o || !d_o || !d_q || !d_k || !d_v) return TL_EINVAL;
+    const int dt = a->dtype, D = a->head_dim;
+    if (!check_rows(*o, dt, a->n_q, a->n_heads, D, false) || !check_rows(*d_o, dt, a->n_q, a->n_heads, D, false) ||
+        !check_rows(*d_q, dt, a->n_q, a->n_heads, D, true) || !check_rows(*d_k, dt, a->n_kv, a->n_kv_heads, D, true) ||
+        !check_rows(*d_v, dt, a->n_kv, a->n_kv_heads, D, true))
+        return TL_EINVAL;
+    if (a->n_trees == 0) return TL_OK;
+    const long long need = workspace(a, AttPlan{}, 1);
+    if (a->n_q > 0 && (!lse || !workspace_p || ((uintptr_t)workspace_p & 15))) return TL_EINVAL;
+    if (need > workspace_bytes) return TL_ELIMIT;
+    const long long rows = (long long)a->n_q * (a->n_heads / a->n_kv_heads);
+    if ((rows / 64 + a->n_trees) * a->n_kv_heads > INT32_MAX || ((long long)a->n_kv / 64 + a->n_trees) * a->n_kv_heads > INT32_MAX ||
+        (long long)a->n_q * a->n_heads / 16 >= INT32_MAX)
+        return TL_EINVAL;
+    AttArgs x = arguments(a);
+    x.o = AttTensor{o->p, o->row, o->head};
+    x.d_o = AttTensor{d_o->p, d_o->row, d_o->head};
+    x.d_q = AttTensor{d_q->p, d_q->row, d_q->head};
+    x.d_k = AttTensor{d_k->p, d_k->row, d_k->head};
+    x.d_v = AttTensor{d_v->p, d_v->row, d_v->head};
+    x.lse = const_cast<float *>(lse);
+    x.delta = static_cast<float *>(workspace_p);
+    x.vec = x.vec && in_pieces(*o, dt, D, 16) && in_pieces(*d_o, dt, D, 16);
+    x.vec_out = pieces_of_4(*d_q, dt, D) && pieces_of_4(*d_k, dt, D) && pieces_of_4(*d_v, dt, D);
+    const hipStream_t st = (hipStream_t)hip_stream;
+    const hipError_t e = dt == TL_DT_F32 ? attend_backward<float>(x, st) : dt == TL_DT_BF16 ? attend_backward<bf16_t>(x, st) : attend_backward<f16_t>(x, st);
+    return e == hipSuccess ? TL_OK : TL_EHIP;
+}
+
+int tl_sample(int dtype, int n_rows, int vocab, const void *logits, int64_t row, const float *u, const float *temperature, const int32_t *top_k,
+              const float *top_p, const float *min_p, int32_t *token, float *logprob, int32_t *kept, void *hip_stream)
+{
+    if (dtype < TL_DT_F32 || dtype > TL_DT_F16 || n_rows < 0 || vocab < 1 || vocab > (1 << 30)) return TL_EINVAL;
+    if (n_rows == 0) return TL_OK;
+    if (!logits || !u || !token || row < 0 || ((uintptr_t)logits & (element_size(dtype) - 1))) return TL_EINVAL;
+    SampleArgs a = {};
+    a.logits = logits;
+    a.row = row;
+    a.u = u;
+    a.temperature = temperature;
+    a.top_k = top_k;
+    a.top_p = top_p;
+    a.min_p = min_p;
+    a.token = token;
+    a.logprob = logprob;
+    a.kept = kept;
+    a.vocab = vocab;
+    int bits = 0;
+    while ((1ll << bits) < vocab) ++bits;
+    a.shift = 62 - bits < 52 ? 62 - bits : 52;
+    const int piece = 4 * element_size(dtype);
+    a.vec = (n_rows == 1 || row % 4 == 0) && ((uintptr_t)logits & (piece - 1)) == 0;
+    const dim3 grid((unsigned)n_rows), block(SMP_THREADS);
+    const hipStream_t st = (hipStream_t)hip_stream;
+    if (dtype == TL_DT_F32) hipLaunchKernelGGL(k_sample<float>, grid, block, 0, st, a);
+    else if (dtype == TL_DT_BF16) hipLaunchKernelGGL(k_sample<bf16_t>, grid, block, 0, st, a);
+    else hipLaunchKernelGGL(k_sample<f16_t>, grid, block, 0, st, a);
+    return hipGetLastError() == hipSuccess ? TL_OK : TL_EHIP;
+}
+
+}  // extern "C"

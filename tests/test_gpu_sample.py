@@ -1,0 +1,191 @@
+"""Sampling against a plain implementation in 64 bits.
+
+Words and counts have to be equal: the reference sums in 64 bits (relative 1e-16 a term, 1e-11 over a row), the kernel in whole
+multiples of at most 2^-42 of the largest weight (rows up to 2^20 words), and a given number falls that close to a border between two words
+with a probability below 1e-6 a row.  logprob is rounded once to fp32 (2^-24 of its value), after the weights of tiny words have lost at most
+2^-43 of the largest weight each, and the sum V times that.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_1809_00832_amd import binding
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def plain(x, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """(token, logprob, kept) of one row of float64 logits."""
+    x = np.where(np.isnan(x), -np.inf, x)
+    top = x.max()
+    if top == -np.inf:
+        return -1, -np.inf, 0
+    if not temperature > 0:
+        return int(np.argmax(x)), 0.0, 1
+    order = np.lexsort((np.arange(len(x)), -x))
+    if 0 < top_k < len(x):
+        order = order[:top_k]
+    order = order[x[order] > -np.inf]
+    with np.errstate(invalid="ignore", over="ignore"):
+        e = np.where(x[order] == top, 0.0, -np.inf if top == np.inf else (x[order] - top) / np.float64(temperature))
+    w = np.exp(e)
+    if top_p < 1:
+        before = np.concatenate([[0.0], np.cumsum(w)[:-1]])
+        keep = before < float(top_p) * w.sum()
+        keep[0] = True
+        order, w, e = order[keep], w[keep], e[keep]
+    if min_p > 0:
+        keep = e >= math.log(min_p)
+        keep[0] = True
+        order, w = order[keep], w[keep]
+    by = np.argsort(order)
+    order, w = order[by], w[by]
+    run = np.cumsum(w)
+    at = int(np.searchsorted(run, float(u) * run[-1], side="right"))
+    at = min(at, int(np.flatnonzero(w > 0)[-1]))
+    return int(order[at]), math.log(w[at] / run[-1]), len(order)
+
+
+def check(logits, u, **cfg):
+    n, vocab = logits.shape
+    kinds = dict(temperature=torch.float32, top_k=torch.int32, top_p=torch.float32, min_p=torch.float32)
+    rows = {k: torch.as_tensor(v, dtype=kinds[k]).expand(n).contiguous() for k, v in cfg.items()}
+    got = binding.tl_sample(logits, u, **{k: v.cuda() for k, v in rows.items()})
+    x, uu = logits.double().cpu().numpy(), u.cpu().numpy()
+    token, logprob, kept = (got[k].cpu().numpy() for k in ("token", "logprob", "kept"))
+    for r in range(n):
+        want = plain(x[r], uu[r], **{k: v[r].item() for k, v in rows.items()})
+        assert (token[r], kept[r]) == (want[0], want[2]), (r, token[r], kept[r], want)
+        if want[1] == -np.inf:
+            assert logprob[r] == -np.inf
+        else:
+            p = math.exp(want[1])
+            assert abs(logprob[r] - want[1]) <= 2.0 ** -23 * abs(want[1]) + 1e-7 + vocab * 2.0 ** -43 / max(p, 1e-300), (r, logprob[r], want)
+    return got
+
+
+def draw(seed, n, vocab, dtype, spread=2.5):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = (torch.randn(n, vocab, generator=g, device="cuda") * spread).to(TYPES[dtype])
+    return x, torch.rand(n, generator=g, device="cuda")
+
+
+FILTERS = [dict(), dict(top_k=1), dict(top_k=5), dict(top_k=40, top_p=0.8), dict(top_p=0.3), dict(top_p=0.95), dict(min_p=0.02),
+           dict(top_k=300, top_p=0.99, min_p=0.001), dict(top_p=1e-6), dict(min_p=1.0), dict(top_p=1.0, top_k=0, min_p=0.0),
+           dict(top_p=0.0), dict(top_p=-1.0), dict(top_k=-3), dict(top_k=1 << 30), dict(top_p=2.0), dict(min_p=2.0)]
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("vocab", [1, 2, 3, 63, 64, 1000, 4096, 4097, 20000])
+def test_against_64_bits(vocab, dtype):
+    for i, f in enumerate(FILTERS):
+        x, u = draw(100 * vocab + i, 6, vocab, dtype)
+        check(x, u, temperature=[0.7, 1.0, 1.5, 0.05, 30.0, 0.0], **f)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("vocab", [50000, 131072, 300001])
+def test_wide_rows(vocab, dtype):
+    x, u = draw(vocab, 5, vocab, dtype)
+    check(x, u, temperature=[1.0, 0.8, 1.0, 2.0, 0.5], top_k=[0, 50, 1000, 0, 7], top_p=[0.9, 1.0, 0.99, 0.5, 0.95], min_p=[0.0, 0.0, 0.01, 0.0, 0.1])
+    check(x, u)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+def test_settings_of_each_row(dtype):
+    n, vocab = 300, 3001
+    x, u = draw(7, n, vocab, dtype)
+    rng = np.random.default_rng(1)
+    check(x, u, temperature=rng.choice([0.0, 0.3, 1.0, 1.7], n).astype(np.float32), top_k=rng.integers(-1, 80, n).astype(np.int32),
+          top_p=rng.choice([0.1, 0.7, 0.97, 1.0], n).astype(np.float32), min_p=rng.choice([0.0, 0.01, 0.2], n).astype(np.float32))
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+def test_ties_go_to_the_lowest_index(dtype):
+    """Rows of a few distinct values: filters cut through runs of equal words."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    for vocab in (10, 5000, 40000):
+        x = torch.randint(0, 4, (8, vocab), generator=g, device="cuda").to(TYPES[dtype])
+        u = torch.rand(8, generator=g, device="cuda")
+        for f in (dict(), dict(top_k=3), dict(top_k=vocab // 3), dict(top_p=0.5), dict(top_p=0.013, top_k=vocab // 2), dict(temperature=0.0)):
+            check(x, u, **f)
+    x = torch.zeros(4, 9000, device="cuda", dtype=TYPES[dtype])
+    x[1::2, ::2] = -0.0                                       # equal to +0
+    check(x, torch.tensor([0.0, 0.25, 0.5, 0.9999], device="cuda"), top_k=1234)
+    got = check(x, torch.zeros(4, device="cuda"), temperature=0.0)
+    assert not got["token"].any()
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+def test_infinities_and_nan(dtype):
+    x, u = draw(11, 9, 700, dtype)
+    low = torch.finfo(TYPES[dtype]).min
+    x[0, ::2] = -math.inf
+    x[1] = -math.inf
+    x[2] = math.nan
+    x[3, 5] = math.nan
+    x[4, [3, 600, 699]] = math.inf
+    x[5, :] = low
+    x[6, :-1] = -math.inf
+    x[7, 100:] = low
+    x[8, 0] = torch.finfo(TYPES[dtype]).max
+    for f in (dict(), dict(top_k=2), dict(top_k=650), dict(top_p=0.7), dict(min_p=0.1), dict(temperature=0.0), dict(temperature=1e-30),
+              dict(temperature=math.inf), dict(temperature=math.nan), dict(temperature=-1.0), dict(top_k=500, top_p=0.9, min_p=0.01)):
+        got = check(x, u, **f)
+        assert got["token"][1] == -1 and got["token"][2] == -1 and got["token"][6] == 699
+
+
+def test_every_word_is_reached():
+    """The numbers in the middle of each word's share give each word."""
+    x, _ = draw(13, 1, 500, "f32", spread=1.0)
+    w = torch.softmax(x[0].double(), 0)
+    mid = (torch.cumsum(w, 0) - w / 2).float()
+    got = binding.tl_sample(x.expand(500, -1), mid)           # rows that repeat: stride 0
+    assert torch.equal(got["token"], torch.arange(500, dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+def test_strides_and_alignment(dtype):
+    x, u = draw(14, 7, 1001, dtype)
+    want = check(x, u, top_p=0.9)
+    for pad, first in ((3, 1), (7, 0), (23, 8)):
+        room = torch.full((7, 1001 + pad + first), math.nan, dtype=TYPES[dtype], device="cuda")
+        view = room[:, first:first + 1001]
+        view.copy_(x)
+        got = check(view, u, top_p=0.9)
+        for k in want:
+            assert torch.equal(got[k], want[k])
+
+
+def test_repeats_on_another_stream_and_in_a_graph():
+    x, u = draw(15, 40, 30000, "bf16")
+    cfg = dict(temperature=torch.full((40,), 0.9, device="cuda"), top_k=torch.full((40,), 300, dtype=torch.int32, device="cuda"),
+               top_p=torch.full((40,), 0.9, device="cuda"))
+    first = binding.tl_sample(x, u, **cfg)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    again = binding.tl_sample(x, u, stream=side, **cfg)
+    side.synchronize()
+    for k in first:
+        assert torch.equal(first[k], again[k])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = binding.tl_sample(x, u, **cfg)
+    for seed in range(4):
+        fx, fu = draw(20 + seed, 40, 30000, "bf16")
+        x.copy_(fx)
+        u.copy_(fu)
+        want = binding.tl_sample(x, u, **cfg)
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in want:
+            assert torch.equal(out[k], want[k])
+
+
+def test_no_rows():
+    got = binding.tl_sample(torch.zeros(0, 10, device="cuda"), torch.zeros(0, device="cuda"))
+    assert all(v.numel() == 0 for v in got.values())
