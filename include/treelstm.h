@@ -524,12 +524,12 @@ int tl_attend_backward(const tl_attention *a, const tl_rows *o, const float *lse
  *     top_k   keeps the first top_k words (off where < 1 or >= vocab)
  *     top_p   keeps, of these, every word whose mass in front of it is below top_p times the total of these; the first one always
  *             (off where not < 1)
- *     min_p   keeps, of these, every word with w_j >= min_p
+ *     min_p   keeps, of these, every word with w_j >= min_p (above 1 as 1)
  *     token   the lowest kept j with sum of w over kept words up to j > u * (sum over all kept words)
  *     logprob log of that word's share of the kept words' weights;   kept: how many words were kept
  * T not above 0 (or NaN): the first word with the largest logit, logprob 0, kept 1.  A row without a value above -infinity: token -1,
  * logprob -infinity, kept 0; words at -infinity are never drawn or kept.  +infinity: the words that have it share the draw.
- * Weights are computed in 64 bits and summed as integers (multiples of 2^-52, from 1024 words on of 2^-(62 - log2 vocab)), so a result
+ * Weights are computed in 64 bits and summed as integers (multiples of 2^-51, above 2048 words of 2^-(62 - log2 vocab)), so a result
  * depends on no order of additions; a word lighter than that is kept but not drawn.
  *   logits [n_rows x vocab] of dtype, `row` elements from one row to the next; 1 <= vocab <= 2^30           DEVICE, read-only
  *   u [n_rows] in [0, 1); temperature, top_p, min_p [n_rows] fp32, top_k [n_rows] int32: NULL turns one off (T = 1)    DEVICE

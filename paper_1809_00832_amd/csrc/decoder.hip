@@ -195,14 +195,12 @@ int tl_sample(int dtype, int n_rows, int vocab, const void *logits, int64_t row,
     a.vocab = vocab;
     int bits = 0;
     while ((1ll << bits) < vocab) ++bits;
-    a.shift = 62 - bits < 52 ? 62 - bits : 52;
-    const int piece = 4 * element_size(dtype);
-    a.vec = (n_rows == 1 || row % 4 == 0) && ((uintptr_t)logits & (piece - 1)) == 0;
+    a.shift = 62 - bits < 51 ? 62 - bits : 51;
     const dim3 grid((unsigned)n_rows), block(SMP_THREADS);
     const hipStream_t st = (hipStream_t)hip_stream;
-    if (dtype == TL_DT_F32) hipLaunchKernelGGL(k_sample<float>, grid, block, 0, st, a);
-    else if (dtype == TL_DT_BF16) hipLaunchKernelGGL(k_sample<bf16_t>, grid, block, 0, st, a);
-    else hipLaunchKernelGGL(k_sample<f16_t>, grid, block, 0, st, a);
+    void (*const k)(SampleArgs) = dtype == TL_DT_F32 ? k_sample<float> : dtype == TL_DT_BF16 ? k_sample<bf16_t> : k_sample<f16_t>;
+    if (hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SmpShared)) != hipSuccess) return TL_EHIP;
+    hipLaunchKernelGGL(k, grid, block, sizeof(SmpShared), st, a);
     return hipGetLastError() == hipSuccess ? TL_OK : TL_EHIP;
 }
 

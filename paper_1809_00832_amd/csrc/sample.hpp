@@ -5,11 +5,16 @@
 //   which the running sum of the kept weights exceeds u times their total.
 //
 // Which word that is hangs on sums over the whole row, so weights are taken in 64 bits and summed as whole multiples of 2^-shift (62
-// bits for the sum of all): integers add up to the same total in any order, so that the result does not depend on which thread
-// adds first.  No row is sorted: the last word that top-k or top-p keeps is found digit by digit (11 bits at a time) from histograms of
-// counts and of weights over the ordered bit patterns of the logits.
+// bits for the sum of all): integers add up to the same total in any order, so the result does not depend on which thread adds
+// first.  No row is sorted.  One workgroup walks a row up to four times: the largest and smallest value; a histogram over 2048 equal
+// steps of the value; the words of the step in which a filter ends, which are sorted in LDS; the kept weights per piece
+// of the row, of which one wave then walks the piece that holds the draw.  Equal steps of the value spread a row's words evenly enough that the
+// additions of a wave seldom meet in one counter, which steps of the bit pattern do not (few exponents).  top-k counts words,
+// which needs no weights, and where it leaves no more words than the list holds, top-p is answered from the list; else a histogram
+// of weights follows.  A step that holds more words than the list (long runs of equal values) is resolved digit by digit of the bit pattern.
 #pragma once
 
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -20,8 +25,8 @@ namespace tl {
 constexpr int SMP_THREADS = 1024;
 constexpr int SMP_WAVES = SMP_THREADS / 64;
 constexpr int SMP_BINS = 2048;
-constexpr int SMP_TILE = SMP_THREADS * 4;       // words that a workgroup looks at in one step
-constexpr int SMP_CHUNKS = 256;                 // pieces of a row whose weights are summed apart
+constexpr int SMP_LIST = 4096;                  // words of one step that are sorted in LDS; also the pieces of a row whose weights are summed apart
+constexpr double SMP_REACH = 40.;               // steps cover weights down to e^-40; what lies below is in the last one
 
 struct SampleArgs {
     const void *logits;
@@ -31,353 +36,731 @@ struct SampleArgs {
     int32_t *token, *kept;
     float *logprob;
     int vocab;
-    int shift;                                  // weights are multiples of 2^-shift
-    int vec;
+    int shift;                                  // weights are multiples of 2^-shift, shift <= 51
 };
 
-// Bit patterns in the order of the values; -0 as 0, NaN as -infinity.
-__device__ inline uint32_t smp_key(float x)
-{
-    x = x != x ? -INFINITY : x + 0.f;
-    const uint32_t b = __float_as_uint(x);
-    return b ^ (b >> 31 ? 0xffffffffu : 0x80000000u);
-}
-__device__ inline float smp_value(uint32_t key) { return __uint_as_float(key ^ (key >> 31 ? 0x80000000u : 0xffffffffu)); }
-constexpr uint32_t SMP_KEY_NONE = 0x007fffffu;  // of -infinity
-
-struct SmpWeight {
-    double inv_t, max, one;
-    uint32_t max_key;
-    // (x - max) / T of a word above -infinity; beside a word at +infinity the others have no weight
-    __device__ double exponent(uint32_t key) const
-    {
-        if (key == max_key) return 0.;
-        return max == INFINITY ? -INFINITY : ((double)smp_value(key) - max) * inv_t;
-    }
-    // in units of 2^-shift
-    __device__ uint64_t operator()(uint32_t key) const
-    {
-        if (key <= SMP_KEY_NONE) return 0;
-        return (uint64_t)(exp(exponent(key)) * one + 0.5);
-    }
+struct SmpShared {
+    union {
+        struct {
+            uint64_t mass[SMP_BINS];
+            uint32_t count[SMP_BINS];
+        };
+        uint64_t piece[SMP_LIST];               // (the histogram is over when the pieces are summed)
+    };
+    union {
+        uint64_t list[SMP_LIST];
+        float packed[SMP_WAVES][512];           // kept words of a wave's piece, side by side
+    };
+    uint64_t tmp[SMP_WAVES];
+    uint64_t out[4];
+    uint64_t best;
+    uint32_t low, listed, kept;
 };
+extern __shared__ __align__(16) unsigned char smp_lds[];
+__device__ inline SmpShared &smp_shared() { return *reinterpret_cast<SmpShared *>(smp_lds); }
 
-template <typename V> __device__ inline V smp_wave_sum(V x)
+// The phases are functions of their own, called, so that each has the registers to itself (inlined into one kernel they spill); what they are
+// given is the same in every lane, and is put into scalar registers again.
+template <typename S> __device__ inline S smp_uniform(S x)
 {
+    static_assert(sizeof(S) % 4 == 0, "whole words");
+    uint32_t w[sizeof(S) / 4];
+    __builtin_memcpy(w, &x, sizeof(S));
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o);
+    for (size_t i = 0; i < sizeof(S) / 4; ++i) w[i] = __builtin_amdgcn_readfirstlane(w[i]);
+    __builtin_memcpy(&x, w, sizeof(S));
     return x;
 }
 
-// Sum over the threads in front of this one (exclusive) and over all; `tmp` has SMP_WAVES words.  Everyone must call it.
-template <typename V> __device__ inline V smp_scan(V x, V *tmp, V *total)
+// Bit patterns in the order of the values (of numbers; -0 as 0).
+constexpr uint32_t SMP_KEY_NONE = 0x007fffffu;  // of -infinity
+__device__ inline uint32_t smp_key(float x)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    V s = x;
+    const uint32_t b = __float_as_uint(x + 0.f);
+    return b ^ (b >> 31 ? 0xffffffffu : 0x80000000u);
+}
+__device__ inline float smp_value(uint32_t key) { return __uint_as_float(key ^ (key >> 31 ? 0x80000000u : 0xffffffffu)); }
+
+// log2 of a word's weight is (x - max) per_t.  Where a word is at +infinity, max lies far beyond all other words, so that they
+// have no weight, and what is above 0 counts as 0.
+struct SmpWeight {
+    double per_t, max;                          // log2(e) / T, the row's largest value
+    int shift, pad;
+    __device__ double exponent(float x) const { return ((double)x - max) * per_t; }
+};
+
+// Weights in units of 2^-shift.  2^t = 2^k 2^r with k the nearest whole number to t, found by adding 1.5 * 2^52; 2^r on [-1/2, 1/2] as 1 + r q(r), q the
+// polynomial of degree 8 through (2^r - 1) / r at the nine Chebyshev nodes: good to 4e-14, and exactly 1 at 0; adding 2^52 rounds to whole units and leaves them in the
+// mantissa.  (A table of powers and a shorter polynomial would cost a scattered LDS read a word beside the histogram's additions.)
+// The coefficients are made opaque so that they stay in scalar registers, where a multiply-add takes them from: the compiler would
+// copy each to vector registers for each word.
+struct SmpSeries {
+    double c[10];
+    SmpWeight w;
+    __device__ explicit SmpSeries(const SmpWeight &weight)
+        : c{1., 6.93147180559945286e-01, 2.40226506958129887e-01, 5.55041086647608192e-02, 9.61812915940255843e-03, 1.33335581789866269e-03,
+            1.54034558524538382e-04, 1.52526868763930427e-05, 1.32552248786688168e-06, 1.02031157077784712e-07},
+          w(weight)
+    {
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const V y = __shfl_up(s, o);
-        if (lane >= o) s += y;
+        for (int i = 0; i < 10; ++i) asm volatile("" : "+s"(c[i]));
     }
-    __syncthreads();
-    if (lane == 63) tmp[wave] = s;
-    __syncthreads();
-    V before = 0, all = 0;
+    // 0 for a NaN and for -infinity
+    __device__ uint64_t operator()(float x) const
+    {
+        const double t = fmin(fmax(w.exponent(x), -64.), 0.);
+        const double magic = 6755399441055744.;
+        const double a = t + magic;
+        const double r = t - (a - magic);
+        double e = c[9];
 #pragma unroll
-    for (int w = 0; w < SMP_WAVES; ++w) {
-        if (w < wave) before += tmp[w];
-        all += tmp[w];
+        for (int i = 8; i >= 0; --i) e = fma(e, r, c[i]);
+        const int k = (int)(uint32_t)__double_as_longlong(a);
+        const uint64_t y = __double_as_longlong(e) + ((uint64_t)(uint32_t)(k + w.shift) << 52);
+        return (uint64_t)__double_as_longlong(__longlong_as_double((long long)y) + 4503599627370496.) & 0xfffffffffffffull;
     }
-    *total = all;
-    return before + s - x;
+};
+
+// The share p of a sum, rounded down or up, exactly: a draw or a filter may end right at a border between words.
+__device__ inline uint64_t smp_share(float p, uint64_t of, bool up)
+{
+    if (!(p > 0.f)) return 0;
+    const uint32_t b = __float_as_uint(p), e = b >> 23;
+    const uint64_t m = e ? (b & 0x7fffffu) | 0x800000u : b & 0x7fffffu;
+    const int s = 150 - (int)(e ? e : 1);                       // p = m 2^-s
+    if (s <= 0) return ~0ull;                                   // (2^23 and more)
+    const uint64_t lo = of * m, hi = __umul64hi(of, m);
+    const uint64_t whole = s < 64 ? hi << (64 - s) | lo >> s : s < 128 ? hi >> (s - 64) : 0;
+    const uint64_t rest = s < 64 ? lo << (64 - s) : lo | (s > 64 ? s < 128 ? hi << (128 - s) : hi : 0);
+    return whole + (up && rest ? 1 : 0);
 }
 
-struct SmpShared {
-    uint64_t mass[SMP_BINS];
-    uint32_t count[SMP_BINS];
-    uint64_t chunk[SMP_CHUNKS];
-    uint64_t tmp[SMP_WAVES];
-    uint64_t tmp2[SMP_WAVES];
-    uint64_t out[4];
-    uint64_t best;
-};
+// ---- sums over lanes --------------------------------------------------------------------
 
+// What lane l - n of the row of 16 (or the last lane of the rows in front) holds; zero where there is none.
+template <int CTRL, int ROWS> __device__ inline uint64_t smp_from(uint64_t x)
+{
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, ROWS, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), CTRL, ROWS, 0xf, false);
+    return (uint64_t)hi << 32 | lo;
+}
+__device__ inline uint64_t smp_row_scan(uint64_t x)
+{
+    x += smp_from<0x111, 0xf>(x);
+    x += smp_from<0x112, 0xf>(x);
+    x += smp_from<0x114, 0xf>(x);
+    x += smp_from<0x118, 0xf>(x);
+    return x;
+}
+// Sum over this lane and those in front of it.
+__device__ inline uint64_t smp_wave_scan(uint64_t x)
+{
+    x = smp_row_scan(x);
+    x += smp_from<0x142, 0xa>(x);
+    x += smp_from<0x143, 0xc>(x);
+    return x;
+}
+__device__ inline uint64_t smp_lane(uint64_t x, int lane)
+{
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane);
+}
+
+// Sum over the threads in front of this one and over all.  Everyone must call it.
+__device__ inline uint64_t smp_scan(uint64_t x, uint64_t *total, SmpShared &sh)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint64_t s = smp_wave_scan(x);
+    __syncthreads();
+    if (lane == 63) sh.tmp[wave] = s;
+    __syncthreads();
+    const uint64_t w = smp_row_scan(sh.tmp[lane & (SMP_WAVES - 1)]);
+    *total = smp_lane(w, SMP_WAVES - 1);
+    return (wave ? smp_lane(w, wave - 1) : 0) + s - x;
+}
+
+// ---- a row ------------------------------------------------------------------------------
+
+// A row, walked in steps of SMP_THREADS times W words, 16 bytes a thread; W words from a 16-byte boundary on, so that rows of any length
+// and distance are read in such pieces.  Words outside the row read as -infinity.
 template <typename T> struct SmpRow {
+    static constexpr int W = 16 / (int)sizeof(T);
+    static constexpr int STEP = SMP_THREADS * W;
+    static constexpr int PIECE = 64 * W;        // words of a wave in one step
+    static constexpr int BATCH = 4;             // requests in flight (a short row is bound by their latency)
     const T *p;
-    int n, vec;
-    // the four words from j on (keys; 0, which is no value's key, beyond the row)
-    __device__ void keys4(int j, uint32_t (&k)[4]) const
+    int n, ahead;                               // words, and how many the first 16 bytes hold in front of them
+
+    SmpRow() = default;
+    __device__ SmpRow(const T *row, int words) : p(row), n(words), ahead((int)(((uintptr_t)row & 15) / sizeof(T))) {}
+    __device__ int pieces() const { return (n + ahead + PIECE - 1) / PIECE; }
+    // words j .. j + W - 1, as they are
+    __device__ void raw(int j, T (&v)[W]) const
     {
-        if (vec && j + 3 < n) {
-            T x[4];
-            __builtin_memcpy(x, __builtin_assume_aligned(p + j, 4 * sizeof(T)), 4 * sizeof(T));
-#pragma unroll
-            for (int i = 0; i < 4; ++i) k[i] = smp_key((float)x[i]);
+        typedef const __attribute__((address_space(1))) T *global;
+        const global g = (global)p;
+        if (j >= 0 && j + W <= n) {
+            const u32x4 x = *(const __attribute__((address_space(1))) u32x4 *)(g + j);
+            __builtin_memcpy(v, &x, 16);
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) k[i] = j + i < n ? smp_key((float)p[j + i]) : 0u;
+            for (int i = 0; i < W; ++i) {
+                const T x = g[min(max(j + i, 0), n - 1)];
+                v[i] = (unsigned)(j + i) < (unsigned)n ? x : (T)-INFINITY;
+            }
+        }
+    }
+    // f(W words, index of the first, piece); every lane of a wave calls it equally often.
+    template <typename F> __device__ void each(F f) const
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n_pieces = pieces();
+        for (int q = wave; q < n_pieces; q += BATCH * SMP_WAVES) {
+            const int j = (q * 64 + (int)(threadIdx.x & 63)) * W - ahead;
+            T v[BATCH][W];
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b)
+                if (q + b * SMP_WAVES < n_pieces) raw(j + b * STEP, v[b]);
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b)
+                if (q + b * SMP_WAVES < n_pieces) {
+                    float x[W];
+#pragma unroll
+                    for (int i = 0; i < W; ++i) x[i] = (float)v[b][i];
+                    f(x, j + b * STEP, q + b * SMP_WAVES);
+                }
         }
     }
 };
 
-// The last word, in the order of the values, that a filter keeps: its key, and how many of the words with that key it keeps.  BY_COUNT:
-// the k-th word.  Else: the first word at which the running weight reaches `need`.  above: weight of the words with larger keys.
+// The last word that a filter keeps, in the order of values and indexes: a word is kept if it stands at or before it.
 struct SmpCut {
-    uint32_t key;
-    uint32_t n, of;             // kept words with this key; all of them
-    uint32_t count_above;
-    uint64_t above;
+    float x;
+    int j;
+    uint64_t mass;              // weight of the words up to it
+    __device__ bool keeps(float y, int i) const { return (y > x) | ((y == x) & (i <= j)); }
 };
 
-template <typename T, bool BY_COUNT>
-__device__ SmpCut smp_cut(const SmpRow<T> &row, const SmpWeight &weight, uint32_t k, double need, SmpShared &sh)
+// ---- the cut ----------------------------------------------------------------------------
+
+// Step of a value: 0 for the largest, never smaller for a smaller one.  (+infinity is in front of the largest number; a NaN's step is not asked for.)
+struct SmpSteps {
+    float max, per;
+    __device__ float place(float x) const { return __builtin_amdgcn_fmed3f((max - x) * per, 0.f, (float)(SMP_BINS - 1)); }
+    __device__ int operator()(float x) const { return (int)place(x); }
+};
+
+// Histogram over the steps: of the words above -infinity, or of the weights.
+template <typename T, bool BY_COUNT> __device__ __noinline__ void smp_histogram(SmpRow<T> row, SmpWeight weight, SmpSteps step)
 {
-    constexpr int LEVELS = sizeof(T) == 4 ? 3 : 2;          // a 16-bit type's patterns end above the last 11 bits
-    constexpr int shift_of[3] = {21, 10, 0};
-    SmpCut c = {0, 0, 0, 0, 0};
-    uint32_t prefix = 0;
-    for (int level = 0; level < LEVELS; ++level) {
-        const int sh_l = shift_of[level], bits = level == 2 ? 10 : 11, n_bins = 1 << bits;
-        for (int b = threadIdx.x; b < n_bins; b += SMP_THREADS) {
-            sh.mass[b] = 0;
-            sh.count[b] = 0;
-        }
-        if (threadIdx.x == 0) sh.out[0] = ~0ull;
-        __syncthreads();
-        for (int j = threadIdx.x * 4; j < row.n; j += SMP_TILE) {
-            uint32_t key[4];
-            row.keys4(j, key);
+    constexpr int W = SmpRow<T>::W;
+    SmpShared &sh = smp_shared();
+    row = smp_uniform(row);
+    weight = smp_uniform(weight);
+    step = smp_uniform(step);
+    __syncthreads();
+    for (int b = threadIdx.x; b < SMP_BINS; b += SMP_THREADS) {
+        if (BY_COUNT) sh.count[b] = 0;
+        else sh.mass[b] = 0;
+    }
+    __syncthreads();
+    const SmpSeries series(weight);
+    row.each([&](const float (&x)[W], int, int) {
+        uint64_t w[W];
+        if (!BY_COUNT) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (key[i] == 0u) continue;
-                if (level > 0 && key[i] >> (sh_l + bits) != prefix) continue;
-                const uint32_t b = key[i] >> sh_l & (n_bins - 1);
-                atomicAdd(&sh.count[b], 1u);
-                atomicAdd((unsigned long long *)&sh.mass[b], (unsigned long long)weight(key[i]));
+            for (int i = 0; i < W; ++i) w[i] = series(x[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const int b = step(x[i]);
+            if (BY_COUNT) {
+                if (x[i] > -INFINITY) atomicAdd(&sh.count[b], 1u);
+            } else {
+                if (w[i]) atomicAdd((unsigned long long *)&sh.mass[b], (unsigned long long)w[i]);
+            }
+        }
+    });
+    __syncthreads();
+}
+
+// The first step, from the largest values on, at which `goal` words are reached, or the share `p` of the weight `of` (0: of the whole); the last one that
+// holds anything where they never are.
+struct SmpAt {
+    int at;
+    uint32_t here;              // BY_COUNT: words in it
+    uint64_t above;             // in the steps in front of it
+    uint64_t need;              // weight that is to be reached
+};
+template <bool BY_COUNT> __device__ __noinline__ SmpAt smp_step(uint32_t goal, float p, uint64_t of)
+{
+    SmpShared &sh = smp_shared();
+    goal = smp_uniform(goal);
+    p = smp_uniform(p);
+    of = smp_uniform(of);
+    const int b = 2 * threadIdx.x;
+    const uint64_t m0 = BY_COUNT ? sh.count[b] : sh.mass[b], m1 = BY_COUNT ? sh.count[b + 1] : sh.mass[b + 1];
+    uint64_t all;
+    const uint64_t before = smp_scan(m0 + m1, &all, sh);
+    const uint64_t at0 = before + m0, at1 = at0 + m1;
+    const uint64_t need = smp_share(p, of ? of : all, true);
+    auto short_of = [&](uint64_t x) { return x == 0 || (BY_COUNT ? x < goal : x < need); };
+    // (one step alone: sums in front of it fall short, its own reaches or is the last)
+    if (m0 && short_of(before) && (!short_of(at0) || at0 == all)) {
+        sh.out[0] = b;
+        sh.out[1] = before;
+    }
+    if (m1 && short_of(at0) && (!short_of(at1) || at1 == all)) {
+        sh.out[0] = b + 1;
+        sh.out[1] = at0;
+    }
+    __syncthreads();
+    const int at = (int)sh.out[0];
+    const SmpAt r = {at, BY_COUNT ? sh.count[at] : 0, sh.out[1], need};
+    __syncthreads();
+    return r;
+}
+
+// Lists the words of steps from .. to; how many they are (beyond SMP_LIST: not all are listed).
+template <typename T> __device__ __noinline__ int smp_collect(SmpRow<T> row, SmpSteps step, int from, int to)
+{
+    constexpr int W = SmpRow<T>::W;
+    SmpShared &sh = smp_shared();
+    row = smp_uniform(row);
+    step = smp_uniform(step);
+    const float first = (float)smp_uniform(from), behind = (float)smp_uniform(to) + 1.f;
+    if (threadIdx.x == 0) sh.listed = 0;
+    __syncthreads();
+    row.each([&](const float (&x)[W], int j, int) {
+        unsigned hit = 0;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const float at = step.place(x[i]);
+            hit |= (at >= first) & (at < behind) & (x[i] > -INFINITY) ? 1u << i : 0u;
+        }
+        if (__any(hit != 0)) {
+            const uint32_t upto = (uint32_t)smp_wave_scan((uint64_t)__popc(hit)), all = __builtin_amdgcn_readlane(upto, 63);
+            uint32_t at = 0;
+            if ((threadIdx.x & 63) == 0) at = atomicAdd(&sh.listed, all);
+            at = __builtin_amdgcn_readfirstlane(at) + upto - __popc(hit);
+#pragma unroll
+            for (int i = 0; i < W; ++i)
+                if (hit >> i & 1) {
+                    if (at < SMP_LIST) sh.list[at] = (uint64_t)smp_key(x[i]) << 32 | (uint32_t)~(j + i);
+                    ++at;
+                }
+        }
+    });
+    __syncthreads();
+    return (int)sh.listed;
+}
+
+// Sorts the list by value, then index: exchanges at a distance below 64 stay within a wave, without barriers.
+static __device__ __noinline__ void smp_sort(int n)
+{
+    SmpShared &sh = smp_shared();
+    n = smp_uniform(n);
+    const int lane = threadIdx.x & 63;
+    int size = 64;
+    while (size < n) size *= 2;
+    for (int i = n + threadIdx.x; i < size; i += SMP_THREADS) sh.list[i] = 0;
+    for (int run = 64; run <= size; run *= 2) {
+        for (int d = run / 2; d >= 64; d /= 2) {
+            __syncthreads();
+            for (int e = threadIdx.x; e < size / 2; e += SMP_THREADS) {
+                const int i = 2 * e - (e & (d - 1)), o = i + d;
+                const uint64_t a = sh.list[i], b = sh.list[o];
+                if ((a < b) == ((i & run) == 0)) {
+                    sh.list[i] = b;
+                    sh.list[o] = a;
+                }
             }
         }
         __syncthreads();
-        // from the largest key down: thread t holds bins n - 1 - 2 t and n - 2 - 2 t
-        const int hi = n_bins - 1 - 2 * (int)threadIdx.x;
-        const bool in = hi >= 0;
-        const uint64_t m0 = in ? sh.mass[hi] : 0, m1 = in ? sh.mass[hi - 1] : 0;
-        const uint32_t c0 = in ? sh.count[hi] : 0, c1 = in ? sh.count[hi - 1] : 0;
-        uint64_t all_m, all_c;
-        const uint64_t bm = smp_scan<uint64_t>(m0 + m1, sh.tmp, &all_m), bc = smp_scan<uint64_t>((uint64_t)c0 + c1, sh.tmp2, &all_c);
-        // the first bin at which the bound is reached, or the last one that holds anything
-        bool hit0, hit1;
-        if (BY_COUNT) {
-            hit0 = c0 && c.count_above + bc + c0 >= k;
-            hit1 = c1 && c.count_above + bc + c0 + c1 >= k;
+        for (int i = threadIdx.x; i < size; i += SMP_THREADS) {
+            uint64_t a = sh.list[i];
+            for (int r = run == 64 ? 2 : run; r <= run; r *= 2)          // (the first 21 stages are one walk within waves)
+                for (int d = min(r / 2, 32); d >= 1; d /= 2) {
+                    const uint64_t b = __shfl_xor(a, d);
+                    // the lower place of a pair keeps the larger one where its run descends
+                    const bool keep_larger = ((lane & d) == 0) == ((i & r) == 0);
+                    a = (a > b) == keep_larger ? a : b;
+                }
+            sh.list[i] = a;
+        }
+    }
+    __syncthreads();
+}
+
+// The cut inside a sorted list of n words that stand behind `count_above` words of weight `above`.
+template <bool BY_COUNT> __device__ __noinline__ SmpCut smp_cut_list(int n, SmpWeight weight, uint32_t k, uint64_t need, uint64_t above, uint32_t count_above)
+{
+    SmpShared &sh = smp_shared();
+    n = smp_uniform(n);
+    const SmpSeries series(smp_uniform(weight));
+    constexpr int EACH = SMP_LIST / SMP_THREADS;
+    uint64_t w[EACH] = {}, s = 0;
+    if (EACH * ((int)threadIdx.x & ~63) < n) {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int e = EACH * threadIdx.x + i;
+            const uint64_t y = series(smp_value((uint32_t)(sh.list[e] >> 32)));
+            s += w[i] = e < n ? y : 0;
+        }
+    }
+    uint64_t all;
+    uint64_t run = above + smp_scan(s, &all, sh);
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int e = EACH * threadIdx.x + i;
+        const bool short_before = e == 0 || (BY_COUNT ? count_above + (uint32_t)e < k : run < need);
+        run += w[i];
+        const bool reached = BY_COUNT ? count_above + (uint32_t)e + 1 >= k : run >= need;
+        if (e < n && short_before && (reached || e == n - 1)) {
+            sh.out[0] = e;
+            sh.out[1] = run;
+        }
+    }
+    __syncthreads();
+    const uint64_t e = sh.list[sh.out[0]];
+    const SmpCut c = {smp_value((uint32_t)(e >> 32)), (int)~(uint32_t)e, sh.out[1]};
+    __syncthreads();
+    return c;
+}
+
+// The least value above -infinity whose exponent is not below `least`, for a `least` up to 0: a search over the bit patterns, 64 at a time.
+__device__ inline float smp_least_value(const SmpWeight &weight, float max, double least)
+{
+    uint32_t lo = SMP_KEY_NONE + 1, hi = smp_key(max);                   // hi fits
+    while (lo < hi) {
+        const uint32_t step = (hi - lo) / 64 + 1;
+        const uint64_t at = (uint64_t)lo + (uint64_t)step * (threadIdx.x & 63);
+        const bool fits = at >= hi || !(weight.exponent(smp_value((uint32_t)at)) < least);
+        const int first = __ffsll(__ballot(fits)) - 1;                   // 0: lo itself; -1: beyond the last one
+        if (first == 0) return smp_value(lo);
+        const uint64_t below = (uint64_t)lo + (uint64_t)step * (first < 0 ? 63 : first - 1);
+        if (first >= 0) hi = (uint32_t)min((uint64_t)hi, below + step);
+        lo = (uint32_t)below + 1;
+    }
+    return smp_value(lo);
+}
+
+// ---- the draw ---------------------------------------------------------------------------
+
+// The words that add to the running sum in which the draw is located: with their weights, those that the filters keep; or, to find one of many
+// equal words, each of these with one.
+struct SmpKept {
+    SmpCut cut;
+    SmpWeight weight;
+    float u;                    // the draw, a share of the sum
+    int equal;                  // or 1 + which of the equal words
+    __device__ bool operator()(float x, int j) const { return cut.keeps(x, j) & ((x == cut.x) | !equal); }
+};
+
+struct SmpDraw {
+    int word, kept;
+    uint64_t sum, weight;       // of all, of the word
+};
+
+// The word, by index, at which the running sum first exceeds the draw; the sum of all and how many words add to it.
+template <typename T> __device__ __noinline__ SmpDraw smp_locate(SmpRow<T> row, SmpKept f)
+{
+    typedef SmpRow<T> R;
+    constexpr int W = R::W;
+    SmpShared &sh = smp_shared();
+    row = smp_uniform(row);
+    f = smp_uniform(f);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n_pieces = row.pieces();
+    int group = 0;                                              // 2^group pieces are summed together
+    while (n_pieces >> group >= SMP_LIST) ++group;
+    __syncthreads();
+    for (int i = threadIdx.x; i <= n_pieces >> group; i += SMP_THREADS) sh.piece[i] = 0;
+    if (threadIdx.x == 0) {
+        sh.out[0] = ~0ull;
+        sh.kept = 0;
+    }
+    __syncthreads();
+    const SmpSeries series(f.weight);
+    uint32_t kept = 0;
+    row.each([&](const float (&x)[W], int j, int q) {
+        unsigned mine = 0;
+#pragma unroll
+        for (int i = 0; i < W; ++i) mine |= f(x[i], j + i) ? 1u << i : 0u;
+        if (!__any(mine != 0)) return;
+        const uint32_t count = __popc(mine), upto = (uint32_t)smp_wave_scan((uint64_t)count), all = __builtin_amdgcn_readlane(upto, 63);
+        kept += all;
+        uint64_t s = 0;
+        if (f.equal) {
+            s = count;
+        } else if (4 * all > 3 * R::PIECE) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const uint64_t y = series(x[i]);
+                s += mine >> i & 1 ? y : 0;
+            }
         } else {
-            hit0 = c0 && ((double)(c.above + bm + m0) >= need || bc + c0 == all_c);
-            hit1 = c1 && ((double)(c.above + bm + m0 + m1) >= need || bc + c0 + c1 == all_c);
+            // few: put side by side first, so that a weight is worked out for them alone
+            float *packed = sh.packed[wave];
+            uint32_t at = upto - count;
+#pragma unroll
+            for (int i = 0; i < W; ++i)
+                if (mine >> i & 1) packed[at++] = x[i];
+            __builtin_amdgcn_wave_barrier();
+            for (uint32_t e = lane; e < ((all + 63) & ~63u); e += 64) {
+                const uint64_t y = series(e < all ? packed[e] : -INFINITY);
+                s += y;
+            }
+            __builtin_amdgcn_wave_barrier();
         }
-        if (hit0) atomicMin((unsigned long long *)&sh.out[0], (unsigned long long)(2 * threadIdx.x));
-        else if (hit1) atomicMin((unsigned long long *)&sh.out[0], (unsigned long long)(2 * threadIdx.x + 1));
-        __syncthreads();
-        const uint64_t at = sh.out[0];
-        if (at >> 1 == threadIdx.x) {
-            sh.out[1] = at & 1 ? bm + m0 : bm;
-            sh.out[2] = at & 1 ? bc + c0 : bc;
-            sh.out[3] = at & 1 ? c1 : c0;
-        }
-        __syncthreads();
-        c.above += sh.out[1];
-        c.count_above += (uint32_t)sh.out[2];
-        c.of = (uint32_t)sh.out[3];
-        prefix = prefix << bits | (uint32_t)(n_bins - 1 - (int)at);
-        __syncthreads();
+        s = smp_lane(smp_wave_scan(s), 63);
+        if (lane == 0) atomicAdd((unsigned long long *)&sh.piece[q >> group], (unsigned long long)s);
+    });
+    if (lane == 0) atomicAdd(&sh.kept, kept);
+    __syncthreads();
+    constexpr int EACH = SMP_LIST / SMP_THREADS;
+    uint64_t w[EACH], s = 0, all;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int e = EACH * threadIdx.x + i;
+        s += w[i] = e <= n_pieces >> group ? sh.piece[e] : 0;
     }
-    c.key = prefix;
-    if (LEVELS == 2) {
-        // 22 bits of the pattern; the rest are all zeros, or all ones of a negative value
-        c.key = prefix << 10;
-        if (!(c.key >> 31)) c.key |= 0x3ffu;
-    }
-    if (BY_COUNT) {
-        c.n = k - c.count_above;
+    uint64_t run = smp_scan(s, &all, sh);
+    // exceeded for good: the largest whole number below what the sum has to pass
+    uint64_t goal = 0;
+    if (f.equal) {
+        goal = (uint64_t)f.equal - 1;
     } else {
-        const double w = (double)weight(c.key), left = need - (double)c.above;
-        const double n = w > 0. ? ceil(left / w) : (double)c.of;
-        c.n = n < 1. ? 1u : n > (double)c.of ? c.of : (uint32_t)n;
+        goal = smp_share(f.u, all, false);
+        goal = goal >= all ? all - 1 : goal;
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        if (run <= goal && goal < run + w[i]) {
+            sh.out[0] = EACH * threadIdx.x + i;
+            sh.out[1] = run;
+        }
+        run += w[i];
+    }
+    __syncthreads();
+    SmpDraw d = {0, (int)sh.kept, all, 0};
+    const uint64_t hit = sh.out[0];
+    if (hit == ~0ull) return d;
+    if (wave == 0) {
+        uint64_t at = sh.out[1];
+        for (int q = (int)hit << group; q < min((int)(hit + 1) << group, n_pieces); ++q) {
+            const int j = (q * 64 + lane) * W - row.ahead;
+            T x[W];
+            row.raw(j, x);
+            uint64_t v[W], t = 0;
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const uint64_t y = f.equal ? 1 : series((float)x[i]);
+                t += v[i] = f((float)x[i], j + i) ? y : 0;
+            }
+            const uint64_t scan = smp_wave_scan(t);
+            uint64_t here = at + scan - t;
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                if (here <= goal && goal < here + v[i]) {
+                    sh.out[2] = (uint64_t)(j + i);
+                    sh.out[3] = v[i];
+                }
+                here += v[i];
+            }
+            at += smp_lane(scan, 63);
+            if (at > goal) break;
+        }
+    }
+    __syncthreads();
+    d.word = (int)sh.out[2];
+    d.weight = sh.out[3];
+    __syncthreads();
+    return d;
+}
+
+// The cut of any row, by the bit patterns of its values, 11, 11 and 10 bits at a time; for steps that hold more words than the list.
+template <typename T, bool BY_COUNT> __device__ __noinline__ SmpCut smp_cut_by_digits(SmpRow<T> row, SmpWeight weight, uint32_t k, uint64_t need)
+{
+    constexpr int W = SmpRow<T>::W;
+    SmpShared &sh = smp_shared();
+    row = smp_uniform(row);
+    weight = smp_uniform(weight);
+    k = smp_uniform(k);
+    need = smp_uniform(need);
+    const SmpSeries series(weight);
+    uint32_t prefix = 0, count_above = 0, of = 0;
+    uint64_t above = 0;
+    for (int level = 0; level < 3; ++level) {
+        const int sh_l = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11, n_bins = 1 << bits;
+        __syncthreads();
+        for (int b = threadIdx.x; b < SMP_BINS; b += SMP_THREADS) {
+            sh.mass[b] = 0;
+            sh.count[b] = 0;
+        }
+        __syncthreads();
+        row.each([&](const float (&x)[W], int, int) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const uint32_t key = smp_key(x[i]);
+                if (!(x[i] > -INFINITY) || (level > 0 && key >> (sh_l + bits) != prefix)) continue;
+                const uint32_t b = n_bins - 1 - (key >> sh_l & (n_bins - 1));
+                atomicAdd(&sh.count[b], 1u);
+                atomicAdd((unsigned long long *)&sh.mass[b], (unsigned long long)series(x[i]));
+            }
+        });
+        __syncthreads();
+        const SmpAt s = smp_step<BY_COUNT>(k - count_above, 1.f, BY_COUNT || need <= above ? 1 : need - above);
+        uint64_t c = 0, m = 0, all_c, all_m;                    // of the larger digits
+        for (int i = threadIdx.x; i < s.at; i += SMP_THREADS) {
+            c += sh.count[i];
+            m += sh.mass[i];
+        }
+        smp_scan(c, &all_c, sh);
+        smp_scan(m, &all_m, sh);
+        of = sh.count[s.at];
+        above += all_m;
+        count_above += (uint32_t)all_c;
+        prefix = prefix << bits | (uint32_t)(n_bins - 1 - s.at);
+    }
+    SmpCut c = {smp_value(prefix), row.n, 0};
+    const uint64_t w = series(c.x);
+    uint32_t n = of;                                            // words of this value that are kept: the first ones by index
+    if (BY_COUNT) {
+        n = min(k - count_above, of);
+    } else if (w) {
+        const uint64_t left = need > above ? (need - above + w - 1) / w : 1;
+        n = left > of ? of : (uint32_t)left;
+    }
+    c.mass = above + n * w;
+    if (n < of) {
+        SmpKept f = {};
+        f.cut = c;
+        f.equal = (int)n;
+        c.j = smp_locate(row, f).word;
     }
     return c;
 }
 
-// The first word, by index, at which the running sum of f over the words in front of and at it exceeds `target(sum of all)`; also that
-// sum.  -1 if it is never exceeded.
-template <typename T, typename F, typename G>
-__device__ int smp_locate(const SmpRow<T> &row, F f, G target, uint64_t *sum, SmpShared &sh)
+template <typename T> __global__ __launch_bounds__(SMP_THREADS, 8) void k_sample(const SampleArgs a)
 {
-    const int lane = threadIdx.x & 63;
-    const int n_tiles = (row.n + SMP_TILE - 1) / SMP_TILE;
-    const int per = (n_tiles + SMP_CHUNKS - 1) / SMP_CHUNKS;         // tiles of a chunk
-    for (int b = threadIdx.x; b < SMP_CHUNKS; b += SMP_THREADS) sh.chunk[b] = 0;
-    __syncthreads();
-    for (int t = 0; t < n_tiles; ++t) {
-        const int j = t * SMP_TILE + threadIdx.x * 4;
-        uint64_t s = 0;
-        if (j < row.n) {
-            uint32_t key[4];
-            row.keys4(j, key);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s += key[i] ? f(key[i], j + i) : 0;
-        }
-        s = smp_wave_sum(s);
-        if (lane == 0) atomicAdd((unsigned long long *)&sh.chunk[t / per], (unsigned long long)s);
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) sh.out[0] = ~0ull;
-    uint64_t all;
-    const uint64_t mine = threadIdx.x < SMP_CHUNKS ? sh.chunk[threadIdx.x] : 0;
-    const uint64_t before = smp_scan<uint64_t>(mine, sh.tmp, &all);
-    const uint64_t goal = target(all);
-    if (before <= goal && goal < before + mine) {
-        sh.out[0] = threadIdx.x;
-        sh.out[1] = before;
-    }
-    __syncthreads();
-    *sum = all;
-    const uint64_t chunk = sh.out[0];
-    uint64_t run = sh.out[1];
-    __syncthreads();
-    if (chunk == ~0ull) return -1;
-    if (threadIdx.x == 0) sh.out[0] = ~0ull;
-    for (int t = (int)chunk * per; t < min((int)(chunk + 1) * per, n_tiles); ++t) {
-        const int j = t * SMP_TILE + threadIdx.x * 4;
-        uint64_t w[4] = {0, 0, 0, 0};
-        if (j < row.n) {
-            uint32_t key[4];
-            row.keys4(j, key);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = key[i] ? f(key[i], j + i) : 0;
-        }
-        uint64_t here;
-        uint64_t at = run + smp_scan<uint64_t>(w[0] + w[1] + w[2] + w[3], sh.tmp, &here);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (at <= goal && goal < at + w[i]) sh.out[0] = (uint64_t)(j + i);
-            at += w[i];
-        }
-        run += here;
-        __syncthreads();
-        if (run > goal) break;
-    }
-    const int found = (int)sh.out[0];
-    __syncthreads();
-    return found;
-}
-
-template <typename T> __global__ __launch_bounds__(SMP_THREADS) void k_sample(const SampleArgs a)
-{
-    __shared__ SmpShared sh;
+    SmpShared &sh = smp_shared();
     const int r = blockIdx.x;
-    SmpRow<T> row;
-    row.p = static_cast<const T *>(a.logits) + (long long)r * a.row;
-    row.n = a.vocab;
-    row.vec = a.vec;
+    const SmpRow<T> row(static_cast<const T *>(a.logits) + (long long)r * a.row, a.vocab);
 
-    // the largest value and its first index: keys above, complements of the indexes below
-    if (threadIdx.x == 0) sh.best = 0;
+    // the largest value and its first index, and the smallest value
+    if (threadIdx.x == 0) {
+        sh.best = 0;
+        sh.low = ~0u;
+    }
     __syncthreads();
-    uint64_t best = 0;
-    for (int j = threadIdx.x * 4; j < row.n; j += SMP_TILE) {
-        uint32_t key[4];
-        row.keys4(j, key);
+    {
+        float top = -INFINITY, low = INFINITY;
+        int at = 0;
+        row.each([&](const float (&x)[SmpRow<T>::W], int j, int) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint64_t x = (uint64_t)key[i] << 32 | (uint32_t)~(j + i);
-            best = x > best ? x : best;
+            for (int i = 0; i < SmpRow<T>::W; ++i) {
+                at = x[i] > top ? j + i : at;
+                top = fmaxf(top, x[i]);
+                low = fminf(low, x[i]);
+            }
+        });
+        uint64_t best = top > -INFINITY ? (uint64_t)smp_key(top) << 32 | (uint32_t)~at : 0;
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) {
+            const uint64_t y = __shfl_xor(best, o);
+            best = y > best ? y : best;
+            low = fminf(low, __shfl_xor(low, o));
+        }
+        if ((threadIdx.x & 63) == 0) {
+            atomicMax((unsigned long long *)&sh.best, (unsigned long long)best);
+            atomicMin(&sh.low, smp_key(low));
         }
     }
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-        const uint64_t x = __shfl_xor(best, o);
-        best = x > best ? x : best;
-    }
-    if ((threadIdx.x & 63) == 0) atomicMax((unsigned long long *)&sh.best, (unsigned long long)best);
     __syncthreads();
-    best = sh.best;
-    const uint32_t max_key = (uint32_t)(best >> 32);
+    const uint64_t best = sh.best;
     const float temperature = a.temperature ? a.temperature[r] : 1.f;
-    if (max_key <= SMP_KEY_NONE || !(temperature > 0.f)) {
-        const bool none = max_key <= SMP_KEY_NONE;
+    if (best == 0 || !(temperature > 0.f)) {
         if (threadIdx.x == 0) {
-            a.token[r] = none ? -1 : (int32_t)~(uint32_t)best;
-            if (a.logprob) a.logprob[r] = none ? -INFINITY : 0.f;
-            if (a.kept) a.kept[r] = none ? 0 : 1;
+            a.token[r] = best ? (int32_t)~(uint32_t)best : -1;
+            if (a.logprob) a.logprob[r] = best ? 0.f : -INFINITY;
+            if (a.kept) a.kept[r] = best ? 1 : 0;
         }
         return;
     }
     SmpWeight weight;
-    weight.inv_t = 1. / (double)temperature;
-    weight.max = (double)smp_value(max_key);
-    weight.one = (double)(1ull << a.shift);
-    weight.max_key = max_key;
+    const float max = smp_value((uint32_t)(best >> 32));
+    weight.per_t = max < INFINITY ? 1.4426950408889634 / (double)temperature : 1.;
+    weight.max = max < INFINITY ? (double)max : 1e300;
+    weight.shift = a.shift;
+    weight.pad = 0;
 
-    SmpCut cut = {SMP_KEY_NONE + 1, 0, 0, 0, 0};              // words with keys above, and cut.n of those with cut.key
-    cut.n = cut.of = ~0u;
-    uint64_t total = 0;
-    bool have_total = false;
+    SmpCut cut = {smp_value(SMP_KEY_NONE + 1), row.n, 0};       // every word above -infinity
     const int k = a.top_k ? a.top_k[r] : 0;
-    if (k > 0 && k < row.n) {
-        cut = smp_cut<T, true>(row, weight, (uint32_t)k, 0., sh);
-        if (cut.key <= SMP_KEY_NONE) {                        // fewer than k words above -infinity
-            cut.key = SMP_KEY_NONE + 1;
-            cut.n = cut.of = ~0u;
-        } else {
-            total = cut.above + cut.n * weight(cut.key);
-            have_total = true;
-        }
-    }
     const float p = a.top_p ? a.top_p[r] : 1.f;
-    if (p < 1.f) {
-        if (!have_total) {
-            uint64_t s = 0;
-            for (int j = threadIdx.x * 4; j < row.n; j += SMP_TILE) {
-                uint32_t key[4];
-                row.keys4(j, key);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s += weight(key[i]);
+    const bool by_count = k > 0 && k < row.n;
+    bool by_mass = p < 1.f;
+    if (by_count || by_mass) {
+        SmpSteps step;
+        step.max = fminf(max, FLT_MAX);
+        const float range = fminf(step.max - smp_value(sh.low), (float)(SMP_REACH * (double)temperature));
+        step.per = range > 0.f && range < INFINITY ? fminf((float)SMP_BINS / range, FLT_MAX) : 0.f;
+        if (by_count) {
+            smp_histogram<T, true>(row, weight, step);
+            const SmpAt s = smp_step<true>((uint32_t)k, 0.f, 0);
+            const bool all = s.above + s.here <= SMP_LIST;      // the list holds every word that top-k may keep
+            if (s.here <= SMP_LIST) {
+                uint64_t mass_above = 0;
+                if (by_mass && !all) {
+                    smp_histogram<T, false>(row, weight, step);
+                    uint64_t m = 0;
+                    for (int i = threadIdx.x; i < s.at; i += SMP_THREADS) m += sh.mass[i];
+                    smp_scan(m, &mass_above, sh);
+                }
+                const int n = smp_collect(row, step, all ? 0 : s.at, s.at);
+                smp_sort(n);
+                cut = smp_cut_list<true>(n, weight, (uint32_t)k, 0, mass_above, all ? 0 : (uint32_t)s.above);
+                if (by_mass && all) {
+                    const SmpCut c = smp_cut_list<false>(n, weight, 0, smp_share(p, cut.mass, true), 0, 0);
+                    if (cut.keeps(c.x, c.j)) cut = c;
+                    by_mass = false;
+                }
+            } else {
+                cut = smp_cut_by_digits<T, true>(row, weight, (uint32_t)k, 0);
+                if (by_mass) smp_histogram<T, false>(row, weight, step);
             }
-            smp_scan<uint64_t>(s, sh.tmp, &total);
-            __syncthreads();
+        } else {
+            smp_histogram<T, false>(row, weight, step);
         }
-        const SmpCut c = smp_cut<T, false>(row, weight, 0, (double)p * (double)total, sh);
-        if (c.key > cut.key) cut = c;
-        else if (c.key == cut.key) cut.n = min(cut.n, c.n);
+        if (by_mass) {
+            const SmpAt s = smp_step<false>(0, p, cut.mass);
+            const int n = smp_collect(row, step, s.at, s.at);
+            SmpCut c;
+            if (n <= SMP_LIST) {
+                smp_sort(n);
+                c = smp_cut_list<false>(n, weight, 0, s.need, s.above, 0);
+            } else {
+                c = smp_cut_by_digits<T, false>(row, weight, 0, s.need);
+            }
+            if (cut.keeps(c.x, c.j)) cut = c;
+        }
     }
-    // of words that tie at the cut, the first ones by index
-    int last_tie = row.n;
-    uint64_t sum;
-    if (cut.n < cut.of) {
-        const uint32_t key = cut.key;
-        const uint64_t n = cut.n;
-        last_tie = smp_locate(row, [key](uint32_t x, int) { return (uint64_t)(x == key); }, [n](uint64_t) { return n - 1; }, &sum, sh);
+    // w >= min_p, of the exponents, as a bound of the values (a NaN keeps every word)
+    if (a.min_p) {
+        const double least = fmin(log2((double)a.min_p[r]), 0.);
+        const float x = least > -INFINITY ? smp_least_value(weight, max, least) : -INFINITY;
+        if (x > cut.x) {
+            cut.x = x;
+            cut.j = row.n;
+        }
     }
-    const double floor_e = a.min_p ? log((double)a.min_p[r]) : -INFINITY;      // w >= min_p, of the exponents (a NaN keeps every word)
-    const double u = (double)a.u[r];
-    uint32_t n_kept = 0;
-    bool counting = true;
-    auto kept_weight = [&](uint32_t key, int j) -> uint64_t {
-        if (key < cut.key || (key == cut.key && j > last_tie)) return 0;
-        if (key != max_key && weight.exponent(key) < floor_e) return 0;
-        if (counting) ++n_kept;
-        return weight(key);
-    };
-    int token = smp_locate(row, kept_weight, [&](uint64_t s) {
-        counting = false;
-        const double x = u * (double)s;
-        const uint64_t t = x > 0. ? (uint64_t)x : 0;
-        return t >= s ? s - 1 : t;
-    }, &sum, sh);
-    uint32_t all_kept;
-    smp_scan<uint32_t>(n_kept, (uint32_t *)sh.tmp2, &all_kept);
+    SmpKept f = {};
+    f.cut = cut;
+    f.weight = weight;
+    f.u = a.u[r];
+    const SmpDraw d = smp_locate(row, f);
     if (threadIdx.x == 0) {
-        a.token[r] = token;
-        if (a.logprob) a.logprob[r] = (float)log((double)weight(smp_key((float)row.p[token])) / (double)sum);
-        if (a.kept) a.kept[r] = (int32_t)all_kept;
+        a.token[r] = d.word;
+        if (a.logprob) a.logprob[r] = (float)log((double)d.weight / (double)d.sum);
+        if (a.kept) a.kept[r] = d.kept;
     }
 }
 

@@ -39,8 +39,7 @@ def plain(x, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
         keep[0] = True
         order, w, e = order[keep], w[keep], e[keep]
     if min_p > 0:
-        keep = e >= math.log(min_p)
-        keep[0] = True
+        keep = e >= math.log(min(min_p, 1.0))
         order, w = order[keep], w[keep]
     by = np.argsort(order)
     order, w = order[by], w[by]
@@ -146,6 +145,23 @@ def test_every_word_is_reached():
     mid = (torch.cumsum(w, 0) - w / 2).float()
     got = binding.tl_sample(x.expand(500, -1), mid)           # rows that repeat: stride 0
     assert torch.equal(got["token"], torch.arange(500, dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+def test_steps_of_more_words_than_are_listed(dtype):
+    """Thousands of equal words, or of words so close that a step of the value holds them all, in front of, at and behind the cut."""
+    g = torch.Generator(device="cuda").manual_seed(17)
+    x = (torch.randn(6, 60000, generator=g, device="cuda") * 2).to(TYPES[dtype])
+    x[0, 100:20000] = 1.0
+    x[1, ::2] = 3.0
+    x[2] = 0.5
+    x[3] = torch.where(x[3] < 6, x[3] * 2.0 ** -10, 1000.0)
+    x[4, 5::3] = -1.0
+    x[5, :9000] = 20.0
+    u = torch.rand(6, generator=g, device="cuda")
+    for f in (dict(), dict(top_k=30000), dict(top_p=0.5), dict(top_k=25000, top_p=0.7), dict(top_k=9000, top_p=0.99), dict(top_p=0.97, min_p=1e-4),
+              dict(temperature=1000.0, top_p=0.6), dict(temperature=0.01, top_k=10000, top_p=0.4)):
+        check(x, u, **f)
 
 
 @pytest.mark.parametrize("dtype", sorted(TYPES))
