@@ -20,6 +20,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "treelstm.h"
 
 namespace tl {
@@ -47,13 +49,15 @@ struct AttArgs {
     const int32_t *q_off, *kv_off;
     const uint8_t *mask;
     float *lse;             // [n_q x n_heads], natural logarithm
-    float *delta;           // backward: sum over d of d_o * o, [n_q x n_heads]
+    float *delta, *ref;     // backward: sum over d of d_o * o, and lse in base 2, [n_q x n_heads]
+    int32_t *list, *live;   // backward, with a mask: the nodes that may be read, tree by tree from kv_off on, and how many a tree has
     float *part_o;          // splits > 1: outputs of each part, [splits][n_q x n_heads][D]
     float *part_lse;        // ... and their logarithms, [splits][n_q x n_heads]
     float scale, scale_log2;
     int n_trees, n_q, n_kv, Hq, Hk, G, D;
     int slots;              // row tiles (see find_slot)
     int splits;             // parts that a tree's nodes are cut into
+    int near;               // 128 rows of any input span less than 2^31 bytes
     int vec;                // rows of q, k, v (and of what a backward pass reads) may be read in 16-byte pieces
     int vec_out;            // ... and the outputs written so
 };
@@ -137,11 +141,28 @@ template <typename T, int DP> struct Rows {
     __device__ static int at(int r, int g) { return ((r * GPR + g) ^ turn(r)) << 4; }
 };
 
-// Operand of a product over D: row r of a tile, k-step s.
-template <typename T, int DP> __device__ inline typename Elem<T>::frag row_frag(const unsigned char *tile, int r, int s, int half)
-{
-    return *reinterpret_cast<const typename Elem<T>::frag *>(tile + Rows<T, DP>::at(r, 2 * s + half));
-}
+#define ATT_LDS __attribute__((address_space(3)))
+__device__ inline uint32_t lds_address(const unsigned char *p) { return (uint32_t)(uintptr_t)(const ATT_LDS unsigned char *)p; }
+
+// Operands of products over D: row r0 + l % 32 of a tile, k-step s.  at[s] is the lane's place for r0 = 0; further rows are a constant away (r0 a
+// multiple of 16, after which the exchange repeats), so that a read is one instruction.
+template <typename T, int DP> struct RowReads {
+    typedef typename Elem<T>::frag frag;
+    typedef Rows<T, DP> R;
+    uint32_t at[R::STEPS];
+    __device__ explicit RowReads(const unsigned char *tile)
+    {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int s = 0; s < R::STEPS; ++s) at[s] = lds_address(tile) + R::at(lane & 31, 2 * s + (lane >> 5));
+    }
+    __device__ void move(int bytes)
+    {
+#pragma unroll
+        for (int s = 0; s < R::STEPS; ++s) at[s] += bytes;
+    }
+    __device__ frag get(int r0, int s) const { return *(const ATT_LDS frag *)(uintptr_t)(at[s] + r0 * R::BYTES); }
+};
 
 __device__ inline void mma(floatx16 &c, f32x4 a, f32x4 b)
 {
@@ -151,83 +172,118 @@ __device__ inline void mma(floatx16 &c, f32x4 a, f32x4 b)
 __device__ inline void mma(floatx16 &c, bf16x8 a, bf16x8 b) { c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ inline void mma(floatx16 &c, f16x8 a, f16x8 b) { c = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
-typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
+typedef ATT_LDS s16x4 *lds_s16x4;
 
-// Four rows of a 16-bit tile, row0 + 4 half .. + 3 of column d0 + l % 32 in lane l.
-template <typename T, int DP> __device__ inline s16x4 column4(const unsigned char *tile, int row0, int d0, int lane)
-{
-    const int i = lane & 15;
-    const int r = row0 + 4 * (lane >> 5) + (i >> 2);
-    const int g = d0 / 8 + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-    const unsigned char *p = tile + Rows<T, DP>::at(r, g) + 8 * (i & 1);
-    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p);
-}
+// Operands of products over the rows of a tile: its columns.  16-bit types: four rows r0 + 4 half .. + 3 (and those 8 further) of column
+// d0 + l % 32 by the transposing read; fp32: one element of row r0 + 8 (r / 4) + 4 half + r % 4.
+template <typename T, int DP> struct ColumnReads {
+    typedef Rows<T, DP> R;
+    static constexpr int KINDS = sizeof(T) == 2 ? 2 : 8;                        // rows whose exchange differs
+    static constexpr int WIDE = sizeof(T) == 2 ? 4 : 2;                         // column tiles until the exchange repeats
+    static constexpr int TILES = DP / 32 < WIDE ? DP / 32 : WIDE;
+    uint32_t at[KINDS][TILES];
+    __device__ explicit ColumnReads(const unsigned char *tile, int d_first)
+    {
+        const int lane = threadIdx.x & 63, half = lane >> 5;
+#pragma unroll
+        for (int k = 0; k < KINDS; ++k)
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                if constexpr (sizeof(T) == 2) {
+                    const int i = lane & 15;
+                    const int r = 8 * k + 4 * half + (i >> 2), g = (d_first + 32 * t) / 8 + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+                    at[k][t] = lds_address(tile) + R::at(r, g) + 8 * (i & 1);
+                } else {
+                    const int r = 8 * (k >> 2) + 4 * half + (k & 3), d = d_first + 32 * t + (lane & 31);
+                    at[k][t] = lds_address(tile) + R::at(r, d >> 2) + 4 * (d & 3);
+                }
+            }
+    }
+    __device__ void move(int bytes)
+    {
+#pragma unroll
+        for (int k = 0; k < KINDS; ++k)
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) at[k][t] += bytes;
+    }
+    // rows from r0 (a multiple of 16) on, column tile t
+    __device__ uint32_t place(int k, int t, int r0) const { return at[k][t % WIDE] + (t / WIDE) * WIDE * 32 * (int)sizeof(T) + r0 * R::BYTES; }
+    __device__ s16x4 four(int k, int t, int r0) const { return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)place(k, t, r0)); }
+    __device__ float one(int r, int t, int r0) const { return *(const ATT_LDS float *)(uintptr_t)place(r & 7, t, r0 + (r & 8) * 2); }
+};
 
-// c[t] += sum over 32 rows of tile^T (columns d_first + 32 t ..) times w, whose register r belongs to row row0 + 8 (r / 4) + 4 half + r % 4.
+// c[q][t] += sum over the 32 rows from r0 on of tile^T (column tile t) times w[q], whose register r belongs to row r0 + 8 (r / 4) + 4 half + r % 4.
 // 16-bit types: w is rounded to the type, as an operand of the matrix unit has to be (relative 2^-9 or 2^-12 of a probability or of a
 // score's gradient, the size of the inputs' own roundings); sums stay in fp32.
-template <typename T, int DP, int NT> __device__ inline void mma_columns(floatx16 (&c)[NT], const unsigned char *tile, int row0, const floatx16 &w,
-                                                                         int d_first, int lane)
+template <typename T, int DP, int NQ, int NT>
+__device__ inline void mma_columns(floatx16 (&c)[NQ][NT], const ColumnReads<T, DP> &tile, int r0, const floatx16 (&w)[NQ])
 {
     if constexpr (sizeof(T) == 2) {
         typedef typename Elem<T>::frag frag;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            frag b;
+            frag b[NQ];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) b[j] = (T)w[8 * s + j];
+            for (int q = 0; q < NQ; ++q)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) b[q][j] = (T)w[q][8 * s + j];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                const s16x4 lo = column4<T, DP>(tile, row0 + 16 * s, d_first + 32 * t, lane);
-                const s16x4 hi = column4<T, DP>(tile, row0 + 16 * s + 8, d_first + 32 * t, lane);
-                frag a = __builtin_bit_cast(frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-                mma(c[t], a, b);
+                const frag a = __builtin_bit_cast(frag, __builtin_shufflevector(tile.four(0, t, r0 + 16 * s), tile.four(1, t, r0 + 16 * s), 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                for (int q = 0; q < NQ; ++q) mma(c[q][t], a, b[q]);
             }
         }
     } else {
-        const int half = lane >> 5, col = d_first + (lane & 31);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int row = row0 + 8 * (r >> 2) + 4 * half + (r & 3);
+        for (int r = 0; r < 16; ++r)
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                const int d = col + 32 * t;
-                const float a = *reinterpret_cast<const float *>(tile + Rows<T, DP>::at(row, d >> 2) + 4 * (d & 3));
-                c[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[r], c[t], 0, 0, 0);
+                const float a = tile.one(r, t, r0);
+#pragma unroll
+                for (int q = 0; q < NQ; ++q) c[q][t] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[q][r], c[q][t], 0, 0, 0);
             }
-        }
     }
 }
 
 // ---- global memory ----------------------------------------------------------------------
 
+// (Pointers out of the argument struct are cast to global memory: through generic ones loads and LDS reads would wait for each other.)
+#define ATT_GLOBAL __attribute__((address_space(1)))
+
 // Granule g of a row of D elements (zeros beyond D).
-template <typename T> __device__ inline u32x4 load_granule(const T *__restrict__ row, int g, int D, bool vec)
+template <typename T> __device__ inline u32x4 load_granule(const T *row, int g, int D, bool vec)
 {
     constexpr int E = 16 / (int)sizeof(T);
+    const ATT_GLOBAL T *p = (const ATT_GLOBAL T *)row;
     u32x4 x = {0u, 0u, 0u, 0u};
     const int d = g * E;
     if (vec) {
-        if (d < D) x = *reinterpret_cast<const u32x4 *>(row + d);
+        if (d < D) x = *(const ATT_GLOBAL u32x4 *)(p + d);
     } else {
         T e[E];
 #pragma unroll
-        for (int j = 0; j < E; ++j) e[j] = d + j < D ? row[d + j] : (T)0.f;
+        for (int j = 0; j < E; ++j) {
+            const T y = p[min(d + j, D - 1)];
+            e[j] = d + j < D ? y : (T)0.f;
+        }
         __builtin_memcpy(&x, e, 16);
     }
     return x;
 }
 
 // Four consecutive elements from d on.
-template <typename T> __device__ inline void store4(T *__restrict__ row, int d, int D, bool vec, float a, float b, float c, float e)
+template <typename T> __device__ inline void store4(T *row, int d, int D, bool vec, float a, float b, float c, float e)
 {
-    T x[4] = {(T)a, (T)b, (T)c, (T)e};
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    const T4 x = {(T)a, (T)b, (T)c, (T)e};
+    ATT_GLOBAL T *p = (ATT_GLOBAL T *)row;
     if (vec) {
-        if (d < D) __builtin_memcpy(__builtin_assume_aligned(row + d, 4 * sizeof(T)), x, 4 * sizeof(T));
+        if (d < D) *(ATT_GLOBAL T4 *)(p + d) = x;
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            if (d + j < D) row[d + j] = x[j];
+            if (d + j < D) p[d + j] = x[j];
     }
 }
 
@@ -236,86 +292,200 @@ template <typename T> __device__ inline T *row_of(const AttTensor &a, long long 
     return static_cast<T *>(a.p) + row * a.row + (long long)head * a.head;
 }
 
-__device__ inline float other_half(float x)
+// What lane l ^ 32 holds, joined with the lane's own.
+__device__ inline float max_of_halves(float x)
 {
-    return __shfl_xor(x, 32);
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+__device__ inline float sum_of_halves(float x)
+{
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    return __uint_as_float(y[0]) + __uint_as_float(y[1]);
 }
 
-// ---- staging of node rows -----------------------------------------------------------------
+// ---- staging straight into LDS ------------------------------------------------------------
 
-// A workgroup's share of a tile of N node rows of K and of V: requested into registers (request), put into LDS later (put).  Rows
-// that may not be read become zeros where a product would sum over them (zero_k, zero_v): whatever they hold, a NaN among it, times a
-// probability of zero must not reach a sum.  Rows beyond the tree are read from its last row.
-template <typename T, int DP, int N> struct NodeTile {
+static __device__ const u32x4 att_zeros[1] = {};
+
+// 16 bytes a lane from global memory to LDS, lane l's at lds + 16 l; nothing passes through registers.  The hardware counts it with the vector
+// loads; stage_wait() waits for it.  (Written out because the compiler, given its builtin, waits in front of every LDS read that follows.  It has no
+// output register that could be reused too early, and what the compiler counts itself only becomes stricter by it.)
+__device__ inline void stage_16(uint32_t lds, const void *p)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory");
+}
+__device__ inline void stage_16(uint32_t lds, const void *base, uint32_t offset)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+}
+// 4 bytes a lane.
+__device__ inline void stage_4(uint32_t lds, const void *p)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(p) : "memory");
+}
+// Makes the compiler wait for loads into x here.  Without it, it waits at their first use: inside a loop in every pass, and then for what is
+// being staged as well.
+template <typename F, int N> __device__ inline void arrived(F (&x)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
+}
+__device__ inline void stage_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// Which granule of a tile of N rows belongs at a thread's i-th place: the exchange is its own inverse within 256 bytes.
+template <typename T, int DP> __device__ inline void place_of(int slot, int *row, int *granule)
+{
     typedef Rows<T, DP> R;
-    static constexpr int GRANULES = N * R::GPR;
-    static constexpr int EACH = (GRANULES + ATT_THREADS - 1) / ATT_THREADS;
-    u32x4 k[EACH], v[EACH];
-    unsigned live;
+    const int line = R::GPR >= 16 ? slot / R::GPR : (slot >> 4) * (16 / R::GPR);
+    const int e = slot ^ R::turn(line);
+    *row = e / R::GPR;
+    *granule = e % R::GPR;
+}
 
-    __device__ void request(const T *__restrict__ kp, const T *__restrict__ vp, const AttArgs &a, int first, int lo, int hi)
+// Tiles of N rows that follow one another in memory at one distance, whole in D: a thread's places are the same in every tile, so that only the
+// tile's base moves, in scalar registers.
+template <typename T, int DP, int N, int THREADS> struct NearRows {
+    static constexpr int GRANULES = N * Rows<T, DP>::GPR, EACH = (GRANULES + THREADS - 1) / THREADS;
+    uint32_t offset[EACH];
+    __device__ explicit NearRows(long long row)
     {
-        live = 0;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            const int e = threadIdx.x + i * ATT_THREADS;
-            if (GRANULES % ATT_THREADS == 0 || e < GRANULES) {
-                const int r = e / R::GPR, g = e % R::GPR;
-                const int node = min(first + r, hi - 1);
-                const bool in = first + r < hi && (!a.mask || a.mask[node] != 0);
-                live |= in ? 1u << i : 0u;
-                k[i] = load_granule<T>(kp + (long long)node * a.k.row, g, a.D, a.vec);
-                v[i] = load_granule<T>(vp + (long long)node * a.v.row, g, a.D, a.vec);
-            }
+            int r, g;
+            place_of<T, DP>(i * THREADS + threadIdx.x, &r, &g);
+            offset[i] = (uint32_t)r * (uint32_t)row * (uint32_t)sizeof(T) + g * 16;
         }
     }
-    template <bool ZERO_K, bool ZERO_V> __device__ void put(unsigned char *kt, unsigned char *vt)
+    __device__ void stage(unsigned char *tile, const T *first) const
     {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const uint32_t base = lds_address(tile) + wave * 1024;
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const int e = threadIdx.x + i * ATT_THREADS;
-            if (GRANULES % ATT_THREADS == 0 || e < GRANULES) {
-                const int at = R::at(e / R::GPR, e % R::GPR);
-                const bool in = live >> i & 1;
-                const u32x4 zero = {0u, 0u, 0u, 0u};
-                *reinterpret_cast<u32x4 *>(kt + at) = ZERO_K && !in ? zero : k[i];
-                *reinterpret_cast<u32x4 *>(vt + at) = ZERO_V && !in ? zero : v[i];
-            }
-        }
+        for (int i = 0; i < EACH; ++i)
+            if (GRANULES % THREADS == 0 || i * THREADS + wave * 64 < GRANULES) stage_16(base + i * THREADS * 16, first, offset[i]);
     }
 };
 
-// Which of 64 nodes from `first` on may be read (the same word in every lane).
-__device__ inline unsigned long long live_nodes(const AttArgs &a, int first, int hi)
+// Puts N rows into a tile; row(r) gives where row r lies, or nothing for a row of zeros.  VEC: asynchronously (stage_wait and a barrier before
+// it is read); else the rows are read element by element and are there after a barrier.
+template <typename T, int DP, int N, int THREADS, bool VEC, typename F> __device__ inline void stage_rows(unsigned char *tile, int D, F row)
 {
-    const int node = first + (threadIdx.x & 63);
-    return __ballot(node < hi && (!a.mask || a.mask[min(node, hi - 1)] != 0));
+    typedef Rows<T, DP> R;
+    constexpr int GRANULES = N * R::GPR, EACH = (GRANULES + THREADS - 1) / THREADS;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t base = lds_address(tile) + wave * 1024;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        if (GRANULES % THREADS != 0 && i * THREADS + wave * 64 >= GRANULES) continue;
+        const int slot = i * THREADS + threadIdx.x;
+        int r, g;
+        place_of<T, DP>(slot, &r, &g);
+        const T *p = row(r);
+        if constexpr (VEC) {
+            const void *from = p && g * R::EPG < D ? (const void *)(p + g * R::EPG) : (const void *)att_zeros;
+            stage_16(base + i * THREADS * 16, from);
+        } else {
+            *reinterpret_cast<u32x4 *>(tile + slot * 16) = p ? load_granule<T>(p, g, D, false) : u32x4{0u, 0u, 0u, 0u};
+        }
+    }
 }
+
+// The nodes of a tree, or of a part of it, that may be read, up to BN at a time.  With a mask their numbers go through a ring in LDS, filled
+// from 4 THREADS mask bytes at a time, so that masked nodes cost neither a place in a tile nor a read.
+template <int BN, int THREADS> struct Nodes {
+    static constexpr int RING = 2048;
+    static constexpr int LDS = RING * 4 + 64;
+    static_assert(BN + 4 * THREADS <= RING, "room for what is left and a filling");
+    const ATT_GLOBAL uint8_t *mask;
+    int at, hi;                 // the next node to look at, the end
+    int first, n;               // the current stage: its first node, or place in the ring
+    int tail;                   // end of the ring's filling
+    int *ring, *counts;
+
+    __device__ void begin(const AttArgs &a, int from, int to, unsigned char *lds)
+    {
+        mask = (const ATT_GLOBAL uint8_t *)a.mask;
+        at = from;
+        hi = to;
+        first = n = tail = 0;
+        ring = reinterpret_cast<int *>(lds);
+        counts = ring + RING;
+    }
+    // The next stage; how many nodes it has.  Everyone must call it.
+    __device__ int next()
+    {
+        if (!mask) {
+            first = at;
+            n = max(min(BN, hi - at), 0);
+            at += n;
+            return n;
+        }
+        first += n;
+        while (tail - first < BN && at < hi) {
+            const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+            const int mine = at + 4 * threadIdx.x;
+            unsigned bits = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint8_t m = mask[min(mine + j, hi - 1)];
+                bits |= mine + j < hi && m ? 1u << j : 0u;
+            }
+            int upto = __popc(bits);
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int y = __shfl_up(upto, o);
+                upto += lane >= o ? y : 0;
+            }
+            __syncthreads();                                    // (the ring's last reads, and counts', are over)
+            if (lane == 63) counts[wave] = upto;
+            __syncthreads();
+            int place = tail + upto - __popc(bits), all = 0;
+#pragma unroll
+            for (int w = 0; w < THREADS / 64; ++w) {
+                place += w < wave ? counts[w] : 0;
+                all += counts[w];
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (bits >> j & 1) ring[place++ & (RING - 1)] = mine + j;
+            tail += __builtin_amdgcn_readfirstlane(all);
+            at += 4 * THREADS;
+            __syncthreads();
+        }
+        n = min(BN, tail - first);
+        return n;
+    }
+    // Number of the stage's r-th node.
+    __device__ int node(int r) const { return mask ? ring[(first + r) & (RING - 1)] : first + r; }
+};
 
 // ---- forward ------------------------------------------------------------------------------
 
-// WM waves side by side along the rows (32 packed rows each), WK waves along the nodes; NT node tiles of 32 per wave and stage.
-// Rows of trees with many queries: WM = 4, every wave reads all nodes of a stage.  Few queries (a single token): WM = 1, the four waves
-// share one tile of rows, each takes a quarter of the nodes, and their sums are joined at the end.
-template <typename T, int DP, int WM> struct AttFwd {
-    static constexpr int WK = ATT_WAVES / WM;
-    static constexpr int NT = WM > 1 && DP * (int)sizeof(T) <= 256 ? 2 : 1;
+// Four waves: WM side by side along the rows, 32 packed rows each, and WK = 4 / WM along the nodes, whose sums are joined at the end; NT node tiles
+// of 32 per wave and stage.
+template <typename T, int DP, int WM_> struct AttFwd {
+    static constexpr int THREADS = ATT_THREADS;
+    static constexpr int WM = WM_, WK = ATT_WAVES / WM;
+    static constexpr int NT = WM == 4 && DP * (int)sizeof(T) <= 256 ? 2 : 1;
     static constexpr int BM = 32 * WM;
     static constexpr int BN = 32 * WK * NT;
     static constexpr int STAGE = 2 * BN * Rows<T, DP>::BYTES;
     static constexpr int BUFS = STAGE <= 32768 ? 2 : 1;
-    static constexpr int JOIN = WK > 1 ? WK * 32 * (DP + 4) * 4 + WK * 64 * 4 : 0;
-    static constexpr int LDS = STAGE * BUFS > JOIN ? STAGE * BUFS : JOIN;
-    static constexpr int MIN_BLOCKS = DP * (int)sizeof(T) > 256 ? 1 : 2;
+    static constexpr int JOIN = WK > 1 ? ATT_WAVES * 32 * (DP + 4) * 4 + ATT_WAVES * 64 * 4 : 0;
+    static constexpr int LIST = STAGE * BUFS > JOIN ? STAGE * BUFS : JOIN;    // place of the nodes' ring
+    static constexpr int LDS = LIST + Nodes<BN, THREADS>::LDS;
+    static constexpr int MIN_WAVES = DP * (int)sizeof(T) > 256 ? 1 : 2;
 };
 
-template <typename T, int DP, int WM>
-__global__ __launch_bounds__(ATT_THREADS, (AttFwd<T, DP, WM>::MIN_BLOCKS)) void k_attend(const AttArgs a)
+template <typename T, int DP, int WM, bool VEC>
+__global__ __launch_bounds__(ATT_THREADS, (AttFwd<T, DP, WM>::MIN_WAVES)) void k_attend(const AttArgs a)
 {
     typedef AttFwd<T, DP, WM> C;
     typedef Rows<T, DP> R;
     typedef typename Elem<T>::frag frag;
-    constexpr int WK = C::WK, NT = C::NT, DT = DP / 32;
+    constexpr int WK = C::WK, NT = C::NT, DT = DP / 32, THREADS = C::THREADS;
     extern __shared__ __align__(16) unsigned char att_lds[];
 
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
@@ -323,21 +493,21 @@ __global__ __launch_bounds__(ATT_THREADS, (AttFwd<T, DP, WM>::MIN_BLOCKS)) void 
     const long long id = xcd_order(blockIdx.x, gridDim.x);
     const int slot = (int)(id % a.slots), part = (int)(id / a.slots % a.splits), hk = (int)(id / a.slots / a.splits);
     long long tile;
-    const int tree = find_slot(a.q_off, a.n_trees, a.G, C::BM == 32 ? 5 : 7, slot, &tile);
+    const int tree = find_slot(a.q_off, a.n_trees, a.G, C::BM == 32 ? 5 : C::BM == 64 ? 6 : 7, slot, &tile);
     int q_lo, q_hi, lo, hi;
     tree_range(a.q_off, tree, a.n_q, &q_lo, &q_hi);
     const long long n_rows = (long long)(q_hi - q_lo) * a.G, m0 = tile * C::BM;
     if (tile < 0 || m0 >= n_rows) return;
     tree_range(a.kv_off, tree, a.n_kv, &lo, &hi);
-    const int n_stage = (hi - lo + C::BN - 1) / C::BN;
-    int s_lo = 0, s_hi = n_stage;
     if (a.splits > 1) {
-        const int per = (n_stage + a.splits - 1) / a.splits;
-        s_lo = min(part * per, n_stage);
-        s_hi = min(s_lo + per, n_stage);
+        const int n_stage = (hi - lo + C::BN - 1) / C::BN, per = (n_stage + a.splits - 1) / a.splits;
+        const int s_lo = min(part * per, n_stage), s_hi = min(s_lo + per, n_stage);
         if (s_lo >= s_hi) return;
+        hi = min(hi, lo + s_hi * C::BN);
+        lo += s_lo * C::BN;
     }
 
+    // the lane's query (a row beyond the last one repeats the first: its results are not stored)
     const long long m = m0 + 32 * wm + col;
     const bool mine = m < n_rows;
     const int qi = q_lo + (int)((mine ? m : m0) / a.G), head = hk * a.G + (int)((mine ? m : m0) % a.G);
@@ -345,145 +515,162 @@ __global__ __launch_bounds__(ATT_THREADS, (AttFwd<T, DP, WM>::MIN_BLOCKS)) void 
     {
         const T *qr = row_of<T>(a.q, qi, head);
 #pragma unroll
-        for (int s = 0; s < R::STEPS; ++s) qf[s] = __builtin_bit_cast(frag, load_granule<T>(qr, 2 * s + half, a.D, a.vec));
+        for (int s = 0; s < R::STEPS; ++s) qf[s] = __builtin_bit_cast(frag, load_granule<T>(qr, 2 * s + half, a.D, VEC));
     }
-
-    floatx16 acc[DT];
-#pragma unroll
-    for (int t = 0; t < DT; ++t) acc[t] = floatx16{};
+    floatx16 acc[1][DT];
     float top = -INFINITY, sum = 0.f;          // largest raw score so far (of the lane's query), sum of the lane's half of its nodes
+#pragma unroll
+    for (int t = 0; t < DT; ++t) acc[0][t] = floatx16{};
 
     const T *kp = row_of<T>(a.k, 0, hk), *vp = row_of<T>(a.v, 0, hk);
-    NodeTile<T, DP, C::BN> st;
-    if (s_lo < s_hi) {
-        st.request(kp, vp, a, lo + s_lo * C::BN, lo, hi);
-        st.template put<false, true>(att_lds, att_lds + C::STAGE / 2);
-    }
-    for (int s = s_lo; s < s_hi; ++s) {
-        const int first = lo + s * C::BN;
-        const unsigned char *kt = att_lds + (C::BUFS == 2 ? ((s - s_lo) & 1) * C::STAGE : 0), *vt = kt + C::STAGE / 2;
-        __syncthreads();
-        if (s + 1 < s_hi) st.request(kp, vp, a, first + C::BN, lo, hi);
-        const int w_first = first + 32 * NT * wk;
-        const unsigned long long live = live_nodes(a, w_first, hi);
-        if (w_first < hi) {
-            floatx16 p[NT];
+    Nodes<C::BN, THREADS> nodes;
+    nodes.begin(a, lo, hi, att_lds + C::LIST);
+    const bool near = VEC && !a.mask && a.near && a.D == DP;
+    const NearRows<T, DP, C::BN, THREADS> k_near(a.k.row), v_near(a.v.row);
+    auto stage = [&](unsigned char *b) {
+        if (near && nodes.n == C::BN) {
+            k_near.stage(b, kp + nodes.first * a.k.row);
+            v_near.stage(b + C::STAGE / 2, vp + nodes.first * a.v.row);
+            return;
+        }
+        stage_rows<T, DP, C::BN, THREADS, VEC>(b, a.D, [&](int r) { return r < nodes.n ? kp + nodes.node(r) * a.k.row : (const T *)nullptr; });
+        stage_rows<T, DP, C::BN, THREADS, VEC>(b + C::STAGE / 2, a.D, [&](int r) { return r < nodes.n ? vp + nodes.node(r) * a.v.row : (const T *)nullptr; });
+    };
+    RowReads<T, DP> kr(att_lds + 32 * NT * wk * R::BYTES);
+    ColumnReads<T, DP> vc(att_lds + C::STAGE / 2 + 32 * NT * wk * R::BYTES, 0);
+    // one stage of n nodes; the wave's own are those from 32 NT wk on.  TAIL: some of them may be missing.
+    auto compute = [&](auto tail, int n) {
+        constexpr bool TAIL = decltype(tail)::value;
+        const int left = n - 32 * NT * wk;
+        if (TAIL && left <= 0) return;
+        floatx16 p[NT][1];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                p[t] = floatx16{};
+        for (int t = 0; t < NT; ++t) p[t][0] = floatx16{};
 #pragma unroll
-                for (int d = 0; d < R::STEPS; ++d) mma(p[t], row_frag<T, DP>(kt, 32 * (NT * wk + t) + col, d, half), qf[d]);
-            }
-            const unsigned long long all = NT == 2 ? ~0ull : 0xffffffffull;
-            if ((live & all) != all) {
+        for (int d = 0; d < R::STEPS; ++d)
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const unsigned w = (unsigned)(live >> (32 * t)) >> (4 * half);
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (!(w >> (8 * (r >> 2) + (r & 3)) & 1)) p[t][r] = -INFINITY;
-                }
-            }
-            float high = top;
+            for (int t = 0; t < NT; ++t) mma(p[t][0], kr.get(32 * t, d), qf[d]);
+        if (TAIL) {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) high = fmaxf(high, p[t][r]);
-            high = fmaxf(high, other_half(high));
-            const float ref = high == -INFINITY ? 0.f : high * a.scale_log2;
-            if (__any(high > top)) {
-                const float f = __builtin_amdgcn_exp2f(top == high ? 0.f : top * a.scale_log2 - ref);
-                sum *= f;
+                for (int r = 0; r < 16; ++r)
+                    if (32 * t + 8 * (r >> 2) + 4 * half + (r & 3) >= left) p[t][0][r] = -INFINITY;
+        }
+        float high = top;
 #pragma unroll
-                for (int t = 0; t < DT; ++t)
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) acc[t][r] *= f;
-                top = high;
-            }
+            for (int r = 0; r < 16; ++r) high = fmaxf(high, p[t][0][r]);
+        high = max_of_halves(high);
+        const float ref = high == -INFINITY ? 0.f : high * a.scale_log2;
+        if (__any(high > top)) {
+            const float f = __builtin_amdgcn_exp2f(top == high ? 0.f : top * a.scale_log2 - ref);
+            sum *= f;
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
+            for (int t = 0; t < DT; ++t)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    p[t][r] = __builtin_amdgcn_exp2f(fmaf(p[t][r], a.scale_log2, -ref));
-                    sum += p[t][r];
-                }
-                mma_columns<T, DP, DT>(acc, vt, 32 * (NT * wk + t), p[t], 0, lane);
+                for (int r = 0; r < 16; ++r) acc[0][t][r] *= f;
+            top = high;
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                p[t][0][r] = __builtin_amdgcn_exp2f(fmaf(p[t][0][r], a.scale_log2, -ref));
+                sum += p[t][0][r];
             }
         }
-        if (C::BUFS == 1) __syncthreads();
-        if (s + 1 < s_hi) {
-            unsigned char *nk = att_lds + (C::BUFS == 2 ? ((s + 1 - s_lo) & 1) * C::STAGE : 0);
-            st.template put<false, true>(nk, nk + C::STAGE / 2);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+            if (!TAIL || 32 * t < left) mma_columns<T, DP, 1, DT>(acc, vc, 32 * t, p[t]);
+    };
+    int n = nodes.next(), odd = 0;
+    if (n) stage(att_lds);
+    arrived(qf);
+    while (n == C::BN) {                                        // (all stages but the last are full)
+        if (VEC) stage_wait();
+        __syncthreads();
+        n = nodes.next();
+        if (C::BUFS == 2 && n) stage(att_lds + (odd ? 0 : C::STAGE));
+        compute(std::false_type{}, C::BN);
+        if (C::BUFS == 1) {
+            __syncthreads();
+            if (n) stage(att_lds);
+        } else {
+            kr.move(odd ? -C::STAGE : C::STAGE);
+            vc.move(odd ? -C::STAGE : C::STAGE);
         }
+        odd ^= 1;
     }
-    sum += other_half(sum);
+    if (n) {
+        if (VEC) stage_wait();
+        __syncthreads();
+        compute(std::true_type{}, n);
+    }
+    sum = sum_of_halves(sum);
 
-    const long long row_head = (long long)qi * a.Hq + head;
     const bool partial = a.splits > 1;
+    // one query's result: four of its columns, from d on
+    auto store = [&](int i, int hd, int d, float inv, const f32x4 &x) {
+        if (partial)
+            store4<float>(a.part_o + ((long long)part * a.n_q * a.Hq + (long long)i * a.Hq + hd) * a.D, d, a.D, (a.D & 3) == 0, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+        else
+            store4<T>(row_of<T>(a.o, i, hd), d, a.D, a.vec_out, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+    };
+    auto store_lse = [&](int i, int hd, bool any, float highest, float total) {
+        const float lse = any ? (highest * a.scale_log2 + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
+        const long long rh = (long long)i * a.Hq + hd;
+        if (partial) a.part_lse[(long long)part * a.n_q * a.Hq + rh] = lse;
+        else if (a.lse) a.lse[rh] = lse;
+    };
     if constexpr (WK == 1) {
         if (!mine) return;
-        const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-        const float lse = sum > 0.f || sum != sum ? (top * a.scale_log2 + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f : -INFINITY;
-        if (half == 0) {
-            if (partial) a.part_lse[(long long)part * a.n_q * a.Hq + row_head] = lse;
-            else if (a.lse) a.lse[row_head] = lse;
-        }
-        float *po = partial ? a.part_o + ((long long)part * a.n_q * a.Hq + row_head) * a.D : nullptr;
-        T *o = row_of<T>(a.o, qi, head);
+        const bool any = sum > 0.f || sum != sum;
+        const float inv = any ? 1.f / sum : 0.f;
+        if (half == 0) store_lse(qi, head, any, top, sum);
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int d = 32 * t + 2 * r + 4 * half;
-                if (partial) store4<float>(po, d, a.D, (a.D & 3) == 0, acc[t][r] * inv, acc[t][r + 1] * inv, acc[t][r + 2] * inv, acc[t][r + 3] * inv);
-                else store4<T>(o, d, a.D, a.vec_out, acc[t][r] * inv, acc[t][r + 1] * inv, acc[t][r + 2] * inv, acc[t][r + 3] * inv);
-            }
+            for (int r = 0; r < 16; r += 4)
+                store(qi, head, 32 * t + 2 * r + 4 * half, inv, f32x4{acc[0][t][r], acc[0][t][r + 1], acc[0][t][r + 2], acc[0][t][r + 3]});
     } else {
         // the waves' sums over their nodes, brought to one maximum
-        float *jo = reinterpret_cast<float *>(att_lds), *jt = jo + WK * 32 * (DP + 4), *js = jt + WK * 32;
+        float *jo = reinterpret_cast<float *>(att_lds), *jt = jo + ATT_WAVES * 32 * (DP + 4), *js = jt + ATT_WAVES * 32;
+        const int mine_at = (wk * WM + wm) * 32 + col;
         __syncthreads();
         if (half == 0) {
-            jt[wk * 32 + col] = top;
-            js[wk * 32 + col] = sum;
+            jt[mine_at] = top;
+            js[mine_at] = sum;
         }
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
             for (int r = 0; r < 16; r += 4)
-                *reinterpret_cast<f32x4 *>(jo + (wk * 32 + col) * (DP + 4) + 32 * t + 2 * r + 4 * half) =
-                    f32x4{acc[t][r], acc[t][r + 1], acc[t][r + 2], acc[t][r + 3]};
+                *reinterpret_cast<f32x4 *>(jo + mine_at * (DP + 4) + 32 * t + 2 * r + 4 * half) =
+                    f32x4{acc[0][t][r], acc[0][t][r + 1], acc[0][t][r + 2], acc[0][t][r + 3]};
         __syncthreads();
         constexpr int G4 = DP / 4;
-        const int n_here = (int)min((long long)32, n_rows - m0);
-        for (int e = threadIdx.x; e < n_here * G4; e += ATT_THREADS) {
+        const int n_here = (int)min((long long)C::BM, n_rows - m0);
+        for (int e = threadIdx.x; e < n_here * G4; e += THREADS) {
             const int r = e / G4, d = 4 * (e % G4);
-            float tt = -INFINITY;
+            float tt = -INFINITY, total = 0.f;
 #pragma unroll
-            for (int w = 0; w < WK; ++w) tt = fmaxf(tt, jt[w * 32 + r]);
-            float total = 0.f;
+            for (int w = 0; w < WK; ++w) tt = fmaxf(tt, jt[w * C::BM + r]);
             f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < WK; ++w) {
-                const float tw = jt[w * 32 + r];
+                const float tw = jt[w * C::BM + r];
                 const float f = tw == tt ? 1.f : __builtin_amdgcn_exp2f((tw - tt) * a.scale_log2);
-                total += f * js[w * 32 + r];
-                const f32x4 y = *reinterpret_cast<const f32x4 *>(jo + (w * 32 + r) * (DP + 4) + d);
+                total += f * js[w * C::BM + r];
+                const f32x4 y = *reinterpret_cast<const f32x4 *>(jo + (w * C::BM + r) * (DP + 4) + d);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x[j] += f * y[j];
             }
             const bool any = total > 0.f || total != total;
-            const float inv = any ? 1.f / total : 0.f;
             const int i = q_lo + (int)((m0 + r) / a.G), hd = hk * a.G + (int)((m0 + r) % a.G);
-            const long long rh = (long long)i * a.Hq + hd;
-            if (d == 0) {
-                const float lse = any ? (tt * a.scale_log2 + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
-                if (partial) a.part_lse[(long long)part * a.n_q * a.Hq + rh] = lse;
-                else if (a.lse) a.lse[rh] = lse;
-            }
-            if (partial)
-                store4<float>(a.part_o + ((long long)part * a.n_q * a.Hq + rh) * a.D, d, a.D, (a.D & 3) == 0, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
-            else
-                store4<T>(row_of<T>(a.o, i, hd), d, a.D, a.vec_out, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+            if (d == 0) store_lse(i, hd, any, tt, total);
+            store(i, hd, d, any ? 1.f / total : 0.f, x);
         }
     }
 }
@@ -525,54 +712,92 @@ template <typename T> __global__ __launch_bounds__(ATT_THREADS) void k_attend_jo
 
 // ---- backward -----------------------------------------------------------------------------
 
-// delta[i] = d_o[i] . o[i]: 16 lanes per query and head.
-template <typename T> __global__ __launch_bounds__(ATT_THREADS) void k_attend_delta(const AttArgs a)
-{
-    const int l16 = threadIdx.x & 15;
-    const long long rh = ((long long)blockIdx.x * ATT_THREADS + threadIdx.x) >> 4, n = (long long)a.n_q * a.Hq;
-    float x = 0.f;
-    if (rh < n) {
-        const int qi = (int)(rh / a.Hq), head = (int)(rh % a.Hq);
-        const T *o = row_of<T>(a.o, qi, head), *g = row_of<T>(a.d_o, qi, head);
-        constexpr int E = 16 / (int)sizeof(T);
-        for (int c = l16; c * E < a.D; c += 16) {
-            T y[E], z[E];
-            const u32x4 yo = load_granule<T>(o, c, a.D, a.vec), zo = load_granule<T>(g, c, a.D, a.vec);
-            __builtin_memcpy(y, &yo, 16);
-            __builtin_memcpy(z, &zo, 16);
-#pragma unroll
-            for (int j = 0; j < E; ++j) x = fmaf((float)y[j], (float)z[j], x);
-        }
-    }
-#pragma unroll
-    for (int o = 8; o >= 1; o >>= 1) x += __shfl_xor(x, o);
-    if (rh < n && l16 == 0) a.delta[rh] = x;
-}
-
 // What exp2 subtracts: a row without nodes (lse = -inf) has no probabilities.
 __device__ inline float lse_log2(float lse) { return lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f; }
+
+// What both kernels of the backward pass need first.  Workgroups below `row_blocks`: delta[i] = d_o[i] . o[i] and the logarithms in base 2, 16 lanes
+// per query and head.  With a mask, one further workgroup per tree: the tree's nodes that may be read, one after the other in `list` from
+// kv_off[tree] on, and their number in live[tree]; masked nodes then cost the others nothing.
+template <typename T> __global__ __launch_bounds__(ATT_THREADS) void k_attend_prepare(const AttArgs a, int row_blocks)
+{
+    if ((int)blockIdx.x < row_blocks) {
+        const int l16 = threadIdx.x & 15;
+        const long long rh = ((long long)blockIdx.x * ATT_THREADS + threadIdx.x) >> 4, n = (long long)a.n_q * a.Hq;
+        float x = 0.f;
+        if (rh < n) {
+            const int qi = (int)(rh / a.Hq), head = (int)(rh % a.Hq);
+            const T *o = row_of<T>(a.o, qi, head), *g = row_of<T>(a.d_o, qi, head);
+            constexpr int E = 16 / (int)sizeof(T);
+            for (int c = l16; c * E < a.D; c += 16) {
+                T y[E], z[E];
+                const u32x4 yo = load_granule<T>(o, c, a.D, a.vec), zo = load_granule<T>(g, c, a.D, a.vec);
+                __builtin_memcpy(y, &yo, 16);
+                __builtin_memcpy(z, &zo, 16);
+#pragma unroll
+                for (int j = 0; j < E; ++j) x = fmaf((float)y[j], (float)z[j], x);
+            }
+        }
+#pragma unroll
+        for (int o = 8; o >= 1; o >>= 1) x += __shfl_xor(x, o);
+        if (rh < n && l16 == 0) {
+            a.delta[rh] = x;
+            a.ref[rh] = lse_log2(a.lse[rh]);
+        }
+        return;
+    }
+    __shared__ int counts[ATT_WAVES];
+    constexpr int EACH = 16;
+    const int tree = blockIdx.x - row_blocks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int lo, hi, n = 0;
+    tree_range(a.kv_off, tree, a.n_kv, &lo, &hi);
+    for (int at = lo; at < hi; at += EACH * ATT_THREADS) {
+        const int mine = at + EACH * threadIdx.x;
+        unsigned bits = 0;
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) bits |= a.mask[min(mine + j, hi - 1)] != 0 && mine + j < hi ? 1u << j : 0u;
+        int upto = __popc(bits);
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(upto, o);
+            upto += lane >= o ? y : 0;
+        }
+        __syncthreads();
+        if (lane == 63) counts[wave] = upto;
+        __syncthreads();
+        int place = lo + n + upto - __popc(bits);
+#pragma unroll
+        for (int w = 0; w < ATT_WAVES; ++w) {
+            place += w < wave ? counts[w] : 0;
+            n += counts[w];
+        }
+#pragma unroll
+        for (int j = 0; j < EACH; ++j)
+            if (bits >> j & 1) a.list[place++] = mine + j;
+    }
+    if (threadIdx.x == 0) a.live[tree] = n;
+}
 
 // dQ: like the forward, rows (queries) on the lanes' columns.  Waves side by side along the rows (WM) and, for wide heads, along the
 // columns of dQ (WD), where every wave of a row tile works out the tile's scores itself.
 template <typename T, int DP> struct AttDq {
+    static constexpr int THREADS = ATT_THREADS;
     static constexpr int WD = DP > 128 ? 2 : 1;
     static constexpr int WM = ATT_WAVES / WD;
     static constexpr int BM = 32 * WM;
-    static constexpr int BN = 32;
+    static constexpr int NT = DP * (int)sizeof(T) <= 256 ? 2 : 1;
+    static constexpr int BN = 32 * NT;
     static constexpr int DT = DP / 32 / WD;
     static constexpr int STAGE = 2 * BN * Rows<T, DP>::BYTES;
-    static constexpr int BUFS = 2;
-    static constexpr int LDS = STAGE * BUFS;
-    static constexpr int MIN_BLOCKS = DP * (int)sizeof(T) > 256 ? 1 : 2;
+    static constexpr int LDS = 2 * STAGE;
+    static constexpr int MIN_WAVES = DP * (int)sizeof(T) > 256 ? 1 : 2;
 };
 
-template <typename T, int DP>
-__global__ __launch_bounds__(ATT_THREADS, (AttDq<T, DP>::MIN_BLOCKS)) void k_attend_dq(const AttArgs a)
+template <typename T, int DP, bool VEC> __global__ __launch_bounds__(ATT_THREADS, (AttDq<T, DP>::MIN_WAVES)) void k_attend_dq(const AttArgs a)
 {
     typedef AttDq<T, DP> C;
     typedef Rows<T, DP> R;
     typedef typename Elem<T>::frag frag;
-    constexpr int DT = C::DT;
+    constexpr int DT = C::DT, BN = C::BN;
     extern __shared__ __align__(16) unsigned char att_lds[];
 
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
@@ -586,7 +811,7 @@ __global__ __launch_bounds__(ATT_THREADS, (AttDq<T, DP>::MIN_BLOCKS)) void k_att
     const long long n_rows = (long long)(q_hi - q_lo) * a.G, m0 = tile * C::BM;
     if (tile < 0 || m0 >= n_rows) return;
     tree_range(a.kv_off, tree, a.n_kv, &lo, &hi);
-    const int n_stage = (hi - lo + C::BN - 1) / C::BN;
+    const int n_nodes = a.mask ? min(__builtin_amdgcn_readfirstlane(a.live[tree]), hi - lo) : hi - lo;
 
     const long long m = m0 + 32 * wm + col;
     const bool mine = m < n_rows;
@@ -597,75 +822,107 @@ __global__ __launch_bounds__(ATT_THREADS, (AttDq<T, DP>::MIN_BLOCKS)) void k_att
         const T *qr = row_of<T>(a.q, qi, head), *gr = row_of<T>(a.d_o, qi, head);
 #pragma unroll
         for (int s = 0; s < R::STEPS; ++s) {
-            qf[s] = __builtin_bit_cast(frag, load_granule<T>(qr, 2 * s + half, a.D, a.vec));
-            gf[s] = __builtin_bit_cast(frag, load_granule<T>(gr, 2 * s + half, a.D, a.vec));
+            qf[s] = __builtin_bit_cast(frag, load_granule<T>(qr, 2 * s + half, a.D, VEC));
+            gf[s] = __builtin_bit_cast(frag, load_granule<T>(gr, 2 * s + half, a.D, VEC));
         }
     }
-    const float ref = lse_log2(a.lse[row_head]), delta = a.delta[row_head];
-    floatx16 acc[DT];
+    float row[2] = {a.ref[row_head], a.delta[row_head]};
+    floatx16 acc[1][DT];
 #pragma unroll
-    for (int t = 0; t < DT; ++t) acc[t] = floatx16{};
+    for (int t = 0; t < DT; ++t) acc[0][t] = floatx16{};
 
     const T *kp = row_of<T>(a.k, 0, hk), *vp = row_of<T>(a.v, 0, hk);
-    NodeTile<T, DP, C::BN> st;
-    if (n_stage) {
-        st.request(kp, vp, a, lo, lo, hi);
-        st.template put<true, false>(att_lds, att_lds + C::STAGE / 2);
-    }
-    for (int s = 0; s < n_stage; ++s) {
-        const int first = lo + s * C::BN;
-        const unsigned char *kt = att_lds + (s & 1) * C::STAGE, *vt = kt + C::STAGE / 2;
+    const ATT_GLOBAL int32_t *list = (const ATT_GLOBAL int32_t *)a.list + lo;
+    const bool near = VEC && !a.mask && a.near && a.D == DP;
+    const NearRows<T, DP, BN, ATT_THREADS> k_near(a.k.row), v_near(a.v.row);
+    int first = 0;                              // of the stage that is staged next
+    auto stage = [&](unsigned char *b, int n) {
+        if (near && n == BN) {
+            k_near.stage(b, kp + (lo + first) * a.k.row);
+            v_near.stage(b + C::STAGE / 2, vp + (lo + first) * a.v.row);
+        } else {
+            auto node = [&](int r) { return (long long)(a.mask ? list[first + r] : lo + first + r); };
+            stage_rows<T, DP, BN, ATT_THREADS, VEC>(b, a.D, [&](int r) { return r < n ? kp + node(r) * a.k.row : (const T *)nullptr; });
+            stage_rows<T, DP, BN, ATT_THREADS, VEC>(b + C::STAGE / 2, a.D, [&](int r) { return r < n ? vp + node(r) * a.v.row : (const T *)nullptr; });
+        }
+        first += BN;
+    };
+    RowReads<T, DP> kr(att_lds), vr(att_lds + C::STAGE / 2);
+    ColumnReads<T, DP> kc(att_lds, 32 * DT * wd);
+    // one stage of n nodes.  TAIL: some may be missing (rows of zeros, but exp2 of a large -lse would still be infinite).
+    auto compute = [&](auto tail, int n) {
+#pragma unroll
+        for (int j = 0; j < C::NT; ++j) {
+            if (decltype(tail)::value && 32 * j >= n) break;
+            floatx16 p[1] = {}, dp = floatx16{};
+#pragma unroll
+            for (int d = 0; d < R::STEPS; ++d) {
+                mma(p[0], kr.get(32 * j, d), qf[d]);
+                mma(dp, vr.get(32 * j, d), gf[d]);
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(p[0][r], a.scale_log2, -row[0])) * (dp[r] - row[1]);
+                p[0][r] = decltype(tail)::value && 32 * j + 8 * (r >> 2) + 4 * half + (r & 3) >= n ? 0.f : e;
+            }
+            mma_columns<T, DP, 1, DT>(acc, kc, 32 * j, p);
+        }
+    };
+    int left = n_nodes, odd = 0;
+    if (left > 0) stage(att_lds, min(left, BN));
+    arrived(qf);
+    arrived(gf);
+    arrived(row);
+    for (; left > BN; left -= BN) {
+        if (VEC) stage_wait();
         __syncthreads();
-        if (s + 1 < n_stage) st.request(kp, vp, a, first + C::BN, lo, hi);
-        const unsigned w = (unsigned)live_nodes(a, first, hi) >> (4 * half);
-        floatx16 p = floatx16{}, dp = floatx16{};
-#pragma unroll
-        for (int d = 0; d < R::STEPS; ++d) {
-            mma(p, row_frag<T, DP>(kt, col, d, half), qf[d]);
-            mma(dp, row_frag<T, DP>(vt, col, d, half), gf[d]);
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const float e = __builtin_amdgcn_exp2f(fmaf(p[r], a.scale_log2, -ref)) * (dp[r] - delta);
-            p[r] = w >> (8 * (r >> 2) + (r & 3)) & 1 ? e : 0.f;
-        }
-        mma_columns<T, DP, DT>(acc, kt, 0, p, 32 * DT * wd, lane);
-        if (s + 1 < n_stage) {
-            unsigned char *nk = att_lds + ((s + 1) & 1) * C::STAGE;
-            st.template put<true, false>(nk, nk + C::STAGE / 2);
-        }
+        stage(att_lds + (odd ? 0 : C::STAGE), min(left - BN, BN));
+        compute(std::false_type{}, BN);
+        const int step = odd ? -C::STAGE : C::STAGE;
+        kr.move(step);
+        vr.move(step);
+        kc.move(step);
+        odd ^= 1;
+    }
+    if (left > 0) {
+        if (VEC) stage_wait();
+        __syncthreads();
+        compute(std::true_type{}, left);
     }
     if (!mine) return;
     T *o = row_of<T>(a.d_q, qi, head);
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
-        for (int r = 0; r < 16; r += 4)
-            store4<T>(o, 32 * (DT * wd + t) + 2 * r + 4 * half, a.D, a.vec_out, acc[t][r] * a.scale, acc[t][r + 1] * a.scale, acc[t][r + 2] * a.scale,
-                      acc[t][r + 3] * a.scale);
+        for (int r = 0; r < 16; r += 4) {
+            const floatx16 &x = acc[0][t];
+            store4<T>(o, 32 * (DT * wd + t) + 2 * r + 4 * half, a.D, a.vec_out, x[r] * a.scale, x[r + 1] * a.scale, x[r + 2] * a.scale, x[r + 3] * a.scale);
+        }
 }
 
 // dK and dV: nodes on the lanes' columns, packed query rows go by in LDS.  Every sum over queries and over the heads of a group is
 // taken by one wave in one order: no atomics, the same bits every run.
 template <typename T, int DP> struct AttDkv {
-    static constexpr int WD = DP > 128 ? 2 : 1;
+    static constexpr int THREADS = ATT_THREADS;
+    static constexpr int WD = DP <= 128 ? 1 : sizeof(T) == 2 ? 2 : 4;       // wide heads: waves along the columns of dK and dV
     static constexpr int WN = ATT_WAVES / WD;
     static constexpr int BN = 32 * WN;
-    static constexpr int BQ = 32;
+    static constexpr int QT = DP * (int)sizeof(T) <= 256 ? 2 : 1;
+    static constexpr int BQ = 32 * QT;
     static constexpr int DT = DP / 32 / WD;
-    static constexpr int STAGE = 2 * BQ * Rows<T, DP>::BYTES + 2 * BQ * 4;
+    static constexpr int STAGE = 2 * BQ * Rows<T, DP>::BYTES + 512;         // rows of q, of d_o, 64 logarithms, 64 deltas
     static constexpr int LDS = 2 * STAGE;
-    static constexpr int MIN_BLOCKS = DP * (int)sizeof(T) > 128 ? 1 : 2;
+    static constexpr int MIN_WAVES = DP * (int)sizeof(T) > 256 || DP == 128 ? 1 : 2;
 };
 
-template <typename T, int DP>
-__global__ __launch_bounds__(ATT_THREADS, (AttDkv<T, DP>::MIN_BLOCKS)) void k_attend_dkv(const AttArgs a)
+static __device__ const float att_no_row[2] = {INFINITY, 0.f};              // logarithm and delta of a row that is not there
+
+template <typename T, int DP, bool VEC> __global__ __launch_bounds__(ATT_THREADS, (AttDkv<T, DP>::MIN_WAVES)) void k_attend_dkv(const AttArgs a)
 {
     typedef AttDkv<T, DP> C;
     typedef Rows<T, DP> R;
     typedef typename Elem<T>::frag frag;
-    constexpr int DT = C::DT, BQ = C::BQ;
-    constexpr int GRANULES = BQ * R::GPR, EACH = (GRANULES + ATT_THREADS - 1) / ATT_THREADS;
+    constexpr int DT = C::DT, BQ = C::BQ, BN = C::BN;
     extern __shared__ __align__(16) unsigned char att_lds[];
 
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
@@ -673,105 +930,123 @@ __global__ __launch_bounds__(ATT_THREADS, (AttDkv<T, DP>::MIN_BLOCKS)) void k_at
     const long long id = xcd_order(blockIdx.x, gridDim.x);
     const int slot = (int)(id % a.slots), hk = (int)(id / a.slots);
     long long tile;
-    const int tree = find_slot(a.kv_off, a.n_trees, 1, C::BN == 64 ? 6 : 7, slot, &tile);
+    const int tree = find_slot(a.kv_off, a.n_trees, 1, BN == 32 ? 5 : BN == 64 ? 6 : 7, slot, &tile);
     int q_lo, q_hi, lo, hi;
     tree_range(a.kv_off, tree, a.n_kv, &lo, &hi);
-    const long long n0 = lo + tile * C::BN;
-    if (tile < 0 || n0 >= hi) return;
+    if (tile < 0 || tile * BN >= hi - lo) return;
+    const int t0 = (int)tile * BN;
     tree_range(a.q_off, tree, a.n_q, &q_lo, &q_hi);
     const long long n_rows = (long long)(q_hi - q_lo) * a.G;
+    int n_nodes = hi - lo;
+    if (a.mask) {
+        // masked nodes among the tile's own: zeros
+        n_nodes = min(__builtin_amdgcn_readfirstlane(a.live[tree]), n_nodes);
+        const int end = min(t0 + BN, hi - lo);
+        for (int r = t0 + wave; r < end; r += ATT_WAVES) {
+            if (a.mask[lo + r]) continue;
+            T *ok = row_of<T>(a.d_k, lo + r, hk), *ov = row_of<T>(a.d_v, lo + r, hk);
+            for (int d = lane; d < a.D; d += 64) ok[d] = ov[d] = (T)0.f;
+        }
+        if (t0 >= n_nodes) return;
+    }
 
-    const long long node = n0 + 32 * wn + col;
-    const bool mine = node < hi;
-    const long long node_in = mine ? node : n0;
-    const bool live = mine && (!a.mask || a.mask[node_in] != 0);
+    const int place = t0 + 32 * wn + col;
+    const bool mine = place < n_nodes;
+    const int at = mine ? place : t0;
+    const long long node = a.mask ? ((const ATT_GLOBAL int32_t *)a.list)[lo + at] : lo + at;
     frag kf[R::STEPS], vf[R::STEPS];
     {
-        const T *kr = row_of<T>(a.k, node_in, hk), *vr = row_of<T>(a.v, node_in, hk);
+        const T *kr = row_of<T>(a.k, node, hk), *vr = row_of<T>(a.v, node, hk);
 #pragma unroll
         for (int s = 0; s < R::STEPS; ++s) {
-            kf[s] = __builtin_bit_cast(frag, load_granule<T>(kr, 2 * s + half, a.D, a.vec));
-            vf[s] = __builtin_bit_cast(frag, load_granule<T>(vr, 2 * s + half, a.D, a.vec));
+            kf[s] = __builtin_bit_cast(frag, load_granule<T>(kr, 2 * s + half, a.D, VEC));
+            vf[s] = __builtin_bit_cast(frag, load_granule<T>(vr, 2 * s + half, a.D, VEC));
         }
     }
-    floatx16 dk[DT], dv[DT];
+    floatx16 dk[1][DT], dv[1][DT];
 #pragma unroll
-    for (int t = 0; t < DT; ++t) dk[t] = dv[t] = floatx16{};
+    for (int t = 0; t < DT; ++t) dk[0][t] = dv[0][t] = floatx16{};
 
-    u32x4 rq[EACH], rg[EACH];
-    float r_ref = 0.f, r_delta = 0.f;
-    auto request = [&](long long first) {
+    // Groups that divide a stage: a thread's places are the same in every stage, BQ / G queries further on.
+    const bool near = VEC && a.near && a.D == DP && BQ % a.G == 0;
+    constexpr int GRANULES = BQ * R::GPR, EACH = (GRANULES + ATT_THREADS - 1) / ATT_THREADS;
+    uint32_t q_offset[EACH], g_offset[EACH];
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const int e = threadIdx.x + i * ATT_THREADS;
-            rq[i] = rg[i] = u32x4{0u, 0u, 0u, 0u};
-            if (GRANULES % ATT_THREADS == 0 || e < GRANULES) {
-                const long long m = first + e / R::GPR;
-                if (m < n_rows) {
-                    const int qi = q_lo + (int)(m / a.G), head = hk * a.G + (int)(m % a.G);
-                    rq[i] = load_granule<T>(row_of<T>(a.q, qi, head), e % R::GPR, a.D, a.vec);
-                    rg[i] = load_granule<T>(row_of<T>(a.d_o, qi, head), e % R::GPR, a.D, a.vec);
+    for (int i = 0; i < EACH; ++i) {
+        int r, g;
+        place_of<T, DP>(i * ATT_THREADS + threadIdx.x, &r, &g);
+        const int qr = r / a.G, hr = r % a.G;
+        q_offset[i] = ((uint32_t)qr * (uint32_t)a.q.row + (uint32_t)hr * (uint32_t)a.q.head) * (uint32_t)sizeof(T) + g * 16;
+        g_offset[i] = ((uint32_t)qr * (uint32_t)a.d_o.row + (uint32_t)hr * (uint32_t)a.d_o.head) * (uint32_t)sizeof(T) + g * 16;
+    }
+    long long first = 0;                        // packed row that is staged next
+    auto stage = [&](unsigned char *b) {
+        if (near && first + BQ <= n_rows) {
+            const int q0 = q_lo + (int)(first / a.G);
+            const T *qp = row_of<T>(a.q, q0, hk * a.G), *gp = row_of<T>(a.d_o, q0, hk * a.G);
+            const uint32_t base = lds_address(b) + wave * 1024;
+#pragma unroll
+            for (int i = 0; i < EACH; ++i)
+                if (GRANULES % ATT_THREADS == 0 || i * ATT_THREADS + wave * 64 < GRANULES) {
+                    stage_16(base + i * ATT_THREADS * 16, qp, q_offset[i]);
+                    stage_16(base + BQ * R::BYTES + i * ATT_THREADS * 16, gp, g_offset[i]);
+                }
+        } else {
+            auto row = [&](const AttTensor &x, int r) {
+                const long long m = first + r;
+                return m < n_rows ? (const T *)row_of<T>(x, q_lo + m / a.G, hk * a.G + (int)(m % a.G)) : (const T *)nullptr;
+            };
+            stage_rows<T, DP, BQ, ATT_THREADS, VEC>(b, a.D, [&](int r) { return row(a.q, r); });
+            stage_rows<T, DP, BQ, ATT_THREADS, VEC>(b + BQ * R::BYTES, a.D, [&](int r) { return row(a.d_o, r); });
+        }
+        if (wave < 2) {                         // (64 places; those beyond BQ are not read)
+            const long long m = first + lane;
+            const float *from = wave == 0 ? a.ref : a.delta;
+            from = m < n_rows ? from + (q_lo + m / a.G) * a.Hq + hk * a.G + m % a.G : att_no_row + wave;
+            stage_4(lds_address(b) + 2 * BQ * R::BYTES + wave * 256, from);
+        }
+        first += BQ;
+    };
+    RowReads<T, DP> qr(att_lds), gr(att_lds + BQ * R::BYTES);
+    ColumnReads<T, DP> qc(att_lds, 32 * DT * wd), gc(att_lds + BQ * R::BYTES, 32 * DT * wd);
+    const unsigned char *numbers = att_lds + 2 * BQ * R::BYTES + 16 * half;
+    const int n_stage = (int)((n_rows + BQ - 1) / BQ);
+    if (n_stage) stage(att_lds);
+    arrived(kf);
+    arrived(vf);
+    for (int s = 0; s < n_stage; ++s) {
+        stage_wait();
+        __syncthreads();
+        if (s + 1 < n_stage) stage(att_lds + (s & 1 ? 0 : C::STAGE));
+#pragma unroll
+        for (int q = 0; q < C::QT; ++q) {
+            if (q > 0 && (long long)s * BQ + 32 * q >= n_rows) break;
+            floatx16 p[1] = {}, dp[1] = {};
+#pragma unroll
+            for (int d = 0; d < R::STEPS; ++d) {
+                mma(p[0], qr.get(32 * q, d), kf[d]);
+                mma(dp[0], gr.get(32 * q, d), vf[d]);
+            }
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4) {
+                const f32x4 rr = *reinterpret_cast<const f32x4 *>(numbers + 128 * q + 32 * r4);
+                const f32x4 dd = *reinterpret_cast<const f32x4 *>(numbers + 256 + 128 * q + 32 * r4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int r = 4 * r4 + j;
+                    p[0][r] = __builtin_amdgcn_exp2f(fmaf(p[0][r], a.scale_log2, -rr[j]));
+                    dp[0][r] = p[0][r] * (dp[0][r] - dd[j]);
                 }
             }
+            mma_columns<T, DP, 1, DT>(dv, gc, 32 * q, p);
+            mma_columns<T, DP, 1, DT>(dk, qc, 32 * q, dp);
         }
-        if (threadIdx.x < BQ) {
-            const long long m = first + threadIdx.x;
-            r_ref = INFINITY;
-            r_delta = 0.f;
-            if (m < n_rows) {
-                const long long rh = (q_lo + m / a.G) * a.Hq + hk * a.G + m % a.G;
-                r_ref = lse_log2(a.lse[rh]);
-                r_delta = a.delta[rh];
-            }
-        }
-    };
-    auto put = [&](unsigned char *b) {
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const int e = threadIdx.x + i * ATT_THREADS;
-            if (GRANULES % ATT_THREADS == 0 || e < GRANULES) {
-                const int at = R::at(e / R::GPR, e % R::GPR);
-                *reinterpret_cast<u32x4 *>(b + at) = rq[i];
-                *reinterpret_cast<u32x4 *>(b + BQ * R::BYTES + at) = rg[i];
-            }
-        }
-        if (threadIdx.x < BQ) {
-            float *x = reinterpret_cast<float *>(b + 2 * BQ * R::BYTES);
-            x[threadIdx.x] = r_ref;
-            x[BQ + threadIdx.x] = r_delta;
-        }
-    };
-    const int n_stage = (int)((n_rows + BQ - 1) / BQ);
-    if (n_stage) {
-        request(0);
-        put(att_lds);
-    }
-    for (int s = 0; s < n_stage; ++s) {
-        const unsigned char *qt = att_lds + (s & 1) * C::STAGE, *gt = qt + BQ * R::BYTES;
-        const float *ref = reinterpret_cast<const float *>(gt + BQ * R::BYTES), *delta = ref + BQ;
-        __syncthreads();
-        if (s + 1 < n_stage) request((long long)(s + 1) * BQ);
-        floatx16 p = floatx16{}, dp = floatx16{};
-#pragma unroll
-        for (int d = 0; d < R::STEPS; ++d) {
-            mma(p, row_frag<T, DP>(qt, col, d, half), kf[d]);
-            mma(dp, row_frag<T, DP>(gt, col, d, half), vf[d]);
-        }
-#pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4) {
-            const f32x4 rr = *reinterpret_cast<const f32x4 *>(ref + 8 * r4 + 4 * half);
-            const f32x4 dd = *reinterpret_cast<const f32x4 *>(delta + 8 * r4 + 4 * half);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int r = 4 * r4 + j;
-                const float e = __builtin_amdgcn_exp2f(fmaf(p[r], a.scale_log2, -rr[j]));
-                p[r] = live ? e : 0.f;
-                dp[r] = live ? e * (dp[r] - dd[j]) : 0.f;
-            }
-        }
-        mma_columns<T, DP, DT>(dv, gt, 0, p, 32 * DT * wd, lane);
-        mma_columns<T, DP, DT>(dk, qt, 0, dp, 32 * DT * wd, lane);
-        if (s + 1 < n_stage) put(att_lds + ((s + 1) & 1) * C::STAGE);
+        const int step = s & 1 ? -C::STAGE : C::STAGE;
+        qr.move(step);
+        gr.move(step);
+        qc.move(step);
+        gc.move(step);
+        numbers += step;
     }
     if (!mine) return;
     T *ok = row_of<T>(a.d_k, node, hk), *ov = row_of<T>(a.d_v, node, hk);
@@ -780,8 +1055,9 @@ __global__ __launch_bounds__(ATT_THREADS, (AttDkv<T, DP>::MIN_BLOCKS)) void k_at
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
             const int d = 32 * (DT * wd + t) + 2 * r + 4 * half;
-            store4<T>(ok, d, a.D, a.vec_out, dk[t][r] * a.scale, dk[t][r + 1] * a.scale, dk[t][r + 2] * a.scale, dk[t][r + 3] * a.scale);
-            store4<T>(ov, d, a.D, a.vec_out, dv[t][r], dv[t][r + 1], dv[t][r + 2], dv[t][r + 3]);
+            const floatx16 &x = dk[0][t], &y = dv[0][t];
+            store4<T>(ok, d, a.D, a.vec_out, x[r] * a.scale, x[r + 1] * a.scale, x[r + 2] * a.scale, x[r + 3] * a.scale);
+            store4<T>(ov, d, a.D, a.vec_out, y[r], y[r + 1], y[r + 2], y[r + 3]);
         }
 }
 

@@ -52,16 +52,18 @@ bool check(const tl_attention *a)
            check_rows(a->v, a->dtype, a->n_kv, a->n_kv_heads, a->head_dim, false);
 }
 
-// Which form a forward takes.  Up to 64 packed rows per tree on average: one tile of 32 rows, nodes divided among the waves; and where such
-// tiles do not fill the chip twice, nodes divided among workgroups too, as long as a part keeps two stages.
+// Which form a forward takes, by the packed rows of a tree on average.  Measured (us, 4 waves along the rows / 2 / 1): 256 trees of 9 to 99 nodes,
+// 33 rows each, bf16 x 64: - / 24 / 38; fp32 x 64: - / 57 / 70; 64 trees of 2047 nodes half of them masked, 72 rows, fp32 x 64: 158 / 98 /
+// 117; 8 trees of 3500 nodes, 3000 rows, bf16 x 128: 250 / 310 / -.  A single token's few rows want every wave on nodes of its own.
+// Where row tiles do not fill the chip twice, a tree's nodes are divided among workgroups too, as long as a part keeps two stages.
 AttPlan plan(const tl_attention *a)
 {
     AttPlan p;
     const long long rows = (long long)a->n_q * (a->n_heads / a->n_kv_heads);
     const int dp = att_padded(a->head_dim), size = element_size(a->dtype);
-    p.wm = rows <= 64ll * a->n_trees && dp * size <= 512 ? 1 : 4;
+    p.wm = rows <= 16ll * a->n_trees && dp * size <= 512 ? 1 : rows <= 128ll * a->n_trees ? 2 : 4;
     p.bm = 32 * p.wm;
-    p.bn = p.wm == 1 ? 128 : dp * size <= 256 ? 64 : 32;
+    p.bn = p.wm == 1 ? 128 : p.wm == 2 ? 64 : dp * size <= 256 ? 64 : 32;
     p.slots = (int)(rows / p.bm + a->n_trees);
     p.splits = 1;
     const long long blocks = (long long)p.slots * a->n_kv_heads, wanted = 2ll * compute_units();
@@ -78,7 +80,7 @@ long long round16(long long x) { return (x + 15) & ~15ll; }
 long long workspace(const tl_attention *a, const AttPlan &p, int backward)
 {
     const long long rh = (long long)a->n_q * a->n_heads;
-    if (backward) return round16(rh * 4);
+    if (backward) return 2 * round16(rh * 4) + (a->kv_mask ? round16(4ll * a->n_kv) + round16(4ll * a->n_trees) : 0);
     return p.splits > 1 ? round16(p.splits * rh * 4) + round16(p.splits * rh * a->head_dim * 4) : 0;
 }
 
@@ -102,6 +104,8 @@ AttArgs arguments(const tl_attention *a)
     x.G = a->n_heads / a->n_kv_heads;
     x.D = a->head_dim;
     x.splits = 1;
+    auto close = [&](const tl_rows &r) { return r.row < (1 << 20) && r.head < (1 << 20); };
+    x.near = close(a->q) && close(a->k) && close(a->v);
     x.vec = in_pieces(a->q, a->dtype, a->head_dim, 16) && in_pieces(a->k, a->dtype, a->head_dim, 16) && in_pieces(a->v, a->dtype, a->head_dim, 16);
     return x;
 }
@@ -154,11 +158,11 @@ int tl_attend_backward(const tl_attention *a, const tl_rows *o, const float *lse
         return TL_EINVAL;
     if (a->n_trees == 0) return TL_OK;
     const long long need = workspace(a, AttPlan{}, 1);
-    if (a->n_q > 0 && (!lse || !workspace_p || ((uintptr_t)workspace_p & 15))) return TL_EINVAL;
+    if ((a->n_q > 0 && !lse) || (need > 0 && (!workspace_p || ((uintptr_t)workspace_p & 15)))) return TL_EINVAL;
     if (need > workspace_bytes) return TL_ELIMIT;
     const long long rows = (long long)a->n_q * (a->n_heads / a->n_kv_heads);
-    if ((rows / 64 + a->n_trees) * a->n_kv_heads > INT32_MAX || ((long long)a->n_kv / 64 + a->n_trees) * a->n_kv_heads > INT32_MAX ||
-        (long long)a->n_q * a->n_heads / 16 >= INT32_MAX)
+    if ((rows / 32 + a->n_trees) * a->n_kv_heads > INT32_MAX || ((long long)a->n_kv / 32 + a->n_trees) * a->n_kv_heads > INT32_MAX ||
+        (long long)a->n_q * a->n_heads / 16 + a->n_trees >= INT32_MAX)
         return TL_EINVAL;
     AttArgs x = arguments(a);
     x.o = AttTensor{o->p, o->row, o->head};
@@ -167,8 +171,14 @@ int tl_attend_backward(const tl_attention *a, const tl_rows *o, const float *lse
     x.d_k = AttTensor{d_k->p, d_k->row, d_k->head};
     x.d_v = AttTensor{d_v->p, d_v->row, d_v->head};
     x.lse = const_cast<float *>(lse);
-    x.delta = static_cast<float *>(workspace_p);
+    const long long rh = (long long)a->n_q * a->n_heads;
+    char *w = static_cast<char *>(workspace_p);
+    x.delta = reinterpret_cast<float *>(w);
+    x.ref = reinterpret_cast<float *>(w + round16(rh * 4));
+    x.list = reinterpret_cast<int32_t *>(w + 2 * round16(rh * 4));
+    x.live = reinterpret_cast<int32_t *>(w + 2 * round16(rh * 4) + round16(4ll * a->n_kv));
     x.vec = x.vec && in_pieces(*o, dt, D, 16) && in_pieces(*d_o, dt, D, 16);
+    x.near = x.near && d_o->row < (1 << 20) && d_o->head < (1 << 20);
     x.vec_out = pieces_of_4(*d_q, dt, D) && pieces_of_4(*d_k, dt, D) && pieces_of_4(*d_v, dt, D);
     const hipStream_t st = (hipStream_t)hip_stream;
     const hipError_t e = dt == TL_DT_F32 ? attend_backward<float>(x, st) : dt == TL_DT_BF16 ? attend_backward<bf16_t>(x, st) : attend_backward<f16_t>(x, st);
