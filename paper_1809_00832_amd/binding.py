@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -97,7 +98,7 @@ def lib():
         L.tl_classify_backward.restype = ci
         L.tl_classify_backward.argtypes = [vp, ci, vp, vp, vp, ci] + [vp] * 7
         L.tl_strerror.argtypes = [ci]
-        attn, rows, i64 = ctypes.POINTER(tl_attention), ctypes.POINTER(tl_rows), ctypes.c_int64
+        attn, rows, i64 = vp, vp, ctypes.c_int64            # the structures by reference, or their bytes
         L.tl_attend_workspace.restype = ci
         L.tl_attend_workspace.argtypes = [attn, ci, ctypes.POINTER(i64)]
         L.tl_attend.restype = ci
@@ -326,36 +327,58 @@ def tl_td_destroy(ctx) -> None:
 
 def _dtype(t) -> int:
     import torch
-    code = {torch.float32: TL_DT_F32, torch.bfloat16: TL_DT_BF16, torch.float16: TL_DT_F16}.get(t.dtype)
-    assert code is not None, "float32, bfloat16 or float16"
-    return code
+    d = t.dtype
+    if d is torch.float32:
+        return TL_DT_F32
+    assert d is torch.bfloat16 or d is torch.float16, "float32, bfloat16 or float16"
+    return TL_DT_BF16 if d is torch.bfloat16 else TL_DT_F16
 
 
-def _rows(t) -> tl_rows:
-    return tl_rows(t.data_ptr(), t.stride(0), t.stride(1))
+def _raw_stream(device) -> int:
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)        # (the public call takes 3 us, as long as a launch)
+    index = torch.cuda.current_device() if device.index is None else device.index
+    return raw(index) if raw else torch.cuda.current_stream(device).cuda_stream
 
 
-def _attention(q, k, v, q_off, kv_off, kv_mask, scale) -> tl_attention:
+# tl_attention and tl_rows as bytes: packing takes a quarter of the time of filling the structures
+_PACK_ATTENTION, _PACK_ROWS = struct.Struct("7if3Q9q").pack, struct.Struct("Q2q").pack
+assert struct.calcsize("7if3Q9q") == ctypes.sizeof(tl_attention) and struct.calcsize("Q2q") == ctypes.sizeof(tl_rows)
+
+
+def _rows(t, like, shape):
+    assert t.is_cuda and t.dtype == like.dtype and t.shape == shape and (shape[2] == 1 or t.stride(2) == 1), "rows, heads and a contiguous head_dim"
+    return _PACK_ROWS(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _attention(q, k, v, q_off, kv_off, kv_mask, scale) -> bytes:
     import torch
     n_q, n_heads, d = q.shape
-    n_kv, n_kv_heads, _ = k.shape
-    assert q.is_cuda and k.is_cuda and v.is_cuda and k.dtype == q.dtype and v.dtype == q.dtype
-    assert k.shape == v.shape and k.shape[2] == d
-    assert d == 1 or (q.stride(2) == 1 and k.stride(2) == 1 and v.stride(2) == 1), "head_dim must be contiguous"
-    for t in (q_off, kv_off):
-        assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous()
-    assert q_off.numel() == kv_off.numel() >= 1
+    n_kv, n_kv_heads, dk = k.shape
+    dtype = q.dtype
+    assert q.is_cuda and k.is_cuda and v.is_cuda and k.dtype == dtype and v.dtype == dtype and dk == d and v.shape == k.shape
+    q_row, q_head, q_d = q.stride()
+    k_row, k_head, k_d = k.stride()
+    v_row, v_head, v_d = v.stride()
+    assert d == 1 or q_d == k_d == v_d == 1, "head_dim must be contiguous"
+    int32 = torch.int32
+    assert q_off.is_cuda and q_off.dtype == int32 and q_off.is_contiguous() and kv_off.is_cuda and kv_off.dtype == int32 and kv_off.is_contiguous()
+    n_off = q_off.numel()
+    assert n_off == kv_off.numel() >= 1
+    mask = 0
     if kv_mask is not None:
         assert kv_mask.is_cuda and kv_mask.dtype in (torch.uint8, torch.bool) and kv_mask.is_contiguous() and kv_mask.numel() == n_kv
-    return tl_attention(_dtype(q), q_off.numel() - 1, n_q, n_kv, n_heads, n_kv_heads, d, d ** -0.5 if scale is None else scale,
-                        q_off.data_ptr(), kv_off.data_ptr(), _ptr(kv_mask), _rows(q), _rows(k), _rows(v))
+        mask = kv_mask.data_ptr()
+    return _PACK_ATTENTION(_dtype(q), n_off - 1, n_q, n_kv, n_heads, n_kv_heads, d, d ** -0.5 if scale is None else scale, q_off.data_ptr(),
+                           kv_off.data_ptr(), mask, q.data_ptr(), q_row, q_head, k.data_ptr(), k_row, k_head, v.data_ptr(), v_row, v_head)
 
 
 def _attend_workspace(a, backward, device):
     import torch
     size = ctypes.c_int64()
-    _check(lib().tl_attend_workspace(ctypes.byref(a), backward, ctypes.byref(size)), "tl_attend_workspace")
-    return torch.empty(size.value, dtype=torch.uint8, device=device) if size.value else None
+    _check(lib().tl_attend_workspace(a, backward, ctypes.byref(size)), "tl_attend_workspace")
+    n = size.value
+    return (torch.empty(n, dtype=torch.uint8, device=device), n) if n else (None, 0)
 
 
 def tl_attend(q, k, v, q_off, kv_off, kv_mask=None, scale=None, o=None, with_lse=False, stream=None):
@@ -367,13 +390,12 @@ def tl_attend(q, k, v, q_off, kv_off, kv_mask=None, scale=None, o=None, with_lse
         with torch.cuda.stream(stream):
             return tl_attend(q, k, v, q_off, kv_off, kv_mask, scale, o, with_lse)
     a = _attention(q, k, v, q_off, kv_off, kv_mask, scale)
+    shape, device = q.shape, q.device
     if o is None:
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    assert o.is_cuda and o.shape == q.shape and o.dtype == q.dtype and (o.shape[2] == 1 or o.stride(2) == 1)
-    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if with_lse else None
-    ws = _attend_workspace(a, 0, q.device)
-    _check(lib().tl_attend(ctypes.byref(a), ctypes.byref(_rows(o)), _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel(),
-                           torch.cuda.current_stream().cuda_stream), "tl_attend")
+        o = q.new_empty(shape)
+    lse = torch.empty(shape[:2], dtype=torch.float32, device=device) if with_lse else None
+    ws, n = _attend_workspace(a, 0, device)
+    _check(lib().tl_attend(a, _rows(o, q, shape), _ptr(lse), _ptr(ws), n, _raw_stream(device)), "tl_attend")
     return (o, lse) if with_lse else o
 
 
@@ -384,17 +406,13 @@ def tl_attend_backward(q, k, v, o, lse, d_o, q_off, kv_off, kv_mask=None, scale=
         with torch.cuda.stream(stream):
             return tl_attend_backward(q, k, v, o, lse, d_o, q_off, kv_off, kv_mask, scale)
     a = _attention(q, k, v, q_off, kv_off, kv_mask, scale)
-    for t in (o, d_o):
-        assert t.is_cuda and t.shape == q.shape and t.dtype == q.dtype and (t.shape[2] == 1 or t.stride(2) == 1)
-    assert lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:2]
-    out = {"d_q": torch.empty(q.shape, dtype=q.dtype, device=q.device), "d_k": torch.empty(k.shape, dtype=q.dtype, device=q.device),
-           "d_v": torch.empty(k.shape, dtype=q.dtype, device=q.device)}
-    ws = _attend_workspace(a, 1, q.device)
-    ref = ctypes.byref
-    _check(lib().tl_attend_backward(ref(a), ref(_rows(o)), lse.data_ptr(), ref(_rows(d_o)), ref(_rows(out["d_q"])), ref(_rows(out["d_k"])),
-                                    ref(_rows(out["d_v"])), _ptr(ws), 0 if ws is None else ws.numel(),
-                                    torch.cuda.current_stream().cuda_stream), "tl_attend_backward")
-    return out
+    q_shape, kv_shape, device = q.shape, k.shape, q.device
+    assert lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q_shape[:2]
+    d_q, d_k, d_v = q.new_empty(q_shape), q.new_empty(kv_shape), q.new_empty(kv_shape)
+    ws, n = _attend_workspace(a, 1, device)
+    _check(lib().tl_attend_backward(a, _rows(o, q, q_shape), lse.data_ptr(), _rows(d_o, q, q_shape), _rows(d_q, q, q_shape), _rows(d_k, q, kv_shape),
+                                    _rows(d_v, q, kv_shape), _ptr(ws), n, _raw_stream(device)), "tl_attend_backward")
+    return {"d_q": d_q, "d_k": d_k, "d_v": d_v}
 
 
 def tl_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
@@ -406,14 +424,15 @@ def tl_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, s
         with torch.cuda.stream(stream):
             return tl_sample(logits, u, temperature, top_k, top_p, min_p)
     n, vocab = logits.shape
+    device = logits.device
     assert logits.is_cuda and (vocab == 1 or logits.stride(1) == 1)
     for t, dt in ((u, torch.float32), (temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32), (min_p, torch.float32)):
         assert t is None or (t.is_cuda and t.dtype == dt and t.is_contiguous() and t.numel() == n)
-    out = {"token": torch.empty(n, dtype=torch.int32, device=logits.device), "logprob": torch.empty(n, dtype=torch.float32, device=logits.device),
-           "kept": torch.empty(n, dtype=torch.int32, device=logits.device)}
+    out = {"token": torch.empty(n, dtype=torch.int32, device=device), "logprob": torch.empty(n, dtype=torch.float32, device=device),
+           "kept": torch.empty(n, dtype=torch.int32, device=device)}
     _check(lib().tl_sample(_dtype(logits), n, vocab, logits.data_ptr(), logits.stride(0), u.data_ptr(), _ptr(temperature), _ptr(top_k),
                            _ptr(top_p), _ptr(min_p), out["token"].data_ptr(), out["logprob"].data_ptr(), out["kept"].data_ptr(),
-                           torch.cuda.current_stream().cuda_stream), "tl_sample")
+                           _raw_stream(device)), "tl_sample")
     return out
 
 

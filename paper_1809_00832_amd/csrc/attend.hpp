@@ -50,6 +50,7 @@ struct AttArgs {
     const uint8_t *mask;
     float *lse;             // [n_q x n_heads], natural logarithm
     float *delta, *ref;     // backward: sum over d of d_o * o, and lse in base 2, [n_q x n_heads]
+    float *size;            // backward, fp16: power of two that brings a row of d_o to a length of one, [n_q x n_heads]
     int32_t *list, *live;   // backward, with a mask: the nodes that may be read, tree by tree from kv_off on, and how many a tree has
     float *part_o;          // splits > 1: outputs of each part, [splits][n_q x n_heads][D]
     float *part_lse;        // ... and their logarithms, [splits][n_q x n_heads]
@@ -212,37 +213,35 @@ template <typename T, int DP> struct ColumnReads {
     __device__ float one(int r, int t, int r0) const { return *(const ATT_LDS float *)(uintptr_t)place(r & 7, t, r0 + (r & 8) * 2); }
 };
 
-// c[q][t] += sum over the 32 rows from r0 on of tile^T (column tile t) times w[q], whose register r belongs to row r0 + 8 (r / 4) + 4 half + r % 4.
-// 16-bit types: w is rounded to the type, as an operand of the matrix unit has to be (relative 2^-9 or 2^-12 of a probability or of a
-// score's gradient, the size of the inputs' own roundings); sums stay in fp32.
-template <typename T, int DP, int NQ, int NT>
-__device__ inline void mma_columns(floatx16 (&c)[NQ][NT], const ColumnReads<T, DP> &tile, int r0, const floatx16 (&w)[NQ])
+// c[t] += sum over the 32 rows from r0 on of tile^T (column tile t) times w, whose register r belongs to row r0 + 8 (r / 4) + 4 half + r % 4.
+// 16-bit types: an operand of the matrix unit has to be of the type.  With TERMS = 1 w is rounded to it once, which adds to a result as much error
+// as its own rounding to the type does; with TERMS = 2 what the rounding left is a second operand (22 or 16 bits of w together).
+// Sums stay in fp32.
+template <typename T, int DP, int TERMS, int NT>
+__device__ inline void mma_columns(floatx16 (&c)[NT], const ColumnReads<T, DP> &tile, int r0, const floatx16 &w)
 {
     if constexpr (sizeof(T) == 2) {
         typedef typename Elem<T>::frag frag;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            frag b[NQ];
+            frag b[TERMS];
 #pragma unroll
-            for (int q = 0; q < NQ; ++q)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) b[q][j] = (T)w[q][8 * s + j];
+            for (int j = 0; j < 8; ++j) {
+                b[0][j] = (T)w[8 * s + j];
+                if (TERMS == 2) b[TERMS - 1][j] = (T)(w[8 * s + j] - (float)b[0][j]);
+            }
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 const frag a = __builtin_bit_cast(frag, __builtin_shufflevector(tile.four(0, t, r0 + 16 * s), tile.four(1, t, r0 + 16 * s), 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-                for (int q = 0; q < NQ; ++q) mma(c[q][t], a, b[q]);
+                for (int q = TERMS - 1; q >= 0; --q) mma(c[t], a, b[q]);
             }
         }
     } else {
 #pragma unroll
         for (int r = 0; r < 16; ++r)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const float a = tile.one(r, t, r0);
-#pragma unroll
-                for (int q = 0; q < NQ; ++q) c[q][t] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[q][r], c[q][t], 0, 0, 0);
-            }
+            for (int t = 0; t < NT; ++t) c[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(tile.one(r, t, r0), w[r], c[t], 0, 0, 0);
     }
 }
 
@@ -469,6 +468,7 @@ template <typename T, int DP, int WM_> struct AttFwd {
     static constexpr int THREADS = ATT_THREADS;
     static constexpr int WM = WM_, WK = ATT_WAVES / WM;
     static constexpr int NT = WM == 4 && DP * (int)sizeof(T) <= 256 ? 2 : 1;
+    static constexpr int TERMS = WM == 4 ? 1 : 2;                   // of a probability: the second one costs time only where there are many rows
     static constexpr int BM = 32 * WM;
     static constexpr int BN = 32 * WK * NT;
     static constexpr int STAGE = 2 * BN * Rows<T, DP>::BYTES;
@@ -517,10 +517,10 @@ __global__ __launch_bounds__(ATT_THREADS, (AttFwd<T, DP, WM>::MIN_WAVES)) void k
 #pragma unroll
         for (int s = 0; s < R::STEPS; ++s) qf[s] = __builtin_bit_cast(frag, load_granule<T>(qr, 2 * s + half, a.D, VEC));
     }
-    floatx16 acc[1][DT];
+    floatx16 acc[DT];
     float top = -INFINITY, sum = 0.f;          // largest raw score so far (of the lane's query), sum of the lane's half of its nodes
 #pragma unroll
-    for (int t = 0; t < DT; ++t) acc[0][t] = floatx16{};
+    for (int t = 0; t < DT; ++t) acc[t] = floatx16{};
 
     const T *kp = row_of<T>(a.k, 0, hk), *vp = row_of<T>(a.v, 0, hk);
     Nodes<C::BN, THREADS> nodes;
@@ -543,25 +543,25 @@ __global__ __launch_bounds__(ATT_THREADS, (AttFwd<T, DP, WM>::MIN_WAVES)) void k
         constexpr bool TAIL = decltype(tail)::value;
         const int left = n - 32 * NT * wk;
         if (TAIL && left <= 0) return;
-        floatx16 p[NT][1];
+        floatx16 p[NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) p[t][0] = floatx16{};
+        for (int t = 0; t < NT; ++t) p[t] = floatx16{};
 #pragma unroll
         for (int d = 0; d < R::STEPS; ++d)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) mma(p[t][0], kr.get(32 * t, d), qf[d]);
+            for (int t = 0; t < NT; ++t) mma(p[t], kr.get(32 * t, d), qf[d]);
         if (TAIL) {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (32 * t + 8 * (r >> 2) + 4 * half + (r & 3) >= left) p[t][0][r] = -INFINITY;
+                    if (32 * t + 8 * (r >> 2) + 4 * half + (r & 3) >= left) p[t][r] = -INFINITY;
         }
         float high = top;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) high = fmaxf(high, p[t][0][r]);
+            for (int r = 0; r < 16; ++r) high = fmaxf(high, p[t][r]);
         high = max_of_halves(high);
         const float ref = high == -INFINITY ? 0.f : high * a.scale_log2;
         if (__any(high > top)) {
@@ -570,20 +570,20 @@ __global__ __launch_bounds__(ATT_THREADS, (AttFwd<T, DP, WM>::MIN_WAVES)) void k
 #pragma unroll
             for (int t = 0; t < DT; ++t)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[0][t][r] *= f;
+                for (int r = 0; r < 16; ++r) acc[t][r] *= f;
             top = high;
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                p[t][0][r] = __builtin_amdgcn_exp2f(fmaf(p[t][0][r], a.scale_log2, -ref));
-                sum += p[t][0][r];
+                p[t][r] = __builtin_amdgcn_exp2f(fmaf(p[t][r], a.scale_log2, -ref));
+                sum += p[t][r];
             }
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t)
-            if (!TAIL || 32 * t < left) mma_columns<T, DP, 1, DT>(acc, vc, 32 * t, p[t]);
+            if (!TAIL || 32 * t < left) mma_columns<T, DP, C::TERMS, DT>(acc, vc, 32 * t, p[t]);
     };
     int n = nodes.next(), odd = 0;
     if (n) stage(att_lds);
@@ -633,7 +633,7 @@ __global__ __launch_bounds__(ATT_THREADS, (AttFwd<T, DP, WM>::MIN_WAVES)) void k
         for (int t = 0; t < DT; ++t)
 #pragma unroll
             for (int r = 0; r < 16; r += 4)
-                store(qi, head, 32 * t + 2 * r + 4 * half, inv, f32x4{acc[0][t][r], acc[0][t][r + 1], acc[0][t][r + 2], acc[0][t][r + 3]});
+                store(qi, head, 32 * t + 2 * r + 4 * half, inv, f32x4{acc[t][r], acc[t][r + 1], acc[t][r + 2], acc[t][r + 3]});
     } else {
         // the waves' sums over their nodes, brought to one maximum
         float *jo = reinterpret_cast<float *>(att_lds), *jt = jo + ATT_WAVES * 32 * (DP + 4), *js = jt + ATT_WAVES * 32;
@@ -648,7 +648,7 @@ __global__ __launch_bounds__(ATT_THREADS, (AttFwd<T, DP, WM>::MIN_WAVES)) void k
 #pragma unroll
             for (int r = 0; r < 16; r += 4)
                 *reinterpret_cast<f32x4 *>(jo + mine_at * (DP + 4) + 32 * t + 2 * r + 4 * half) =
-                    f32x4{acc[0][t][r], acc[0][t][r + 1], acc[0][t][r + 2], acc[0][t][r + 3]};
+                    f32x4{acc[t][r], acc[t][r + 1], acc[t][r + 2], acc[t][r + 3]};
         __syncthreads();
         constexpr int G4 = DP / 4;
         const int n_here = (int)min((long long)C::BM, n_rows - m0);
@@ -716,14 +716,15 @@ template <typename T> __global__ __launch_bounds__(ATT_THREADS) void k_attend_jo
 __device__ inline float lse_log2(float lse) { return lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f; }
 
 // What both kernels of the backward pass need first.  Workgroups below `row_blocks`: delta[i] = d_o[i] . o[i] and the logarithms in base 2, 16 lanes
-// per query and head.  With a mask, one further workgroup per tree: the tree's nodes that may be read, one after the other in `list` from
+// per query and head (fp16: also the power of two that brings the row of d_o to a length of one: score gradients are fp16 operands, which neither
+// a scaled loss may overflow nor a small one let vanish).  With a mask, one further workgroup per tree: the tree's nodes that may be read, one after the other in `list` from
 // kv_off[tree] on, and their number in live[tree]; masked nodes then cost the others nothing.
 template <typename T> __global__ __launch_bounds__(ATT_THREADS) void k_attend_prepare(const AttArgs a, int row_blocks)
 {
     if ((int)blockIdx.x < row_blocks) {
         const int l16 = threadIdx.x & 15;
         const long long rh = ((long long)blockIdx.x * ATT_THREADS + threadIdx.x) >> 4, n = (long long)a.n_q * a.Hq;
-        float x = 0.f;
+        float x = 0.f, sq = 0.f;
         if (rh < n) {
             const int qi = (int)(rh / a.Hq), head = (int)(rh % a.Hq);
             const T *o = row_of<T>(a.o, qi, head), *g = row_of<T>(a.d_o, qi, head);
@@ -734,14 +735,21 @@ template <typename T> __global__ __launch_bounds__(ATT_THREADS) void k_attend_pr
                 __builtin_memcpy(y, &yo, 16);
                 __builtin_memcpy(z, &zo, 16);
 #pragma unroll
-                for (int j = 0; j < E; ++j) x = fmaf((float)y[j], (float)z[j], x);
+                for (int j = 0; j < E; ++j) {
+                    x = fmaf((float)y[j], (float)z[j], x);
+                    sq = fmaf((float)z[j], (float)z[j], sq);
+                }
             }
         }
 #pragma unroll
-        for (int o = 8; o >= 1; o >>= 1) x += __shfl_xor(x, o);
+        for (int o = 8; o >= 1; o >>= 1) {
+            x += __shfl_xor(x, o);
+            sq += __shfl_xor(sq, o);
+        }
         if (rh < n && l16 == 0) {
             a.delta[rh] = x;
             a.ref[rh] = lse_log2(a.lse[rh]);
+            if (std::is_same<T, f16_t>::value) a.size[rh] = sq > 0.f && sq < INFINITY ? exp2f(-ceilf(0.5f * log2f(sq))) : 1.f;
         }
         return;
     }
@@ -777,31 +785,32 @@ template <typename T> __global__ __launch_bounds__(ATT_THREADS) void k_attend_pr
     if (threadIdx.x == 0) a.live[tree] = n;
 }
 
-// dQ: like the forward, rows (queries) on the lanes' columns.  Waves side by side along the rows (WM) and, for wide heads, along the
-// columns of dQ (WD), where every wave of a row tile works out the tile's scores itself.
-template <typename T, int DP> struct AttDq {
-    static constexpr int THREADS = ATT_THREADS;
+// dQ: like the forward, rows (queries) on the lanes' columns.  Four waves: WM side by side along the rows, WK along the nodes (their sums are joined
+// at the end) and, for wide heads, WD along the columns of dQ, where every wave of a row tile works out the tile's scores itself.
+template <typename T, int DP, int WM_> struct AttDq {
     static constexpr int WD = DP > 128 ? 2 : 1;
-    static constexpr int WM = ATT_WAVES / WD;
+    static constexpr int WM = DP > 128 ? 2 : WM_;
+    static constexpr int WK = ATT_WAVES / WM / WD;
     static constexpr int BM = 32 * WM;
-    static constexpr int NT = DP * (int)sizeof(T) <= 256 ? 2 : 1;
-    static constexpr int BN = 32 * NT;
+    static constexpr int NT = WK == 1 && DP * (int)sizeof(T) <= 256 ? 2 : 1;
+    static constexpr int BN = 32 * WK * NT;
     static constexpr int DT = DP / 32 / WD;
     static constexpr int STAGE = 2 * BN * Rows<T, DP>::BYTES;
-    static constexpr int LDS = 2 * STAGE;
+    static constexpr int JOIN = WK > 1 ? WM * 32 * (DP + 4) * 4 : 0;
+    static constexpr int LDS = 2 * STAGE > JOIN ? 2 * STAGE : JOIN;
     static constexpr int MIN_WAVES = DP * (int)sizeof(T) > 256 ? 1 : 2;
 };
 
-template <typename T, int DP, bool VEC> __global__ __launch_bounds__(ATT_THREADS, (AttDq<T, DP>::MIN_WAVES)) void k_attend_dq(const AttArgs a)
+template <typename T, int DP, int WM, bool VEC> __global__ __launch_bounds__(ATT_THREADS, (AttDq<T, DP, WM>::MIN_WAVES)) void k_attend_dq(const AttArgs a)
 {
-    typedef AttDq<T, DP> C;
+    typedef AttDq<T, DP, WM> C;
     typedef Rows<T, DP> R;
     typedef typename Elem<T>::frag frag;
     constexpr int DT = C::DT, BN = C::BN;
     extern __shared__ __align__(16) unsigned char att_lds[];
 
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / C::WD, wd = wave % C::WD;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wd = wave % C::WD, wm = wave / C::WD % C::WM, wk = wave / C::WD / C::WM;
     const long long id = xcd_order(blockIdx.x, gridDim.x);
     const int slot = (int)(id % a.slots), hk = (int)(id / a.slots);
     long long tile;
@@ -826,10 +835,12 @@ template <typename T, int DP, bool VEC> __global__ __launch_bounds__(ATT_THREADS
             gf[s] = __builtin_bit_cast(frag, load_granule<T>(gr, 2 * s + half, a.D, VEC));
         }
     }
-    float row[2] = {a.ref[row_head], a.delta[row_head]};
-    floatx16 acc[1][DT];
+    float row[3] = {a.ref[row_head], a.delta[row_head], sizeof(T) == 2 && std::is_same<T, f16_t>::value ? a.size[row_head] : 1.f};
+    row[1] *= row[2];
+    const float out_scale = a.scale / row[2];
+    floatx16 acc[DT];
 #pragma unroll
-    for (int t = 0; t < DT; ++t) acc[0][t] = floatx16{};
+    for (int t = 0; t < DT; ++t) acc[t] = floatx16{};
 
     const T *kp = row_of<T>(a.k, 0, hk), *vp = row_of<T>(a.v, 0, hk);
     const ATT_GLOBAL int32_t *list = (const ATT_GLOBAL int32_t *)a.list + lo;
@@ -847,25 +858,27 @@ template <typename T, int DP, bool VEC> __global__ __launch_bounds__(ATT_THREADS
         }
         first += BN;
     };
-    RowReads<T, DP> kr(att_lds), vr(att_lds + C::STAGE / 2);
-    ColumnReads<T, DP> kc(att_lds, 32 * DT * wd);
+    const int own = 32 * C::NT * wk * R::BYTES;
+    RowReads<T, DP> kr(att_lds + own), vr(att_lds + C::STAGE / 2 + own);
+    ColumnReads<T, DP> kc(att_lds + own, 32 * DT * wd);
     // one stage of n nodes.  TAIL: some may be missing (rows of zeros, but exp2 of a large -lse would still be infinite).
     auto compute = [&](auto tail, int n) {
+        n -= 32 * C::NT * wk;
 #pragma unroll
         for (int j = 0; j < C::NT; ++j) {
             if (decltype(tail)::value && 32 * j >= n) break;
-            floatx16 p[1] = {}, dp = floatx16{};
+            floatx16 p = {}, dp = {};
 #pragma unroll
             for (int d = 0; d < R::STEPS; ++d) {
-                mma(p[0], kr.get(32 * j, d), qf[d]);
+                mma(p, kr.get(32 * j, d), qf[d]);
                 mma(dp, vr.get(32 * j, d), gf[d]);
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(p[0][r], a.scale_log2, -row[0])) * (dp[r] - row[1]);
-                p[0][r] = decltype(tail)::value && 32 * j + 8 * (r >> 2) + 4 * half + (r & 3) >= n ? 0.f : e;
+                const float e = __builtin_amdgcn_exp2f(fmaf(p[r], a.scale_log2, -row[0])) * fmaf(dp[r], row[2], -row[1]);
+                p[r] = decltype(tail)::value && 32 * j + 8 * (r >> 2) + 4 * half + (r & 3) >= n ? 0.f : e;
             }
-            mma_columns<T, DP, 1, DT>(acc, kc, 32 * j, p);
+            mma_columns<T, DP, 2, DT>(acc, kc, 32 * j, p);
         }
     };
     int left = n_nodes, odd = 0;
@@ -889,44 +902,64 @@ template <typename T, int DP, bool VEC> __global__ __launch_bounds__(ATT_THREADS
         __syncthreads();
         compute(std::true_type{}, left);
     }
+    if constexpr (C::WK == 2) {
+        float *join = reinterpret_cast<float *>(att_lds) + (wm * 32 + col) * (DP + 4);
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                if (wk == 1) *reinterpret_cast<f32x4 *>(join + 32 * t + 2 * r + 4 * half) = f32x4{acc[t][r], acc[t][r + 1], acc[t][r + 2], acc[t][r + 3]};
+        __syncthreads();
+        if (wk == 1) return;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const f32x4 y = *reinterpret_cast<const f32x4 *>(join + 32 * t + 2 * r + 4 * half);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[t][r + j] += y[j];
+            }
+    }
     if (!mine) return;
     T *o = row_of<T>(a.d_q, qi, head);
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
-            const floatx16 &x = acc[0][t];
-            store4<T>(o, 32 * (DT * wd + t) + 2 * r + 4 * half, a.D, a.vec_out, x[r] * a.scale, x[r + 1] * a.scale, x[r + 2] * a.scale, x[r + 3] * a.scale);
+            const floatx16 &x = acc[t];
+            store4<T>(o, 32 * (DT * wd + t) + 2 * r + 4 * half, a.D, a.vec_out, x[r] * out_scale, x[r + 1] * out_scale, x[r + 2] * out_scale, x[r + 3] * out_scale);
         }
 }
 
 // dK and dV: nodes on the lanes' columns, packed query rows go by in LDS.  Every sum over queries and over the heads of a group is
 // taken by one wave in one order: no atomics, the same bits every run.
-template <typename T, int DP> struct AttDkv {
-    static constexpr int THREADS = ATT_THREADS;
+template <typename T, int DP, int WN_> struct AttDkv {
     static constexpr int WD = DP <= 128 ? 1 : sizeof(T) == 2 ? 2 : 4;       // wide heads: waves along the columns of dK and dV
-    static constexpr int WN = ATT_WAVES / WD;
+    static constexpr int WN = DP <= 128 ? WN_ : ATT_WAVES / WD;
+    static constexpr int WQ = ATT_WAVES / WN / WD;                          // waves along the rows; their sums are joined at the end
     static constexpr int BN = 32 * WN;
-    static constexpr int QT = DP * (int)sizeof(T) <= 256 ? 2 : 1;
-    static constexpr int BQ = 32 * QT;
+    static constexpr int QT = WQ == 1 && DP * (int)sizeof(T) <= 256 ? 2 : 1;
+    static constexpr int BQ = 32 * WQ * QT;
     static constexpr int DT = DP / 32 / WD;
     static constexpr int STAGE = 2 * BQ * Rows<T, DP>::BYTES + 512;         // rows of q, of d_o, 64 logarithms, 64 deltas
-    static constexpr int LDS = 2 * STAGE;
+    static constexpr int JOIN = WQ > 1 ? WN * 32 * 2 * (DP + 4) * 4 : 0;
+    static constexpr int LDS = 2 * STAGE > JOIN ? 2 * STAGE : JOIN;
     static constexpr int MIN_WAVES = DP * (int)sizeof(T) > 256 || DP == 128 ? 1 : 2;
 };
 
 static __device__ const float att_no_row[2] = {INFINITY, 0.f};              // logarithm and delta of a row that is not there
 
-template <typename T, int DP, bool VEC> __global__ __launch_bounds__(ATT_THREADS, (AttDkv<T, DP>::MIN_WAVES)) void k_attend_dkv(const AttArgs a)
+template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT_THREADS, (AttDkv<T, DP, WN>::MIN_WAVES)) void k_attend_dkv(const AttArgs a)
 {
-    typedef AttDkv<T, DP> C;
+    typedef AttDkv<T, DP, WN> C;
     typedef Rows<T, DP> R;
     typedef typename Elem<T>::frag frag;
     constexpr int DT = C::DT, BQ = C::BQ, BN = C::BN;
     extern __shared__ __align__(16) unsigned char att_lds[];
 
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wn = wave / C::WD, wd = wave % C::WD;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wd = wave % C::WD, wn = wave / C::WD % C::WN, wq = wave / C::WD / C::WN;
     const long long id = xcd_order(blockIdx.x, gridDim.x);
     const int slot = (int)(id % a.slots), hk = (int)(id / a.slots);
     long long tile;
@@ -963,9 +996,9 @@ template <typename T, int DP, bool VEC> __global__ __launch_bounds__(ATT_THREADS
             vf[s] = __builtin_bit_cast(frag, load_granule<T>(vr, 2 * s + half, a.D, VEC));
         }
     }
-    floatx16 dk[1][DT], dv[1][DT];
+    floatx16 dk[DT], dv[DT];
 #pragma unroll
-    for (int t = 0; t < DT; ++t) dk[0][t] = dv[0][t] = floatx16{};
+    for (int t = 0; t < DT; ++t) dk[t] = dv[t] = floatx16{};
 
     // Groups that divide a stage: a thread's places are the same in every stage, BQ / G queries further on.
     const bool near = VEC && a.near && a.D == DP && BQ % a.G == 0;
@@ -1007,11 +1040,24 @@ template <typename T, int DP, bool VEC> __global__ __launch_bounds__(ATT_THREADS
         }
         first += BQ;
     };
-    RowReads<T, DP> qr(att_lds), gr(att_lds + BQ * R::BYTES);
-    ColumnReads<T, DP> qc(att_lds, 32 * DT * wd), gc(att_lds + BQ * R::BYTES, 32 * DT * wd);
-    const unsigned char *numbers = att_lds + 2 * BQ * R::BYTES + 16 * half;
+    const int own = 32 * C::QT * wq;            // the wave's first row of a stage
+    const unsigned char *q_own = att_lds + own * R::BYTES, *g_own = q_own + BQ * R::BYTES;
+    RowReads<T, DP> qr(q_own), gr(g_own);
+    ColumnReads<T, DP> qc(q_own, 32 * DT * wd), gc(g_own, 32 * DT * wd);
+    const unsigned char *numbers = att_lds + 2 * BQ * R::BYTES + 16 * half + 4 * own;
     const int n_stage = (int)((n_rows + BQ - 1) / BQ);
     if (n_stage) stage(att_lds);
+    // score gradients as fp16 operands: brought to the size of the tree's largest row of d_o
+    constexpr bool F16 = std::is_same<T, f16_t>::value;
+    float size = 1.f;
+    if constexpr (F16) {
+        float s = INFINITY;
+        for (long long m = lane; m < n_rows; m += 64) s = fminf(s, a.size[(q_lo + m / a.G) * a.Hq + hk * a.G + m % a.G]);
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) s = fminf(s, __shfl_xor(s, o));
+        size = s < INFINITY ? s : 1.f;
+    }
+    const float k_scale = a.scale / size;
     arrived(kf);
     arrived(vf);
     for (int s = 0; s < n_stage; ++s) {
@@ -1020,12 +1066,12 @@ template <typename T, int DP, bool VEC> __global__ __launch_bounds__(ATT_THREADS
         if (s + 1 < n_stage) stage(att_lds + (s & 1 ? 0 : C::STAGE));
 #pragma unroll
         for (int q = 0; q < C::QT; ++q) {
-            if (q > 0 && (long long)s * BQ + 32 * q >= n_rows) break;
-            floatx16 p[1] = {}, dp[1] = {};
+            if ((long long)s * BQ + own + 32 * q >= n_rows) break;
+            floatx16 p = {}, dp = {};
 #pragma unroll
             for (int d = 0; d < R::STEPS; ++d) {
-                mma(p[0], qr.get(32 * q, d), kf[d]);
-                mma(dp[0], gr.get(32 * q, d), vf[d]);
+                mma(p, qr.get(32 * q, d), kf[d]);
+                mma(dp, gr.get(32 * q, d), vf[d]);
             }
 #pragma unroll
             for (int r4 = 0; r4 < 4; ++r4) {
@@ -1034,12 +1080,12 @@ template <typename T, int DP, bool VEC> __global__ __launch_bounds__(ATT_THREADS
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int r = 4 * r4 + j;
-                    p[0][r] = __builtin_amdgcn_exp2f(fmaf(p[0][r], a.scale_log2, -rr[j]));
-                    dp[0][r] = p[0][r] * (dp[0][r] - dd[j]);
+                    p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], a.scale_log2, -rr[j]));
+                    dp[r] = p[r] * (F16 ? (dp[r] - dd[j]) * size : dp[r] - dd[j]);
                 }
             }
-            mma_columns<T, DP, 1, DT>(dv, gc, 32 * q, p);
-            mma_columns<T, DP, 1, DT>(dk, qc, 32 * q, dp);
+            mma_columns<T, DP, 2, DT>(dv, gc, 32 * q, p);
+            mma_columns<T, DP, 2, DT>(dk, qc, 32 * q, dp);
         }
         const int step = s & 1 ? -C::STAGE : C::STAGE;
         qr.move(step);
@@ -1048,6 +1094,31 @@ template <typename T, int DP, bool VEC> __global__ __launch_bounds__(ATT_THREADS
         gc.move(step);
         numbers += step;
     }
+    if constexpr (C::WQ == 2) {
+        float *join = reinterpret_cast<float *>(att_lds) + (wn * 32 + col) * 2 * (DP + 4);
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                if (wq == 1) {
+                    *reinterpret_cast<f32x4 *>(join + 32 * t + 2 * r + 4 * half) = f32x4{dk[t][r], dk[t][r + 1], dk[t][r + 2], dk[t][r + 3]};
+                    *reinterpret_cast<f32x4 *>(join + DP + 4 + 32 * t + 2 * r + 4 * half) = f32x4{dv[t][r], dv[t][r + 1], dv[t][r + 2], dv[t][r + 3]};
+                }
+        __syncthreads();
+        if (wq == 1) return;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const f32x4 y = *reinterpret_cast<const f32x4 *>(join + 32 * t + 2 * r + 4 * half), z = *reinterpret_cast<const f32x4 *>(join + DP + 4 + 32 * t + 2 * r + 4 * half);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    dk[t][r + j] += y[j];
+                    dv[t][r + j] += z[j];
+                }
+            }
+    }
     if (!mine) return;
     T *ok = row_of<T>(a.d_k, node, hk), *ov = row_of<T>(a.d_v, node, hk);
 #pragma unroll
@@ -1055,8 +1126,8 @@ template <typename T, int DP, bool VEC> __global__ __launch_bounds__(ATT_THREADS
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
             const int d = 32 * (DT * wd + t) + 2 * r + 4 * half;
-            const floatx16 &x = dk[0][t], &y = dv[0][t];
-            store4<T>(ok, d, a.D, a.vec_out, x[r] * a.scale, x[r + 1] * a.scale, x[r + 2] * a.scale, x[r + 3] * a.scale);
+            const floatx16 &x = dk[t], &y = dv[t];
+            store4<T>(ok, d, a.D, a.vec_out, x[r] * k_scale, x[r + 1] * k_scale, x[r + 2] * k_scale, x[r + 3] * k_scale);
             store4<T>(ov, d, a.D, a.vec_out, y[r], y[r + 1], y[r + 2], y[r + 3]);
         }
 }

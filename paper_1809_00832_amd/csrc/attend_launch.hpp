@@ -18,11 +18,25 @@ struct AttPlan {
 template <typename T> hipError_t attend_forward(const AttArgs &a, const AttPlan &p, hipStream_t st);
 template <typename T> hipError_t attend_backward(const AttArgs &a, hipStream_t st);
 
-template <typename K> hipError_t att_launch(K kernel, long long blocks, int threads, size_t lds, const AttArgs &a, hipStream_t st)
+// Allows a kernel its dynamic LDS, once per kernel and device (the call takes about as long as a launch).
+template <auto KERNEL> hipError_t att_allow(size_t lds)
 {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    static unsigned long long allowed;                          // devices
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3((unsigned)threads), lds, st, a);
+    const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
+    if (__atomic_load_n(&allowed, __ATOMIC_RELAXED) & bit) return hipSuccess;
+    e = hipFuncSetAttribute(reinterpret_cast<const void *>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e == hipSuccess) __atomic_fetch_or(&allowed, bit, __ATOMIC_RELAXED);
+    return e;
+}
+
+template <auto KERNEL> hipError_t att_launch(long long blocks, size_t lds, const AttArgs &a, hipStream_t st)
+{
+    const hipError_t e = att_allow<KERNEL>(lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(KERNEL, dim3((unsigned)blocks), dim3(ATT_THREADS), lds, st, a);
     return hipGetLastError();
 }
 
@@ -30,7 +44,7 @@ template <typename T, int DP, int WM> hipError_t att_forward_of(const AttArgs &a
 {
     typedef AttFwd<T, DP, WM> C;
     const long long blocks = (long long)a.slots * a.splits * a.Hk;
-    return a.vec ? att_launch(k_attend<T, DP, WM, true>, blocks, C::THREADS, C::LDS, a, st) : att_launch(k_attend<T, DP, WM, false>, blocks, C::THREADS, C::LDS, a, st);
+    return a.vec ? att_launch<k_attend<T, DP, WM, true>>(blocks, C::LDS, a, st) : att_launch<k_attend<T, DP, WM, false>>(blocks, C::LDS, a, st);
 }
 
 template <typename T, int DP> hipError_t att_forward_at(const AttArgs &a, const AttPlan &p, hipStream_t st)
@@ -41,7 +55,21 @@ template <typename T, int DP> hipError_t att_forward_at(const AttArgs &a, const 
     return att_forward_of<T, DP, 4>(a, st);
 }
 
-template <typename T, int DP, bool VEC> hipError_t att_backward_of(AttArgs a, hipStream_t st)
+template <typename T, int DP, int WM, bool VEC> hipError_t att_dq_of(AttArgs a, hipStream_t st)
+{
+    typedef AttDq<T, DP, WM> C;
+    a.slots = (int)((long long)a.n_q * a.G / C::BM + a.n_trees);
+    return att_launch<k_attend_dq<T, DP, C::WM, VEC>>((long long)a.slots * a.Hk, C::LDS, a, st);
+}
+
+template <typename T, int DP, int WN, bool VEC> hipError_t att_dkv_of(AttArgs a, hipStream_t st)
+{
+    typedef AttDkv<T, DP, WN> C;
+    a.slots = a.n_kv / C::BN + a.n_trees;
+    return att_launch<k_attend_dkv<T, DP, C::WN, VEC>>((long long)a.slots * a.Hk, C::LDS, a, st);
+}
+
+template <typename T, int DP, bool VEC> hipError_t att_backward_of(const AttArgs &a, hipStream_t st)
 {
     const long long rows = (long long)a.n_q * a.G, row_blocks = ((long long)a.n_q * a.Hq + 15) / 16;
     if (row_blocks + (a.mask ? a.n_trees : 0) > 0) {
@@ -49,15 +77,14 @@ template <typename T, int DP, bool VEC> hipError_t att_backward_of(AttArgs a, hi
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
+    // Short trees (their rows, or their nodes, on average): fewer of them at a time, and the other side divided among the waves instead.  Measured (us,
+    // 2 / 4 waves side by side): 256 trees of 33 rows, 54 nodes, fp32 x 64: dQ 73 / 93, dK and dV 97 / 96; 25 such trees, x 30: 12 / 14 and 10 / 12; 8 trees
+    // of 1536 rows, 1200 nodes, bf16 x 128: 177 / 127 and 206 / 180.
     if (a.n_q > 0) {
-        a.slots = (int)(rows / AttDq<T, DP>::BM + a.n_trees);
-        const hipError_t e = att_launch(k_attend_dq<T, DP, VEC>, (long long)a.slots * a.Hk, ATT_THREADS, AttDq<T, DP>::LDS, a, st);
+        const hipError_t e = rows <= 128 * (long long)a.n_trees ? att_dq_of<T, DP, 2, VEC>(a, st) : att_dq_of<T, DP, 4, VEC>(a, st);
         if (e != hipSuccess) return e;
     }
-    if (a.n_kv > 0) {
-        a.slots = a.n_kv / AttDkv<T, DP>::BN + a.n_trees;
-        return att_launch(k_attend_dkv<T, DP, VEC>, (long long)a.slots * a.Hk, ATT_THREADS, AttDkv<T, DP>::LDS, a, st);
-    }
+    if (a.n_kv > 0) return a.n_kv <= 128 * (long long)a.n_trees ? att_dkv_of<T, DP, 2, VEC>(a, st) : att_dkv_of<T, DP, 4, VEC>(a, st);
     return hipSuccess;
 }
 

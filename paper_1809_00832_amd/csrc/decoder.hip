@@ -80,7 +80,7 @@ long long round16(long long x) { return (x + 15) & ~15ll; }
 long long workspace(const tl_attention *a, const AttPlan &p, int backward)
 {
     const long long rh = (long long)a->n_q * a->n_heads;
-    if (backward) return 2 * round16(rh * 4) + (a->kv_mask ? round16(4ll * a->n_kv) + round16(4ll * a->n_trees) : 0);
+    if (backward) return (a->dtype == TL_DT_F16 ? 3 : 2) * round16(rh * 4) + (a->kv_mask ? round16(4ll * a->n_kv) + round16(4ll * a->n_trees) : 0);
     return p.splits > 1 ? round16(p.splits * rh * 4) + round16(p.splits * rh * a->head_dim * 4) : 0;
 }
 
@@ -111,6 +111,14 @@ AttArgs arguments(const tl_attention *a)
 }
 
 bool pieces_of_4(const tl_rows &t, int dtype, int D) { return in_pieces(t, dtype, D, 4 * element_size(dtype)); }
+
+template <typename T> hipError_t sample(const SampleArgs &a, int n_rows, hipStream_t st)
+{
+    const hipError_t e = att_allow<k_sample<T>>(sizeof(SmpShared));
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(k_sample<T>, dim3((unsigned)n_rows), dim3(SMP_THREADS), sizeof(SmpShared), st, a);
+    return hipGetLastError();
+}
 
 }  // namespace
 
@@ -175,8 +183,13 @@ int tl_attend_backward(const tl_attention *a, const tl_rows *o, const float *lse
     char *w = static_cast<char *>(workspace_p);
     x.delta = reinterpret_cast<float *>(w);
     x.ref = reinterpret_cast<float *>(w + round16(rh * 4));
-    x.list = reinterpret_cast<int32_t *>(w + 2 * round16(rh * 4));
-    x.live = reinterpret_cast<int32_t *>(w + 2 * round16(rh * 4) + round16(4ll * a->n_kv));
+    w += 2 * round16(rh * 4);
+    if (dt == TL_DT_F16) {
+        x.size = reinterpret_cast<float *>(w);
+        w += round16(rh * 4);
+    }
+    x.list = reinterpret_cast<int32_t *>(w);
+    x.live = reinterpret_cast<int32_t *>(w + round16(4ll * a->n_kv));
     x.vec = x.vec && in_pieces(*o, dt, D, 16) && in_pieces(*d_o, dt, D, 16);
     x.near = x.near && d_o->row < (1 << 20) && d_o->head < (1 << 20);
     x.vec_out = pieces_of_4(*d_q, dt, D) && pieces_of_4(*d_k, dt, D) && pieces_of_4(*d_v, dt, D);
@@ -206,12 +219,9 @@ int tl_sample(int dtype, int n_rows, int vocab, const void *logits, int64_t row,
     int bits = 0;
     while ((1ll << bits) < vocab) ++bits;
     a.shift = 62 - bits < 51 ? 62 - bits : 51;
-    const dim3 grid((unsigned)n_rows), block(SMP_THREADS);
     const hipStream_t st = (hipStream_t)hip_stream;
-    void (*const k)(SampleArgs) = dtype == TL_DT_F32 ? k_sample<float> : dtype == TL_DT_BF16 ? k_sample<bf16_t> : k_sample<f16_t>;
-    if (hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SmpShared)) != hipSuccess) return TL_EHIP;
-    hipLaunchKernelGGL(k, grid, block, sizeof(SmpShared), st, a);
-    return hipGetLastError() == hipSuccess ? TL_OK : TL_EHIP;
+    const hipError_t e = dtype == TL_DT_F32 ? sample<float>(a, n_rows, st) : dtype == TL_DT_BF16 ? sample<bf16_t>(a, n_rows, st) : sample<f16_t>(a, n_rows, st);
+    return e == hipSuccess ? TL_OK : TL_EHIP;
 }
 
 }  // extern "C"

@@ -387,3 +387,20 @@ def test_an_encoders_states_are_read_and_given_gradients():
     grads = binding.tl_backward(net.ctx, batch, g_h, w.params.embed_dim)
     assert grads["d_u"].isfinite().all() and grads["d_u"].any()
     net.close()
+
+
+@pytest.mark.parametrize("size", [2.0 ** -14, 1.0, 2.0 ** 10])
+def test_fp16_gradients_of_any_size(size):
+    """Score gradients as operands of 16 bits: upstream gradients near the type's least normal value, and large ones of a scaled loss, beside rows a
+    thousand times smaller in another tree.  The bound is that of test_against_64_bits; gradients whose values fp16 cannot hold are left out."""
+    s = tensors(22, torch.float16, [40, 3, 150], [50, 70, 90], 4, 2, 64, 0.2)
+    s["d_o"] = (s["d_o"].float() * size).half()
+    s["d_o"][40:43] *= 2.0 ** -6
+    ref, err = plain(s)
+    got = call(s)
+    for n in got:
+        fits = ref[n].abs() < 6e4
+        assert fits.float().mean() > 0.99
+        x = got[n].double()
+        bad = fits & (x != ref[n]) & ~((x - ref[n]).abs() <= err[n])
+        assert not bad.any(), n
