@@ -50,10 +50,11 @@ struct AttArgs {
     const uint8_t *mask;
     float *lse;             // [n_q x n_heads], natural logarithm
     float *delta, *ref;     // backward: sum over d of d_o * o, and lse in base 2, [n_q x n_heads]
-    float *size;            // backward, fp16: power of two that brings a row of d_o to a length of one, [n_q x n_heads]
+    float *size;            // backward, fp16: power of two that brings a row of d_o to a length of 2^10, [n_q x n_heads]
     int32_t *list, *live;   // backward, with a mask: the nodes that may be read, tree by tree from kv_off on, and how many a tree has
     float *part_o;          // splits > 1: outputs of each part, [splits][n_q x n_heads][D]
     float *part_lse;        // ... and their logarithms, [splits][n_q x n_heads]
+    float *part_q, *part_kv; // backward, splits > 1: parts of dQ [splits][n_q x n_heads][D], of dK and dV [splits][n_kv x n_kv_heads][2][D]
     float scale, scale_log2;
     int n_trees, n_q, n_kv, Hq, Hk, G, D;
     int slots;              // row tiles (see find_slot)
@@ -245,6 +246,40 @@ __device__ inline void mma_columns(floatx16 (&c)[NT], const ColumnReads<T, DP> &
     }
 }
 
+// What lane l ^ 32 holds, joined with the lane's own.
+__device__ inline float max_of_halves(float x)
+{
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+__device__ inline float sum_of_halves(float x)
+{
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    return __uint_as_float(y[0]) + __uint_as_float(y[1]);
+}
+
+// fp16 score gradients on their way into a product: neither may a scaled loss overflow them nor a small one let them vanish.  A lane's column of the
+// sums c carries a power of two, `size`, which is lowered (and the sums with it) when a gradient would come near the type's largest value.
+template <int NT> __device__ inline void fit_fp16(floatx16 &w, float &size, floatx16 (&c)[NT])
+{
+    float high = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) high = fmaxf(high, fabsf(w[r]));
+    high = max_of_halves(high) * size;
+    if (__any(high > 32768.f)) {
+        const float f = high > 32768.f ? exp2f(-ceilf(log2f(high * 0x1p-10f))) : 1.f;
+        size *= f;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) c[t][r] *= f;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) w[r] *= size;
+}
+
 // ---- global memory ----------------------------------------------------------------------
 
 // (Pointers out of the argument struct are cast to global memory: through generic ones loads and LDS reads would wait for each other.)
@@ -289,20 +324,6 @@ template <typename T> __device__ inline void store4(T *row, int d, int D, bool v
 template <typename T> __device__ inline T *row_of(const AttTensor &a, long long row, int head)
 {
     return static_cast<T *>(a.p) + row * a.row + (long long)head * a.head;
-}
-
-// What lane l ^ 32 holds, joined with the lane's own.
-__device__ inline float max_of_halves(float x)
-{
-    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-    const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
-    return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
-}
-__device__ inline float sum_of_halves(float x)
-{
-    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-    const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
-    return __uint_as_float(y[0]) + __uint_as_float(y[1]);
 }
 
 // ---- staging straight into LDS ------------------------------------------------------------
@@ -716,8 +737,7 @@ template <typename T> __global__ __launch_bounds__(ATT_THREADS) void k_attend_jo
 __device__ inline float lse_log2(float lse) { return lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f; }
 
 // What both kernels of the backward pass need first.  Workgroups below `row_blocks`: delta[i] = d_o[i] . o[i] and the logarithms in base 2, 16 lanes
-// per query and head (fp16: also the power of two that brings the row of d_o to a length of one: score gradients are fp16 operands, which neither
-// a scaled loss may overflow nor a small one let vanish).  With a mask, one further workgroup per tree: the tree's nodes that may be read, one after the other in `list` from
+// per query and head (fp16: also the power of two that brings the row of d_o to a length of 2^10, see fit_fp16).  With a mask, one further workgroup per tree: the tree's nodes that may be read, one after the other in `list` from
 // kv_off[tree] on, and their number in live[tree]; masked nodes then cost the others nothing.
 template <typename T> __global__ __launch_bounds__(ATT_THREADS) void k_attend_prepare(const AttArgs a, int row_blocks)
 {
@@ -749,7 +769,7 @@ template <typename T> __global__ __launch_bounds__(ATT_THREADS) void k_attend_pr
         if (rh < n && l16 == 0) {
             a.delta[rh] = x;
             a.ref[rh] = lse_log2(a.lse[rh]);
-            if (std::is_same<T, f16_t>::value) a.size[rh] = sq > 0.f && sq < INFINITY ? exp2f(-ceilf(0.5f * log2f(sq))) : 1.f;
+            if (std::is_same<T, f16_t>::value) a.size[rh] = sq > 0.f && sq < INFINITY ? exp2f(10.f - ceilf(0.5f * log2f(sq))) : 1.f;
         }
         return;
     }
@@ -812,7 +832,7 @@ template <typename T, int DP, int WM, bool VEC> __global__ __launch_bounds__(ATT
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wd = wave % C::WD, wm = wave / C::WD % C::WM, wk = wave / C::WD / C::WM;
     const long long id = xcd_order(blockIdx.x, gridDim.x);
-    const int slot = (int)(id % a.slots), hk = (int)(id / a.slots);
+    const int slot = (int)(id % a.slots), part = (int)(id / a.slots % a.splits), hk = (int)(id / a.slots / a.splits);
     long long tile;
     const int tree = find_slot(a.q_off, a.n_trees, a.G, C::BM == 64 ? 6 : 7, slot, &tile);
     int q_lo, q_hi, lo, hi;
@@ -820,7 +840,13 @@ template <typename T, int DP, int WM, bool VEC> __global__ __launch_bounds__(ATT
     const long long n_rows = (long long)(q_hi - q_lo) * a.G, m0 = tile * C::BM;
     if (tile < 0 || m0 >= n_rows) return;
     tree_range(a.kv_off, tree, a.n_kv, &lo, &hi);
-    const int n_nodes = a.mask ? min(__builtin_amdgcn_readfirstlane(a.live[tree]), hi - lo) : hi - lo;
+    int n_nodes = a.mask ? min(__builtin_amdgcn_readfirstlane(a.live[tree]), hi - lo) : hi - lo;
+    int first = 0;                              // of the stage that is staged next
+    if (a.splits > 1) {
+        const int n_stage = (n_nodes + BN - 1) / BN, per = (n_stage + a.splits - 1) / a.splits;
+        first = min(part * per * BN, n_nodes);
+        n_nodes = min(first + per * BN, n_nodes);
+    }
 
     const long long m = m0 + 32 * wm + col;
     const bool mine = m < n_rows;
@@ -835,9 +861,8 @@ template <typename T, int DP, int WM, bool VEC> __global__ __launch_bounds__(ATT
             gf[s] = __builtin_bit_cast(frag, load_granule<T>(gr, 2 * s + half, a.D, VEC));
         }
     }
-    float row[3] = {a.ref[row_head], a.delta[row_head], sizeof(T) == 2 && std::is_same<T, f16_t>::value ? a.size[row_head] : 1.f};
-    row[1] *= row[2];
-    const float out_scale = a.scale / row[2];
+    constexpr bool F16 = std::is_same<T, f16_t>::value;
+    float row[3] = {a.ref[row_head], a.delta[row_head], F16 ? a.size[row_head] : 1.f};
     floatx16 acc[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) acc[t] = floatx16{};
@@ -846,7 +871,6 @@ template <typename T, int DP, int WM, bool VEC> __global__ __launch_bounds__(ATT
     const ATT_GLOBAL int32_t *list = (const ATT_GLOBAL int32_t *)a.list + lo;
     const bool near = VEC && !a.mask && a.near && a.D == DP;
     const NearRows<T, DP, BN, ATT_THREADS> k_near(a.k.row), v_near(a.v.row);
-    int first = 0;                              // of the stage that is staged next
     auto stage = [&](unsigned char *b, int n) {
         if (near && n == BN) {
             k_near.stage(b, kp + (lo + first) * a.k.row);
@@ -875,13 +899,14 @@ template <typename T, int DP, int WM, bool VEC> __global__ __launch_bounds__(ATT
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(p[r], a.scale_log2, -row[0])) * fmaf(dp[r], row[2], -row[1]);
+                const float e = __builtin_amdgcn_exp2f(fmaf(p[r], a.scale_log2, -row[0])) * (dp[r] - row[1]);
                 p[r] = decltype(tail)::value && 32 * j + 8 * (r >> 2) + 4 * half + (r & 3) >= n ? 0.f : e;
             }
+            if constexpr (F16) fit_fp16(p, row[2], acc);
             mma_columns<T, DP, 2, DT>(acc, kc, 32 * j, p);
         }
     };
-    int left = n_nodes, odd = 0;
+    int left = n_nodes - first, odd = 0;
     if (left > 0) stage(att_lds, min(left, BN));
     arrived(qf);
     arrived(gf);
@@ -902,6 +927,9 @@ template <typename T, int DP, int WM, bool VEC> __global__ __launch_bounds__(ATT
         __syncthreads();
         compute(std::true_type{}, left);
     }
+    const float out_scale = a.scale / row[2];
+#pragma unroll
+    for (int t = 0; t < DT; ++t) acc[t] *= out_scale;
     if constexpr (C::WK == 2) {
         float *join = reinterpret_cast<float *>(att_lds) + (wm * 32 + col) * (DP + 4);
         __syncthreads();
@@ -923,12 +951,15 @@ template <typename T, int DP, int WM, bool VEC> __global__ __launch_bounds__(ATT
     }
     if (!mine) return;
     T *o = row_of<T>(a.d_q, qi, head);
+    float *po = a.part_q + ((long long)part * a.n_q * a.Hq + row_head) * a.D;
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
-            const floatx16 &x = acc[t];
-            store4<T>(o, 32 * (DT * wd + t) + 2 * r + 4 * half, a.D, a.vec_out, x[r] * out_scale, x[r + 1] * out_scale, x[r + 2] * out_scale, x[r + 3] * out_scale);
+            const int d = 32 * (DT * wd + t) + 2 * r + 4 * half;
+            const f32x4 x = {acc[t][r], acc[t][r + 1], acc[t][r + 2], acc[t][r + 3]};
+            if (a.splits > 1) store4<float>(po, d, a.D, (a.D & 3) == 0, x[0], x[1], x[2], x[3]);
+            else store4<T>(o, d, a.D, a.vec_out, x[0], x[1], x[2], x[3]);
         }
 }
 
@@ -961,7 +992,7 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wd = wave % C::WD, wn = wave / C::WD % C::WN, wq = wave / C::WD / C::WN;
     const long long id = xcd_order(blockIdx.x, gridDim.x);
-    const int slot = (int)(id % a.slots), hk = (int)(id / a.slots);
+    const int slot = (int)(id % a.slots), part = (int)(id / a.slots % a.splits), hk = (int)(id / a.slots / a.splits);
     long long tile;
     const int tree = find_slot(a.kv_off, a.n_trees, 1, BN == 32 ? 5 : BN == 64 ? 6 : 7, slot, &tile);
     int q_lo, q_hi, lo, hi;
@@ -974,7 +1005,7 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
     if (a.mask) {
         // masked nodes among the tile's own: zeros
         n_nodes = min(__builtin_amdgcn_readfirstlane(a.live[tree]), n_nodes);
-        const int end = min(t0 + BN, hi - lo);
+        const int end = part == 0 ? min(t0 + BN, hi - lo) : t0;
         for (int r = t0 + wave; r < end; r += ATT_WAVES) {
             if (a.mask[lo + r]) continue;
             T *ok = row_of<T>(a.d_k, lo + r, hk), *ov = row_of<T>(a.d_v, lo + r, hk);
@@ -1012,7 +1043,13 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
         q_offset[i] = ((uint32_t)qr * (uint32_t)a.q.row + (uint32_t)hr * (uint32_t)a.q.head) * (uint32_t)sizeof(T) + g * 16;
         g_offset[i] = ((uint32_t)qr * (uint32_t)a.d_o.row + (uint32_t)hr * (uint32_t)a.d_o.head) * (uint32_t)sizeof(T) + g * 16;
     }
-    long long first = 0;                        // packed row that is staged next
+    int n_stage = (int)((n_rows + BQ - 1) / BQ), s_lo = 0;
+    if (a.splits > 1) {
+        const int per = (n_stage + a.splits - 1) / a.splits;
+        s_lo = min(part * per, n_stage);
+        n_stage = min(s_lo + per, n_stage);
+    }
+    long long first = (long long)s_lo * BQ;     // packed row that is staged next
     auto stage = [&](unsigned char *b) {
         if (near && first + BQ <= n_rows) {
             const int q0 = q_lo + (int)(first / a.G);
@@ -1045,9 +1082,8 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
     RowReads<T, DP> qr(q_own), gr(g_own);
     ColumnReads<T, DP> qc(q_own, 32 * DT * wd), gc(g_own, 32 * DT * wd);
     const unsigned char *numbers = att_lds + 2 * BQ * R::BYTES + 16 * half + 4 * own;
-    const int n_stage = (int)((n_rows + BQ - 1) / BQ);
-    if (n_stage) stage(att_lds);
-    // score gradients as fp16 operands: brought to the size of the tree's largest row of d_o
+    if (s_lo < n_stage) stage(att_lds);
+    // score gradients as fp16 operands: begin at the size of the tree's largest row of d_o
     constexpr bool F16 = std::is_same<T, f16_t>::value;
     float size = 1.f;
     if constexpr (F16) {
@@ -1057,13 +1093,12 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
         for (int o = 32; o >= 1; o >>= 1) s = fminf(s, __shfl_xor(s, o));
         size = s < INFINITY ? s : 1.f;
     }
-    const float k_scale = a.scale / size;
     arrived(kf);
     arrived(vf);
-    for (int s = 0; s < n_stage; ++s) {
+    for (int s = s_lo, odd = 0; s < n_stage; ++s, odd ^= 1) {
         stage_wait();
         __syncthreads();
-        if (s + 1 < n_stage) stage(att_lds + (s & 1 ? 0 : C::STAGE));
+        if (s + 1 < n_stage) stage(att_lds + (odd ? 0 : C::STAGE));
 #pragma unroll
         for (int q = 0; q < C::QT; ++q) {
             if ((long long)s * BQ + own + 32 * q >= n_rows) break;
@@ -1081,19 +1116,23 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
                 for (int j = 0; j < 4; ++j) {
                     const int r = 4 * r4 + j;
                     p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], a.scale_log2, -rr[j]));
-                    dp[r] = p[r] * (F16 ? (dp[r] - dd[j]) * size : dp[r] - dd[j]);
+                    dp[r] = p[r] * (dp[r] - dd[j]);
                 }
             }
             mma_columns<T, DP, 2, DT>(dv, gc, 32 * q, p);
+            if constexpr (F16) fit_fp16(dp, size, dk);
             mma_columns<T, DP, 2, DT>(dk, qc, 32 * q, dp);
         }
-        const int step = s & 1 ? -C::STAGE : C::STAGE;
+        const int step = odd ? -C::STAGE : C::STAGE;
         qr.move(step);
         gr.move(step);
         qc.move(step);
         gc.move(step);
         numbers += step;
     }
+    const float k_scale = a.scale / size;
+#pragma unroll
+    for (int t = 0; t < DT; ++t) dk[t] *= k_scale;
     if constexpr (C::WQ == 2) {
         float *join = reinterpret_cast<float *>(att_lds) + (wn * 32 + col) * 2 * (DP + 4);
         __syncthreads();
@@ -1121,15 +1160,48 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
     }
     if (!mine) return;
     T *ok = row_of<T>(a.d_k, node, hk), *ov = row_of<T>(a.d_v, node, hk);
+    float *pk = a.part_kv + (((long long)part * a.n_kv + node) * a.Hk + hk) * 2 * a.D, *pv = pk + a.D;
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
             const int d = 32 * (DT * wd + t) + 2 * r + 4 * half;
-            const floatx16 &x = dk[t], &y = dv[t];
-            store4<T>(ok, d, a.D, a.vec_out, x[r] * k_scale, x[r + 1] * k_scale, x[r + 2] * k_scale, x[r + 3] * k_scale);
-            store4<T>(ov, d, a.D, a.vec_out, y[r], y[r + 1], y[r + 2], y[r + 3]);
+            const f32x4 x = {dk[t][r], dk[t][r + 1], dk[t][r + 2], dk[t][r + 3]}, y = {dv[t][r], dv[t][r + 1], dv[t][r + 2], dv[t][r + 3]};
+            if (a.splits > 1) {
+                store4<float>(pk, d, a.D, (a.D & 3) == 0, x[0], x[1], x[2], x[3]);
+                store4<float>(pv, d, a.D, (a.D & 3) == 0, y[0], y[1], y[2], y[3]);
+            } else {
+                store4<T>(ok, d, a.D, a.vec_out, x[0], x[1], x[2], x[3]);
+                store4<T>(ov, d, a.D, a.vec_out, y[0], y[1], y[2], y[3]);
+            }
         }
+}
+
+// Adds up the parts of split gradients, part by part: workgroups below `q_blocks` those of dQ (q_splits parts), the others those of dK and dV.  A wave takes
+// a row of D elements.
+template <typename T> __global__ __launch_bounds__(ATT_THREADS) void k_attend_sum(const AttArgs a, int q_blocks, int q_splits, int kv_splits)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool of_q = (int)blockIdx.x < q_blocks;
+    const long long i = (long long)((int)blockIdx.x - (of_q ? 0 : q_blocks)) * ATT_WAVES + wave, n = of_q ? (long long)a.n_q * a.Hq : 2ll * a.n_kv * a.Hk;
+    if (i >= n) return;
+    const float *from = (of_q ? a.part_q : a.part_kv) + i * a.D;
+    T *to;
+    bool dead = false;
+    if (of_q) {
+        to = row_of<T>(a.d_q, i / a.Hq, (int)(i % a.Hq));
+    } else {
+        const long long node = i / 2 / a.Hk;
+        dead = a.mask && !a.mask[node];         // (its parts were not written)
+        to = row_of<T>(i & 1 ? a.d_v : a.d_k, node, (int)(i / 2 % a.Hk));
+    }
+    const int parts = of_q ? q_splits : kv_splits;
+    for (int d = lane; d < a.D; d += 64) {
+        float x = 0.f;
+        if (!dead)
+            for (int p = 0; p < parts; ++p) x += from[p * n * a.D + d];
+        to[d] = (T)x;
+    }
 }
 
 }  // namespace tl

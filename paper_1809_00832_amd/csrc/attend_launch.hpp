@@ -15,8 +15,14 @@ struct AttPlan {
     int slots, splits;
 };
 
+// ... and a backward call: waves side by side along the rows (AttDq) and the nodes (AttDkv), parts that a tree's nodes and its rows are cut into.
+struct AttBackPlan {
+    int q_waves, kv_waves;
+    int q_splits, kv_splits;
+};
+
 template <typename T> hipError_t attend_forward(const AttArgs &a, const AttPlan &p, hipStream_t st);
-template <typename T> hipError_t attend_backward(const AttArgs &a, hipStream_t st);
+template <typename T> hipError_t attend_backward(const AttArgs &a, const AttBackPlan &p, hipStream_t st);
 
 // Allows a kernel its dynamic LDS, once per kernel and device (the call takes about as long as a launch).
 template <auto KERNEL> hipError_t att_allow(size_t lds)
@@ -55,42 +61,44 @@ template <typename T, int DP> hipError_t att_forward_at(const AttArgs &a, const 
     return att_forward_of<T, DP, 4>(a, st);
 }
 
-template <typename T, int DP, int WM, bool VEC> hipError_t att_dq_of(AttArgs a, hipStream_t st)
+template <typename T, int DP, int WM, bool VEC> hipError_t att_dq_of(AttArgs a, int splits, hipStream_t st)
 {
     typedef AttDq<T, DP, WM> C;
     a.slots = (int)((long long)a.n_q * a.G / C::BM + a.n_trees);
-    return att_launch<k_attend_dq<T, DP, C::WM, VEC>>((long long)a.slots * a.Hk, C::LDS, a, st);
+    a.splits = splits;
+    return att_launch<k_attend_dq<T, DP, C::WM, VEC>>((long long)a.slots * splits * a.Hk, C::LDS, a, st);
 }
 
-template <typename T, int DP, int WN, bool VEC> hipError_t att_dkv_of(AttArgs a, hipStream_t st)
+template <typename T, int DP, int WN, bool VEC> hipError_t att_dkv_of(AttArgs a, int splits, hipStream_t st)
 {
     typedef AttDkv<T, DP, WN> C;
     a.slots = a.n_kv / C::BN + a.n_trees;
-    return att_launch<k_attend_dkv<T, DP, C::WN, VEC>>((long long)a.slots * a.Hk, C::LDS, a, st);
+    a.splits = splits;
+    return att_launch<k_attend_dkv<T, DP, C::WN, VEC>>((long long)a.slots * splits * a.Hk, C::LDS, a, st);
 }
 
-template <typename T, int DP, bool VEC> hipError_t att_backward_of(const AttArgs &a, hipStream_t st)
+template <typename T, int DP, bool VEC> hipError_t att_backward_of(const AttArgs &a, const AttBackPlan &p, hipStream_t st)
 {
-    const long long rows = (long long)a.n_q * a.G, row_blocks = ((long long)a.n_q * a.Hq + 15) / 16;
+    hipError_t e = hipSuccess;
+    const long long row_blocks = ((long long)a.n_q * a.Hq + 15) / 16;
     if (row_blocks + (a.mask ? a.n_trees : 0) > 0) {
         hipLaunchKernelGGL(k_attend_prepare<T>, dim3((unsigned)(row_blocks + (a.mask ? a.n_trees : 0))), dim3(ATT_THREADS), 0, st, a, (int)row_blocks);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
+        e = hipGetLastError();
     }
-    // Short trees (their rows, or their nodes, on average): fewer of them at a time, and the other side divided among the waves instead.  Measured (us,
-    // 2 / 4 waves side by side): 256 trees of 33 rows, 54 nodes, fp32 x 64: dQ 73 / 93, dK and dV 97 / 96; 25 such trees, x 30: 12 / 14 and 10 / 12; 8 trees
-    // of 1536 rows, 1200 nodes, bf16 x 128: 177 / 127 and 206 / 180.
-    if (a.n_q > 0) {
-        const hipError_t e = rows <= 128 * (long long)a.n_trees ? att_dq_of<T, DP, 2, VEC>(a, st) : att_dq_of<T, DP, 4, VEC>(a, st);
-        if (e != hipSuccess) return e;
+    if (e == hipSuccess && a.n_q > 0) e = p.q_waves == 2 ? att_dq_of<T, DP, 2, VEC>(a, p.q_splits, st) : att_dq_of<T, DP, 4, VEC>(a, p.q_splits, st);
+    if (e == hipSuccess && a.n_kv > 0) e = p.kv_waves == 2 ? att_dkv_of<T, DP, 2, VEC>(a, p.kv_splits, st) : att_dkv_of<T, DP, 4, VEC>(a, p.kv_splits, st);
+    if (e == hipSuccess && (p.q_splits > 1 || p.kv_splits > 1)) {
+        const long long q_blocks = p.q_splits > 1 ? ((long long)a.n_q * a.Hq + ATT_WAVES - 1) / ATT_WAVES : 0;
+        const long long kv_blocks = p.kv_splits > 1 ? (2ll * a.n_kv * a.Hk + ATT_WAVES - 1) / ATT_WAVES : 0;
+        hipLaunchKernelGGL(k_attend_sum<T>, dim3((unsigned)(q_blocks + kv_blocks)), dim3(ATT_THREADS), 0, st, a, (int)q_blocks, p.q_splits, p.kv_splits);
+        e = hipGetLastError();
     }
-    if (a.n_kv > 0) return a.n_kv <= 128 * (long long)a.n_trees ? att_dkv_of<T, DP, 2, VEC>(a, st) : att_dkv_of<T, DP, 4, VEC>(a, st);
-    return hipSuccess;
+    return e;
 }
 
-template <typename T, int DP> hipError_t att_backward_at(const AttArgs &a, hipStream_t st)
+template <typename T, int DP> hipError_t att_backward_at(const AttArgs &a, const AttBackPlan &p, hipStream_t st)
 {
-    return a.vec ? att_backward_of<T, DP, true>(a, st) : att_backward_of<T, DP, false>(a, st);
+    return a.vec ? att_backward_of<T, DP, true>(a, p, st) : att_backward_of<T, DP, false>(a, p, st);
 }
 
 #define ATT_INSTANCES(T)                                                                                                       \
@@ -109,13 +117,13 @@ template <typename T, int DP> hipError_t att_backward_at(const AttArgs &a, hipSt
                            p.bn);                                                                                              \
         return hipGetLastError();                                                                                              \
     }                                                                                                                          \
-    template <> hipError_t attend_backward<T>(const AttArgs &a, hipStream_t st)                                                \
+    template <> hipError_t attend_backward<T>(const AttArgs &a, const AttBackPlan &p, hipStream_t st)                          \
     {                                                                                                                          \
         switch (att_padded(a.D)) {                                                                                             \
-        case 32: return att_backward_at<T, 32>(a, st);                                                                         \
-        case 64: return att_backward_at<T, 64>(a, st);                                                                         \
-        case 128: return att_backward_at<T, 128>(a, st);                                                                       \
-        default: return att_backward_at<T, 256>(a, st);                                                                        \
+        case 32: return att_backward_at<T, 32>(a, p, st);                                                                      \
+        case 64: return att_backward_at<T, 64>(a, p, st);                                                                      \
+        case 128: return att_backward_at<T, 128>(a, p, st);                                                                    \
+        default: return att_backward_at<T, 256>(a, p, st);                                                                     \
         }                                                                                                                      \
     }
 

@@ -52,6 +52,15 @@ bool check(const tl_attention *a)
            check_rows(a->v, a->dtype, a->n_kv, a->n_kv_heads, a->head_dim, false);
 }
 
+// Parts that a loop of `stages` (on average) is cut into where its `blocks` workgroups do not fill the chip twice, as long as a part keeps two.
+int splits(long long blocks, long long stages)
+{
+    const long long wanted = 2ll * compute_units();
+    if (blocks >= wanted || stages < 4) return 1;
+    const long long s = wanted / blocks < stages / 2 ? wanted / blocks : stages / 2;
+    return (int)(s < 1 ? 1 : s > 256 ? 256 : s);
+}
+
 // Which form a forward takes, by the packed rows of a tree on average.  Measured (us, 4 waves along the rows / 2 / 1): 256 trees of 9 to 99 nodes,
 // 33 rows each, bf16 x 64: - / 24 / 38; fp32 x 64: - / 57 / 70; 64 trees of 2047 nodes half of them masked, 72 rows, fp32 x 64: 158 / 98 /
 // 117; 8 trees of 3500 nodes, 3000 rows, bf16 x 128: 250 / 310 / -.  A single token's few rows want every wave on nodes of its own.
@@ -65,23 +74,51 @@ AttPlan plan(const tl_attention *a)
     p.bm = 32 * p.wm;
     p.bn = p.wm == 1 ? 128 : p.wm == 2 ? 64 : dp * size <= 256 ? 64 : 32;
     p.slots = (int)(rows / p.bm + a->n_trees);
-    p.splits = 1;
-    const long long blocks = (long long)p.slots * a->n_kv_heads, wanted = 2ll * compute_units();
-    const long long stages = a->n_kv / ((long long)p.bn * a->n_trees);
-    if (blocks < wanted && stages >= 4) {
-        const long long s = wanted / blocks < stages / 2 ? wanted / blocks : stages / 2;
-        p.splits = (int)(s < 1 ? 1 : s > 256 ? 256 : s);
-    }
+    p.splits = splits((long long)p.slots * a->n_kv_heads, a->n_kv / ((long long)p.bn * a->n_trees));
+    return p;
+}
+
+// The same for a backward pass, whose gradient of the queries sums over nodes and whose gradients of keys and values over rows.  Short trees (their rows,
+// or their nodes, on average): fewer of them at a time, and the other side divided among the waves instead.  Measured (us, 2 / 4 waves side by
+// side): 256 trees of 33 rows, 54 nodes, fp32 x 64: dQ 73 / 93, dK and dV 97 / 96; 25 such trees, x 30: 12 / 14 and 10 / 12; 8 trees
+// of 1536 rows, 1200 nodes, bf16 x 128: 177 / 127 and 206 / 180.
+AttBackPlan back_plan(const tl_attention *a)
+{
+    AttBackPlan p;
+    const long long rows = (long long)a->n_q * (a->n_heads / a->n_kv_heads), trees = a->n_trees;
+    p.q_waves = rows <= 128 * trees ? 2 : 4;
+    p.kv_waves = a->n_kv <= 128 * trees ? 2 : 4;
+    p.q_splits = a->n_q == 0 ? 1 : splits((rows / (32 * p.q_waves) + trees) * a->n_kv_heads, a->n_kv / (64 * trees));
+    p.kv_splits = a->n_kv == 0 ? 1 : splits((a->n_kv / (32 * p.kv_waves) + trees) * a->n_kv_heads, rows / (64 * trees));
     return p;
 }
 
 long long round16(long long x) { return (x + 15) & ~15ll; }
 
-long long workspace(const tl_attention *a, const AttPlan &p, int backward)
+long long workspace(const tl_attention *a, const AttPlan &p)
 {
     const long long rh = (long long)a->n_q * a->n_heads;
-    if (backward) return (a->dtype == TL_DT_F16 ? 3 : 2) * round16(rh * 4) + (a->kv_mask ? round16(4ll * a->n_kv) + round16(4ll * a->n_trees) : 0);
     return p.splits > 1 ? round16(p.splits * rh * 4) + round16(p.splits * rh * a->head_dim * 4) : 0;
+}
+
+// The backward pass's workspace, in this order; null where a part is not needed.  Returns its size.
+long long lay_out(const tl_attention *a, const AttBackPlan &p, char *base, AttArgs *x)
+{
+    long long at = 0;
+    auto take = [&](long long bytes) {
+        char *q = base + at;
+        at += round16(bytes);
+        return bytes ? (void *)q : nullptr;
+    };
+    const long long rh = (long long)a->n_q * a->n_heads, D = a->head_dim;
+    x->delta = static_cast<float *>(take(rh * 4));
+    x->ref = static_cast<float *>(take(rh * 4));
+    x->size = static_cast<float *>(take(a->dtype == TL_DT_F16 ? rh * 4 : 0));
+    x->list = static_cast<int32_t *>(take(a->kv_mask ? 4ll * a->n_kv : 0));
+    x->live = static_cast<int32_t *>(take(a->kv_mask ? 4ll * a->n_trees : 0));
+    x->part_q = static_cast<float *>(take(p.q_splits > 1 ? p.q_splits * rh * D * 4 : 0));
+    x->part_kv = static_cast<float *>(take(p.kv_splits > 1 ? 2ll * p.kv_splits * a->n_kv * a->n_kv_heads * D * 4 : 0));
+    return at;
 }
 
 AttArgs arguments(const tl_attention *a)
@@ -127,7 +164,8 @@ extern "C" {
 int tl_attend_workspace(const tl_attention *a, int backward, int64_t *bytes)
 {
     if (!bytes || !check(a)) return TL_EINVAL;
-    *bytes = a->n_trees == 0 ? 0 : workspace(a, plan(a), backward);
+    AttArgs unused;
+    *bytes = a->n_trees == 0 ? 0 : backward ? lay_out(a, back_plan(a), nullptr, &unused) : workspace(a, plan(a));
     return TL_OK;
 }
 
@@ -137,7 +175,7 @@ int tl_attend(const tl_attention *a, const tl_rows *o, float *lse, void *workspa
     if (a->n_trees == 0 || a->n_q == 0) return TL_OK;
     const AttPlan p = plan(a);
     if ((long long)p.slots * p.splits * a->n_kv_heads > INT32_MAX) return TL_EINVAL;
-    const long long need = workspace(a, p, 0);
+    const long long need = workspace(a, p);
     if (need > 0 && (!workspace_p || ((uintptr_t)workspace_p & 15))) return TL_EINVAL;
     if (need > workspace_bytes) return TL_ELIMIT;
     AttArgs x = arguments(a);
@@ -165,36 +203,26 @@ int tl_attend_backward(const tl_attention *a, const tl_rows *o, const float *lse
         !check_rows(*d_v, dt, a->n_kv, a->n_kv_heads, D, true))
         return TL_EINVAL;
     if (a->n_trees == 0) return TL_OK;
-    const long long need = workspace(a, AttPlan{}, 1);
+    const AttBackPlan p = back_plan(a);
+    AttArgs x = arguments(a);
+    const long long need = lay_out(a, p, static_cast<char *>(workspace_p), &x);
     if ((a->n_q > 0 && !lse) || (need > 0 && (!workspace_p || ((uintptr_t)workspace_p & 15)))) return TL_EINVAL;
     if (need > workspace_bytes) return TL_ELIMIT;
     const long long rows = (long long)a->n_q * (a->n_heads / a->n_kv_heads);
-    if ((rows / 32 + a->n_trees) * a->n_kv_heads > INT32_MAX || ((long long)a->n_kv / 32 + a->n_trees) * a->n_kv_heads > INT32_MAX ||
-        (long long)a->n_q * a->n_heads / 16 + a->n_trees >= INT32_MAX)
+    if ((rows / 32 + a->n_trees) * a->n_kv_heads * p.q_splits > INT32_MAX || ((long long)a->n_kv / 32 + a->n_trees) * a->n_kv_heads * p.kv_splits > INT32_MAX ||
+        (long long)a->n_q * a->n_heads / 4 + a->n_trees + (long long)a->n_kv * a->n_kv_heads / 2 >= INT32_MAX)
         return TL_EINVAL;
-    AttArgs x = arguments(a);
     x.o = AttTensor{o->p, o->row, o->head};
     x.d_o = AttTensor{d_o->p, d_o->row, d_o->head};
     x.d_q = AttTensor{d_q->p, d_q->row, d_q->head};
     x.d_k = AttTensor{d_k->p, d_k->row, d_k->head};
     x.d_v = AttTensor{d_v->p, d_v->row, d_v->head};
     x.lse = const_cast<float *>(lse);
-    const long long rh = (long long)a->n_q * a->n_heads;
-    char *w = static_cast<char *>(workspace_p);
-    x.delta = reinterpret_cast<float *>(w);
-    x.ref = reinterpret_cast<float *>(w + round16(rh * 4));
-    w += 2 * round16(rh * 4);
-    if (dt == TL_DT_F16) {
-        x.size = reinterpret_cast<float *>(w);
-        w += round16(rh * 4);
-    }
-    x.list = reinterpret_cast<int32_t *>(w);
-    x.live = reinterpret_cast<int32_t *>(w + round16(4ll * a->n_kv));
     x.vec = x.vec && in_pieces(*o, dt, D, 16) && in_pieces(*d_o, dt, D, 16);
     x.near = x.near && d_o->row < (1 << 20) && d_o->head < (1 << 20);
     x.vec_out = pieces_of_4(*d_q, dt, D) && pieces_of_4(*d_k, dt, D) && pieces_of_4(*d_v, dt, D);
     const hipStream_t st = (hipStream_t)hip_stream;
-    const hipError_t e = dt == TL_DT_F32 ? attend_backward<float>(x, st) : dt == TL_DT_BF16 ? attend_backward<bf16_t>(x, st) : attend_backward<f16_t>(x, st);
+    const hipError_t e = dt == TL_DT_F32 ? attend_backward<float>(x, p, st) : dt == TL_DT_BF16 ? attend_backward<bf16_t>(x, p, st) : attend_backward<f16_t>(x, p, st);
     return e == hipSuccess ? TL_OK : TL_EHIP;
 }
 

@@ -404,3 +404,16 @@ def test_fp16_gradients_of_any_size(size):
         x = got[n].double()
         bad = fits & (x != ref[n]) & ~((x - ref[n]).abs() <= err[n])
         assert not bad.any(), n
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("lq,lk", [([2], [5001]), ([1100], [3]), ([3, 0, 900, 1], [4000, 50, 2, 0]), ([600, 2], [700, 2500])])
+def test_gradients_of_few_trees(lq, lk, dtype):
+    """Sums over many nodes, or over many rows, of few trees: divided among workgroups, joined by a second launch; masked nodes among them."""
+    for heads, kv_heads, d, mask in ((2, 2, 64, 0.0), (4, 1, 128, 0.25), (3, 1, 33, 0.25), (1, 1, 256, 0.0)):
+        s = tensors(23, TYPES[dtype], lq, lk, heads, kv_heads, d, mask)
+        ref, err = plain(s)
+        got = call(s)
+        close(got, ref, err)
+        for n, x in call(s).items():
+            assert torch.equal(x, got[n]), n
