@@ -285,7 +285,10 @@ template <int NT> __device__ inline void fit_fp16(floatx16 &w, float &size, floa
 // (Pointers out of the argument struct are cast to global memory: through generic ones loads and LDS reads would wait for each other.)
 #define ATT_GLOBAL __attribute__((address_space(1)))
 
-// Granule g of a row of D elements (zeros beyond D).
+typedef u32x4 u32x4_any __attribute__((aligned(2)));          // at any address of an element
+
+// Granule g of a row of D elements (zeros beyond D).  Rows that do not divide into granules are read in 16 bytes at any address, the last of them
+// ending with the row and shifted into place.
 template <typename T> __device__ inline u32x4 load_granule(const T *row, int g, int D, bool vec)
 {
     constexpr int E = 16 / (int)sizeof(T);
@@ -294,6 +297,16 @@ template <typename T> __device__ inline u32x4 load_granule(const T *row, int g, 
     const int d = g * E;
     if (vec) {
         if (d < D) x = *(const ATT_GLOBAL u32x4 *)(p + d);
+    } else if (D >= E) {
+        const int at = min(d, D - E);
+        x = *(const ATT_GLOBAL u32x4_any *)(p + at);
+        const int bits = 8 * (int)sizeof(T) * (d - at);
+        if (bits > 0) {
+            uint64_t lo = (uint64_t)x[1] << 32 | x[0], hi = (uint64_t)x[3] << 32 | x[2];
+            lo = bits < 64 ? lo >> bits | hi << (64 - bits) : bits < 128 ? hi >> (bits - 64) : 0;
+            hi = bits < 64 ? hi >> bits : 0;
+            x = u32x4{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
+        }
     } else {
         T e[E];
 #pragma unroll
@@ -388,29 +401,42 @@ template <typename T, int DP, int N, int THREADS> struct NearRows {
     }
 };
 
-// Puts N rows into a tile; row(r) gives where row r lies, or nothing for a row of zeros.  VEC: asynchronously (stage_wait and a barrier before
-// it is read); else the rows are read element by element and are there after a barrier.
-template <typename T, int DP, int N, int THREADS, bool VEC, typename F> __device__ inline void stage_rows(unsigned char *tile, int D, F row)
-{
+// Puts N rows into a tile; row(r) gives where row r lies, or nothing for a row of zeros.  VEC: straight into LDS (stage_wait and a barrier before
+// it is read).  Else, rows that do not divide into granules: through registers, requested by request() and put into place by put().
+template <typename T, int DP, int N, int THREADS, bool VEC> struct StageRows {
     typedef Rows<T, DP> R;
-    constexpr int GRANULES = N * R::GPR, EACH = (GRANULES + THREADS - 1) / THREADS;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t base = lds_address(tile) + wave * 1024;
+    static constexpr int GRANULES = N * R::GPR, EACH = (GRANULES + THREADS - 1) / THREADS;
+    u32x4 held[VEC ? 1 : EACH];
+
+    template <typename F> __device__ void request(unsigned char *tile, int D, F row)
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const uint32_t base = lds_address(tile) + wave * 1024;
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        if (GRANULES % THREADS != 0 && i * THREADS + wave * 64 >= GRANULES) continue;
-        const int slot = i * THREADS + threadIdx.x;
-        int r, g;
-        place_of<T, DP>(slot, &r, &g);
-        const T *p = row(r);
-        if constexpr (VEC) {
-            const void *from = p && g * R::EPG < D ? (const void *)(p + g * R::EPG) : (const void *)att_zeros;
-            stage_16(base + i * THREADS * 16, from);
-        } else {
-            *reinterpret_cast<u32x4 *>(tile + slot * 16) = p ? load_granule<T>(p, g, D, false) : u32x4{0u, 0u, 0u, 0u};
+        for (int i = 0; i < EACH; ++i) {
+            if (GRANULES % THREADS != 0 && i * THREADS + wave * 64 >= GRANULES) continue;
+            int r, g;
+            place_of<T, DP>(i * THREADS + threadIdx.x, &r, &g);
+            const T *p = row(r);
+            if constexpr (VEC) {
+                const void *from = p && g * R::EPG < D ? (const void *)(p + g * R::EPG) : (const void *)att_zeros;
+                stage_16(base + i * THREADS * 16, from);
+            } else {
+                held[i] = p ? load_granule<T>(p, g, D, false) : u32x4{0u, 0u, 0u, 0u};
+            }
         }
     }
-}
+    __device__ void put(unsigned char *tile) const
+    {
+        if constexpr (!VEC) {
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                if (GRANULES % THREADS != 0 && i * THREADS + (threadIdx.x & ~63) >= GRANULES) continue;
+                *reinterpret_cast<u32x4 *>(tile + (i * THREADS + threadIdx.x) * 16) = held[i];
+            }
+        }
+    }
+};
 
 // The nodes of a tree, or of a part of it, that may be read, up to BN at a time.  With a mask their numbers go through a ring in LDS, filled
 // from 4 THREADS mask bytes at a time, so that masked nodes cost neither a place in a tile nor a read.
@@ -501,7 +527,7 @@ template <typename T, int DP, int WM_> struct AttFwd {
 };
 
 template <typename T, int DP, int WM, bool VEC>
-__global__ __launch_bounds__(ATT_THREADS, (AttFwd<T, DP, WM>::MIN_WAVES)) void k_attend(const AttArgs a)
+__global__ __launch_bounds__(ATT_THREADS, (VEC || DP < 128 ? AttFwd<T, DP, WM>::MIN_WAVES : 1)) void k_attend(const AttArgs a)
 {
     typedef AttFwd<T, DP, WM> C;
     typedef Rows<T, DP> R;
@@ -548,14 +574,19 @@ __global__ __launch_bounds__(ATT_THREADS, (AttFwd<T, DP, WM>::MIN_WAVES)) void k
     nodes.begin(a, lo, hi, att_lds + C::LIST);
     const bool near = VEC && !a.mask && a.near && a.D == DP;
     const NearRows<T, DP, C::BN, THREADS> k_near(a.k.row), v_near(a.v.row);
-    auto stage = [&](unsigned char *b) {
+    StageRows<T, DP, C::BN, THREADS, VEC> ks, vs;
+    auto request = [&](unsigned char *b) {
         if (near && nodes.n == C::BN) {
             k_near.stage(b, kp + nodes.first * a.k.row);
             v_near.stage(b + C::STAGE / 2, vp + nodes.first * a.v.row);
             return;
         }
-        stage_rows<T, DP, C::BN, THREADS, VEC>(b, a.D, [&](int r) { return r < nodes.n ? kp + nodes.node(r) * a.k.row : (const T *)nullptr; });
-        stage_rows<T, DP, C::BN, THREADS, VEC>(b + C::STAGE / 2, a.D, [&](int r) { return r < nodes.n ? vp + nodes.node(r) * a.v.row : (const T *)nullptr; });
+        ks.request(b, a.D, [&](int r) { return r < nodes.n ? kp + nodes.node(r) * a.k.row : (const T *)nullptr; });
+        vs.request(b + C::STAGE / 2, a.D, [&](int r) { return r < nodes.n ? vp + nodes.node(r) * a.v.row : (const T *)nullptr; });
+    };
+    auto put = [&](unsigned char *b) {
+        ks.put(b);
+        vs.put(b + C::STAGE / 2);
     };
     RowReads<T, DP> kr(att_lds + 32 * NT * wk * R::BYTES);
     ColumnReads<T, DP> vc(att_lds + C::STAGE / 2 + 32 * NT * wk * R::BYTES, 0);
@@ -607,21 +638,26 @@ __global__ __launch_bounds__(ATT_THREADS, (AttFwd<T, DP, WM>::MIN_WAVES)) void k
             if (!TAIL || 32 * t < left) mma_columns<T, DP, C::TERMS, DT>(acc, vc, 32 * t, p[t]);
     };
     int n = nodes.next(), odd = 0;
-    if (n) stage(att_lds);
+    if (n) {
+        request(att_lds);
+        put(att_lds);
+    }
     arrived(qf);
     while (n == C::BN) {                                        // (all stages but the last are full)
+        unsigned char *next = att_lds + (C::BUFS == 2 && !odd ? C::STAGE : 0);
         if (VEC) stage_wait();
         __syncthreads();
         n = nodes.next();
-        if (C::BUFS == 2 && n) stage(att_lds + (odd ? 0 : C::STAGE));
+        if ((!VEC || C::BUFS == 2) && n) request(next);
         compute(std::false_type{}, C::BN);
         if (C::BUFS == 1) {
             __syncthreads();
-            if (n) stage(att_lds);
+            if (VEC && n) request(next);
         } else {
             kr.move(odd ? -C::STAGE : C::STAGE);
             vc.move(odd ? -C::STAGE : C::STAGE);
         }
+        if (n) put(next);
         odd ^= 1;
     }
     if (n) {
@@ -821,7 +857,7 @@ template <typename T, int DP, int WM_> struct AttDq {
     static constexpr int MIN_WAVES = DP * (int)sizeof(T) > 256 ? 1 : 2;
 };
 
-template <typename T, int DP, int WM, bool VEC> __global__ __launch_bounds__(ATT_THREADS, (AttDq<T, DP, WM>::MIN_WAVES)) void k_attend_dq(const AttArgs a)
+template <typename T, int DP, int WM, bool VEC> __global__ __launch_bounds__(ATT_THREADS, (VEC || DP < 128 ? AttDq<T, DP, WM>::MIN_WAVES : 1)) void k_attend_dq(const AttArgs a)
 {
     typedef AttDq<T, DP, WM> C;
     typedef Rows<T, DP> R;
@@ -871,16 +907,21 @@ template <typename T, int DP, int WM, bool VEC> __global__ __launch_bounds__(ATT
     const ATT_GLOBAL int32_t *list = (const ATT_GLOBAL int32_t *)a.list + lo;
     const bool near = VEC && !a.mask && a.near && a.D == DP;
     const NearRows<T, DP, BN, ATT_THREADS> k_near(a.k.row), v_near(a.v.row);
-    auto stage = [&](unsigned char *b, int n) {
+    StageRows<T, DP, BN, ATT_THREADS, VEC> ks, vs;
+    auto request = [&](unsigned char *b, int n) {
         if (near && n == BN) {
             k_near.stage(b, kp + (lo + first) * a.k.row);
             v_near.stage(b + C::STAGE / 2, vp + (lo + first) * a.v.row);
         } else {
             auto node = [&](int r) { return (long long)(a.mask ? list[first + r] : lo + first + r); };
-            stage_rows<T, DP, BN, ATT_THREADS, VEC>(b, a.D, [&](int r) { return r < n ? kp + node(r) * a.k.row : (const T *)nullptr; });
-            stage_rows<T, DP, BN, ATT_THREADS, VEC>(b + C::STAGE / 2, a.D, [&](int r) { return r < n ? vp + node(r) * a.v.row : (const T *)nullptr; });
+            ks.request(b, a.D, [&](int r) { return r < n ? kp + node(r) * a.k.row : (const T *)nullptr; });
+            vs.request(b + C::STAGE / 2, a.D, [&](int r) { return r < n ? vp + node(r) * a.v.row : (const T *)nullptr; });
         }
         first += BN;
+    };
+    auto put = [&](unsigned char *b) {
+        ks.put(b);
+        vs.put(b + C::STAGE / 2);
     };
     const int own = 32 * C::NT * wk * R::BYTES;
     RowReads<T, DP> kr(att_lds + own), vr(att_lds + C::STAGE / 2 + own);
@@ -907,15 +948,20 @@ template <typename T, int DP, int WM, bool VEC> __global__ __launch_bounds__(ATT
         }
     };
     int left = n_nodes - first, odd = 0;
-    if (left > 0) stage(att_lds, min(left, BN));
+    if (left > 0) {
+        request(att_lds, min(left, BN));
+        put(att_lds);
+    }
     arrived(qf);
     arrived(gf);
     arrived(row);
     for (; left > BN; left -= BN) {
         if (VEC) stage_wait();
         __syncthreads();
-        stage(att_lds + (odd ? 0 : C::STAGE), min(left - BN, BN));
+        unsigned char *next = att_lds + (odd ? 0 : C::STAGE);
+        request(next, min(left - BN, BN));
         compute(std::false_type{}, BN);
+        put(next);
         const int step = odd ? -C::STAGE : C::STAGE;
         kr.move(step);
         vr.move(step);
@@ -1050,7 +1096,8 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
         n_stage = min(s_lo + per, n_stage);
     }
     long long first = (long long)s_lo * BQ;     // packed row that is staged next
-    auto stage = [&](unsigned char *b) {
+    StageRows<T, DP, BQ, ATT_THREADS, VEC> qs, gs;
+    auto request = [&](unsigned char *b) {
         if (near && first + BQ <= n_rows) {
             const int q0 = q_lo + (int)(first / a.G);
             const T *qp = row_of<T>(a.q, q0, hk * a.G), *gp = row_of<T>(a.d_o, q0, hk * a.G);
@@ -1066,8 +1113,8 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
                 const long long m = first + r;
                 return m < n_rows ? (const T *)row_of<T>(x, q_lo + m / a.G, hk * a.G + (int)(m % a.G)) : (const T *)nullptr;
             };
-            stage_rows<T, DP, BQ, ATT_THREADS, VEC>(b, a.D, [&](int r) { return row(a.q, r); });
-            stage_rows<T, DP, BQ, ATT_THREADS, VEC>(b + BQ * R::BYTES, a.D, [&](int r) { return row(a.d_o, r); });
+            qs.request(b, a.D, [&](int r) { return row(a.q, r); });
+            gs.request(b + BQ * R::BYTES, a.D, [&](int r) { return row(a.d_o, r); });
         }
         if (wave < 2) {                         // (64 places; those beyond BQ are not read)
             const long long m = first + lane;
@@ -1077,12 +1124,19 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
         }
         first += BQ;
     };
+    auto put = [&](unsigned char *b) {
+        qs.put(b);
+        gs.put(b + BQ * R::BYTES);
+    };
     const int own = 32 * C::QT * wq;            // the wave's first row of a stage
     const unsigned char *q_own = att_lds + own * R::BYTES, *g_own = q_own + BQ * R::BYTES;
     RowReads<T, DP> qr(q_own), gr(g_own);
     ColumnReads<T, DP> qc(q_own, 32 * DT * wd), gc(g_own, 32 * DT * wd);
     const unsigned char *numbers = att_lds + 2 * BQ * R::BYTES + 16 * half + 4 * own;
-    if (s_lo < n_stage) stage(att_lds);
+    if (s_lo < n_stage) {
+        request(att_lds);
+        put(att_lds);
+    }
     // score gradients as fp16 operands: begin at the size of the tree's largest row of d_o
     constexpr bool F16 = std::is_same<T, f16_t>::value;
     float size = 1.f;
@@ -1098,7 +1152,8 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
     for (int s = s_lo, odd = 0; s < n_stage; ++s, odd ^= 1) {
         stage_wait();
         __syncthreads();
-        if (s + 1 < n_stage) stage(att_lds + (odd ? 0 : C::STAGE));
+        unsigned char *next = att_lds + (odd ? 0 : C::STAGE);
+        if (s + 1 < n_stage) request(next);
 #pragma unroll
         for (int q = 0; q < C::QT; ++q) {
             if ((long long)s * BQ + own + 32 * q >= n_rows) break;
@@ -1123,6 +1178,7 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
             if constexpr (F16) fit_fp16(dp, size, dk);
             mma_columns<T, DP, 2, DT>(dk, qc, 32 * q, dp);
         }
+        if (s + 1 < n_stage) put(next);
         const int step = odd ? -C::STAGE : C::STAGE;
         qr.move(step);
         gr.move(step);
