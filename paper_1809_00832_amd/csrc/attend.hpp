@@ -287,35 +287,43 @@ template <int NT> __device__ inline void fit_fp16(floatx16 &w, float &size, floa
 
 typedef u32x4 u32x4_any __attribute__((aligned(2)));          // at any address of an element
 
-// Granule g of a row of D elements (zeros beyond D).  Rows that do not divide into granules are read in 16 bytes at any address, the last of them
-// ending with the row and shifted into place.
-template <typename T> __device__ inline u32x4 load_granule(const T *row, int g, int D, bool vec)
+// Granule g of a row of D elements that does not divide into granules: 16 bytes at any address, those of the last granule ending with the row;
+// shifted into place, with zeros beyond D, by granule_in_place, which waits for the load.
+template <typename T> __device__ inline u32x4 granule_anywhere(const T *row, int g, int D)
 {
     constexpr int E = 16 / (int)sizeof(T);
     const ATT_GLOBAL T *p = (const ATT_GLOBAL T *)row;
-    u32x4 x = {0u, 0u, 0u, 0u};
-    const int d = g * E;
-    if (vec) {
-        if (d < D) x = *(const ATT_GLOBAL u32x4 *)(p + d);
-    } else if (D >= E) {
-        const int at = min(d, D - E);
-        x = *(const ATT_GLOBAL u32x4_any *)(p + at);
-        const int bits = 8 * (int)sizeof(T) * (d - at);
-        if (bits > 0) {
-            uint64_t lo = (uint64_t)x[1] << 32 | x[0], hi = (uint64_t)x[3] << 32 | x[2];
-            lo = bits < 64 ? lo >> bits | hi << (64 - bits) : bits < 128 ? hi >> (bits - 64) : 0;
-            hi = bits < 64 ? hi >> bits : 0;
-            x = u32x4{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
-        }
-    } else {
-        T e[E];
+    if (D >= E) return *(const ATT_GLOBAL u32x4_any *)(p + min(g * E, D - E));
+    T e[E];
+    u32x4 x;
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-            const T y = p[min(d + j, D - 1)];
-            e[j] = d + j < D ? y : (T)0.f;
-        }
-        __builtin_memcpy(&x, e, 16);
+    for (int j = 0; j < E; ++j) e[j] = p[min(j, D - 1)];
+    __builtin_memcpy(&x, e, 16);
+    return x;
+}
+template <typename T> __device__ inline u32x4 granule_in_place(u32x4 x, int g, int D)
+{
+    constexpr int E = 16 / (int)sizeof(T), BITS = 8 * (int)sizeof(T);
+    uint64_t lo = (uint64_t)x[1] << 32 | x[0], hi = (uint64_t)x[3] << 32 | x[2];
+    if (D >= E) {
+        const int bits = BITS * max(g * E - (D - E), 0);
+        lo = bits < 64 ? lo >> bits | (bits ? hi << (64 - bits) : 0) : bits < 128 ? hi >> (bits - 64) : 0;
+        hi = bits < 64 ? hi >> bits : 0;
+    } else {
+        const int bits = g ? 0 : BITS * D;                      // that belong to the row
+        lo = bits < 64 ? lo & ~(~0ull << bits) : lo;
+        hi = bits > 64 ? hi & ~(~0ull << (bits - 64)) : 0;
     }
+    return u32x4{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
+}
+
+// Granule g of a row of D elements (zeros beyond D); vec: rows divide into granules and lie on 16-byte boundaries.
+template <typename T> __device__ inline u32x4 load_granule(const T *row, int g, int D, bool vec)
+{
+    constexpr int E = 16 / (int)sizeof(T);
+    if (!vec) return granule_in_place<T>(granule_anywhere<T>(row, g, D), g, D);
+    u32x4 x = {0u, 0u, 0u, 0u};
+    if (g * E < D) x = *(const ATT_GLOBAL u32x4 *)((const ATT_GLOBAL T *)row + g * E);
     return x;
 }
 
@@ -422,17 +430,19 @@ template <typename T, int DP, int N, int THREADS, bool VEC> struct StageRows {
                 const void *from = p && g * R::EPG < D ? (const void *)(p + g * R::EPG) : (const void *)att_zeros;
                 stage_16(base + i * THREADS * 16, from);
             } else {
-                held[i] = p ? load_granule<T>(p, g, D, false) : u32x4{0u, 0u, 0u, 0u};
+                held[i] = p ? granule_anywhere<T>(p, g, D) : u32x4{0u, 0u, 0u, 0u};
             }
         }
     }
-    __device__ void put(unsigned char *tile) const
+    __device__ void put(unsigned char *tile, int D) const
     {
         if constexpr (!VEC) {
 #pragma unroll
             for (int i = 0; i < EACH; ++i) {
                 if (GRANULES % THREADS != 0 && i * THREADS + (threadIdx.x & ~63) >= GRANULES) continue;
-                *reinterpret_cast<u32x4 *>(tile + (i * THREADS + threadIdx.x) * 16) = held[i];
+                int r, g;
+                place_of<T, DP>(i * THREADS + threadIdx.x, &r, &g);
+                *reinterpret_cast<u32x4 *>(tile + (i * THREADS + threadIdx.x) * 16) = granule_in_place<T>(held[i], g, D);
             }
         }
     }
@@ -585,8 +595,8 @@ __global__ __launch_bounds__(ATT_THREADS, (VEC || DP < 128 ? AttFwd<T, DP, WM>::
         vs.request(b + C::STAGE / 2, a.D, [&](int r) { return r < nodes.n ? vp + nodes.node(r) * a.v.row : (const T *)nullptr; });
     };
     auto put = [&](unsigned char *b) {
-        ks.put(b);
-        vs.put(b + C::STAGE / 2);
+        ks.put(b, a.D);
+        vs.put(b + C::STAGE / 2, a.D);
     };
     RowReads<T, DP> kr(att_lds + 32 * NT * wk * R::BYTES);
     ColumnReads<T, DP> vc(att_lds + C::STAGE / 2 + 32 * NT * wk * R::BYTES, 0);
@@ -920,8 +930,8 @@ template <typename T, int DP, int WM, bool VEC> __global__ __launch_bounds__(ATT
         first += BN;
     };
     auto put = [&](unsigned char *b) {
-        ks.put(b);
-        vs.put(b + C::STAGE / 2);
+        ks.put(b, a.D);
+        vs.put(b + C::STAGE / 2, a.D);
     };
     const int own = 32 * C::NT * wk * R::BYTES;
     RowReads<T, DP> kr(att_lds + own), vr(att_lds + C::STAGE / 2 + own);
@@ -1125,8 +1135,8 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
         first += BQ;
     };
     auto put = [&](unsigned char *b) {
-        qs.put(b);
-        gs.put(b + BQ * R::BYTES);
+        qs.put(b, a.D);
+        gs.put(b + BQ * R::BYTES, a.D);
     };
     const int own = 32 * C::QT * wq;            // the wave's first row of a stage
     const unsigned char *q_own = att_lds + own * R::BYTES, *g_own = q_own + BQ * R::BYTES;
