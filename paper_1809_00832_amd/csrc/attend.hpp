@@ -59,6 +59,8 @@ struct AttArgs {
     int n_trees, n_q, n_kv, Hq, Hk, G, D;
     int slots;              // row tiles (see find_slot)
     int splits;             // parts that a tree's nodes are cut into
+    int bufs;               // stages that LDS holds: 2, the next one arriving while one is worked on, or 1
+    int kv_slots, kv_splits, kv_bufs, kv_blocks;    // backward: the same of the gradients of keys and values, and their workgroups
     int near;               // 128 rows of any input span less than 2^31 bytes
     int vec;                // rows of q, k, v (and of what a backward pass reads) may be read in 16-byte pieces
     int vec_out;            // ... and the outputs written so
@@ -113,11 +115,33 @@ __device__ inline void tree_range(const int32_t *__restrict__ off, int t, int n,
 
 // Workgroups that read the same nodes follow one another in `logical`; the chip deals workgroups to its eight L2 domains in turn,
 // so consecutive logical numbers are given to one domain.
-__device__ inline long long xcd_order(long long id, long long n)
+__device__ inline uint32_t xcd_order(uint32_t id, uint32_t n)
 {
-    const long long per = n >> 3, rest = n & 7, x = id & 7, y = id >> 3;
+    const uint32_t per = n >> 3, rest = n & 7, x = id & 7, y = id >> 3;
     return x * per + min(x, rest) + y;
 }
+
+// (Division in 64 bits takes some hundred instructions.)
+__device__ inline long long divide(long long a, int b) { return a >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b); }
+
+// Query and head of the group of packed rows m0 + r for r below 256, all of it in 32 bits.  (x + 1/2) / G lies 1 / (2 G) or more from a
+// whole number, and x < 4096 + 256: far more than rounding moves it.
+struct Packed {
+    int G, q0, first;
+    float per;
+    __device__ Packed(int q_lo, long long m0, int group) : G(group), per(__builtin_amdgcn_rcpf((float)group))
+    {
+        const long long k = divide(m0, G);
+        q0 = q_lo + (int)k;
+        first = (int)(m0 - k * G);
+    }
+    __device__ void at(int r, int *query, int *head) const
+    {
+        const int k = (int)(((float)(first + r) + 0.5f) * per);
+        *query = q0 + k;
+        *head = first + r - k * G;
+    }
+};
 
 // ---- LDS tiles --------------------------------------------------------------------------
 
@@ -529,10 +553,11 @@ template <typename T, int DP, int WM_> struct AttFwd {
     static constexpr int BM = 32 * WM;
     static constexpr int BN = 32 * WK * NT;
     static constexpr int STAGE = 2 * BN * Rows<T, DP>::BYTES;
-    static constexpr int BUFS = STAGE <= 32768 ? 2 : 1;
-    static constexpr int JOIN = WK > 1 ? ATT_WAVES * 32 * (DP + 4) * 4 + ATT_WAVES * 64 * 4 : 0;
-    static constexpr int LIST = STAGE * BUFS > JOIN ? STAGE * BUFS : JOIN;    // place of the nodes' ring
-    static constexpr int LDS = LIST + Nodes<BN, THREADS>::LDS;
+    static constexpr int MAX_BUFS = STAGE <= 32768 ? 2 : 1;
+    static constexpr int JOIN_WAVES = WK == 4 ? 4 : WK - 1;
+    static constexpr int JOIN = JOIN_WAVES * WM * 32 * (DP + 6) * 4;
+    __host__ __device__ static constexpr int list(int bufs) { return STAGE * bufs > JOIN ? STAGE * bufs : JOIN; }    // place of the nodes' ring
+    __host__ __device__ static constexpr int lds(int bufs, bool mask) { return list(bufs) + (mask ? Nodes<BN, THREADS>::LDS : 0); }
     static constexpr int MIN_WAVES = DP * (int)sizeof(T) > 256 ? 1 : 2;
 };
 
@@ -547,8 +572,8 @@ __global__ __launch_bounds__(ATT_THREADS, (VEC || DP < 128 ? AttFwd<T, DP, WM>::
 
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave % WM, wk = wave / WM;
-    const long long id = xcd_order(blockIdx.x, gridDim.x);
-    const int slot = (int)(id % a.slots), part = (int)(id / a.slots % a.splits), hk = (int)(id / a.slots / a.splits);
+    const uint32_t id = xcd_order(blockIdx.x, gridDim.x), lists = id / (uint32_t)a.slots;
+    const int slot = (int)(id - lists * a.slots), hk = (int)(lists / (uint32_t)a.splits), part = (int)(lists - hk * (uint32_t)a.splits);
     long long tile;
     const int tree = find_slot(a.q_off, a.n_trees, a.G, C::BM == 32 ? 5 : C::BM == 64 ? 6 : 7, slot, &tile);
     int q_lo, q_hi, lo, hi;
@@ -567,7 +592,10 @@ __global__ __launch_bounds__(ATT_THREADS, (VEC || DP < 128 ? AttFwd<T, DP, WM>::
     // the lane's query (a row beyond the last one repeats the first: its results are not stored)
     const long long m = m0 + 32 * wm + col;
     const bool mine = m < n_rows;
-    const int qi = q_lo + (int)((mine ? m : m0) / a.G), head = hk * a.G + (int)((mine ? m : m0) % a.G);
+    const Packed rows(q_lo, m0, a.G);
+    int qi, head;
+    rows.at(mine ? 32 * wm + col : 0, &qi, &head);
+    head += hk * a.G;
     frag qf[R::STEPS];
     {
         const T *qr = row_of<T>(a.q, qi, head);
@@ -581,7 +609,8 @@ __global__ __launch_bounds__(ATT_THREADS, (VEC || DP < 128 ? AttFwd<T, DP, WM>::
 
     const T *kp = row_of<T>(a.k, 0, hk), *vp = row_of<T>(a.v, 0, hk);
     Nodes<C::BN, THREADS> nodes;
-    nodes.begin(a, lo, hi, att_lds + C::LIST);
+    const bool two = C::MAX_BUFS == 2 && a.bufs == 2;
+    nodes.begin(a, lo, hi, att_lds + C::list(two ? 2 : 1));
     const bool near = VEC && !a.mask && a.near && a.D == DP;
     const NearRows<T, DP, C::BN, THREADS> k_near(a.k.row), v_near(a.v.row);
     StageRows<T, DP, C::BN, THREADS, VEC> ks, vs;
@@ -654,13 +683,13 @@ __global__ __launch_bounds__(ATT_THREADS, (VEC || DP < 128 ? AttFwd<T, DP, WM>::
     }
     arrived(qf);
     while (n == C::BN) {                                        // (all stages but the last are full)
-        unsigned char *next = att_lds + (C::BUFS == 2 && !odd ? C::STAGE : 0);
+        unsigned char *next = att_lds + (two && !odd ? C::STAGE : 0);
         if (VEC) stage_wait();
         __syncthreads();
         n = nodes.next();
-        if ((!VEC || C::BUFS == 2) && n) request(next);
+        if ((!VEC || two) && n) request(next);
         compute(std::false_type{}, C::BN);
-        if (C::BUFS == 1) {
+        if (!two) {
             __syncthreads();
             if (VEC && n) request(next);
         } else {
@@ -691,7 +720,38 @@ __global__ __launch_bounds__(ATT_THREADS, (VEC || DP < 128 ? AttFwd<T, DP, WM>::
         if (partial) a.part_lse[(long long)part * a.n_q * a.Hq + rh] = lse;
         else if (a.lse) a.lse[rh] = lse;
     };
-    if constexpr (WK == 1) {
+    if constexpr (WK <= 2) {
+        if constexpr (WK == 2) {
+            // the second wave's sums over its nodes, brought to one maximum with the first one's
+            float *jo = reinterpret_cast<float *>(att_lds) + (32 * wm + col) * (DP + 4), *jt = reinterpret_cast<float *>(att_lds) + WM * 32 * (DP + 4) + (32 * wm + col) * 2;
+            __syncthreads();
+            if (wk == 1) {
+                if (half == 0) {
+                    jt[0] = top;
+                    jt[1] = sum;
+                }
+#pragma unroll
+                for (int t = 0; t < DT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; r += 4)
+                        *reinterpret_cast<f32x4 *>(jo + 32 * t + 2 * r + 4 * half) = f32x4{acc[t][r], acc[t][r + 1], acc[t][r + 2], acc[t][r + 3]};
+            }
+            __syncthreads();
+            if (wk == 1) return;
+            const float other = jt[0], highest = fmaxf(top, other);
+            const float f = top == highest ? 1.f : __builtin_amdgcn_exp2f((top - highest) * a.scale_log2);
+            const float g = other == highest ? 1.f : __builtin_amdgcn_exp2f((other - highest) * a.scale_log2);
+            top = highest;
+            sum = f * sum + g * jt[1];
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const f32x4 y = *reinterpret_cast<const f32x4 *>(jo + 32 * t + 2 * r + 4 * half);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[t][r + j] = f * acc[t][r + j] + g * y[j];
+                }
+        }
         if (!mine) return;
         const bool any = sum > 0.f || sum != sum;
         const float inv = any ? 1.f / sum : 0.f;
@@ -735,46 +795,68 @@ __global__ __launch_bounds__(ATT_THREADS, (VEC || DP < 128 ? AttFwd<T, DP, WM>::
                 for (int j = 0; j < 4; ++j) x[j] += f * y[j];
             }
             const bool any = total > 0.f || total != total;
-            const int i = q_lo + (int)((m0 + r) / a.G), hd = hk * a.G + (int)((m0 + r) % a.G);
+            int i, hd;
+            rows.at(r, &i, &hd);
+            hd += hk * a.G;
             if (d == 0) store_lse(i, hd, any, tt, total);
             store(i, hd, d, any ? 1.f / total : 0.f, x);
         }
     }
 }
 
-// Joins the parts of a split forward: one wave per query and head.  BN: nodes per stage of the kernel that made them.
+// Joins the parts of a split forward: one workgroup per query and head, waves along the parts, lanes along the columns, so that a chain of loads is
+// a quarter of the parts long and its loads do not wait for each other.  BN: nodes per stage of the kernel that made them.
 template <typename T> __global__ __launch_bounds__(ATT_THREADS) void k_attend_join(const AttArgs a, int bn)
 {
-    const int lane = threadIdx.x & 63;
-    const long long rh = (long long)blockIdx.x * ATT_WAVES + (threadIdx.x >> 6), n = (long long)a.n_q * a.Hq;
-    if (rh >= n) return;
-    const int qi = (int)(rh / a.Hq), head = (int)(rh % a.Hq);
+    __shared__ float sums[ATT_WAVES][256], weights[256];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long long rh = blockIdx.x, n = (long long)a.n_q * a.Hq;
+    const int qi = (int)divide(rh, a.Hq), head = (int)(rh - (long long)qi * a.Hq);
     int lo, hi;
     const int tree = find_last(a.n_trees, qi, [&](int t) { return (long long)a.q_off[t]; });
     tree_range(a.kv_off, tree, a.n_kv, &lo, &hi);
     const int n_stage = (hi - lo + bn - 1) / bn, per = (n_stage + a.splits - 1) / a.splits;
     const int parts = per ? (n_stage + per - 1) / per : 0;
-    float top = -INFINITY;
-    for (int j = lane; j < parts; j += 64) top = fmaxf(top, a.part_lse[j * n + rh]);
+    // the parts' logarithms (at most 256 parts): every wave works out the largest and the total
+    float l[4], top = -INFINITY, total = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        l[i] = lane + 64 * i < parts ? a.part_lse[(lane + 64 * i) * n + rh] : -INFINITY;
+        top = fmaxf(top, l[i]);
+    }
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    float total = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int j = 0; j < parts; ++j) {
-        const float l = a.part_lse[j * n + rh];
-        const float f = l == -INFINITY ? 0.f : __expf(l - top);
-        total += f;
-        const float *po = a.part_o + (j * n + rh) * a.D;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        l[i] = l[i] == -INFINITY ? 0.f : __expf(l[i] - top);
+        total += l[i];
+        if (wave == 0) weights[lane + 64 * i] = l[i];
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o);
+    __syncthreads();
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int j = wave; j < parts; j += ATT_WAVES) {
+        const ATT_GLOBAL float *po = (const ATT_GLOBAL float *)a.part_o + (j * n + rh) * a.D;
+        const float f = weights[j];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
-            if (lane + 64 * t < a.D) x[t] += f * po[lane + 64 * t];
+            if (lane + 64 * t < a.D) x[t] = fmaf(f, po[lane + 64 * t], x[t]);
     }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) sums[wave][lane + 64 * t] = x[t];
+    __syncthreads();
     const bool any = total > 0.f || total != total;
     const float inv = any ? 1.f / total : 0.f;
-    T *o = row_of<T>(a.o, qi, head);
+    const int d = threadIdx.x;
+    if (d < a.D) {
+        float y = 0.f;
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-        if (lane + 64 * t < a.D) o[lane + 64 * t] = (T)(x[t] * inv);
-    if (a.lse && lane == 0) a.lse[rh] = any ? top + __logf(total) : -INFINITY;
+        for (int w = 0; w < ATT_WAVES; ++w) y += sums[w][d];
+        row_of<T>(a.o, qi, head)[d] = (T)(y * inv);
+    }
+    if (a.lse && d == 0) a.lse[rh] = any ? top + __logf(total) : -INFINITY;
 }
 
 // ---- backward -----------------------------------------------------------------------------
@@ -792,7 +874,7 @@ template <typename T> __global__ __launch_bounds__(ATT_THREADS) void k_attend_pr
         const long long rh = ((long long)blockIdx.x * ATT_THREADS + threadIdx.x) >> 4, n = (long long)a.n_q * a.Hq;
         float x = 0.f, sq = 0.f;
         if (rh < n) {
-            const int qi = (int)(rh / a.Hq), head = (int)(rh % a.Hq);
+            const int qi = (int)divide(rh, a.Hq), head = (int)(rh - (long long)qi * a.Hq);
             const T *o = row_of<T>(a.o, qi, head), *g = row_of<T>(a.d_o, qi, head);
             constexpr int E = 16 / (int)sizeof(T);
             for (int c = l16; c * E < a.D; c += 16) {
@@ -862,12 +944,12 @@ template <typename T, int DP, int WM_> struct AttDq {
     static constexpr int BN = 32 * WK * NT;
     static constexpr int DT = DP / 32 / WD;
     static constexpr int STAGE = 2 * BN * Rows<T, DP>::BYTES;
+    static constexpr int TERMS = WM == 4 && !std::is_same<T, f16_t>::value ? 1 : 2;     // of a score gradient (see AttFwd)
     static constexpr int JOIN = WK > 1 ? WM * 32 * (DP + 4) * 4 : 0;
-    static constexpr int LDS = 2 * STAGE > JOIN ? 2 * STAGE : JOIN;
-    static constexpr int MIN_WAVES = DP * (int)sizeof(T) > 256 ? 1 : 2;
+    static constexpr int lds(int bufs) { return bufs * STAGE > JOIN ? bufs * STAGE : JOIN; }
 };
 
-template <typename T, int DP, int WM, bool VEC> __global__ __launch_bounds__(ATT_THREADS, (VEC || DP < 128 ? AttDq<T, DP, WM>::MIN_WAVES : 1)) void k_attend_dq(const AttArgs a)
+template <typename T, int DP, int WM, bool VEC> __device__ __forceinline__ void attend_dq(const AttArgs &a, uint32_t block, uint32_t blocks)
 {
     typedef AttDq<T, DP, WM> C;
     typedef Rows<T, DP> R;
@@ -877,8 +959,9 @@ template <typename T, int DP, int WM, bool VEC> __global__ __launch_bounds__(ATT
 
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wd = wave % C::WD, wm = wave / C::WD % C::WM, wk = wave / C::WD / C::WM;
-    const long long id = xcd_order(blockIdx.x, gridDim.x);
-    const int slot = (int)(id % a.slots), part = (int)(id / a.slots % a.splits), hk = (int)(id / a.slots / a.splits);
+    const bool two = a.bufs == 2;
+    const uint32_t id = xcd_order(block, blocks), lists = id / (uint32_t)a.slots;
+    const int slot = (int)(id - lists * a.slots), hk = (int)(lists / (uint32_t)a.splits), part = (int)(lists - hk * (uint32_t)a.splits);
     long long tile;
     const int tree = find_slot(a.q_off, a.n_trees, a.G, C::BM == 64 ? 6 : 7, slot, &tile);
     int q_lo, q_hi, lo, hi;
@@ -896,7 +979,9 @@ template <typename T, int DP, int WM, bool VEC> __global__ __launch_bounds__(ATT
 
     const long long m = m0 + 32 * wm + col;
     const bool mine = m < n_rows;
-    const int qi = q_lo + (int)((mine ? m : m0) / a.G), head = hk * a.G + (int)((mine ? m : m0) % a.G);
+    int qi, head;
+    Packed(q_lo, m0, a.G).at(mine ? 32 * wm + col : 0, &qi, &head);
+    head += hk * a.G;
     const long long row_head = (long long)qi * a.Hq + head;
     frag qf[R::STEPS], gf[R::STEPS];
     {
@@ -934,7 +1019,7 @@ template <typename T, int DP, int WM, bool VEC> __global__ __launch_bounds__(ATT
         vs.put(b + C::STAGE / 2, a.D);
     };
     const int own = 32 * C::NT * wk * R::BYTES;
-    RowReads<T, DP> kr(att_lds + own), vr(att_lds + C::STAGE / 2 + own);
+    RowReads<T, DP> kr(att_lds + own);          // (rows of v lie BN rows behind)
     ColumnReads<T, DP> kc(att_lds + own, 32 * DT * wd);
     // one stage of n nodes.  TAIL: some may be missing (rows of zeros, but exp2 of a large -lse would still be infinite).
     auto compute = [&](auto tail, int n) {
@@ -946,7 +1031,7 @@ template <typename T, int DP, int WM, bool VEC> __global__ __launch_bounds__(ATT
 #pragma unroll
             for (int d = 0; d < R::STEPS; ++d) {
                 mma(p, kr.get(32 * j, d), qf[d]);
-                mma(dp, vr.get(32 * j, d), gf[d]);
+                mma(dp, kr.get(32 * j + BN, d), gf[d]);
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -954,7 +1039,7 @@ template <typename T, int DP, int WM, bool VEC> __global__ __launch_bounds__(ATT
                 p[r] = decltype(tail)::value && 32 * j + 8 * (r >> 2) + 4 * half + (r & 3) >= n ? 0.f : e;
             }
             if constexpr (F16) fit_fp16(p, row[2], acc);
-            mma_columns<T, DP, 2, DT>(acc, kc, 32 * j, p);
+            mma_columns<T, DP, C::TERMS, DT>(acc, kc, 32 * j, p);
         }
     };
     int left = n_nodes - first, odd = 0;
@@ -968,13 +1053,16 @@ template <typename T, int DP, int WM, bool VEC> __global__ __launch_bounds__(ATT
     for (; left > BN; left -= BN) {
         if (VEC) stage_wait();
         __syncthreads();
-        unsigned char *next = att_lds + (odd ? 0 : C::STAGE);
-        request(next, min(left - BN, BN));
+        unsigned char *next = att_lds + (!two || odd ? 0 : C::STAGE);
+        if (!VEC || two) request(next, min(left - BN, BN));
         compute(std::false_type{}, BN);
+        if (!two) {
+            __syncthreads();
+            if (VEC) request(next, min(left - BN, BN));
+        }
         put(next);
-        const int step = odd ? -C::STAGE : C::STAGE;
+        const int step = !two ? 0 : odd ? -C::STAGE : C::STAGE;
         kr.move(step);
-        vr.move(step);
         kc.move(step);
         odd ^= 1;
     }
@@ -1026,18 +1114,19 @@ template <typename T, int DP, int WN_> struct AttDkv {
     static constexpr int WN = DP <= 128 ? WN_ : ATT_WAVES / WD;
     static constexpr int WQ = ATT_WAVES / WN / WD;                          // waves along the rows; their sums are joined at the end
     static constexpr int BN = 32 * WN;
-    static constexpr int QT = WQ == 1 && DP * (int)sizeof(T) <= 256 ? 2 : 1;
+    static constexpr int QT = WQ == 1 && DP * (int)sizeof(T) <= 128 ? 2 : 1;
     static constexpr int BQ = 32 * WQ * QT;
     static constexpr int DT = DP / 32 / WD;
     static constexpr int STAGE = 2 * BQ * Rows<T, DP>::BYTES + 512;         // rows of q, of d_o, 64 logarithms, 64 deltas
     static constexpr int JOIN = WQ > 1 ? WN * 32 * 2 * (DP + 4) * 4 : 0;
-    static constexpr int LDS = 2 * STAGE > JOIN ? 2 * STAGE : JOIN;
-    static constexpr int MIN_WAVES = DP * (int)sizeof(T) > 256 || DP == 128 ? 1 : 2;
+    static constexpr int TERMS = DP <= 128 && WN == 4 && !std::is_same<T, f16_t>::value ? 1 : 2;
+    static constexpr int lds(int bufs) { return bufs * STAGE > JOIN ? bufs * STAGE : JOIN; }
+    static constexpr int MIN_WAVES = DP * (int)sizeof(T) > 256 ? 1 : 2;
 };
 
 static __device__ const float att_no_row[2] = {INFINITY, 0.f};              // logarithm and delta of a row that is not there
 
-template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT_THREADS, (AttDkv<T, DP, WN>::MIN_WAVES)) void k_attend_dkv(const AttArgs a)
+template <typename T, int DP, int WN, bool VEC> __device__ __forceinline__ void attend_dkv(const AttArgs &a, uint32_t block, uint32_t blocks)
 {
     typedef AttDkv<T, DP, WN> C;
     typedef Rows<T, DP> R;
@@ -1047,8 +1136,10 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
 
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wd = wave % C::WD, wn = wave / C::WD % C::WN, wq = wave / C::WD / C::WN;
-    const long long id = xcd_order(blockIdx.x, gridDim.x);
-    const int slot = (int)(id % a.slots), part = (int)(id / a.slots % a.splits), hk = (int)(id / a.slots / a.splits);
+    const bool two = a.kv_bufs == 2;
+    const uint32_t id = xcd_order(block, blocks), lists = id / (uint32_t)a.kv_slots;
+    const int slot = (int)(id - lists * a.kv_slots), hk = (int)(lists / (uint32_t)a.kv_splits), part = (int)(lists - hk * (uint32_t)a.kv_splits);
+    if (hk >= a.Hk) return;                     // (the launch rounds up)
     long long tile;
     const int tree = find_slot(a.kv_off, a.n_trees, 1, BN == 32 ? 5 : BN == 64 ? 6 : 7, slot, &tile);
     int q_lo, q_hi, lo, hi;
@@ -1095,22 +1186,23 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
     for (int i = 0; i < EACH; ++i) {
         int r, g;
         place_of<T, DP>(i * ATT_THREADS + threadIdx.x, &r, &g);
-        const int qr = r / a.G, hr = r % a.G;
+        const int qr = (uint32_t)r / (uint32_t)a.G, hr = r - qr * a.G;
         q_offset[i] = ((uint32_t)qr * (uint32_t)a.q.row + (uint32_t)hr * (uint32_t)a.q.head) * (uint32_t)sizeof(T) + g * 16;
         g_offset[i] = ((uint32_t)qr * (uint32_t)a.d_o.row + (uint32_t)hr * (uint32_t)a.d_o.head) * (uint32_t)sizeof(T) + g * 16;
     }
     int n_stage = (int)((n_rows + BQ - 1) / BQ), s_lo = 0;
-    if (a.splits > 1) {
-        const int per = (n_stage + a.splits - 1) / a.splits;
+    if (a.kv_splits > 1) {
+        const int per = (n_stage + a.kv_splits - 1) / a.kv_splits;
         s_lo = min(part * per, n_stage);
         n_stage = min(s_lo + per, n_stage);
     }
     long long first = (long long)s_lo * BQ;     // packed row that is staged next
     StageRows<T, DP, BQ, ATT_THREADS, VEC> qs, gs;
     auto request = [&](unsigned char *b) {
-        if (near && first + BQ <= n_rows) {
-            const int q0 = q_lo + (int)(first / a.G);
-            const T *qp = row_of<T>(a.q, q0, hk * a.G), *gp = row_of<T>(a.d_o, q0, hk * a.G);
+        const Packed rows(q_lo, first, a.G);
+        const int left = (int)min(n_rows - first, (long long)BQ);
+        if (near && left == BQ) {
+            const T *qp = row_of<T>(a.q, rows.q0, hk * a.G), *gp = row_of<T>(a.d_o, rows.q0, hk * a.G);
             const uint32_t base = lds_address(b) + wave * 1024;
 #pragma unroll
             for (int i = 0; i < EACH; ++i)
@@ -1120,16 +1212,18 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
                 }
         } else {
             auto row = [&](const AttTensor &x, int r) {
-                const long long m = first + r;
-                return m < n_rows ? (const T *)row_of<T>(x, q_lo + m / a.G, hk * a.G + (int)(m % a.G)) : (const T *)nullptr;
+                int i, hd;
+                rows.at(r, &i, &hd);
+                return r < left ? (const T *)row_of<T>(x, i, hk * a.G + hd) : (const T *)nullptr;
             };
             qs.request(b, a.D, [&](int r) { return row(a.q, r); });
             gs.request(b + BQ * R::BYTES, a.D, [&](int r) { return row(a.d_o, r); });
         }
         if (wave < 2) {                         // (64 places; those beyond BQ are not read)
-            const long long m = first + lane;
+            int i, hd;
+            rows.at(lane, &i, &hd);
             const float *from = wave == 0 ? a.ref : a.delta;
-            from = m < n_rows ? from + (q_lo + m / a.G) * a.Hq + hk * a.G + m % a.G : att_no_row + wave;
+            from = lane < left ? from + (long long)i * a.Hq + hk * a.G + hd : att_no_row + wave;
             stage_4(lds_address(b) + 2 * BQ * R::BYTES + wave * 256, from);
         }
         first += BQ;
@@ -1139,9 +1233,8 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
         gs.put(b + BQ * R::BYTES, a.D);
     };
     const int own = 32 * C::QT * wq;            // the wave's first row of a stage
-    const unsigned char *q_own = att_lds + own * R::BYTES, *g_own = q_own + BQ * R::BYTES;
-    RowReads<T, DP> qr(q_own), gr(g_own);
-    ColumnReads<T, DP> qc(q_own, 32 * DT * wd), gc(g_own, 32 * DT * wd);
+    RowReads<T, DP> qr(att_lds + own * R::BYTES);               // (those of d_o lie BQ rows behind)
+    ColumnReads<T, DP> qc(att_lds + own * R::BYTES, 32 * DT * wd);
     const unsigned char *numbers = att_lds + 2 * BQ * R::BYTES + 16 * half + 4 * own;
     if (s_lo < n_stage) {
         request(att_lds);
@@ -1152,7 +1245,10 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
     float size = 1.f;
     if constexpr (F16) {
         float s = INFINITY;
-        for (long long m = lane; m < n_rows; m += 64) s = fminf(s, a.size[(q_lo + m / a.G) * a.Hq + hk * a.G + m % a.G]);
+        for (long long m = lane; m < n_rows; m += 64) {
+            const long long i = divide(m, a.G);
+            s = fminf(s, a.size[(q_lo + i) * a.Hq + hk * a.G + (m - i * a.G)]);
+        }
 #pragma unroll
         for (int o = 32; o >= 1; o >>= 1) s = fminf(s, __shfl_xor(s, o));
         size = s < INFINITY ? s : 1.f;
@@ -1162,8 +1258,8 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
     for (int s = s_lo, odd = 0; s < n_stage; ++s, odd ^= 1) {
         stage_wait();
         __syncthreads();
-        unsigned char *next = att_lds + (odd ? 0 : C::STAGE);
-        if (s + 1 < n_stage) request(next);
+        unsigned char *next = att_lds + (!two || odd ? 0 : C::STAGE);
+        if (two && s + 1 < n_stage) request(next);
 #pragma unroll
         for (int q = 0; q < C::QT; ++q) {
             if ((long long)s * BQ + own + 32 * q >= n_rows) break;
@@ -1171,7 +1267,7 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
 #pragma unroll
             for (int d = 0; d < R::STEPS; ++d) {
                 mma(p, qr.get(32 * q, d), kf[d]);
-                mma(dp, gr.get(32 * q, d), vf[d]);
+                mma(dp, qr.get(32 * q + BQ, d), vf[d]);
             }
 #pragma unroll
             for (int r4 = 0; r4 < 4; ++r4) {
@@ -1184,16 +1280,18 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
                     dp[r] = p[r] * (dp[r] - dd[j]);
                 }
             }
-            mma_columns<T, DP, 2, DT>(dv, gc, 32 * q, p);
+            mma_columns<T, DP, C::TERMS, DT>(dv, qc, 32 * q + BQ, p);
             if constexpr (F16) fit_fp16(dp, size, dk);
-            mma_columns<T, DP, 2, DT>(dk, qc, 32 * q, dp);
+            mma_columns<T, DP, C::TERMS, DT>(dk, qc, 32 * q, dp);
+        }
+        if (!two && s + 1 < n_stage) {
+            __syncthreads();
+            request(next);
         }
         if (s + 1 < n_stage) put(next);
-        const int step = odd ? -C::STAGE : C::STAGE;
+        const int step = !two ? 0 : odd ? -C::STAGE : C::STAGE;
         qr.move(step);
-        gr.move(step);
         qc.move(step);
-        gc.move(step);
         numbers += step;
     }
     const float k_scale = a.scale / size;
@@ -1233,7 +1331,7 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
         for (int r = 0; r < 16; r += 4) {
             const int d = 32 * (DT * wd + t) + 2 * r + 4 * half;
             const f32x4 x = {dk[t][r], dk[t][r + 1], dk[t][r + 2], dk[t][r + 3]}, y = {dv[t][r], dv[t][r + 1], dv[t][r + 2], dv[t][r + 3]};
-            if (a.splits > 1) {
+            if (a.kv_splits > 1) {
                 store4<float>(pk, d, a.D, (a.D & 3) == 0, x[0], x[1], x[2], x[3]);
                 store4<float>(pv, d, a.D, (a.D & 3) == 0, y[0], y[1], y[2], y[3]);
             } else {
@@ -1241,6 +1339,14 @@ template <typename T, int DP, int WN, bool VEC> __global__ __launch_bounds__(ATT
                 store4<T>(ov, d, a.D, a.vec_out, y[0], y[1], y[2], y[3]);
             }
         }
+}
+
+// Both in one launch: neither needs the other's results, and the workgroups of one fill the compute units that those of the other leave idle at its end.  Keys
+// and values first, whose workgroups take longer.
+template <typename T, int DP, int WM, int WN, bool VEC> __global__ __launch_bounds__(ATT_THREADS, (AttDkv<T, DP, WN>::MIN_WAVES)) void k_attend_back(const AttArgs a)
+{
+    if ((int)blockIdx.x < a.kv_blocks) attend_dkv<T, DP, WN, VEC>(a, blockIdx.x, a.kv_blocks);
+    else attend_dq<T, DP, WM, VEC>(a, blockIdx.x - a.kv_blocks, gridDim.x - a.kv_blocks);
 }
 
 // Adds up the parts of split gradients, part by part: workgroups below `q_blocks` those of dQ (q_splits parts), the others those of dK and dV.  A wave takes
@@ -1255,11 +1361,12 @@ template <typename T> __global__ __launch_bounds__(ATT_THREADS) void k_attend_su
     T *to;
     bool dead = false;
     if (of_q) {
-        to = row_of<T>(a.d_q, i / a.Hq, (int)(i % a.Hq));
+        const long long row = divide(i, a.Hq);
+        to = row_of<T>(a.d_q, row, (int)(i - row * a.Hq));
     } else {
-        const long long node = i / 2 / a.Hk;
+        const long long node = divide(i / 2, a.Hk);
         dead = a.mask && !a.mask[node];         // (its parts were not written)
-        to = row_of<T>(i & 1 ? a.d_v : a.d_k, node, (int)(i / 2 % a.Hk));
+        to = row_of<T>(i & 1 ? a.d_v : a.d_k, node, (int)(i / 2 - node * a.Hk));
     }
     const int parts = of_q ? q_splits : kv_splits;
     for (int d = lane; d < a.D; d += 64) {

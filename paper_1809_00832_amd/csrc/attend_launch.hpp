@@ -13,12 +13,14 @@ struct AttPlan {
     int wm;                 // waves along the rows (AttFwd)
     int bm, bn;             // packed rows and nodes of a workgroup's tile
     int slots, splits;
+    int bufs;               // stages in LDS
 };
 
 // ... and a backward call: waves side by side along the rows (AttDq) and the nodes (AttDkv), parts that a tree's nodes and its rows are cut into.
 struct AttBackPlan {
     int q_waves, kv_waves;
     int q_splits, kv_splits;
+    int q_bufs, kv_bufs;
 };
 
 template <typename T> hipError_t attend_forward(const AttArgs &a, const AttPlan &p, hipStream_t st);
@@ -38,9 +40,9 @@ template <auto KERNEL> hipError_t att_allow(size_t lds)
     return e;
 }
 
-template <auto KERNEL> hipError_t att_launch(long long blocks, size_t lds, const AttArgs &a, hipStream_t st)
+template <auto KERNEL> hipError_t att_launch(long long blocks, size_t lds, size_t most_lds, const AttArgs &a, hipStream_t st)
 {
-    const hipError_t e = att_allow<KERNEL>(lds);
+    const hipError_t e = att_allow<KERNEL>(most_lds);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(KERNEL, dim3((unsigned)blocks), dim3(ATT_THREADS), lds, st, a);
     return hipGetLastError();
@@ -50,7 +52,8 @@ template <typename T, int DP, int WM> hipError_t att_forward_of(const AttArgs &a
 {
     typedef AttFwd<T, DP, WM> C;
     const long long blocks = (long long)a.slots * a.splits * a.Hk;
-    return a.vec ? att_launch<k_attend<T, DP, WM, true>>(blocks, C::LDS, a, st) : att_launch<k_attend<T, DP, WM, false>>(blocks, C::LDS, a, st);
+    const size_t lds = C::lds(a.bufs < C::MAX_BUFS ? a.bufs : C::MAX_BUFS, a.mask), most = C::lds(C::MAX_BUFS, true);
+    return a.vec ? att_launch<k_attend<T, DP, WM, true>>(blocks, lds, most, a, st) : att_launch<k_attend<T, DP, WM, false>>(blocks, lds, most, a, st);
 }
 
 template <typename T, int DP> hipError_t att_forward_at(const AttArgs &a, const AttPlan &p, hipStream_t st)
@@ -61,20 +64,21 @@ template <typename T, int DP> hipError_t att_forward_at(const AttArgs &a, const 
     return att_forward_of<T, DP, 4>(a, st);
 }
 
-template <typename T, int DP, int WM, bool VEC> hipError_t att_dq_of(AttArgs a, int splits, hipStream_t st)
+template <typename T, int DP, int WM, int WN, bool VEC> hipError_t att_both_of(AttArgs a, const AttBackPlan &p, hipStream_t st)
 {
-    typedef AttDq<T, DP, WM> C;
-    a.slots = (int)((long long)a.n_q * a.G / C::BM + a.n_trees);
-    a.splits = splits;
-    return att_launch<k_attend_dq<T, DP, C::WM, VEC>>((long long)a.slots * splits * a.Hk, C::LDS, a, st);
-}
-
-template <typename T, int DP, int WN, bool VEC> hipError_t att_dkv_of(AttArgs a, int splits, hipStream_t st)
-{
-    typedef AttDkv<T, DP, WN> C;
-    a.slots = a.n_kv / C::BN + a.n_trees;
-    a.splits = splits;
-    return att_launch<k_attend_dkv<T, DP, C::WN, VEC>>((long long)a.slots * splits * a.Hk, C::LDS, a, st);
+    typedef AttDq<T, DP, WM> Q;
+    typedef AttDkv<T, DP, WN> KV;
+    a.slots = (int)((long long)a.n_q * a.G / Q::BM + a.n_trees);
+    a.splits = p.q_splits;
+    a.bufs = p.q_bufs;
+    a.kv_slots = a.n_kv / KV::BN + a.n_trees;
+    a.kv_splits = p.kv_splits;
+    a.kv_bufs = p.kv_bufs;
+    // (a multiple of eight, so that consecutive workgroups of both kinds lie in one L2 domain)
+    a.kv_blocks = a.n_kv > 0 ? (int)(((long long)a.kv_slots * a.kv_splits * a.Hk + 7) & ~7ll) : 0;
+    const long long q_blocks = a.n_q > 0 ? (long long)a.slots * a.splits * a.Hk : 0;
+    const size_t lds_q = Q::lds(a.bufs), lds_kv = KV::lds(a.kv_bufs), most_q = Q::lds(2), most_kv = KV::lds(2);
+    return att_launch<k_attend_back<T, DP, Q::WM, KV::WN, VEC>>(a.kv_blocks + q_blocks, lds_q > lds_kv ? lds_q : lds_kv, most_q > most_kv ? most_q : most_kv, a, st);
 }
 
 template <typename T, int DP, bool VEC> hipError_t att_backward_of(const AttArgs &a, const AttBackPlan &p, hipStream_t st)
@@ -85,8 +89,9 @@ template <typename T, int DP, bool VEC> hipError_t att_backward_of(const AttArgs
         hipLaunchKernelGGL(k_attend_prepare<T>, dim3((unsigned)(row_blocks + (a.mask ? a.n_trees : 0))), dim3(ATT_THREADS), 0, st, a, (int)row_blocks);
         e = hipGetLastError();
     }
-    if (e == hipSuccess && a.n_q > 0) e = p.q_waves == 2 ? att_dq_of<T, DP, 2, VEC>(a, p.q_splits, st) : att_dq_of<T, DP, 4, VEC>(a, p.q_splits, st);
-    if (e == hipSuccess && a.n_kv > 0) e = p.kv_waves == 2 ? att_dkv_of<T, DP, 2, VEC>(a, p.kv_splits, st) : att_dkv_of<T, DP, 4, VEC>(a, p.kv_splits, st);
+    if (e == hipSuccess && (a.n_q > 0 || a.n_kv > 0))
+        e = p.q_waves == 2 ? (p.kv_waves == 2 ? att_both_of<T, DP, 2, 2, VEC>(a, p, st) : att_both_of<T, DP, 2, 4, VEC>(a, p, st))
+                           : (p.kv_waves == 2 ? att_both_of<T, DP, 4, 2, VEC>(a, p, st) : att_both_of<T, DP, 4, 4, VEC>(a, p, st));
     if (e == hipSuccess && (p.q_splits > 1 || p.kv_splits > 1)) {
         const long long q_blocks = p.q_splits > 1 ? ((long long)a.n_q * a.Hq + ATT_WAVES - 1) / ATT_WAVES : 0;
         const long long kv_blocks = p.kv_splits > 1 ? (2ll * a.n_kv * a.Hk + ATT_WAVES - 1) / ATT_WAVES : 0;
@@ -112,9 +117,7 @@ template <typename T, int DP> hipError_t att_backward_at(const AttArgs &a, const
         default: e = att_forward_at<T, 256>(a, p, st);                                                                         \
         }                                                                                                                      \
         if (e != hipSuccess || a.splits == 1) return e;                                                                        \
-        const long long rh = (long long)a.n_q * a.Hq;                                                                          \
-        hipLaunchKernelGGL(k_attend_join<T>, dim3((unsigned)((rh + ATT_WAVES - 1) / ATT_WAVES)), dim3(ATT_THREADS), 0, st, a,  \
-                           p.bn);                                                                                              \
+        hipLaunchKernelGGL(k_attend_join<T>, dim3((unsigned)((long long)a.n_q * a.Hq)), dim3(ATT_THREADS), 0, st, a, p.bn);    \
         return hipGetLastError();                                                                                              \
     }                                                                                                                          \
     template <> hipError_t attend_backward<T>(const AttArgs &a, const AttBackPlan &p, hipStream_t st)                          \

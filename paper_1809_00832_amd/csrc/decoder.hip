@@ -61,6 +61,9 @@ int splits(long long blocks, long long stages)
     return (int)(s < 1 ? 1 : s > 256 ? 256 : s);
 }
 
+// Lists that mostly end within a stage need no second one in LDS, and twice as many workgroups then fit a compute unit.
+bool one_stage(long long rows, long long trees, int stage) { return 2 * rows <= 3ll * stage * trees; }
+
 // Which form a forward takes, by the packed rows of a tree on average.  Measured (us, 4 waves along the rows / 2 / 1): 256 trees of 9 to 99 nodes,
 // 33 rows each, bf16 x 64: - / 24 / 38; fp32 x 64: - / 57 / 70; 64 trees of 2047 nodes half of them masked, 72 rows, fp32 x 64: 158 / 98 /
 // 117; 8 trees of 3500 nodes, 3000 rows, bf16 x 128: 250 / 310 / -.  A single token's few rows want every wave on nodes of its own.
@@ -75,6 +78,7 @@ AttPlan plan(const tl_attention *a)
     p.bn = p.wm == 1 ? 128 : p.wm == 2 ? 64 : dp * size <= 256 ? 64 : 32;
     p.slots = (int)(rows / p.bm + a->n_trees);
     p.splits = splits((long long)p.slots * a->n_kv_heads, a->n_kv / ((long long)p.bn * a->n_trees));
+    p.bufs = one_stage(a->n_kv, a->n_trees, p.bn) ? 1 : 2;
     return p;
 }
 
@@ -90,6 +94,8 @@ AttBackPlan back_plan(const tl_attention *a)
     p.kv_waves = a->n_kv <= 128 * trees ? 2 : 4;
     p.q_splits = a->n_q == 0 ? 1 : splits((rows / (32 * p.q_waves) + trees) * a->n_kv_heads, a->n_kv / (64 * trees));
     p.kv_splits = a->n_kv == 0 ? 1 : splits((a->n_kv / (32 * p.kv_waves) + trees) * a->n_kv_heads, rows / (64 * trees));
+    p.q_bufs = one_stage(a->n_kv, trees, 64) ? 1 : 2;
+    p.kv_bufs = one_stage(rows, trees, 64) ? 1 : 2;
     return p;
 }
 
@@ -184,6 +190,7 @@ int tl_attend(const tl_attention *a, const tl_rows *o, float *lse, void *workspa
     x.vec_out = pieces_of_4(*o, a->dtype, a->head_dim);
     x.slots = p.slots;
     x.splits = p.splits;
+    x.bufs = p.bufs;
     if (p.splits > 1) {
         x.part_lse = static_cast<float *>(workspace_p);
         x.part_o = reinterpret_cast<float *>(static_cast<char *>(workspace_p) + round16((long long)p.splits * a->n_q * a->n_heads * 4));
@@ -209,7 +216,7 @@ int tl_attend_backward(const tl_attention *a, const tl_rows *o, const float *lse
     if ((a->n_q > 0 && !lse) || (need > 0 && (!workspace_p || ((uintptr_t)workspace_p & 15)))) return TL_EINVAL;
     if (need > workspace_bytes) return TL_ELIMIT;
     const long long rows = (long long)a->n_q * (a->n_heads / a->n_kv_heads);
-    if ((rows / 32 + a->n_trees) * a->n_kv_heads * p.q_splits > INT32_MAX || ((long long)a->n_kv / 32 + a->n_trees) * a->n_kv_heads * p.kv_splits > INT32_MAX ||
+    if ((rows / 32 + a->n_trees) * a->n_kv_heads * p.q_splits + ((long long)a->n_kv / 32 + a->n_trees) * a->n_kv_heads * p.kv_splits > INT32_MAX - 8 ||
         (long long)a->n_q * a->n_heads / 4 + a->n_trees + (long long)a->n_kv * a->n_kv_heads / 2 >= INT32_MAX)
         return TL_EINVAL;
     x.o = AttTensor{o->p, o->row, o->head};
