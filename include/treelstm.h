@@ -149,7 +149,7 @@ enum tl_error {
     TL_ESTALL = -5,    /* TL_SCHED_READY made no progress within its spin budget (nodes that are
                           unreachable from any leaf, e.g. a cycle); outputs are incomplete.  The
                           level schedulers report such a batch as TL_ESTRUCT.                   */
-    TL_ELIMIT = -6     /* tl_forward_noalloc: the batch does not fit the fixed workspace         */
+    TL_ELIMIT = -6     /* tl_forward_noalloc: the batch does not fit the fixed workspace; tl_attend*: theirs is too small */
 };
 
 typedef struct {

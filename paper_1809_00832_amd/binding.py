@@ -392,10 +392,14 @@ def tl_attend(q, k, v, q_off, kv_off, kv_mask=None, scale=None, o=None, with_lse
     a = _attention(q, k, v, q_off, kv_off, kv_mask, scale)
     shape, device = q.shape, q.device
     if o is None:
-        o = q.new_empty(shape)
+        o = torch.empty_like(q) if q.is_contiguous() else q.new_empty(shape)
     lse = torch.empty(shape[:2], dtype=torch.float32, device=device) if with_lse else None
-    ws, n = _attend_workspace(a, 0, device)
-    _check(lib().tl_attend(a, _rows(o, q, shape), _ptr(lse), _ptr(ws), n, _raw_stream(device)), "tl_attend")
+    call, rows, at, st = lib().tl_attend, _rows(o, q, shape), _ptr(lse), _raw_stream(device)
+    code = call(a, rows, at, None, 0, st)
+    if code == TL_ELIMIT:                                       # (most calls need no workspace: asking first would cost them a call)
+        ws, n = _attend_workspace(a, 0, device)
+        code = call(a, rows, at, _ptr(ws), n, st)
+    _check(code, "tl_attend")
     return (o, lse) if with_lse else o
 
 

@@ -76,7 +76,8 @@ AttPlan plan(const tl_attention *a)
     p.wm = rows <= 16ll * a->n_trees && dp * size <= 512 ? 1 : rows <= 128ll * a->n_trees ? 2 : 4;
     p.bm = 32 * p.wm;
     p.bn = p.wm == 1 ? 128 : p.wm == 2 ? 64 : dp * size <= 256 ? 64 : 32;
-    p.slots = (int)(rows / p.bm + a->n_trees);
+    const long long slots = rows / p.bm + a->n_trees;
+    p.slots = (int)(slots < INT32_MAX ? slots : INT32_MAX);     // (tl_attend refuses such)
     p.splits = splits((long long)p.slots * a->n_kv_heads, a->n_kv / ((long long)p.bn * a->n_trees));
     p.bufs = one_stage(a->n_kv, a->n_trees, p.bn) ? 1 : 2;
     return p;
@@ -180,10 +181,10 @@ int tl_attend(const tl_attention *a, const tl_rows *o, float *lse, void *workspa
     if (!check(a) || !o || !check_rows(*o, a->dtype, a->n_q, a->n_heads, a->head_dim, true)) return TL_EINVAL;
     if (a->n_trees == 0 || a->n_q == 0) return TL_OK;
     const AttPlan p = plan(a);
-    if ((long long)p.slots * p.splits * a->n_kv_heads > INT32_MAX) return TL_EINVAL;
+    if ((long long)p.slots * p.splits * a->n_kv_heads >= INT32_MAX) return TL_EINVAL;
     const long long need = workspace(a, p);
-    if (need > 0 && (!workspace_p || ((uintptr_t)workspace_p & 15))) return TL_EINVAL;
     if (need > workspace_bytes) return TL_ELIMIT;
+    if (need > 0 && (!workspace_p || ((uintptr_t)workspace_p & 15))) return TL_EINVAL;
     AttArgs x = arguments(a);
     x.o = AttTensor{o->p, o->row, o->head};
     x.lse = lse;
