@@ -47,7 +47,7 @@ class Decoder:
         def matrix(rows, cols):
             return (torch.randn(rows, cols, generator=g) * rows ** -0.5).to(device).requires_grad_()
 
-        self.words = (torch.randn(vocab, hidden, generator=g) * 0.5).to(device).requires_grad_()
+        self.words = (torch.randn(vocab, hidden, generator=g) * hidden ** -0.5).to(device).requires_grad_()
         self.w_state, self.w_q, self.w_kv, self.w_o = matrix(hidden, hidden), matrix(hidden, hidden), matrix(hidden, kv), matrix(hidden, hidden)
 
     def parameters(self):

@@ -61,7 +61,8 @@ int splits(long long blocks, long long stages)
     return (int)(s < 1 ? 1 : s > 256 ? 256 : s);
 }
 
-// Lists that mostly end within a stage need no second one in LDS, and twice as many workgroups then fit a compute unit.
+// Lists that mostly end within a stage need no second one in LDS, and twice as many workgroups then fit a compute unit.  Measured (us, two stages / one):
+// 256 trees of 54 nodes, 33 rows each: bf16 x 64 read 23.9 / 20.0, fp32 x 64 58 / 50.
 bool one_stage(long long rows, long long trees, int stage) { return 2 * rows <= 3ll * stage * trees; }
 
 // Which form a forward takes, by the packed rows of a tree on average.  Measured (us, 4 waves along the rows / 2 / 1): 256 trees of 9 to 99 nodes,

@@ -162,6 +162,17 @@ __device__ inline uint64_t smp_wave_scan(uint64_t x)
     x += smp_from<0x143, 0xc>(x);
     return x;
 }
+// The same for counts.
+__device__ inline uint32_t smp_wave_count(uint32_t x)
+{
+    x += __builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);
+    return x;
+}
 __device__ inline uint64_t smp_lane(uint64_t x, int lane)
 {
     return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane);
@@ -388,7 +399,7 @@ template <typename T> __device__ __noinline__ int smp_collect(SmpRow<T> row, Smp
             hit |= (at >= first) & (at < behind) & (x[i] > -INFINITY) ? 1u << i : 0u;
         }
         if (__any(hit != 0)) {
-            const uint32_t upto = (uint32_t)smp_wave_scan((uint64_t)__popc(hit)), all = __builtin_amdgcn_readlane(upto, 63);
+            const uint32_t upto = smp_wave_count(__popc(hit)), all = __builtin_amdgcn_readlane(upto, 63);
             uint32_t at = 0;
             if ((threadIdx.x & 63) == 0) at = atomicAdd(&sh.listed, all);
             at = __builtin_amdgcn_readfirstlane(at) + upto - __popc(hit);
@@ -404,12 +415,23 @@ template <typename T> __device__ __noinline__ int smp_collect(SmpRow<T> row, Smp
     return (int)sh.listed;
 }
 
-// Sorts the list by value, then index: exchanges at a distance below 64 stay within a wave, without barriers.
+// Sorts the list by value, then index: a few words by how many are larger; else exchanges at a distance below 64 stay within a wave, without barriers.
 static __device__ __noinline__ void smp_sort(int n)
 {
     SmpShared &sh = smp_shared();
     n = smp_uniform(n);
     const int lane = threadIdx.x & 63;
+    if (n <= 64) {
+        if (threadIdx.x < 64) {
+            const uint64_t mine = lane < n ? sh.list[lane] : 0;
+            int larger = 0;
+            for (int i = 0; i < n; ++i) larger += smp_lane(mine, i) > mine ? 1 : 0;
+            __builtin_amdgcn_wave_barrier();
+            if (lane < n) sh.list[larger] = mine;
+        }
+        __syncthreads();
+        return;
+    }
     int size = 64;
     while (size < n) size *= 2;
     for (int i = n + threadIdx.x; i < size; i += SMP_THREADS) sh.list[i] = 0;
@@ -546,7 +568,7 @@ template <typename T> __device__ __noinline__ SmpDraw smp_locate(SmpRow<T> row, 
             for (int i = 0; i < W; ++i) mine |= x[i] >= least ? 1u << i : 0u;
         }
         if (!__any(mine != 0)) return;
-        const uint32_t count = __popc(mine), upto = (uint32_t)smp_wave_scan((uint64_t)count), all = __builtin_amdgcn_readlane(upto, 63);
+        const uint32_t count = __popc(mine), upto = smp_wave_count(count), all = __builtin_amdgcn_readlane(upto, 63);
         kept += all;
         uint64_t s = 0;
         if (f.equal) {
@@ -767,6 +789,9 @@ template <typename T, bool INDEX> __device__ __noinline__ void smp_extremes(SmpR
     __syncthreads();
 }
 
+// One workgroup a row, two rows a compute unit: registers are held to 64 for that.  Bound by the instructions of the weights (vector unit 81 % busy), not by
+// memory, which the second and later walks find in the L2.  us: a row of 20 000 words (fp32, top-p) 26, of which 9 for the draw's walk and 7 for
+// the histogram; 256 rows of 50 000 (fp32, all filters) 46; 512 rows of 131 072 (bf16, top-p) 141, 0.95 TB/s.
 template <typename T> __global__ __launch_bounds__(SMP_THREADS, 8) void k_sample(const SampleArgs a)
 {
     SmpShared &sh = smp_shared();
