@@ -940,8 +940,8 @@ template <typename T> __global__ __launch_bounds__(ATT_THREADS) void k_attend_pr
 
 // Both gradients take the scores and probabilities again from lse: five products a pair of tiles would do, seven are done, so that neither side needs
 // the other's sums or atomics.  Scores, probabilities and d_o . v stay in a lane's registers and are operands of the second products as they stand.
-// The launch of both (us): 8 documents of 1 700 nodes, 70 % of them read, 384 tokens x 16 heads, bf16 x 128: 227 (apart, and each product with two
-// terms: 314); 256 trees of 54 nodes, 33 words, fp32 x 64, 8 heads: 165 (matrix unit 31 % busy, 40 % of it on places that short trees leave
+// The launch of both (us): 8 documents of 1 700 nodes, 70 % of them read, 384 tokens x 16 heads, bf16 x 128: 243 (apart, and with two
+// terms of the probabilities too: 314); 256 trees of 54 nodes, 33 words, fp32 x 64, 8 heads: 165 (matrix unit 31 % busy, 40 % of it on places that short trees leave
 // empty; the rest is reads, stage by stage, at two waves per SIMD); 25 trees, x 30: 14.
 //
 // dQ: like the forward, rows (queries) on the lanes' columns.  Four waves: WM side by side along the rows, WK along the nodes (their sums are joined
@@ -955,7 +955,6 @@ template <typename T, int DP, int WM_> struct AttDq {
     static constexpr int BN = 32 * WK * NT;
     static constexpr int DT = DP / 32 / WD;
     static constexpr int STAGE = 2 * BN * Rows<T, DP>::BYTES;
-    static constexpr int TERMS = WM == 4 && !std::is_same<T, f16_t>::value ? 1 : 2;     // of a score gradient (see AttFwd)
     static constexpr int JOIN = WK > 1 ? WM * 32 * (DP + 4) * 4 : 0;
     static constexpr int lds(int bufs) { return bufs * STAGE > JOIN ? bufs * STAGE : JOIN; }
 };
@@ -1050,7 +1049,7 @@ template <typename T, int DP, int WM, bool VEC> __device__ __forceinline__ void 
                 p[r] = decltype(tail)::value && 32 * j + 8 * (r >> 2) + 4 * half + (r & 3) >= n ? 0.f : e;
             }
             if constexpr (F16) fit_fp16(p, row[2], acc);
-            mma_columns<T, DP, C::TERMS, DT>(acc, kc, 32 * j, p);
+            mma_columns<T, DP, 2, DT>(acc, kc, 32 * j, p);
         }
     };
     int left = n_nodes - first, odd = 0;
@@ -1130,6 +1129,8 @@ template <typename T, int DP, int WN_> struct AttDkv {
     static constexpr int DT = DP / 32 / WD;
     static constexpr int STAGE = 2 * BQ * Rows<T, DP>::BYTES + 512;         // rows of q, of d_o, 64 logarithms, 64 deltas
     static constexpr int JOIN = WQ > 1 ? WN * 32 * 2 * (DP + 4) * 4 : 0;
+    // Of a probability: the second one costs time only where there are many rows.  (Of a score gradient always two: it is a difference, and the error of d_k
+    // from rounding it once is up to 1.6 times that of d_k's own rounding.)
     static constexpr int TERMS = DP <= 128 && WN == 4 && !std::is_same<T, f16_t>::value ? 1 : 2;
     static constexpr int lds(int bufs) { return bufs * STAGE > JOIN ? bufs * STAGE : JOIN; }
     static constexpr int MIN_WAVES = DP * (int)sizeof(T) > 256 ? 1 : 2;
@@ -1293,7 +1294,7 @@ template <typename T, int DP, int WN, bool VEC> __device__ __forceinline__ void 
             }
             mma_columns<T, DP, C::TERMS, DT>(dv, qc, 32 * q + BQ, p);
             if constexpr (F16) fit_fp16(dp, size, dk);
-            mma_columns<T, DP, C::TERMS, DT>(dk, qc, 32 * q, dp);
+            mma_columns<T, DP, 2, DT>(dk, qc, 32 * q, dp);
         }
         if (!two && s + 1 < n_stage) {
             __syncthreads();
