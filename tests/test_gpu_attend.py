@@ -417,3 +417,19 @@ def test_gradients_of_few_trees(lq, lk, dtype):
         close(got, ref, err)
         for n, x in call(s).items():
             assert torch.equal(x, got[n]), n
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("heads,kv_heads,d,mask", [(2, 2, 64, 0.0), (6, 2, 33, 0.0), (3, 1, 128, 0.3), (1, 1, 256, 0.3)])
+def test_a_long_tree_among_short_ones(heads, kv_heads, d, mask, dtype):
+    """Short trees on average, so that LDS holds one stage at a time, and trees among them that need many stages of nodes and of rows."""
+    lq, lk = [3, 1, 0, 2] * 12, [9, 1, 13, 0] * 12
+    lq[5], lk[5] = 2, 500
+    lq[21], lk[21] = 260, 7
+    lq[40], lk[40] = 150, 333
+    s = tensors(24, TYPES[dtype], lq, lk, heads, kv_heads, d, mask)
+    ref, err = plain(s)
+    got = call(s)
+    close(got, ref, err)
+    for n, x in call(s).items():
+        assert torch.equal(x, got[n]), n

@@ -205,3 +205,28 @@ def test_repeats_on_another_stream_and_in_a_graph():
 def test_no_rows():
     got = binding.tl_sample(torch.zeros(0, 10, device="cuda"), torch.zeros(0, device="cuda"))
     assert all(v.numel() == 0 for v in got.values())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_long_rows_of_16_bits(dtype):
+    """Words of 16-bit types are counted per value between 2^-10 and 2^6 in long rows: words below and above that, zeros of both signs, infinities and NaN among
+    them, and rows of nothing else."""
+    g = torch.Generator(device="cuda").manual_seed(18)
+    x = torch.randn(9, 30001, generator=g, device="cuda") * 2
+    x[0] *= 2.0 ** -12
+    x[1] *= 300.0
+    x[2, ::3] = 0.0
+    x[2, 1::3] = -0.0
+    x[3, ::2] = -math.inf
+    x[3, 1::4] = math.nan
+    x[4, 77] = -math.nan
+    x[5] = torch.where(x[5] > 5, x[5] * 20, x[5])
+    x[6, :30000] = torch.finfo(TYPES[dtype]).min
+    x[7] = -70.0 - x[7].abs()
+    x[8, [5, 29999]] = math.inf
+    x = x.to(TYPES[dtype])
+    x[4, 78:90] = torch.tensor(-1, dtype=torch.int16, device="cuda").view(TYPES[dtype])         # NaN with its sign set
+    u = torch.rand(9, generator=g, device="cuda")
+    for f in (dict(), dict(top_p=0.9), dict(top_p=0.3, temperature=3.0), dict(top_k=6000, top_p=0.95), dict(top_p=0.99, temperature=1e-30),
+              dict(top_p=0.5, temperature=1e30), dict(temperature=0.0), dict(top_p=0.7, min_p=0.02)):
+        check(x, u, **f)
