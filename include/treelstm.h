@@ -467,7 +467,8 @@ enum tl_dtype { TL_DT_F32 = 0, TL_DT_BF16 = 1, TL_DT_F16 = 2 };
 
 /* Rows x heads x head_dim elements: element (r, j, d) lies at p + r * row + j * head + d (strides in elements, >= 0; p aligned to
  * its element).  Inputs may repeat rows or heads (stride 0); an output's rows and heads must not overlap.  Where head_dim and the
- * strides are multiples of 16 bytes and p is aligned to 16 bytes, rows are read in pieces of 16 bytes, else element by element. */
+ * strides are multiples of 16 bytes and p is aligned to 16 bytes, rows go straight into LDS; else 16 bytes at
+ * any address are read and shifted into place, which takes longer. */
 typedef struct {
     void *p;
     int64_t row, head;

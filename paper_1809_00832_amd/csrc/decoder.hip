@@ -86,7 +86,7 @@ AttPlan plan(const tl_attention *a)
 
 // The same for a backward pass, whose gradient of the queries sums over nodes and whose gradients of keys and values over rows.  Short trees (their rows,
 // or their nodes, on average): fewer of them at a time, and the other side divided among the waves instead.  Measured (us, 2 / 4 waves side by
-// side): 256 trees of 33 rows, 54 nodes, fp32 x 64: dQ 73 / 93, dK and dV 97 / 96; 25 such trees, x 30: 12 / 14 and 10 / 12; 8 trees
+// side, each gradient launched by itself): 256 trees of 33 rows, 54 nodes, fp32 x 64: dQ 73 / 93, dK and dV 97 / 96; 25 such trees, x 30: 12 / 14 and 10 / 12; 8 trees
 // of 1536 rows, 1200 nodes, bf16 x 128: 177 / 127 and 206 / 180.
 AttBackPlan back_plan(const tl_attention *a)
 {
