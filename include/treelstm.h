@@ -526,7 +526,7 @@ int tl_attend_backward(const tl_attention *a, const tl_rows *o, const float *lse
  *     top_k   keeps the first top_k words (off where < 1 or >= vocab)
  *     top_p   keeps, of these, every word whose mass in front of it is below top_p times the total of these; the first one always
  *             (off where not < 1)
- *     min_p   keeps, of these, every word with w_j >= min_p (above 1 as 1)
+ *     min_p   keeps, of these, every word with w_j >= min_p (above 1 as 1; off where not above 0, NaN included)
  *     token   the lowest kept j with sum of w over kept words up to j > u * (sum over all kept words)
  *     logprob log of that word's share of the kept words' weights;   kept: how many words were kept
  * T not above 0 (or NaN): the first word with the largest logit, logprob 0, kept 1.  A row without a value above -infinity: token -1,

@@ -868,10 +868,11 @@ template <typename T> __global__ __launch_bounds__(SMP_THREADS, 8) void k_sample
             if (cut.keeps(c.x, c.j)) cut = c;
         }
     }
-    // w >= min_p, of the exponents, as a bound of the values (a NaN keeps every word)
-    if (a.min_p) {
-        const double least = fmin(log2((double)a.min_p[r]), 0.);
-        const float x = least > -INFINITY ? smp_least_value(weight, max, least) : -INFINITY;
+    // w >= min_p, of the exponents, as a bound of the values.  A min_p not above 0, or a NaN, keeps every word; its logarithm is not asked for (a
+    // NaN, which fmin would take for the bound of the largest value).
+    const float m = a.min_p ? a.min_p[r] : 0.f;
+    if (m > 0.f) {
+        const float x = smp_least_value(weight, max, fmin(log2((double)m), 0.));
         if (x > cut.x) {
             cut.x = x;
             cut.j = row.n;

@@ -230,3 +230,16 @@ def test_long_rows_of_16_bits(dtype):
     for f in (dict(), dict(top_p=0.9), dict(top_p=0.3, temperature=3.0), dict(top_k=6000, top_p=0.95), dict(top_p=0.99, temperature=1e-30),
               dict(top_p=0.5, temperature=1e30), dict(temperature=0.0), dict(top_p=0.7, min_p=0.02)):
         check(x, u, **f)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("off", [-1.0, -1e-30, -0.0, math.nan, -math.inf])
+def test_min_p_that_keeps_every_word(off, dtype):
+    """Not above zero, or NaN: no word is lighter, so the filter is off; beside rows where it is on."""
+    for i, f in enumerate((dict(), dict(top_k=40, top_p=0.8), dict(top_p=0.95), dict(temperature=[0.7, 1.0, 1.5, 0.05, 30.0, 0.0]))):
+        x, u = draw(40 + i, 6, 20000, dtype)
+        want = check(x, u, **f)
+        got = check(x, u, min_p=off, **f)
+        for k in want:
+            assert torch.equal(got[k], want[k])
+        check(x, u, min_p=[0.02, off, 0.5, off, 0.001, off], **f)
