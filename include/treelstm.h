@@ -479,8 +479,9 @@ typedef struct {
  *     s_ij = scale * q_i . k_j     over the nodes j of i's tree with kv_mask[j] != 0
  *     o_i  = sum_j softmax_j(s_ij) v_j,    lse_i = log sum_j exp(s_ij)
  * for every one of n_heads heads; query head g reads head g / (n_heads / n_kv_heads) of k and v.  A query whose tree has no node that
- * may be read (or only scores of -infinity) gets o_i = 0 and lse_i = -infinity, and its gradients are zero.  What masked rows
- * of k and v hold, NaN and infinities included, has no effect on any result.
+ * may be read (or only scores of -infinity) gets o_i = 0 and lse_i = -infinity, its d_q is zero, and it adds nothing to d_k and d_v
+ * (unless its own q or d_o holds an infinity or NaN: zero times that is NaN, there as in every sum).  What masked rows of k and v hold, NaN
+ * and infinities included, has no effect on any result.
  */
 typedef struct {
     int dtype;               /* enum tl_dtype: of q, k, v, o and their gradients.  Sums, maxima and lse are fp32; with TL_DT_F32 so are all

@@ -761,6 +761,10 @@ __global__ __launch_bounds__(ATT_THREADS, (VEC || DP < 128 ? AttFwd<T, DP, WM>::
         const bool any = sum > 0.f || sum != sum;
         const float inv = any ? 1.f / sum : 0.f;
         if (half == 0) store_lse(qi, head, any, top, sum);
+        if (!any) {                                             // (zero times an infinite value is a NaN)
+#pragma unroll
+            for (int t = 0; t < DT; ++t) acc[t] = floatx16{};
+        }
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -804,7 +808,7 @@ __global__ __launch_bounds__(ATT_THREADS, (VEC || DP < 128 ? AttFwd<T, DP, WM>::
             rows.at(r, &i, &hd);
             hd += hk * a.G;
             if (d == 0) store_lse(i, hd, any, tt, total);
-            store(i, hd, d, any ? 1.f / total : 0.f, x);
+            store(i, hd, d, any ? 1.f / total : 0.f, any ? x : f32x4{0.f, 0.f, 0.f, 0.f});
         }
     }
 }
@@ -868,6 +872,11 @@ template <typename T> __global__ __launch_bounds__(ATT_THREADS) void k_attend_jo
 
 // What exp2 subtracts: a row without nodes (lse = -inf) has no probabilities.
 __device__ inline float lse_log2(float lse) { return lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f; }
+
+// P (dP - delta); zero where the probability is, also beside an infinite value: v_mul_legacy_f32, whose zero times anything is zero.  (The compiler's
+// intrinsic by its name: there is no builtin for it, and written as assembly it would not be scheduled.)
+extern "C" __device__ float mul_zero_wins(float, float) __asm("llvm.amdgcn.fmul.legacy");
+__device__ inline float score_gradient(float p, float gap) { return mul_zero_wins(p, gap); }
 
 // What both kernels of the backward pass need first.  Workgroups below `row_blocks`: delta[i] = d_o[i] . o[i] and the logarithms in base 2, 16 lanes
 // per query and head (fp16: also the power of two that brings the row of d_o to a length of 2^10, see fit_fp16).  With a mask, one further workgroup per tree: the tree's nodes that may be read, one after the other in `list` from
@@ -1045,7 +1054,7 @@ template <typename T, int DP, int WM, bool VEC> __device__ __forceinline__ void 
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(p[r], a.scale_log2, -row[0])) * (dp[r] - row[1]);
+                const float e = score_gradient(__builtin_amdgcn_exp2f(fmaf(p[r], a.scale_log2, -row[0])), dp[r] - row[1]);
                 p[r] = decltype(tail)::value && 32 * j + 8 * (r >> 2) + 4 * half + (r & 3) >= n ? 0.f : e;
             }
             if constexpr (F16) fit_fp16(p, row[2], acc);
@@ -1081,9 +1090,11 @@ template <typename T, int DP, int WM, bool VEC> __device__ __forceinline__ void 
         __syncthreads();
         compute(std::true_type{}, left);
     }
+    // (a row whose scores are all -infinity: its zeros may have met infinite keys)
+    const bool none = row[0] == INFINITY;
     const float out_scale = a.scale / row[2];
 #pragma unroll
-    for (int t = 0; t < DT; ++t) acc[t] *= out_scale;
+    for (int t = 0; t < DT; ++t) acc[t] = none ? floatx16{} : acc[t] * out_scale;
     if constexpr (C::WK == 2) {
         float *join = reinterpret_cast<float *>(att_lds) + (wm * 32 + col) * (DP + 4);
         __syncthreads();
@@ -1223,13 +1234,14 @@ template <typename T, int DP, int WN, bool VEC> __device__ __forceinline__ void 
                     stage_16(base + BQ * R::BYTES + i * ATT_THREADS * 16, gp, g_offset[i]);
                 }
         } else {
+            // (a row that is not there is the last one's query without a gradient: the score of a row of zeros would be a NaN beside an infinite key)
             auto row = [&](const AttTensor &x, int r) {
                 int i, hd;
-                rows.at(r, &i, &hd);
-                return r < left ? (const T *)row_of<T>(x, i, hk * a.G + hd) : (const T *)nullptr;
+                rows.at(min(r, left - 1), &i, &hd);
+                return (const T *)row_of<T>(x, i, hk * a.G + hd);
             };
             qs.request(b, a.D, [&](int r) { return row(a.q, r); });
-            gs.request(b + BQ * R::BYTES, a.D, [&](int r) { return row(a.d_o, r); });
+            gs.request(b + BQ * R::BYTES, a.D, [&](int r) { return r < left ? row(a.d_o, r) : (const T *)nullptr; });
         }
         if (wave < 2) {                         // (64 places; those beyond BQ are not read)
             int i, hd;
@@ -1289,7 +1301,7 @@ template <typename T, int DP, int WN, bool VEC> __device__ __forceinline__ void 
                 for (int j = 0; j < 4; ++j) {
                     const int r = 4 * r4 + j;
                     p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], a.scale_log2, -rr[j]));
-                    dp[r] = p[r] * (dp[r] - dd[j]);
+                    dp[r] = score_gradient(p[r], dp[r] - dd[j]);
                 }
             }
             mma_columns<T, DP, C::TERMS, DT>(dv, qc, 32 * q + BQ, p);
