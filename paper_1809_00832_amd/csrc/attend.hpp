@@ -49,8 +49,8 @@ struct AttArgs {
     const int32_t *q_off, *kv_off;
     const uint8_t *mask;
     float *lse;             // [n_q x n_heads], natural logarithm
-    float *delta, *ref;     // backward: sum over d of d_o * o, and lse in base 2, [n_q x n_heads]
-    float *size;            // backward, fp16: power of two that brings a row of d_o to a length of 2^10, [n_q x n_heads]
+    float *delta, *ref;     // backward: sum over d of d_o * o, and lse in base 2 (less ATT_LIFT), [n_q x n_heads]
+    float *size;            // backward, fp16: power of two that brings a row of d_o, lifted, to a length of 2^10, [n_q x n_heads]
     int32_t *list, *live;   // backward, with a mask: the nodes that may be read, tree by tree from kv_off on, and how many a tree has
     float *part_o;          // splits > 1: outputs of each part, [splits][n_q x n_heads][D]
     float *part_lse;        // ... and their logarithms, [splits][n_q x n_heads]
@@ -240,8 +240,8 @@ template <typename T, int DP> struct ColumnReads {
 
 // c[t] += sum over the 32 rows from r0 on of tile^T (column tile t) times w, whose register r belongs to row r0 + 8 (r / 4) + 4 half + r % 4.
 // 16-bit types: an operand of the matrix unit has to be of the type.  With TERMS = 1 w is rounded to it once, which adds to a result as much error
-// as its own rounding to the type does; with TERMS = 2 what the rounding left is a second operand (22 or 16 bits of w together).
-// Sums stay in fp32.
+// as its own rounding to the type does; with TERMS = 2 what the rounding left is a second operand (16 bits of w together, in fp16 22).
+// fp16 holds these bits only from 2^-14 (2^-3) on: probabilities and score gradients come scaled (ATT_LIFT, fit_fp16).  Sums stay in fp32.
 template <typename T, int DP, int TERMS, int NT>
 __device__ inline void mma_columns(floatx16 (&c)[NT], const ColumnReads<T, DP> &tile, int r0, const floatx16 &w)
 {
@@ -283,6 +283,12 @@ __device__ inline float sum_of_halves(float x)
     const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
     return __uint_as_float(y[0]) + __uint_as_float(y[1]);
 }
+
+// fp16 probabilities are operands times 2^14, and so are the sums until the end: of thousands of nodes most have less than fp16's least normal value, 2^-14,
+// and below it steps no longer shrink.  So scaled, all bits of one term are there from 2^-28 on, of two from 2^-17.  They do not exceed 1, so
+// that 2^14 is far from the type's largest value.  exp2 adds the 14 for nothing, in what it subtracts.
+template <typename T> constexpr float ATT_LIFT = std::is_same<T, f16_t>::value ? 14.f : 0.f;
+template <typename T> constexpr float ATT_LIFTED = std::is_same<T, f16_t>::value ? 16384.f : 1.f;
 
 // fp16 score gradients on their way into a product: neither may a scaled loss overflow them nor a small one let them vanish.  A lane's column of the
 // sums c carries a power of two, `size`, which is lowered (and the sums with it) when a gradient would come near the type's largest value.
@@ -659,7 +665,7 @@ __global__ __launch_bounds__(ATT_THREADS, (VEC || DP < 128 ? AttFwd<T, DP, WM>::
 #pragma unroll
             for (int r = 0; r < 16; ++r) high = fmaxf(high, p[t][r]);
         high = max_of_halves(high);
-        const float ref = high == -INFINITY ? 0.f : high * a.scale_log2;
+        const float ref = high == -INFINITY ? 0.f : high * a.scale_log2, less = ATT_LIFT<T> > 0.f ? ATT_LIFT<T> - ref : -ref;
         if (__any(high > top)) {
             const float f = __builtin_amdgcn_exp2f(top == high ? 0.f : top * a.scale_log2 - ref);
             sum *= f;
@@ -673,7 +679,7 @@ __global__ __launch_bounds__(ATT_THREADS, (VEC || DP < 128 ? AttFwd<T, DP, WM>::
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                p[t][r] = __builtin_amdgcn_exp2f(fmaf(p[t][r], a.scale_log2, -ref));
+                p[t][r] = __builtin_amdgcn_exp2f(fmaf(p[t][r], a.scale_log2, less));
                 sum += p[t][r];
             }
         }
@@ -720,7 +726,7 @@ __global__ __launch_bounds__(ATT_THREADS, (VEC || DP < 128 ? AttFwd<T, DP, WM>::
             store4<T>(row_of<T>(a.o, i, hd), d, a.D, a.vec_out, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
     };
     auto store_lse = [&](int i, int hd, bool any, float highest, float total) {
-        const float lse = any ? (highest * a.scale_log2 + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : -INFINITY;
+        const float lse = any ? (highest * a.scale_log2 + (__builtin_amdgcn_logf(total) - ATT_LIFT<T>)) * 0.6931471805599453f : -INFINITY;
         const long long rh = (long long)i * a.Hq + hd;
         if (partial) a.part_lse[(long long)part * a.n_q * a.Hq + rh] = lse;
         else if (a.lse) a.lse[rh] = lse;
@@ -910,8 +916,9 @@ template <typename T> __global__ __launch_bounds__(ATT_THREADS) void k_attend_pr
         }
         if (rh < n && l16 == 0) {
             a.delta[rh] = x;
-            a.ref[rh] = lse_log2(a.lse[rh]);
-            if (std::is_same<T, f16_t>::value) a.size[rh] = sq > 0.f && sq < INFINITY ? exp2f(10.f - ceilf(0.5f * log2f(sq))) : 1.f;
+            a.ref[rh] = lse_log2(a.lse[rh]) - ATT_LIFT<T>;
+            // (of the lifted score gradients, so without the lift)
+            if (std::is_same<T, f16_t>::value) a.size[rh] = sq > 0.f && sq < INFINITY ? exp2f(10.f - ATT_LIFT<T> - ceilf(0.5f * log2f(sq))) : 1.f / ATT_LIFTED<T>;
         }
         return;
     }
@@ -1092,7 +1099,7 @@ template <typename T, int DP, int WM, bool VEC> __device__ __forceinline__ void 
     }
     // (a row whose scores are all -infinity: its zeros may have met infinite keys)
     const bool none = row[0] == INFINITY;
-    const float out_scale = a.scale / row[2];
+    const float out_scale = a.scale / (row[2] * ATT_LIFTED<T>);
 #pragma unroll
     for (int t = 0; t < DT; ++t) acc[t] = none ? floatx16{} : acc[t] * out_scale;
     if constexpr (C::WK == 2) {
@@ -1275,7 +1282,7 @@ template <typename T, int DP, int WN, bool VEC> __device__ __forceinline__ void 
         }
 #pragma unroll
         for (int o = 32; o >= 1; o >>= 1) s = fminf(s, __shfl_xor(s, o));
-        size = s < INFINITY ? s : 1.f;
+        size = s < INFINITY ? s : 1.f / ATT_LIFTED<T>;
     }
     arrived(kf);
     arrived(vf);
@@ -1318,9 +1325,12 @@ template <typename T, int DP, int WN, bool VEC> __device__ __forceinline__ void 
         qc.move(step);
         numbers += step;
     }
-    const float k_scale = a.scale / size;
+    const float k_scale = a.scale / (size * ATT_LIFTED<T>);
 #pragma unroll
-    for (int t = 0; t < DT; ++t) dk[t] *= k_scale;
+    for (int t = 0; t < DT; ++t) {
+        dk[t] *= k_scale;
+        dv[t] *= 1.f / ATT_LIFTED<T>;
+    }
     if constexpr (C::WQ == 2) {
         float *join = reinterpret_cast<float *>(att_lds) + (wn * 32 + col) * 2 * (DP + 4);
         __syncthreads();

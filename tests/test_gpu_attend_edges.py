@@ -1,10 +1,21 @@
-"""Cross attention at the edges of its number range; bounds as in test_gpu_attend.py."""
+"""Cross attention at the edges of its number range: infinite inputs, probabilities far below the largest, gradients given what tl_attend stored.
+
+stored() has what tl_attend_backward returns for the o and lse that it is given, in 64 bits, so that the rounding of o is an input and no error.
+With u = 2^-24 and h = half a step of the operands' type:
+  probability 2^x of a sum of D products, two roundings of the scale, lse in base 2, the fp16 forms' shift by 2^14 and the difference:
+              relative |ds| + (4 |s| + 4 |lse| + 24) u  with  |ds| <= (D + 4) u * scale * sum |q||k|; 0 below 2^-126
+  as operand  16 bits in one term: h; in two terms: h^2, of what the first left; fp16, shifted by 2^14, below its normal range 2^-25 2^-14
+  score gradient  P (dP - delta): that of P, (D + 4) u of both sums' absolute values; two terms: h^2.  fp16: a row of d_o is brought to a length of
+              2^9 .. 2^10, and where a score gradient passes 2^15 it is brought to that: 2^-25 2^-9 of the larger one below the normal range
+  sums        (2 n + 8) u of the products' absolute values (two terms are two products); rounded once to the type.
+"""
 import math
 
 import pytest
 import torch
 
-from test_gpu_attend import TYPES, call, close, plain, tensors
+from paper_1809_00832_amd import binding
+from test_gpu_attend import TYPES, U, call, close, half_step, plain, tensors, where
 
 pytestmark = pytest.mark.gpu
 
@@ -50,3 +61,86 @@ def test_a_key_at_minus_infinity_gets_no_gradient(d, lq, lk, dtype):
         assert got[n].isfinite().all(), n
     assert (got["d_k"][7] == 0).all() and (got["d_v"][7] == 0).all()
     close(got, want, err, ["o", "lse", "d_k", "d_v"])
+
+
+def stored(s, o, lse, p_terms):
+    """d_q, d_k, d_v from o and lse, and a bound of the error of each.  p_terms: 16-bit terms of a probability in d_v's product."""
+    q, k, v, g, o = (x.double() for x in (s["q"], s["k"], s["v"], s["d_o"], o))
+    lse = lse.double()
+    dtype, scale = s["q"].dtype, s["scale"]
+    G, D = q.shape[1] // k.shape[1], q.shape[2]
+    h = half_step(dtype) if dtype != torch.float32 else 0.0
+    f16 = dtype == torch.float16
+    out = {"d_q": torch.zeros_like(q), "d_k": torch.zeros_like(k), "d_v": torch.zeros_like(v)}
+    err = {n: torch.zeros_like(x) for n, x in out.items()}
+    a = b = 0
+    for nq, nk in zip(s["lq"], s["lk"]):
+        rows, cols = slice(a, a + nq), slice(b, b + nk)
+        a, b = a + nq, b + nk
+        for j in range(q.shape[1]):
+            Q, K, V, dO, O, L = q[rows, j], k[cols, j // G], v[cols, j // G], g[rows, j], o[rows, j], lse[rows, j, None]
+            S = Q @ K.t() * scale
+            P = torch.exp(S - L)
+            rel = (D + 4) * U * scale * (Q.abs() @ K.abs().t()) + (4 * S.abs() + 4 * L.abs() + 24) * U
+            gap = dO @ V.t() - (dO * O).sum(1, keepdim=True)
+            dS = P * gap
+            e_dS = rel * dS.abs() + P * (1 + rel) * ((D + 4) * U * (dO.abs() @ V.abs().t() + (dO.abs() * O.abs()).sum(1, keepdim=True)) + 2 * U * gap.abs())
+            e_dS = e_dS + h * h * (dS.abs() + e_dS) + 2.0 ** -126 * gap.abs()
+            low_q = low_k = 0.0
+            if f16:
+                size, top = dO.norm(dim=1, keepdim=True), dS.abs()
+                low_q = 2.0 ** -34 * torch.maximum(size, top.amax(1, keepdim=True))
+                low_k = 2.0 ** -34 * torch.maximum(size.amax(), top.amax(0, keepdim=True))
+            m = nq * G
+            e_P = (rel + h ** p_terms) * P + (2.0 ** -39 if f16 else 2.0 ** -126)
+            dq, dk, dv = scale * dS @ K, scale * dS.t() @ Q, P.t() @ dO
+            e_q = scale * ((e_dS + low_q) @ K.abs() + (2 * nk + 8) * U * (dS.abs() @ K.abs()))
+            out["d_q"][rows, j], err["d_q"][rows, j] = dq, e_q
+            out["d_k"][cols, j // G] += dk
+            out["d_v"][cols, j // G] += dv
+            err["d_k"][cols, j // G] += scale * ((e_dS + low_k).t() @ Q.abs() + (2 * m + 8) * U * (dS.abs().t() @ Q.abs()))
+            err["d_v"][cols, j // G] += e_P.t() @ dO.abs() + (2 * m + 8) * U * (P.t() @ dO.abs())
+    for n in out:
+        err[n] = err[n] + half_step(dtype) * (out[n].abs() + err[n]) + (2.0 ** -25 if f16 else 1e-36)
+    return out, err
+
+
+def gradients(s):
+    o, lse = binding.tl_attend(s["q"], s["k"], s["v"], with_lse=True, **where(s))
+    return o, lse, binding.tl_attend_backward(s["q"], s["k"], s["v"], o, lse, s["d_o"], **where(s))
+
+
+@pytest.mark.parametrize("lq", [[1], [40], [300]])
+def test_fp16_outputs_of_many_small_probabilities(lq):
+    """One node far ahead of the others, whose probabilities are some 2^-22 each: unscaled they would be four or five of fp16's smallest steps.  The leading
+    node's value is zero, so that the output is made of the others alone (in one tile with it: a list this short is not divided)."""
+    d, n = 64, 250
+    s = tensors(33, torch.float16, lq, [n], 1, 1, d)
+    s["q"][:], s["k"][:] = 0, 0
+    s["q"][:, 0, 0] = 8
+    s["k"][17, 0, 0] = 15.13                                  # times 8 / sqrt(64): the score, beside zeros
+    s["v"][:] = s["v"].abs() + 1
+    s["v"][17] = 0
+    got, _ = binding.tl_attend(s["q"], s["k"], s["v"], with_lse=True, **where(s))
+    Q, K, V = (s[name].double()[:, 0] for name in "qkv")
+    P = torch.softmax(Q @ K.t() * s["scale"], 1)
+    O = P @ V
+    h = half_step(torch.float16)
+    e = (2 * (d + 4) * U * 15.2 + (8 * 15.2 + n + 24) * U + h) * O + 2.0 ** -39 * V.sum(0)
+    e = e + h * (O + e)
+    assert ((got[:, 0].double() - O).abs() <= e).all(), float(((got[:, 0].double() - O).abs() / e).max())
+
+
+@pytest.mark.parametrize("lq,lk,terms", [([600], [20000], 2), ([900, 31], [90, 120], 2), ([64], [16384], 2)])
+@pytest.mark.parametrize("size", [1.0, 512.0])
+def test_fp16_value_gradients_of_small_probabilities(lq, lk, terms, size):
+    """Probabilities far below fp16's normal range, with upstream gradients of a scaled loss: d_v of every node."""
+    s = tensors(34, torch.float16, lq, lk, 1, 1, 64, spread=1.0)
+    s["q"] *= 2
+    s["d_o"] *= size
+    o, lse, got = gradients(s)
+    ref, err = stored(s, o, lse, terms)
+    fits = {n: ref[n].abs() < 6e4 for n in ref}
+    for n in ref:
+        bad = fits[n] & ~((got[n].double() - ref[n]).abs() <= err[n])
+        assert fits[n].float().mean() > 0.99 and not bad.any(), (n, int(bad.sum()))
