@@ -461,7 +461,8 @@ int tl_td_destroy(tl_td_ctx *ctx);
  * produces a sentence from a tree reads those rows by cross attention and draws its words.  The
  * three operators below need no context; they launch on the current HIP device and on hip_stream, allocate
  * nothing, never synchronise, and may be captured in a HIP graph.  TL_OK, TL_EINVAL (see each argument;
- * nothing is enqueued), TL_EHIP.
+ * nothing is enqueued; also for attention over so many trees or rows that a launch would have 2^32 threads: from some 2^24 /
+ * n_kv_heads trees on), TL_EHIP.
  */
 enum tl_dtype { TL_DT_F32 = 0, TL_DT_BF16 = 1, TL_DT_F16 = 2 };
 

@@ -21,7 +21,17 @@ struct AttBackPlan {
     int q_waves, kv_waves;
     int q_splits, kv_splits;
     int q_bufs, kv_bufs;
+    int q_slots, kv_slots;          // row tiles and node tiles (see find_slot)
+    int q_blocks, kv_blocks;        // workgroups of each kind, a multiple of eight of the latter
+    int prepare_blocks, sum_blocks_q, sum_blocks_kv;
 };
+
+// A launch has fewer than 2^32 threads in all.
+constexpr long long ATT_MOST_BLOCKS = (1ll << 32) / ATT_THREADS - 1;
+
+// Packed rows of AttDq's tile and nodes of AttDkv's.
+constexpr int att_dq_rows(int dp, int waves) { return 32 * (dp > 128 ? 2 : waves); }
+constexpr int att_dkv_nodes(int dp, int size, int waves) { return 32 * (dp <= 128 ? waves : size == 2 ? 2 : 1); }
 
 template <typename T> hipError_t attend_forward(const AttArgs &a, const AttPlan &p, hipStream_t st);
 template <typename T> hipError_t attend_backward(const AttArgs &a, const AttBackPlan &p, hipStream_t st);
@@ -68,34 +78,31 @@ template <typename T, int DP, int WM, int WN, bool VEC> hipError_t att_both_of(A
 {
     typedef AttDq<T, DP, WM> Q;
     typedef AttDkv<T, DP, WN> KV;
-    a.slots = (int)((long long)a.n_q * a.G / Q::BM + a.n_trees);
+    static_assert(Q::BM == att_dq_rows(DP, WM) && KV::BN == att_dkv_nodes(DP, sizeof(T), WN), "the plan's tiles");
+    a.slots = p.q_slots;
     a.splits = p.q_splits;
     a.bufs = p.q_bufs;
-    a.kv_slots = a.n_kv / KV::BN + a.n_trees;
+    a.kv_slots = p.kv_slots;
     a.kv_splits = p.kv_splits;
     a.kv_bufs = p.kv_bufs;
-    // (a multiple of eight, so that consecutive workgroups of both kinds lie in one L2 domain)
-    a.kv_blocks = a.n_kv > 0 ? (int)(((long long)a.kv_slots * a.kv_splits * a.Hk + 7) & ~7ll) : 0;
-    const long long q_blocks = a.n_q > 0 ? (long long)a.slots * a.splits * a.Hk : 0;
+    a.kv_blocks = p.kv_blocks;
     const size_t lds_q = Q::lds(a.bufs), lds_kv = KV::lds(a.kv_bufs), most_q = Q::lds(2), most_kv = KV::lds(2);
-    return att_launch<k_attend_back<T, DP, Q::WM, KV::WN, VEC>>(a.kv_blocks + q_blocks, lds_q > lds_kv ? lds_q : lds_kv, most_q > most_kv ? most_q : most_kv, a, st);
+    return att_launch<k_attend_back<T, DP, Q::WM, KV::WN, VEC>>((long long)p.kv_blocks + p.q_blocks, lds_q > lds_kv ? lds_q : lds_kv, most_q > most_kv ? most_q : most_kv, a, st);
 }
 
 template <typename T, int DP, bool VEC> hipError_t att_backward_of(const AttArgs &a, const AttBackPlan &p, hipStream_t st)
 {
     hipError_t e = hipSuccess;
-    const long long row_blocks = ((long long)a.n_q * a.Hq + 15) / 16;
-    if (row_blocks + (a.mask ? a.n_trees : 0) > 0) {
-        hipLaunchKernelGGL(k_attend_prepare<T>, dim3((unsigned)(row_blocks + (a.mask ? a.n_trees : 0))), dim3(ATT_THREADS), 0, st, a, (int)row_blocks);
+    if (p.prepare_blocks > 0) {
+        const int row_blocks = p.prepare_blocks - (a.mask ? a.n_trees : 0);
+        hipLaunchKernelGGL(k_attend_prepare<T>, dim3(p.prepare_blocks), dim3(ATT_THREADS), 0, st, a, row_blocks);
         e = hipGetLastError();
     }
     if (e == hipSuccess && (a.n_q > 0 || a.n_kv > 0))
         e = p.q_waves == 2 ? (p.kv_waves == 2 ? att_both_of<T, DP, 2, 2, VEC>(a, p, st) : att_both_of<T, DP, 2, 4, VEC>(a, p, st))
                            : (p.kv_waves == 2 ? att_both_of<T, DP, 4, 2, VEC>(a, p, st) : att_both_of<T, DP, 4, 4, VEC>(a, p, st));
-    if (e == hipSuccess && (p.q_splits > 1 || p.kv_splits > 1)) {
-        const long long q_blocks = p.q_splits > 1 ? ((long long)a.n_q * a.Hq + ATT_WAVES - 1) / ATT_WAVES : 0;
-        const long long kv_blocks = p.kv_splits > 1 ? (2ll * a.n_kv * a.Hk + ATT_WAVES - 1) / ATT_WAVES : 0;
-        hipLaunchKernelGGL(k_attend_sum<T>, dim3((unsigned)(q_blocks + kv_blocks)), dim3(ATT_THREADS), 0, st, a, (int)q_blocks, p.q_splits, p.kv_splits);
+    if (e == hipSuccess && p.sum_blocks_q + p.sum_blocks_kv > 0) {
+        hipLaunchKernelGGL(k_attend_sum<T>, dim3(p.sum_blocks_q + p.sum_blocks_kv), dim3(ATT_THREADS), 0, st, a, p.sum_blocks_q, p.q_splits, p.kv_splits);
         e = hipGetLastError();
     }
     return e;

@@ -69,36 +69,56 @@ bool one_stage(long long rows, long long trees, int stage) { return 2 * rows <= 
 // 33 rows each, bf16 x 64: - / 24 / 38; fp32 x 64: - / 57 / 70; 64 trees of 2047 nodes half of them masked, 72 rows, fp32 x 64: 158 / 98 /
 // 117; 8 trees of 3500 nodes, 3000 rows, bf16 x 128: 250 / 310 / -.  A single token's few rows want every wave on nodes of its own.
 // Where row tiles do not fill the chip twice, a tree's nodes are divided among workgroups too, as long as a part keeps two stages.
-AttPlan plan(const tl_attention *a)
+// False where a launch would be too large.
+bool plan(const tl_attention *a, AttPlan *out)
 {
-    AttPlan p;
+    AttPlan &p = *out;
     const long long rows = (long long)a->n_q * (a->n_heads / a->n_kv_heads);
     const int dp = att_padded(a->head_dim), size = element_size(a->dtype);
     p.wm = rows <= 16ll * a->n_trees && dp * size <= 512 ? 1 : rows <= 128ll * a->n_trees ? 2 : 4;
     p.bm = 32 * p.wm;
     p.bn = p.wm == 1 ? 128 : p.wm == 2 ? 64 : dp * size <= 256 ? 64 : 32;
     const long long slots = rows / p.bm + a->n_trees;
-    p.slots = (int)(slots < INT32_MAX ? slots : INT32_MAX);     // (tl_attend refuses such)
-    p.splits = splits((long long)p.slots * a->n_kv_heads, a->n_kv / ((long long)p.bn * a->n_trees));
+    if (slots > ATT_MOST_BLOCKS) return false;
+    p.slots = (int)slots;
+    p.splits = splits(slots * a->n_kv_heads, a->n_kv / ((long long)p.bn * a->n_trees));
     p.bufs = one_stage(a->n_kv, a->n_trees, p.bn) ? 1 : 2;
-    return p;
+    return slots * p.splits * a->n_kv_heads <= ATT_MOST_BLOCKS && (p.splits == 1 || (long long)a->n_q * a->n_heads <= ATT_MOST_BLOCKS);
 }
 
 // The same for a backward pass, whose gradient of the queries sums over nodes and whose gradients of keys and values over rows.  Short trees (their rows,
 // or their nodes, on average): fewer of them at a time, and the other side divided among the waves instead.  Measured (us, 2 / 4 waves side by
 // side, each gradient launched by itself): 256 trees of 33 rows, 54 nodes, fp32 x 64: dQ 73 / 93, dK and dV 97 / 96; 25 such trees, x 30: 12 / 14 and 10 / 12; 8 trees
 // of 1536 rows, 1200 nodes, bf16 x 128: 177 / 127 and 206 / 180.
-AttBackPlan back_plan(const tl_attention *a)
+bool back_plan(const tl_attention *a, AttBackPlan *out)
 {
-    AttBackPlan p;
-    const long long rows = (long long)a->n_q * (a->n_heads / a->n_kv_heads), trees = a->n_trees;
+    AttBackPlan &p = *out;
+    const long long rows = (long long)a->n_q * (a->n_heads / a->n_kv_heads), trees = a->n_trees, heads = a->n_kv_heads;
     p.q_waves = rows <= 128 * trees ? 2 : 4;
     p.kv_waves = a->n_kv <= 128 * trees ? 2 : 4;
-    p.q_splits = a->n_q == 0 ? 1 : splits((rows / (32 * p.q_waves) + trees) * a->n_kv_heads, a->n_kv / (64 * trees));
-    p.kv_splits = a->n_kv == 0 ? 1 : splits((a->n_kv / (32 * p.kv_waves) + trees) * a->n_kv_heads, rows / (64 * trees));
+    p.q_splits = a->n_q == 0 ? 1 : splits((rows / (32 * p.q_waves) + trees) * heads, a->n_kv / (64 * trees));
+    p.kv_splits = a->n_kv == 0 ? 1 : splits((a->n_kv / (32 * p.kv_waves) + trees) * heads, rows / (64 * trees));
     p.q_bufs = one_stage(a->n_kv, trees, 64) ? 1 : 2;
     p.kv_bufs = one_stage(rows, trees, 64) ? 1 : 2;
-    return p;
+    const int dp = att_padded(a->head_dim);
+    const long long q_slots = rows / att_dq_rows(dp, p.q_waves) + trees, kv_slots = a->n_kv / att_dkv_nodes(dp, element_size(a->dtype), p.kv_waves) + trees;
+    const long long row_heads = (long long)a->n_q * a->n_heads;
+    const long long q_blocks = a->n_q > 0 ? q_slots * p.q_splits * heads : 0;
+    // (a multiple of eight, so that consecutive workgroups of both kinds lie in one L2 domain)
+    const long long kv_blocks = a->n_kv > 0 ? (kv_slots * p.kv_splits * heads + 7) & ~7ll : 0;
+    const long long prepare = (row_heads + 15) / 16 + (a->kv_mask ? trees : 0);
+    const long long sum_q = p.q_splits > 1 ? (row_heads + ATT_WAVES - 1) / ATT_WAVES : 0;
+    const long long sum_kv = p.kv_splits > 1 ? (2ll * a->n_kv * heads + ATT_WAVES - 1) / ATT_WAVES : 0;
+    if (q_slots > INT32_MAX || kv_slots > INT32_MAX || q_blocks + kv_blocks > ATT_MOST_BLOCKS || prepare > ATT_MOST_BLOCKS || sum_q + sum_kv > ATT_MOST_BLOCKS)
+        return false;
+    p.q_slots = (int)q_slots;
+    p.kv_slots = (int)kv_slots;
+    p.q_blocks = (int)q_blocks;
+    p.kv_blocks = (int)kv_blocks;
+    p.prepare_blocks = (int)prepare;
+    p.sum_blocks_q = (int)sum_q;
+    p.sum_blocks_kv = (int)sum_kv;
+    return true;
 }
 
 long long round16(long long x) { return (x + 15) & ~15ll; }
@@ -172,8 +192,18 @@ extern "C" {
 int tl_attend_workspace(const tl_attention *a, int backward, int64_t *bytes)
 {
     if (!bytes || !check(a)) return TL_EINVAL;
-    AttArgs unused;
-    *bytes = a->n_trees == 0 ? 0 : backward ? lay_out(a, back_plan(a), nullptr, &unused) : workspace(a, plan(a));
+    *bytes = 0;
+    if (a->n_trees == 0) return TL_OK;
+    if (backward) {
+        AttBackPlan p;
+        AttArgs unused;
+        if (!back_plan(a, &p)) return TL_EINVAL;
+        *bytes = lay_out(a, p, nullptr, &unused);
+    } else if (a->n_q > 0) {
+        AttPlan p;
+        if (!plan(a, &p)) return TL_EINVAL;
+        *bytes = workspace(a, p);
+    }
     return TL_OK;
 }
 
@@ -181,8 +211,8 @@ int tl_attend(const tl_attention *a, const tl_rows *o, float *lse, void *workspa
 {
     if (!check(a) || !o || !check_rows(*o, a->dtype, a->n_q, a->n_heads, a->head_dim, true)) return TL_EINVAL;
     if (a->n_trees == 0 || a->n_q == 0) return TL_OK;
-    const AttPlan p = plan(a);
-    if ((long long)p.slots * p.splits * a->n_kv_heads >= INT32_MAX) return TL_EINVAL;
+    AttPlan p;
+    if (!plan(a, &p)) return TL_EINVAL;
     const long long need = workspace(a, p);
     if (need > workspace_bytes) return TL_ELIMIT;
     if (need > 0 && (!workspace_p || ((uintptr_t)workspace_p & 15))) return TL_EINVAL;
@@ -212,15 +242,12 @@ int tl_attend_backward(const tl_attention *a, const tl_rows *o, const float *lse
         !check_rows(*d_v, dt, a->n_kv, a->n_kv_heads, D, true))
         return TL_EINVAL;
     if (a->n_trees == 0) return TL_OK;
-    const AttBackPlan p = back_plan(a);
+    AttBackPlan p;
+    if (!back_plan(a, &p)) return TL_EINVAL;
     AttArgs x = arguments(a);
     const long long need = lay_out(a, p, static_cast<char *>(workspace_p), &x);
     if ((a->n_q > 0 && !lse) || (need > 0 && (!workspace_p || ((uintptr_t)workspace_p & 15)))) return TL_EINVAL;
     if (need > workspace_bytes) return TL_ELIMIT;
-    const long long rows = (long long)a->n_q * (a->n_heads / a->n_kv_heads);
-    if ((rows / 32 + a->n_trees) * a->n_kv_heads * p.q_splits + ((long long)a->n_kv / 32 + a->n_trees) * a->n_kv_heads * p.kv_splits > INT32_MAX - 8 ||
-        (long long)a->n_q * a->n_heads / 4 + a->n_trees + (long long)a->n_kv * a->n_kv_heads / 2 >= INT32_MAX)
-        return TL_EINVAL;
     x.o = AttTensor{o->p, o->row, o->head};
     x.d_o = AttTensor{d_o->p, d_o->row, d_o->head};
     x.d_q = AttTensor{d_q->p, d_q->row, d_q->head};

@@ -102,3 +102,28 @@ def test_sampling_refuses(change):
 
 def test_sampling_no_rows():
     assert sample(n_rows=0, logits=None, u=None, token=None) == OK
+
+
+LIMIT = (1 << 24) - 1       # workgroups of 256 threads in a launch
+
+
+def test_launches_that_would_be_too_large():
+    """2^32 threads and more: refused before anything is enqueued, also where only the second launch of a call would be too large."""
+    def both(n, code, **change):
+        a = attention(n_trees=n, **change)
+        assert workspace(a)[0] == code and workspace(a, 1)[0] == code
+        if code == EINVAL:
+            assert attend(a) == EINVAL and backward(a) == EINVAL
+
+    for n in (LIMIT // 2 + 1, LIMIT, 1 << 30, (1 << 31) - 1):                # a tree has a workgroup of its own for each of two heads
+        both(n, EINVAL, n_q=n, n_kv=n)
+    both(LIMIT // 4 - 8, OK, n_q=3, n_kv=50)
+    assert workspace(attention(n_trees=LIMIT // 2, n_q=3))[0] == OK         # (a backward pass has both kinds of workgroups)
+    # many rows of one tree: forward tiles of 128 are still few enough, the backward pass's first launch has a workgroup for 16 row heads
+    a = attention(n_trees=1, n_q=1 << 26, n_kv=1)
+    assert workspace(a)[0] == OK
+    assert workspace(a, 1)[0] == EINVAL and backward(a) == EINVAL
+    # no rows at all, a mask: one workgroup per tree
+    for n in (1 << 24, (1 << 31) - 1):
+        a = attention(n_trees=n, n_q=0, n_kv=0, kv_mask=P, q=rows(4, 64, p=None), k=rows(2, 64, p=None), v=rows(2, 64, p=None))
+        assert backward(a) == EINVAL
