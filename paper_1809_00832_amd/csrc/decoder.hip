@@ -177,12 +177,27 @@ AttArgs arguments(const tl_attention *a)
 
 bool pieces_of_4(const tl_rows &t, int dtype, int D) { return in_pieces(t, dtype, D, 4 * element_size(dtype)); }
 
-template <typename T> hipError_t sample(const SampleArgs &a, int n_rows, hipStream_t st)
+// A workgroup a row; a launch has fewer than 2^32 threads in all, so very many rows take several.
+template <typename T> hipError_t sample(SampleArgs a, int n_rows, hipStream_t st)
 {
-    const hipError_t e = att_allow<k_sample<T>>(sizeof(SmpShared));
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_sample<T>, dim3((unsigned)n_rows), dim3(SMP_THREADS), sizeof(SmpShared), st, a);
-    return hipGetLastError();
+    constexpr int MOST = 1 << 21;
+    hipError_t e = att_allow<k_sample<T>>(sizeof(SmpShared));
+    while (e == hipSuccess) {
+        const int n = n_rows < MOST ? n_rows : MOST;
+        hipLaunchKernelGGL(k_sample<T>, dim3(n), dim3(SMP_THREADS), sizeof(SmpShared), st, a);
+        e = hipGetLastError();
+        n_rows -= n;
+        if (n_rows == 0) break;
+        a.logits = static_cast<const T *>(a.logits) + n * a.row;
+        a.u += n;
+        a.token += n;
+        for (const float **x : {&a.temperature, &a.top_p, &a.min_p})
+            if (*x) *x += n;
+        if (a.top_k) a.top_k += n;
+        if (a.logprob) a.logprob += n;
+        if (a.kept) a.kept += n;
+    }
+    return e;
 }
 
 }  // namespace

@@ -243,3 +243,19 @@ def test_min_p_that_keeps_every_word(off, dtype):
         for k in want:
             assert torch.equal(got[k], want[k])
         check(x, u, min_p=[0.02, off, 0.5, off, 0.001, off], **f)
+
+
+def test_rows_of_several_launches():
+    """More rows than the 2^22 workgroups of 1024 threads that a launch may have: the words are those of the rows by themselves."""
+    n, vocab = (1 << 22) + 5, 3
+    x, u = draw(19, n, vocab, "bf16")
+    g = torch.Generator(device="cuda").manual_seed(20)
+    cfg = dict(temperature=torch.rand(n, generator=g, device="cuda"), top_k=torch.randint(0, 4, (n,), generator=g, device="cuda", dtype=torch.int32),
+               top_p=torch.rand(n, generator=g, device="cuda"), min_p=torch.rand(n, generator=g, device="cuda") - 0.5)
+    got = binding.tl_sample(x, u, **cfg)
+    for first in (0, (1 << 21) - 50, (1 << 22) - 50, n - 100):
+        part = slice(first, first + 100)
+        want = check(x[part], u[part], **{k: v[part].cpu() for k, v in cfg.items()})
+        for k in want:
+            assert torch.equal(got[k][part], want[k])
+    assert int(got["token"].min()) >= 0 and int(got["token"].max()) < vocab and int(got["kept"].min()) >= 1
