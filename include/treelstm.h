@@ -489,7 +489,7 @@ typedef struct {
                                 operands, with the 16-bit types probabilities and score gradients are operands of the type in their
                                 second products: score gradients, and probabilities where rows are few, with what
                                 the rounding left as a second operand, probabilities of many rows rounded once.          */
-    int n_trees, n_q, n_kv;  /* >= 0                                                                                       */
+    int n_trees, n_q, n_kv;  /* >= 0; n_q and n_kv below 2^31 - 2^16                                                       */
     int n_heads, n_kv_heads; /* >= 1, n_heads a multiple of n_kv_heads, n_heads <= 4096                                    */
     int head_dim;            /* 1 .. 256                                                                                   */
     float scale;             /* finite, > 0                                                                                */

@@ -127,3 +127,16 @@ def test_launches_that_would_be_too_large():
     for n in (1 << 24, (1 << 31) - 1):
         a = attention(n_trees=n, n_q=0, n_kv=0, kv_mask=P, q=rows(4, 64, p=None), k=rows(2, 64, p=None), v=rows(2, 64, p=None))
         assert backward(a) == EINVAL
+
+
+@pytest.mark.parametrize("name", ["n_q", "n_kv"])
+@pytest.mark.parametrize("mask", [None, P])
+def test_rows_whose_numbers_would_pass_32_bits(name, mask):
+    """The kernels' place in a list of nodes runs past its end by up to 2^15 before it is bounded."""
+    few = dict(n_trees=1, n_q=1, n_kv=1, n_heads=1, n_kv_heads=1, head_dim=1, kv_mask=mask, q=rows(1, 1), k=rows(1, 1), v=rows(1, 1))
+    most = (1 << 31) - 1 - (1 << 16)
+    one = dict(o=rows(1, 1), d_o=rows(1, 1), d_q=rows(1, 1), d_k=rows(1, 1), d_v=rows(1, 1))
+    for n in (most + 1, (1 << 31) - 1):
+        a = attention(**dict(few, **{name: n}))
+        assert workspace(a)[0] == EINVAL and workspace(a, 1)[0] == EINVAL and attend(a, o=rows(1, 1)) == EINVAL and backward(a, **one) == EINVAL
+    assert workspace(attention(**dict(few, n_kv=most)))[0] == OK and workspace(attention(**dict(few, n_kv=most)), 1)[0] == OK
