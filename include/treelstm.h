@@ -492,7 +492,7 @@ typedef struct {
     int n_trees, n_q, n_kv;  /* >= 0; n_q and n_kv below 2^31 - 2^16                                                       */
     int n_heads, n_kv_heads; /* >= 1, n_heads a multiple of n_kv_heads, n_heads <= 4096                                    */
     int head_dim;            /* 1 .. 256                                                                                   */
-    float scale;             /* finite, > 0                                                                                */
+    float scale;             /* > 0, at most 2.3e38 (in base 2 it has to be finite)                                        */
     const int32_t *q_off;    /* [n_trees+1], from 0 to n_q, ascending (equal ones: a tree without queries)       DEVICE     */
     const int32_t *kv_off;   /* [n_trees+1], from 0 to n_kv: tree_off of the forward                             DEVICE
                                 Offsets outside these bounds: results are unspecified, nothing outside the arrays is accessed.  */

@@ -40,6 +40,8 @@ bool in_pieces(const tl_rows &t, int dtype, int D, int bytes)
     return D % n == 0 && t.row % n == 0 && t.head % n == 0 && ((uintptr_t)t.p & (bytes - 1)) == 0;
 }
 
+constexpr float LOG2_E = 1.4426950408889634f;    // exponentials are powers of two
+
 // The kernels count in 32 bits and look up to 2^15 rows beyond the last one (4096 mask bytes at a time; 256 parts of whole stages) before they bound it.
 constexpr int MOST_ROWS = INT32_MAX - 65536;
 
@@ -48,7 +50,7 @@ bool check(const tl_attention *a)
     if (!a || a->dtype < TL_DT_F32 || a->dtype > TL_DT_F16) return false;
     if (a->n_trees < 0 || a->n_q < 0 || a->n_kv < 0 || a->n_q > MOST_ROWS || a->n_kv > MOST_ROWS || a->n_heads < 1 || a->n_heads > 4096 || a->n_kv_heads < 1) return false;
     if (a->n_heads % a->n_kv_heads || a->head_dim < 1 || a->head_dim > 256) return false;
-    if (!(a->scale > 0.f) || !isfinite(a->scale)) return false;
+    if (!(a->scale > 0.f) || !isfinite(a->scale * LOG2_E)) return false;
     if (a->n_trees == 0) return a->n_q == 0 && a->n_kv == 0;
     if (!a->q_off || !a->kv_off) return false;
     return check_rows(a->q, a->dtype, a->n_q, a->n_heads, a->head_dim, false) && check_rows(a->k, a->dtype, a->n_kv, a->n_kv_heads, a->head_dim, false) &&
@@ -163,7 +165,7 @@ AttArgs arguments(const tl_attention *a)
     x.kv_off = a->kv_off;
     x.mask = a->kv_mask;
     x.scale = a->scale;
-    x.scale_log2 = a->scale * 1.4426950408889634f;
+    x.scale_log2 = a->scale * LOG2_E;
     x.n_trees = a->n_trees;
     x.n_q = a->n_q;
     x.n_kv = a->n_kv;

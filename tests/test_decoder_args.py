@@ -140,3 +140,11 @@ def test_rows_whose_numbers_would_pass_32_bits(name, mask):
         a = attention(**dict(few, **{name: n}))
         assert workspace(a)[0] == EINVAL and workspace(a, 1)[0] == EINVAL and attend(a, o=rows(1, 1)) == EINVAL and backward(a, **one) == EINVAL
     assert workspace(attention(**dict(few, n_kv=most)))[0] == OK and workspace(attention(**dict(few, n_kv=most)), 1)[0] == OK
+
+
+def test_scale_in_base_2():
+    """The kernels multiply scores by scale * log2(e): where that is infinite a score of zero would be a NaN."""
+    assert workspace(attention(scale=2.3e38))[0] == OK
+    for scale in (2.4e38, 3.4e38):
+        a = attention(scale=scale)
+        assert workspace(a)[0] == EINVAL and attend(a) == EINVAL and backward(a) == EINVAL
