@@ -384,19 +384,24 @@ static __device__ const u32x4 att_zeros[1] = {};
 // 16 bytes a lane from global memory to LDS, lane l's at lds + 16 l; nothing passes through registers.  The hardware counts it with the vector
 // loads; stage_wait() waits for it.  (Written out because the compiler, given its builtin, waits in front of every LDS read that follows.  It has no
 // output register that could be reused too early, and what the compiler counts itself only becomes stricter by it.)
+// (m0 is named as written: it is reserved, so that the compiler keeps nothing of its own there and warns of the name, but where it sets m0 for an
+// instruction of its own it may do so far ahead.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ inline void stage_16(uint32_t lds, const void *p)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory", "m0");
 }
 __device__ inline void stage_16(uint32_t lds, const void *base, uint32_t offset)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0");
 }
 // 4 bytes a lane.
 __device__ inline void stage_4(uint32_t lds, const void *p)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(p) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(p) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 // Makes the compiler wait for loads into x here.  Without it, it waits at their first use: inside a loop in every pass, and then for what is
 // being staged as well.
 template <typename F, int N> __device__ inline void arrived(F (&x)[N])

@@ -148,3 +148,17 @@ def test_scale_in_base_2():
     for scale in (2.4e38, 3.4e38):
         a = attention(scale=scale)
         assert workspace(a)[0] == EINVAL and attend(a) == EINVAL and backward(a) == EINVAL
+
+
+def test_assembly_names_m0_as_written():
+    import glob
+    import os
+    import re
+    found = 0
+    for path in glob.glob(os.path.join(os.path.dirname(binding.__file__), "csrc", "*.h*")):
+        with open(path) as f:
+            for statement in re.findall(r"asm volatile\((.*?)\);", f.read(), re.S):
+                if re.search(r"s_mov_b32 m0|s_add_u32 m0", statement):
+                    found += 1
+                    assert '"m0"' in statement, (path, statement)
+    assert found
