@@ -334,11 +334,18 @@ def _dtype(t) -> int:
     return TL_DT_BF16 if d is torch.bfloat16 else TL_DT_F16
 
 
-def _raw_stream(device) -> int:
+def _raw_stream(index) -> int:
     import torch
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)        # (the public call takes 3 us, as long as a launch)
-    index = torch.cuda.current_device() if device.index is None else device.index
-    return raw(index) if raw else torch.cuda.current_stream(device).cuda_stream
+    return raw(index) if raw else torch.cuda.current_stream(index).cuda_stream
+
+
+def _elsewhere(index, stream):
+    """A context in which launches go to the given stream, or to the device `index` where that is not the current one.  (The callers compare with
+    torch._C._cuda_getDevice, which is torch.cuda.current_device without its check of the set-up: a short call is bound by the host's time.)"""
+    import torch
+    assert index >= 0 and (stream is None or stream.device_index == index), "CUDA tensors, and a stream of their device"
+    return torch.cuda.stream(stream) if stream is not None else torch.cuda.device(index)
 
 
 # tl_attention and tl_rows as bytes: packing takes a quarter of the time of filling the structures
@@ -346,28 +353,29 @@ _PACK_ATTENTION, _PACK_ROWS = struct.Struct("7if3Q9q").pack, struct.Struct("Q2q"
 assert struct.calcsize("7if3Q9q") == ctypes.sizeof(tl_attention) and struct.calcsize("Q2q") == ctypes.sizeof(tl_rows)
 
 
-def _rows(t, like, shape):
-    assert t.is_cuda and t.dtype == like.dtype and t.shape == shape and (shape[2] == 1 or t.stride(2) == 1), "rows, heads and a contiguous head_dim"
+def _rows(t, like, shape, index):
+    assert t.get_device() == index and t.dtype == like.dtype and t.shape == shape and (shape[2] == 1 or t.stride(2) == 1), "rows, heads and a contiguous head_dim"
     return _PACK_ROWS(t.data_ptr(), t.stride(0), t.stride(1))
 
 
-def _attention(q, k, v, q_off, kv_off, kv_mask, scale) -> bytes:
+def _attention(q, k, v, q_off, kv_off, kv_mask, scale, index) -> bytes:
     import torch
     n_q, n_heads, d = q.shape
     n_kv, n_kv_heads, dk = k.shape
     dtype = q.dtype
-    assert q.is_cuda and k.is_cuda and v.is_cuda and k.dtype == dtype and v.dtype == dtype and dk == d and v.shape == k.shape
+    assert index == k.get_device() == v.get_device() == q_off.get_device() == kv_off.get_device(), "tensors of one device"
+    assert k.dtype == dtype and v.dtype == dtype and dk == d and v.shape == k.shape
     q_row, q_head, q_d = q.stride()
     k_row, k_head, k_d = k.stride()
     v_row, v_head, v_d = v.stride()
     assert d == 1 or q_d == k_d == v_d == 1, "head_dim must be contiguous"
     int32 = torch.int32
-    assert q_off.is_cuda and q_off.dtype == int32 and q_off.is_contiguous() and kv_off.is_cuda and kv_off.dtype == int32 and kv_off.is_contiguous()
+    assert q_off.dtype == int32 and q_off.is_contiguous() and kv_off.dtype == int32 and kv_off.is_contiguous()
     n_off = q_off.numel()
     assert n_off == kv_off.numel() >= 1
     mask = 0
     if kv_mask is not None:
-        assert kv_mask.is_cuda and kv_mask.dtype in (torch.uint8, torch.bool) and kv_mask.is_contiguous() and kv_mask.numel() == n_kv
+        assert kv_mask.get_device() == index and kv_mask.dtype in (torch.uint8, torch.bool) and kv_mask.is_contiguous() and kv_mask.numel() == n_kv
         mask = kv_mask.data_ptr()
     return _PACK_ATTENTION(_dtype(q), n_off - 1, n_q, n_kv, n_heads, n_kv_heads, d, d ** -0.5 if scale is None else scale, q_off.data_ptr(),
                            kv_off.data_ptr(), mask, q.data_ptr(), q_row, q_head, k.data_ptr(), k_row, k_head, v.data_ptr(), v_row, v_head)
@@ -384,17 +392,19 @@ def _attend_workspace(a, backward, device):
 def tl_attend(q, k, v, q_off, kv_off, kv_mask=None, scale=None, o=None, with_lse=False, stream=None):
     """Cross attention of every tree's queries to its nodes.  q [n_q, heads, D], k and v [n_kv, kv_heads, D]: CUDA tensors of one type
     (float32, bfloat16, float16) with any strides of rows and heads; q_off, kv_off [n_trees + 1] int32; kv_mask [n_kv] uint8 or bool,
-    0 for nodes that are not read; scale: 1 / sqrt(D) if None.  Returns o, or (o, lse [n_q, heads] float32)."""
+    0 for nodes that are not read; scale: 1 / sqrt(D) if None.  All on one device, where the call goes, on its current stream or `stream`.
+    Returns o, or (o, lse [n_q, heads] float32)."""
     import torch
-    if stream is not None:
-        with torch.cuda.stream(stream):
+    index = q.get_device()
+    if stream is not None or torch._C._cuda_getDevice() != index:
+        with _elsewhere(index, stream):
             return tl_attend(q, k, v, q_off, kv_off, kv_mask, scale, o, with_lse)
-    a = _attention(q, k, v, q_off, kv_off, kv_mask, scale)
+    a = _attention(q, k, v, q_off, kv_off, kv_mask, scale, index)
     shape, device = q.shape, q.device
     if o is None:
         o = torch.empty_like(q) if q.is_contiguous() else q.new_empty(shape)
     lse = torch.empty(shape[:2], dtype=torch.float32, device=device) if with_lse else None
-    call, rows, at, st = lib().tl_attend, _rows(o, q, shape), _ptr(lse), _raw_stream(device)
+    call, rows, at, st = lib().tl_attend, _rows(o, q, shape, index), _ptr(lse), _raw_stream(index)
     code = call(a, rows, at, None, 0, st)
     if code == TL_ELIMIT:                                       # (most calls need no workspace: asking first would cost them a call)
         ws, n = _attend_workspace(a, 0, device)
@@ -406,16 +416,17 @@ def tl_attend(q, k, v, q_off, kv_off, kv_mask=None, scale=None, o=None, with_lse
 def tl_attend_backward(q, k, v, o, lse, d_o, q_off, kv_off, kv_mask=None, scale=None, stream=None):
     """Gradients of tl_attend for its arguments and what it returned; d_o like o.  Returns dict(d_q, d_k, d_v) of new tensors."""
     import torch
-    if stream is not None:
-        with torch.cuda.stream(stream):
+    index = q.get_device()
+    if stream is not None or torch._C._cuda_getDevice() != index:
+        with _elsewhere(index, stream):
             return tl_attend_backward(q, k, v, o, lse, d_o, q_off, kv_off, kv_mask, scale)
-    a = _attention(q, k, v, q_off, kv_off, kv_mask, scale)
+    a = _attention(q, k, v, q_off, kv_off, kv_mask, scale, index)
     q_shape, kv_shape, device = q.shape, k.shape, q.device
-    assert lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q_shape[:2]
+    assert lse.get_device() == index and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q_shape[:2]
     d_q, d_k, d_v = q.new_empty(q_shape), q.new_empty(kv_shape), q.new_empty(kv_shape)
     ws, n = _attend_workspace(a, 1, device)
-    _check(lib().tl_attend_backward(a, _rows(o, q, q_shape), lse.data_ptr(), _rows(d_o, q, q_shape), _rows(d_q, q, q_shape), _rows(d_k, q, kv_shape),
-                                    _rows(d_v, q, kv_shape), _ptr(ws), n, _raw_stream(device)), "tl_attend_backward")
+    _check(lib().tl_attend_backward(a, _rows(o, q, q_shape, index), lse.data_ptr(), _rows(d_o, q, q_shape, index), _rows(d_q, q, q_shape, index), _rows(d_k, q, kv_shape, index),
+                                    _rows(d_v, q, kv_shape, index), _ptr(ws), n, _raw_stream(index)), "tl_attend_backward")
     return {"d_q": d_q, "d_k": d_k, "d_v": d_v}
 
 
@@ -424,19 +435,20 @@ def tl_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, s
     temperature, top_p, min_p [n] float32 and top_k [n] int32 CUDA tensors, None: off.  Returns dict(token int32, logprob float32,
     kept int32) of new tensors [n]."""
     import torch
-    if stream is not None:
-        with torch.cuda.stream(stream):
+    index = logits.get_device()
+    if stream is not None or torch._C._cuda_getDevice() != index:
+        with _elsewhere(index, stream):
             return tl_sample(logits, u, temperature, top_k, top_p, min_p)
     n, vocab = logits.shape
     device = logits.device
-    assert logits.is_cuda and (vocab == 1 or logits.stride(1) == 1)
+    assert vocab == 1 or logits.stride(1) == 1
     for t, dt in ((u, torch.float32), (temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32), (min_p, torch.float32)):
-        assert t is None or (t.is_cuda and t.dtype == dt and t.is_contiguous() and t.numel() == n)
+        assert t is None or (t.get_device() == index and t.dtype == dt and t.is_contiguous() and t.numel() == n)
     out = {"token": torch.empty(n, dtype=torch.int32, device=device), "logprob": torch.empty(n, dtype=torch.float32, device=device),
            "kept": torch.empty(n, dtype=torch.int32, device=device)}
     _check(lib().tl_sample(_dtype(logits), n, vocab, logits.data_ptr(), logits.stride(0), u.data_ptr(), _ptr(temperature), _ptr(top_k),
                            _ptr(top_p), _ptr(min_p), out["token"].data_ptr(), out["logprob"].data_ptr(), out["kept"].data_ptr(),
-                           _raw_stream(device)), "tl_sample")
+                           _raw_stream(index)), "tl_sample")
     return out
 
 
