@@ -20,7 +20,7 @@ from paper_1809_00832_amd import binding, synth  # noqa: E402
 
 
 class Attend(torch.autograd.Function):
-    """tl_attend with its gradients for torch's autograd."""
+    """tl_attend with its gradients for torch's autograd (first ones only: a second derivative raises)."""
 
     @staticmethod
     def forward(ctx, q, k, v, q_off, kv_off, kv_mask):
@@ -29,6 +29,7 @@ class Attend(torch.autograd.Function):
         return o
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, d_o):
         q, k, v, o, lse, q_off, kv_off, kv_mask = ctx.saved_tensors
         g = binding.tl_attend_backward(q, k, v, o, lse, d_o.contiguous(), q_off, kv_off, kv_mask)

@@ -91,3 +91,15 @@ def test_training_lowers_the_loss(example, trees):
     assert all(b < a for a, b in zip(losses, losses[1:]))
     net.forward()
     assert not torch.equal(before, batch["h"])                 # the encoder has been trained too
+
+
+def test_gradients_of_gradients_are_refused(example, trees):
+    """Attend's backward pass is not made of differentiable steps: a second derivative raises instead of leaving out what went through it."""
+    _, _, batch = trees
+    n = batch["B"]
+    off = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    q, k, v = (torch.randn(rows, 2, 16, device="cuda").requires_grad_() for rows in (n, batch["h"].shape[0], batch["h"].shape[0]))
+    o = example.Attend.apply(q, k, v, off, batch["tree_off"], None)
+    d_q, = torch.autograd.grad(o.square().sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (d_q.square().sum() + q.sum()).backward()
