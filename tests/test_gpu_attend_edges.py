@@ -3,7 +3,7 @@
 stored() has what tl_attend_backward returns for the o and lse that it is given, in 64 bits, so that the rounding of o is an input and no error.
 With u = 2^-24 and h = half a step of the operands' type:
   probability 2^x of a sum of D products, two roundings of the scale, lse in base 2, the fp16 forms' shift by 2^14 and the difference:
-              relative |ds| + (4 |s| + 4 |lse| + 24) u  with  |ds| <= (D + 4) u * scale * sum |q||k|; 0 below 2^-126
+              relative |ds| + (4 |s| + 4 |lse| + 24) u  with  |ds| <= (D + 4) u * scale * sum |q||k|; 0 below 2^-126, as are operands
   as operand  16 bits in one term: h; in two terms: h^2, of what the first left; fp16, shifted by 2^14, below its normal range 2^-25 2^-14
   score gradient  P (dP - delta): that of P, (D + 4) u of both sums' absolute values; two terms: h^2.  fp16: a row of d_o is brought to a length of
               2^9 .. 2^10, and where a score gradient passes 2^15 it is brought to that: 2^-25 2^-9 of the larger one below the normal range
@@ -85,14 +85,14 @@ def stored(s, o, lse, p_terms):
             gap = dO @ V.t() - (dO * O).sum(1, keepdim=True)
             dS = P * gap
             e_dS = rel * dS.abs() + P * (1 + rel) * ((D + 4) * U * (dO.abs() @ V.abs().t() + (dO.abs() * O.abs()).sum(1, keepdim=True)) + 2 * U * gap.abs())
-            e_dS = e_dS + h * h * (dS.abs() + e_dS) + 2.0 ** -126 * gap.abs()
+            e_dS = e_dS + h * h * (dS.abs() + e_dS) + 2.0 ** -126 * gap.abs() + 2.0 ** -125
             low_q = low_k = 0.0
             if f16:
                 size, top = dO.norm(dim=1, keepdim=True), dS.abs()
                 low_q = 2.0 ** -34 * torch.maximum(size, top.amax(1, keepdim=True))
                 low_k = 2.0 ** -34 * torch.maximum(size.amax(), top.amax(0, keepdim=True))
             m = nq * G
-            e_P = (rel + h ** p_terms) * P + (2.0 ** -39 if f16 else 2.0 ** -126)
+            e_P = (rel + h ** p_terms) * P + (2.0 ** -39 if f16 else 2.0 ** -125)
             dq, dk, dv = scale * dS @ K, scale * dS.t() @ Q, P.t() @ dO
             e_q = scale * ((e_dS + low_q) @ K.abs() + (2 * nk + 8) * U * (dS.abs() @ K.abs()))
             out["d_q"][rows, j], err["d_q"][rows, j] = dq, e_q
@@ -144,3 +144,49 @@ def test_fp16_value_gradients_of_small_probabilities(lq, lk, terms, size):
     for n in ref:
         bad = fits[n] & ~((got[n].double() - ref[n]).abs() <= err[n])
         assert fits[n].float().mean() > 0.99 and not bad.any(), (n, int(bad.sum()))
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("heads,kv_heads,d,lq,lk,p_terms", [(4, 2, 64, [33, 60, 5], [54, 99, 9], 2), (2, 1, 128, [700, 40], [900, 600], 1),
+                                                            (1, 1, 256, [100, 9], [300, 40], 2), (6, 3, 30, [200, 90], [100, 90], 2)])
+def test_gradients_from_what_was_stored(heads, kv_heads, d, lq, lk, p_terms, dtype):
+    """Score gradients in one term of 16 bits, or such probabilities where two are promised, would pass these bounds by far."""
+    s = tensors(35, TYPES[dtype], lq, lk, heads, kv_heads, d)
+    o, lse, got = gradients(s)
+    ref, err = stored(s, o, lse, 2 if dtype == "f16" else p_terms)
+    close(got, ref, err)
+
+
+@pytest.mark.parametrize("spread", [6.0, 20.0])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradients_where_scores_are_large(spread, dtype):
+    """Scores of hundreds and thousands: probabilities taken again from lse, whose rounding grows with its size."""
+    s = tensors(36, TYPES[dtype], [60, 90, 1], [350, 500, 33], 2, 2, 128, spread=spread)
+    o, lse, got = gradients(s)
+    ref, err = stored(s, o, lse, 1)
+    close(got, ref, err)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("heads,kv_heads,d,lq,lk", [(4, 2, 64, [33, 60], [54, 200]), (8, 2, 128, [1, 1, 1], [700, 40, 5000]), (3, 3, 30, [1, 2], [9, 90]),
+                                                    (2, 1, 256, [100, 9], [300, 40])])
+def test_outputs_of_few_rows_keep_both_terms(heads, kv_heads, d, lq, lk, dtype):
+    """Up to 128 packed rows a tree: probabilities in two terms, so that an output is off by little more than its own rounding."""
+    s = tensors(37, TYPES[dtype], lq, lk, heads, kv_heads, d)
+    o, _ = binding.tl_attend(s["q"], s["k"], s["v"], with_lse=True, **where(s))
+    h = half_step(TYPES[dtype]) if dtype != "f32" else 0.0
+    a = b = 0
+    for nq, nk in zip(lq, lk):
+        rows, cols = slice(a, a + nq), slice(b, b + nk)
+        a, b = a + nq, b + nk
+        for j in range(heads):
+            Q, K, V = s["q"][rows, j].double(), s["k"][cols, j * kv_heads // heads].double(), s["v"][cols, j * kv_heads // heads].double()
+            S = Q @ K.t() * s["scale"]
+            P = torch.softmax(S, 1)
+            O = P @ V
+            ds = (d + 4) * U * s["scale"] * (Q.abs() @ K.abs().t()).amax(1, keepdim=True)
+            rel = 2 * ds + (8 * S.abs().amax(1, keepdim=True) + nk + 24) * U
+            e = (rel + h * h + (2 * nk + 8) * U) * (P @ V.abs()) + (2.0 ** -39 if dtype == "f16" else 2.0 ** -125) * V.abs().sum(0)
+            e = e + half_step(TYPES[dtype]) * (O.abs() + e) + (2.0 ** -25 if dtype == "f16" else 1e-36)
+            bad = ~((o[rows, j].double() - O).abs() <= e)
+            assert not bad.any(), (int(bad.sum()), float(((o[rows, j].double() - O).abs() / e).max()))
