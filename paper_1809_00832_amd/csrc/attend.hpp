@@ -1246,13 +1246,14 @@ template <typename T, int DP, int WN, bool VEC> __device__ __forceinline__ void 
                     stage_16(base + BQ * R::BYTES + i * ATT_THREADS * 16, gp, g_offset[i]);
                 }
         } else {
-            // (a row that is not there is the last one's query without a gradient: the score of a row of zeros would be a NaN beside an infinite key)
             auto row = [&](const AttTensor &x, int r) {
                 int i, hd;
-                rows.at(min(r, left - 1), &i, &hd);
+                rows.at(r, &i, &hd);
                 return (const T *)row_of<T>(x, i, hk * a.G + hd);
             };
-            qs.request(b, a.D, [&](int r) { return row(a.q, r); });
+            // (a row that is not there is the tree's first query without a gradient: the score of a row of zeros would be a NaN beside an infinite key)
+            const T *some = row_of<T>(a.q, q_lo, hk * a.G);
+            qs.request(b, a.D, [&](int r) { return r < left ? row(a.q, r) : some; });
             gs.request(b + BQ * R::BYTES, a.D, [&](int r) { return r < left ? row(a.d_o, r) : (const T *)nullptr; });
         }
         if (wave < 2) {                         // (64 places; those beyond BQ are not read)
@@ -1332,10 +1333,7 @@ template <typename T, int DP, int WN, bool VEC> __device__ __forceinline__ void 
     }
     const float k_scale = a.scale / (size * ATT_LIFTED<T>);
 #pragma unroll
-    for (int t = 0; t < DT; ++t) {
-        dk[t] *= k_scale;
-        dv[t] *= 1.f / ATT_LIFTED<T>;
-    }
+    for (int t = 0; t < DT; ++t) dk[t] *= k_scale;
     if constexpr (C::WQ == 2) {
         float *join = reinterpret_cast<float *>(att_lds) + (wn * 32 + col) * 2 * (DP + 4);
         __syncthreads();
@@ -1369,7 +1367,8 @@ template <typename T, int DP, int WN, bool VEC> __device__ __forceinline__ void 
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
             const int d = 32 * (DT * wd + t) + 2 * r + 4 * half;
-            const f32x4 x = {dk[t][r], dk[t][r + 1], dk[t][r + 2], dk[t][r + 3]}, y = {dv[t][r], dv[t][r + 1], dv[t][r + 2], dv[t][r + 3]};
+            const f32x4 x = {dk[t][r], dk[t][r + 1], dk[t][r + 2], dk[t][r + 3]};
+            const f32x4 y = f32x4{dv[t][r], dv[t][r + 1], dv[t][r + 2], dv[t][r + 3]} * (1.f / ATT_LIFTED<T>);
             if (a.kv_splits > 1) {
                 store4<float>(pk, d, a.D, (a.D & 3) == 0, x[0], x[1], x[2], x[3]);
                 store4<float>(pv, d, a.D, (a.D & 3) == 0, y[0], y[1], y[2], y[3]);
