@@ -488,7 +488,9 @@ typedef struct {
     int dtype;               /* enum tl_dtype: of q, k, v, o and their gradients.  Sums, maxima and lse are fp32; with TL_DT_F32 so are all
                                 operands, with the 16-bit types probabilities and score gradients are operands of the type in their
                                 second products: score gradients, and probabilities where rows are few, with what
-                                the rounding left as a second operand, probabilities of many rows rounded once.          */
+                                the rounding left as a second operand, probabilities of many rows rounded once.
+                                Gradients take d_o . o from the o that was stored, and probabilities from lse: relative
+                                errors of these of some 2^-22 |lse|.                                                     */
     int n_trees, n_q, n_kv;  /* >= 0; n_q and n_kv below 2^31 - 2^16                                                       */
     int n_heads, n_kv_heads; /* >= 1, n_heads a multiple of n_kv_heads, n_heads <= 4096                                    */
     int head_dim;            /* 1 .. 256                                                                                   */

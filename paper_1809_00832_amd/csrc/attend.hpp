@@ -559,13 +559,15 @@ template <int BN, int THREADS> struct Nodes {
 // One pass over a tree's nodes: scores of a stage, their maximum and sum joined with those so far (what is summed is scaled when the maximum moves),
 // probabilities, their product with the values.  Bounds and measurements (us of the kernel): few rows, long trees: memory (4 documents of 40 000
 // to 65 000 nodes, one token, bf16, 8 heads of 128: 177, 4.9 TB/s); many rows: LDS reads, exponentials and products of two waves per SIMD one after
-// the other (8 documents, 768 tokens x 16 heads, bf16 x 128: 232, 770 TFLOP/s); short trees: the chain of reads in front of the first product
-// (256 trees of 54 nodes: one token 7.5, 33 words of bf16 x 64 20).
+// the other (8 documents, 768 tokens x 16 heads, bf16 x 128: 234 to 247 from machine to machine, 720 to 760 TFLOP/s); short trees: one chain of reads and products, and tiles that
+// their rows and nodes fill to 40 % (256 trees of 54 nodes: one token 7.5, 33 words of bf16 x 64 20).
 template <typename T, int DP, int WM_> struct AttFwd {
     static constexpr int THREADS = ATT_THREADS;
     static constexpr int WM = WM_, WK = ATT_WAVES / WM;
     static constexpr int NT = WM == 4 && DP * (int)sizeof(T) <= 256 ? 2 : 1;
-    static constexpr int TERMS = WM == 4 ? 1 : 2;                   // of a probability: the second one costs time only where there are many rows
+    // Of a probability: the second one costs time only where there are many rows.  One term: o is off by 0.0023 of its size in bf16 where its own
+    // rounding is 0.0017.
+    static constexpr int TERMS = WM == 4 ? 1 : 2;
     static constexpr int BM = 32 * WM;
     static constexpr int BN = 32 * WK * NT;
     static constexpr int STAGE = 2 * BN * Rows<T, DP>::BYTES;
@@ -889,9 +891,10 @@ __device__ inline float lse_log2(float lse) { return lse == -INFINITY ? INFINITY
 extern "C" __device__ float mul_zero_wins(float, float) __asm("llvm.amdgcn.fmul.legacy");
 __device__ inline float score_gradient(float p, float gap) { return mul_zero_wins(p, gap); }
 
-// What both kernels of the backward pass need first.  Workgroups below `row_blocks`: delta[i] = d_o[i] . o[i] and the logarithms in base 2, 16 lanes
-// per query and head (fp16: also the power of two that brings the row of d_o to a length of 2^10, see fit_fp16).  With a mask, one further workgroup per tree: the tree's nodes that may be read, one after the other in `list` from
-// kv_off[tree] on, and their number in live[tree]; masked nodes then cost the others nothing.
+// What both kernels of the backward pass need first.  Workgroups below `row_blocks`: delta[i] = d_o[i] . o[i] (of the o that was stored, rounded to the type: an
+// output of fp32 beside it would be twice its bytes to write and to read again) and the logarithms in base 2, 16 lanes per query and head (fp16: also the
+// power of two that brings the row of d_o to a length of 2^10, see fit_fp16).  With a mask, one further workgroup per tree: the tree's nodes that may be
+// read, one after the other in `list` from kv_off[tree] on, and their number in live[tree]; masked nodes then cost the others nothing.
 template <typename T> __global__ __launch_bounds__(ATT_THREADS) void k_attend_prepare(const AttArgs a, int row_blocks)
 {
     if ((int)blockIdx.x < row_blocks) {
@@ -962,8 +965,8 @@ template <typename T> __global__ __launch_bounds__(ATT_THREADS) void k_attend_pr
 // Both gradients take the scores and probabilities again from lse: five products a pair of tiles would do, seven are done, so that neither side needs
 // the other's sums or atomics.  Scores, probabilities and d_o . v stay in a lane's registers and are operands of the second products as they stand.
 // The launch of both (us): 8 documents of 1 700 nodes, 70 % of them read, 384 tokens x 16 heads, bf16 x 128: 243 (apart, and with two
-// terms of the probabilities too: 314); 256 trees of 54 nodes, 33 words, fp32 x 64, 8 heads: 165 (matrix unit 31 % busy, 40 % of it on places that short trees leave
-// empty; the rest is reads, stage by stage, at two waves per SIMD); 25 trees, x 30: 14.
+// terms of the probabilities too: 314); 256 trees of 54 nodes, 33 words, fp32 x 64, 8 heads: 165 (matrix unit 31 % busy, 60 % of it on places that short trees leave
+// empty; most of the rest is waiting, at two waves per SIMD, for what is not known: a shorter search for the tree changed nothing); 25 trees, x 30: 14.
 //
 // dQ: like the forward, rows (queries) on the lanes' columns.  Four waves: WM side by side along the rows, WK along the nodes (their sums are joined
 // at the end) and, for wide heads, WD along the columns of dQ, where every wave of a row tile works out the tile's scores itself.

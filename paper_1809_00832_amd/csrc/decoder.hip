@@ -70,7 +70,8 @@ int splits(long long blocks, long long stages)
 // 256 trees of 54 nodes, 33 rows each: bf16 x 64 read 23.9 / 20.0, fp32 x 64 58 / 50.
 bool one_stage(long long rows, long long trees, int stage) { return 2 * rows <= 3ll * stage * trees; }
 
-// Which form a forward takes, by the packed rows of a tree on average.  Measured (us, 4 waves along the rows / 2 / 1): 256 trees of 9 to 99 nodes,
+// Which form a forward takes, by the packed rows of a tree on average: the host does not know the lengths, and a batch with one tree much longer than the others
+// waits for it (256 trees of 54 nodes, bf16 x 64, one token: 9 us; one of them of 20 000 nodes: 184).  Measured (us, 4 waves along the rows / 2 / 1): 256 trees of 9 to 99 nodes,
 // 33 rows each, bf16 x 64: - / 24 / 38; fp32 x 64: - / 57 / 70; 64 trees of 2047 nodes half of them masked, 72 rows, fp32 x 64: 158 / 98 /
 // 117; 8 trees of 3500 nodes, 3000 rows, bf16 x 128: 250 / 310 / -.  A single token's few rows want every wave on nodes of its own.
 // Where row tiles do not fill the chip twice, a tree's nodes are divided among workgroups too, as long as a part keeps two stages.

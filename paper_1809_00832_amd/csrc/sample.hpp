@@ -6,9 +6,10 @@
 //
 // Which word that is hangs on sums over the whole row, so weights are taken in 64 bits and summed as whole multiples of 2^-shift (62
 // bits for the sum of all): integers add up to the same total in any order, so the result does not depend on which thread adds
-// first.  No row is sorted.  One workgroup walks a row up to four times: the largest and smallest value; a histogram over 2048 equal
+// first.  No row is sorted.  One workgroup walks a row two to four times: the largest and smallest value; a histogram over 2048 equal
 // steps of the value; the words of the step in which a filter ends, which are sorted in LDS; the kept weights per piece
-// of the row, of which one wave then walks the piece that holds the draw.  Equal steps of the value spread a row's words evenly enough that the
+// of the row, of which one wave then walks the piece that holds the draw.  (Without top-k and top-p the second and third are left out; both with more words
+// than the list holds: six walks; 16-bit rows with a NaN: one more; each filter that goes by digits, below: two to four more.)  Equal steps of the value spread a row's words evenly enough that the
 // additions of a wave seldom meet in one counter, which steps of the bit pattern do not (few exponents).  top-k counts words,
 // which needs no weights, and where it leaves no more words than the list holds, top-p is answered from the list; else a histogram
 // of weights follows.  A step that holds more words than the list (long runs of equal values) is resolved digit by digit of the bit pattern.
@@ -267,7 +268,8 @@ struct SmpSteps {
 
 // The histogram of weights of a long row of bf16: a row's words share few values, so words are counted per value and a weight is worked out once for each
 // value that occurs.  Counted are magnitudes of 2^-10 to 2^6; the few words outside that have a weight at all are added by themselves.  The sums are whole
-// numbers, so they are the same as word by word.  (A word costs some 9 instructions instead of 30: 512 rows of 131 072, top-p alone, 168 -> 142 us.)
+// numbers, so they are the same as word by word.  (A word costs some 9 instructions instead of 30: 512 rows of 131 072, top-p alone, 168 -> 142 us.  The same
+// rows 60 or 100 higher, where bf16 has few values: 530 and 960, word by word 555 and 929, most of it additions that meet in one counter.)
 static __device__ void smp_histogram_of_values(const SmpRow<bf16_t> &row, const SmpWeight &weight, const SmpSteps &step)
 {
     constexpr int W = SmpRow<bf16_t>::W;
@@ -789,7 +791,7 @@ template <typename T, bool INDEX> __device__ __noinline__ void smp_extremes(SmpR
     __syncthreads();
 }
 
-// One workgroup a row, two rows a compute unit: registers are held to 64 for that.  Bound by the instructions of the weights (vector unit 81 % busy), not by
+// One workgroup a row, two rows a compute unit: registers are held to 64 for that.  Bound by the instructions of the weights (vector unit 73 % busy in 512 rows of bf16), not by
 // memory, which the second and later walks find in the L2.  us: a row of 20 000 words (fp32, top-p) 26, of which 9 for the draw's walk and 7 for
 // the histogram; 256 rows of 50 000 (fp32, all filters) 46; 512 rows of 131 072 (bf16, top-p) 141, 0.95 TB/s.
 template <typename T> __global__ __launch_bounds__(SMP_THREADS, 8) void k_sample(const SampleArgs a)
