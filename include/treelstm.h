@@ -502,8 +502,8 @@ typedef struct {
     tl_rows q, k, v;         /* [n_q, n_heads], [n_kv, n_kv_heads] twice                                         DEVICE     */
 } tl_attention;
 
-/* Bytes of DEVICE memory that tl_attend (backward == 0) or tl_attend_backward needs as workspace; depends on the counts
- * alone, 0 where none is needed. */
+/* Bytes of DEVICE memory that tl_attend (backward == 0) or tl_attend_backward needs as workspace; depends on the counts, the type,
+ * whether there is a mask, and the current device's compute units; 0 where none is needed. */
 int tl_attend_workspace(const tl_attention *a, int backward, int64_t *bytes);
 
 /*
