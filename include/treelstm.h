@@ -149,7 +149,7 @@ enum tl_error {
     TL_ESTALL = -5,    /* TL_SCHED_READY made no progress within its spin budget (nodes that are
                           unreachable from any leaf, e.g. a cycle); outputs are incomplete.  The
                           level schedulers report such a batch as TL_ESTRUCT.                   */
-    TL_ELIMIT = -6     /* tl_forward_noalloc: the batch does not fit the fixed workspace; tl_attend*: theirs is too small */
+    TL_ELIMIT = -6     /* tl_forward_noalloc: the batch does not fit the fixed workspace; tl_attend*, tl_recur*, tl_score: theirs is too small */
 };
 
 typedef struct {
@@ -544,6 +544,107 @@ int tl_attend_backward(const tl_attention *a, const tl_rows *o, const float *lse
 int tl_sample(int dtype, int n_rows, int vocab, const void *logits, int64_t row, const float *u, const float *temperature,
               const int32_t *top_k, const float *top_p, const float *min_p, int32_t *token, float *logprob, int32_t *kept,
               void *hip_stream);
+
+/*
+ * ---- Between a decoder's attention and its update ---------------------------------------------------
+ *
+ * What carries a state from word to word, regularises a training step, and says how probable words are.  As above: no context; the
+ * current HIP device and hip_stream; nothing is allocated, nothing waits, and every call may be captured in a HIP graph.  Outputs must not overlap
+ * inputs unless it is said below that they may.
+ */
+
+/*
+ * A gated linear recurrence along sentences.  Rows are all sentences' words one after the other, cut by off; per channel
+ *     h_t = f_t h_(t-1) + i_t x_t          h before a sentence's first word: its row of h0
+ *     TL_GATE_SIGMOID  f = 1 / (1 + exp(-g)),  i = 1 - f        TL_GATE_GIVEN  f = g,  i = 1
+ * States and sums are fp32 whatever the type; h is rounded once, when it is stored.  Words that are far apart are joined as runs, so the last
+ * bits differ from those of a loop over words, but infinities and NaN appear where the formula has them and reach only later words of
+ * their channel and sentence.  Results repeat bit for bit.
+ */
+enum tl_gate { TL_GATE_SIGMOID = 0, TL_GATE_GIVEN = 1 };
+
+typedef struct {
+    int dtype;               /* enum tl_dtype: of g, x, h and their gradients                                             */
+    int gate;                /* enum tl_gate                                                                              */
+    int n_trees, n_rows;     /* sentences and rows, >= 0; n_rows below 2^31 - 2^16                                        */
+    int channels;            /* 1 .. 2^20                                                                                 */
+    const int32_t *off;      /* [n_trees+1], from 0 to at most n_rows, ascending (equal ones: no words)       DEVICE
+                                Offsets outside these bounds: results are unspecified, nothing outside the arrays is accessed.  */
+    const void *g, *x;       /* rows of `channels` values, `g_row` and `x_row` elements apart (>= 0)         DEVICE, read-only */
+    int64_t g_row, x_row;
+} tl_recurrence;
+
+/* Bytes of DEVICE memory that tl_recur (backward == 0) or tl_recur_backward needs as workspace; depends on the counts, the type, and the current
+ * device's compute units; 0 unless sentences are few and long, which are then divided among workgroups. */
+int tl_recur_workspace(const tl_recurrence *r, int backward, int64_t *bytes);
+
+/*
+ *   h0      [n_trees x channels] fp32, NULL: zero                                        DEVICE, read-only
+ *   h       rows of `channels` values, h_row elements apart, out; rows behind the last sentence are left as they were   DEVICE
+ *   h_last  [n_trees x channels] fp32 out, may be NULL: the state behind each sentence's last word, its row of h0 where there is none.  May be
+ *           h0 itself: with one word per sentence that is a decoder's step                DEVICE
+ *   tape    [(n_rows / 64 + n_trees) x channels] fp32 out, may be NULL: what tl_recur_backward needs   DEVICE
+ *   workspace  as for tl_attend: 16-byte aligned, free once the stream has passed the call, TL_ELIMIT if it is smaller than it has to be
+ */
+int tl_recur(const tl_recurrence *r, const float *h0, void *h, int64_t h_row, float *h_last, float *tape, void *workspace, int64_t workspace_bytes,
+             void *hip_stream);
+
+/*
+ * Gradients of tl_recur, from those of h and h_last: with l_t = d_h_t + f_(t+1) l_(t+1), d_last behind the last word,
+ *     d_x_t = i_t l_t     d_g_t = l_t (h_(t-1) - x_t) f_t i_t  (TL_GATE_GIVEN: l_t h_(t-1))     d_h0 = f_1 l_1
+ * h_(t-1) is taken again from the tape in fp32, not from the rounded h.
+ *   tape                   what tl_recur wrote for the same arguments                   DEVICE, read-only
+ *   d_h                    rows like h, NULL: zero;  d_last [n_trees x channels] fp32, NULL: zero    DEVICE, read-only
+ *   d_g, d_x               rows like h, out; rows behind the last sentence are zero     DEVICE
+ *   d_h0                   [n_trees x channels] fp32 out, may be NULL                   DEVICE
+ * Where rows of g or x are one row repeated (g_row or x_row 0) the gradients still have a row for every word: the caller sums them.
+ */
+int tl_recur_backward(const tl_recurrence *r, const float *tape, const void *d_h, int64_t d_h_row, const float *d_last, void *d_g, int64_t d_g_row,
+                      void *d_x, int64_t d_x_row, float *d_h0, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * How probable words are.  With x a row of logits (a NaN counts as -infinity) and p = softmax(x):
+ *     logprob  log p_w of the row's given word w; 0 where w is outside [0, vocab): such a row has no word
+ *     entropy  - sum_j p_j log p_j
+ *     top      the n_top words of largest x, equal ones by index, and their log p; behind the last word above -infinity: -1 and -infinity
+ * Words at -infinity have log p = -infinity.  A row without a value above -infinity: every log p -infinity, entropy 0.  +infinity: the words that have it
+ * share the mass.  Weights are exp(x - max x), summed in fp32 by a fixed scheme: results repeat bit for bit.
+ *   logits [n_rows x vocab] of dtype, `row` elements (>= 0) from one row to the next; 1 <= vocab <= 2^30     DEVICE, read-only
+ *   word   [n_rows] int32, may be NULL if logprob is                                       DEVICE, read-only
+ *   n_top  0 .. 64
+ *   logprob [n_rows] fp32 out, may be NULL                                                 DEVICE
+ *   stats  [3 x n_rows] fp32 out, may be NULL: each row's largest logit, then each row's sum of exp(x - it), then the entropies   DEVICE
+ *   top_word [n_rows x n_top] int32 out, top_logprob [n_rows x n_top] fp32 out; not written if n_top = 0    DEVICE
+ *   workspace  of at least the bytes that tl_score_workspace names, as for tl_attend; 0 bytes unless rows are few and long
+ */
+int tl_score_workspace(int dtype, int n_rows, int vocab, int n_top, int64_t *bytes);
+int tl_score(int dtype, int n_rows, int vocab, const void *logits, int64_t row, const int32_t *word, int n_top, float *logprob, float *stats,
+             int32_t *top_word, float *top_logprob, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * Gradient of a loss that depends on log probabilities (cross entropy: d_logprob = -1 / n_rows in every row) and entropies:
+ *     d_logits_j = d_logprob ([j = w] - p_j) - d_entropy p_j (log p_j + entropy)
+ * Rows without a word have no part of the first term, rows without a value above -infinity have a gradient of zero.  A row whose two factors are zero is
+ * not read.
+ *   logits, row, word  as in tl_score;  stats: what it wrote                               DEVICE, read-only
+ *   d_logprob, d_entropy [n_rows] fp32, NULL: zero                                          DEVICE, read-only
+ *   d_logits rows like logits, d_row >= vocab elements apart, out; may be logits itself     DEVICE
+ */
+int tl_score_backward(int dtype, int n_rows, int vocab, const void *logits, int64_t row, const int32_t *word, const float *stats, const float *d_logprob,
+                      const float *d_entropy, void *d_logits, int64_t d_row, void *hip_stream);
+
+/*
+ * Dropout with a mask that is made again wherever it is needed and never stored: y = residual + kept(x) 65536 / (65536 - t), t = p times 65536, rounded to
+ * even.  numbers[0] is a seed, numbers[1] a step: the value in row r, column c is dropped if a piece of 16 bits of
+ * Philox4x32-10 (Salmon, Moraes, Dror, Shaw 2011) is below t: key (seed, seed >> 32), counter (c / 8, r, step, step >> 32), of its four words the
+ * piece c % 8, low halves first.  Its gradient is the same call on dL/dy without a residual.  A seed in device memory can be
+ * changed between replays of a captured graph.  Dropped values are zero whatever they were; t = 65536 drops all.
+ *   x, residual, y   [n_rows x n_cols] of dtype, `..._row` elements apart; residual may be NULL; y may be x or residual itself    DEVICE
+ *   p                0 .. 1
+ *   numbers [2]      uint64                                                                 DEVICE, read-only
+ */
+int tl_dropout(int dtype, int n_rows, int n_cols, const void *x, int64_t x_row, const void *residual, int64_t residual_row, void *y, int64_t y_row,
+               float p, const uint64_t *numbers, void *hip_stream);
 
 const char *tl_strerror(int code);
 

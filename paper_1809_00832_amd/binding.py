@@ -21,12 +21,14 @@ TL_OK, TL_EINVAL, TL_ENOMEM, TL_EHIP, TL_ESTRUCT, TL_ESTALL, TL_ELIMIT = 0, -1, 
 TL_NOALLOC_MAX_NODES = 16384
 TL_N_STAGES, TL_PROFILE_RING = 5, 128
 TL_DT_F32, TL_DT_BF16, TL_DT_F16 = 0, 1, 2
+TL_GATE_SIGMOID, TL_GATE_GIVEN = 0, 1
 SCHEDULERS = {"ready": TL_SCHED_READY, "level_device": TL_SCHED_LEVEL_DEVICE, "level_host": TL_SCHED_LEVEL_HOST,
               "ready_priority": TL_SCHED_READY_PRIORITY, "dataflow": TL_SCHED_DATAFLOW}
 
 EXPORTS = ("tl_create", "tl_forward", "tl_forward_noalloc", "tl_status", "tl_set_profiling", "tl_stage_ms", "tl_last_stats", "tl_backward",
            "tl_set_keep_gates", "tl_set_async_backward", "tl_sgd_update", "tl_get_params", "tl_classify", "tl_classify_backward", "tl_td_create", "tl_td_generate", "tl_td_status", "tl_td_destroy", "tl_strerror", "tl_destroy",
-           "tl_attend", "tl_attend_backward", "tl_attend_workspace", "tl_sample")
+           "tl_attend", "tl_attend_backward", "tl_attend_workspace", "tl_sample",
+           "tl_recur", "tl_recur_backward", "tl_recur_workspace", "tl_score", "tl_score_backward", "tl_score_workspace", "tl_dropout")
 
 
 class tl_config(ctypes.Structure):
@@ -46,6 +48,11 @@ class tl_attention(ctypes.Structure):
                 ("n_heads", ctypes.c_int), ("n_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int), ("scale", ctypes.c_float),
                 ("q_off", ctypes.c_void_p), ("kv_off", ctypes.c_void_p), ("kv_mask", ctypes.c_void_p),
                 ("q", tl_rows), ("k", tl_rows), ("v", tl_rows)]
+
+
+class tl_recurrence(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("gate", ctypes.c_int), ("n_trees", ctypes.c_int), ("n_rows", ctypes.c_int), ("channels", ctypes.c_int),
+                ("off", ctypes.c_void_p), ("g", ctypes.c_void_p), ("x", ctypes.c_void_p), ("g_row", ctypes.c_int64), ("x_row", ctypes.c_int64)]
 
 
 _lib = None
@@ -107,6 +114,14 @@ def lib():
         L.tl_attend_backward.argtypes = [attn, rows, vp, rows, rows, rows, rows, vp, i64, vp]
         L.tl_sample.restype = ci
         L.tl_sample.argtypes = [ci, ci, ci, vp, i64] + [vp] * 9
+        f32 = ctypes.c_float
+        for name, args in (("tl_recur_workspace", [vp, ci, ctypes.POINTER(i64)]), ("tl_recur", [vp, vp, vp, i64, vp, vp, vp, i64, vp]),
+                           ("tl_recur_backward", [vp, vp, vp, i64, vp, vp, i64, vp, i64, vp, vp, i64, vp]),
+                           ("tl_score_workspace", [ci, ci, ci, ci, ctypes.POINTER(i64)]),
+                           ("tl_score", [ci, ci, ci, vp, i64, vp, ci, vp, vp, vp, vp, vp, i64, vp]),
+                           ("tl_score_backward", [ci, ci, ci, vp, i64, vp, vp, vp, vp, vp, i64, vp]),
+                           ("tl_dropout", [ci, ci, ci, vp, i64, vp, i64, vp, i64, f32, vp, vp])):
+            getattr(L, name).restype, getattr(L, name).argtypes = ci, args
         L.tl_destroy.restype = ci
         L.tl_destroy.argtypes = [vp]
         _lib = L
@@ -450,6 +465,177 @@ def tl_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, s
                            _ptr(top_p), _ptr(min_p), out["token"].data_ptr(), out["logprob"].data_ptr(), out["kept"].data_ptr(),
                            _raw_stream(index)), "tl_sample")
     return out
+
+
+_PACK_RECURRENCE = struct.Struct("5i4x3Q2q").pack
+assert struct.calcsize("5i4x3Q2q") == ctypes.sizeof(tl_recurrence)
+
+
+def _recurrence(g, x, off, gate, index) -> bytes:
+    import torch
+    n, channels = g.shape
+    assert index == x.get_device() == off.get_device(), "tensors of one device"
+    assert x.dtype == g.dtype and x.shape == g.shape
+    g_row, g_c = g.stride()
+    x_row, x_c = x.stride()
+    assert channels == 1 or g_c == x_c == 1, "channels must be contiguous"
+    assert off.dtype == torch.int32 and off.is_contiguous() and off.numel() >= 1
+    return _PACK_RECURRENCE(_dtype(g), gate, off.numel() - 1, n, channels, off.data_ptr(), g.data_ptr(), x.data_ptr(), g_row, x_row)
+
+
+def _recur_workspace(r, backward, device):
+    import torch
+    size = ctypes.c_int64()
+    _check(lib().tl_recur_workspace(r, backward, ctypes.byref(size)), "tl_recur_workspace")
+    n = size.value
+    return (torch.empty(n, dtype=torch.uint8, device=device), n) if n else (None, 0)
+
+
+def _states(t, index, shape):
+    import torch
+    assert t is None or (t.get_device() == index and t.dtype == torch.float32 and t.is_contiguous() and tuple(t.shape) == shape)
+    return _ptr(t)
+
+
+def _like(t, like, index):
+    """Rows of the type and shape of `like`: address and stride."""
+    assert t.get_device() == index and t.dtype == like.dtype and t.shape == like.shape and (t.shape[1] == 1 or t.stride(1) == 1)
+    return t.data_ptr(), t.stride(0)
+
+
+def tl_recur(g, x, off, h0=None, gate=TL_GATE_SIGMOID, h=None, h_last=None, with_last=False, with_tape=False, stream=None):
+    """h_t = f_t h_(t-1) + i_t x_t along the rows of every sentence.  g, x [n, channels]: CUDA tensors of one type (float32, bfloat16, float16)
+    with rows any stride apart; off [sentences + 1] int32, from 0 to at most n; h0 [sentences, channels] float32, None: zero.  Returns dict(h,
+    h_last with with_last or where one is given, tape with with_tape): h is new unless given (its rows behind the last sentence are left
+    as they were, of a new one undefined), h_last [sentences, channels] float32 may be h0 itself, the tape is for tl_recur_backward."""
+    import torch
+    index = g.get_device()
+    if stream is not None or torch._C._cuda_getDevice() != index:
+        with _elsewhere(index, stream):
+            return tl_recur(g, x, off, h0, gate, h, h_last, with_last, with_tape)
+    r = _recurrence(g, x, off, gate, index)
+    n, channels = g.shape
+    trees, device = off.numel() - 1, g.device
+    state = (trees, channels)
+    if h is None:
+        h = torch.empty((n, channels), dtype=g.dtype, device=device)
+    out = {"h": h}
+    if h_last is None and with_last:
+        h_last = torch.empty(state, dtype=torch.float32, device=device)
+    if h_last is not None:
+        out["h_last"] = h_last
+    if with_tape:
+        out["tape"] = torch.empty((n // 64 + trees, channels), dtype=torch.float32, device=device)
+    at, row = _like(h, g, index)
+    call, first, last, tape, st = lib().tl_recur, _states(h0, index, state), _states(h_last, index, state), _ptr(out.get("tape")), _raw_stream(index)
+    code = call(r, first, at, row, last, tape, None, 0, st)
+    if code == TL_ELIMIT:
+        ws, size = _recur_workspace(r, 0, device)
+        code = call(r, first, at, row, last, tape, _ptr(ws), size, st)
+    _check(code, "tl_recur")
+    return out
+
+
+def tl_recur_backward(g, x, off, tape, d_h=None, d_last=None, gate=TL_GATE_SIGMOID, stream=None):
+    """Gradients of tl_recur for its arguments and its tape: d_h [n, channels] of the type of g, d_last [sentences, channels] float32, None: zero.
+    Returns dict(d_g, d_x, d_h0) of new tensors; rows of d_g and d_x behind the last sentence are zero."""
+    import torch
+    index = g.get_device()
+    if stream is not None or torch._C._cuda_getDevice() != index:
+        with _elsewhere(index, stream):
+            return tl_recur_backward(g, x, off, tape, d_h, d_last, gate)
+    r = _recurrence(g, x, off, gate, index)
+    n, channels = g.shape
+    trees, device = off.numel() - 1, g.device
+    state = (trees, channels)
+    d_g, d_x = (torch.empty((n, channels), dtype=g.dtype, device=device) for _ in range(2))
+    d_h0 = torch.empty(state, dtype=torch.float32, device=device)
+    at, row = _like(d_h, g, index) if d_h is not None else (None, 0)
+    call, kept, last, st = lib().tl_recur_backward, _states(tape, index, (n // 64 + trees, channels)), _states(d_last, index, state), _raw_stream(index)
+    rest = (d_g.data_ptr(), channels, d_x.data_ptr(), channels, d_h0.data_ptr())
+    code = call(r, kept, at, row, last, *rest, None, 0, st)
+    if code == TL_ELIMIT:
+        ws, size = _recur_workspace(r, 1, device)
+        code = call(r, kept, at, row, last, *rest, _ptr(ws), size, st)
+    _check(code, "tl_recur_backward")
+    return {"d_g": d_g, "d_x": d_x, "d_h0": d_h0}
+
+
+def _words(t, n, index):
+    import torch
+    assert t is None or (t.get_device() == index and t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n)
+    return _ptr(t)
+
+
+def tl_score(logits, word=None, n_top=0, stream=None):
+    """Log probabilities of given words, entropies, and the n_top (up to 64) most probable words of rows of logits [n, vocab] (float32, bfloat16 or
+    float16; rows any stride apart); word [n] int32, outside [0, vocab) where a row has none.  Returns dict(entropy [n], stats [3, n] for
+    tl_score_backward, logprob [n] with words, top_word [n, n_top] int32 and top_logprob [n, n_top] with n_top > 0) of new tensors."""
+    import torch
+    index = logits.get_device()
+    if stream is not None or torch._C._cuda_getDevice() != index:
+        with _elsewhere(index, stream):
+            return tl_score(logits, word, n_top)
+    n, vocab = logits.shape
+    device, dtype = logits.device, _dtype(logits)
+    assert vocab == 1 or logits.stride(1) == 1
+    words = _words(word, n, index)
+    stats = torch.empty((3, n), dtype=torch.float32, device=device)
+    out = {"entropy": stats[2], "stats": stats}
+    if word is not None:
+        out["logprob"] = torch.empty(n, dtype=torch.float32, device=device)
+    if n_top > 0:
+        out["top_word"] = torch.empty((n, n_top), dtype=torch.int32, device=device)
+        out["top_logprob"] = torch.empty((n, n_top), dtype=torch.float32, device=device)
+    call, st = lib().tl_score, _raw_stream(index)
+    args = (dtype, n, vocab, logits.data_ptr(), logits.stride(0), words, n_top, _ptr(out.get("logprob")), stats.data_ptr(), _ptr(out.get("top_word")),
+            _ptr(out.get("top_logprob")))
+    code = call(*args, None, 0, st)
+    if code == TL_ELIMIT:
+        size = ctypes.c_int64()
+        _check(lib().tl_score_workspace(dtype, n, vocab, n_top, ctypes.byref(size)), "tl_score_workspace")
+        ws = torch.empty(size.value, dtype=torch.uint8, device=device)
+        code = call(*args, ws.data_ptr(), size.value, st)
+    _check(code, "tl_score")
+    return out
+
+
+def tl_score_backward(logits, word, stats, d_logprob=None, d_entropy=None, d_logits=None, stream=None):
+    """Gradient of the logits from those of tl_score's logprob and entropy ([n] float32, None: zero), its arguments and its stats.  d_logits may be
+    logits itself (new if None) and is returned."""
+    import torch
+    index = logits.get_device()
+    if stream is not None or torch._C._cuda_getDevice() != index:
+        with _elsewhere(index, stream):
+            return tl_score_backward(logits, word, stats, d_logprob, d_entropy, d_logits)
+    n, vocab = logits.shape
+    assert vocab == 1 or logits.stride(1) == 1
+    if d_logits is None:
+        d_logits = torch.empty((n, vocab), dtype=logits.dtype, device=logits.device)
+    at, row = _like(d_logits, logits, index)
+    _check(lib().tl_score_backward(_dtype(logits), n, vocab, logits.data_ptr(), logits.stride(0), _words(word, n, index), _states(stats, index, (3, n)),
+                                   _states(d_logprob, index, (n,)), _states(d_entropy, index, (n,)), at, row, _raw_stream(index)), "tl_score_backward")
+    return d_logits
+
+
+def tl_dropout(x, p, numbers, residual=None, y=None, stream=None):
+    """y = residual + dropout(x): x, residual, y [n, columns] CUDA tensors of one type (float32, bfloat16, float16) with rows any stride apart; p: share of
+    dropped values; numbers [2] int64: seed and step.  y may be x or residual (new if None) and is returned.  The gradient of x is the same
+    call on that of y without a residual."""
+    import torch
+    index = x.get_device()
+    if stream is not None or torch._C._cuda_getDevice() != index:
+        with _elsewhere(index, stream):
+            return tl_dropout(x, p, numbers, residual, y)
+    n, cols = x.shape
+    assert numbers.get_device() == index and numbers.dtype in (torch.int64, torch.uint64) and numbers.is_contiguous() and numbers.numel() == 2
+    if y is None:
+        y = torch.empty((n, cols), dtype=x.dtype, device=x.device)
+    x_at, x_row = _like(x, x, index)
+    r_at, r_row = _like(residual, x, index) if residual is not None else (None, 0)
+    y_at, y_row = _like(y, x, index)
+    _check(lib().tl_dropout(_dtype(x), n, cols, x_at, x_row, r_at, r_row, y_at, y_row, p, numbers.data_ptr(), _raw_stream(index)), "tl_dropout")
+    return y
 
 
 def tl_strerror(code: int) -> str:

@@ -6,7 +6,7 @@ import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SOURCES = ("treelstm", "attend_f32", "attend_bf16", "attend_f16", "decoder")
+SOURCES = ("treelstm", "attend_f32", "attend_bf16", "attend_f16", "decoder", "recur", "score", "dropout")
 SRC = os.path.join(HERE, "csrc", "treelstm.hip")
 LIB = os.path.join(HERE, "libtreelstm.so")
 

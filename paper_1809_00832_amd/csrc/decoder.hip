@@ -2,25 +2,12 @@
 #include <math.h>
 
 #include "attend_launch.hpp"
+#include "entry.hpp"
 #include "sample.hpp"
 
 using namespace tl;
 
 namespace {
-
-// Compute units of the current device (asked for once per device).
-int compute_units()
-{
-    static int known[64];
-    int dev = 0, n = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0) return 256;
-    if (dev < 64 && __atomic_load_n(&known[dev], __ATOMIC_RELAXED)) return __atomic_load_n(&known[dev], __ATOMIC_RELAXED);
-    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) return 256;
-    if (dev < 64) __atomic_store_n(&known[dev], n, __ATOMIC_RELAXED);
-    return n;
-}
-
-int element_size(int dtype) { return dtype == TL_DT_F32 ? 4 : 2; }
 
 bool check_rows(const tl_rows &t, int dtype, long long rows, long long heads, int D, bool out)
 {
@@ -126,8 +113,6 @@ bool back_plan(const tl_attention *a, AttBackPlan *out)
     p.sum_blocks_kv = (int)sum_kv;
     return true;
 }
-
-long long round16(long long x) { return (x + 15) & ~15ll; }
 
 long long workspace(const tl_attention *a, const AttPlan &p)
 {

@@ -1,0 +1,397 @@
+"""The recurrence along sentences and its gradients against loops over the words in 64 bits.
+
+Tolerances are first-order error bounds, taken with the reference in 64 bits.  u = 2^-24.  A sigmoid gate is met to (2 |g| + 8) u of itself: its exponent is
+a product with a rounded constant (2 |g| u), then an exponential and a reciprocal (2 u each), a sum and a product.  Every word multiplies and adds
+once, and pairs of runs do so again: 4 u more.  With d the sum of these, errors of a state grow like its magnitudes: M_t = |f_t| M_(t-1) + |i_t x_t|, E_t = |f_t| E_(t-1) + d_t M_t,
+and those of what goes back in the same way.  Storing h, d_g, d_x rounds once more, by half a step of the type.
+"""
+import numpy as np
+import pytest
+import torch
+
+from paper_1809_00832_amd import binding
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+SIGMOID, GIVEN = binding.TL_GATE_SIGMOID, binding.TL_GATE_GIVEN
+
+
+def offsets(lengths):
+    return torch.from_numpy(np.concatenate([[0], np.cumsum(lengths)]).astype(np.int32)).cuda()
+
+
+def host(t):
+    return t.double().cpu().numpy()
+
+
+def half_step(dtype, value):
+    """Half a step of the type at that value, subnormal steps included."""
+    tiny = {torch.float32: 2.0 ** -150, torch.bfloat16: 2.0 ** -134, torch.float16: 2.0 ** -25}[dtype]
+    return np.abs(value) * torch.finfo(dtype).eps / 2 + tiny
+
+
+def gates(g, gate):
+    if gate == GIVEN:
+        return g, np.ones_like(g), np.full_like(g, 4 * U)
+    f = 1 / (1 + np.exp(-g))
+    return f, 1 / (1 + np.exp(g)), (2 * np.abs(g) + 12) * U
+
+
+def reference(g, x, lengths, h0, gate, d_h=None, d_last=None):
+    """Every output in 64 bits, and a bound of its error before it is stored."""
+    f, i, d = gates(g, gate)
+    n, C = g.shape
+    out = {k: np.zeros((n, C)) for k in ("h", "d_g", "d_x")}
+    err = {k: np.zeros((n, C)) for k in out}
+    for k in ("h_last", "d_h0"):
+        out[k], err[k] = np.zeros((len(lengths), C)), np.zeros((len(lengths), C))
+    a = 0
+    for s, L in enumerate(lengths):
+        h = h0[s].copy() if h0 is not None else np.zeros(C)
+        m, e = np.abs(h), np.zeros(C)
+        before, before_err = np.zeros((L, C)), np.zeros((L, C))
+        for t in range(L):
+            r = a + t
+            before[t], before_err[t] = h, e
+            h = f[r] * h + i[r] * x[r]
+            m = np.abs(f[r]) * m + np.abs(i[r] * x[r])
+            e = np.abs(f[r]) * e + d[r] * m
+            out["h"][r], err["h"][r] = h, e
+        out["h_last"][s], err["h_last"][s] = h, e
+        if d_h is not None:
+            back = d_last[s].copy()
+            m, e = np.abs(back), np.zeros(C)
+            for t in range(L - 1, -1, -1):
+                r = a + t
+                lam, lam_m, lam_e = back + d_h[r], m + np.abs(d_h[r]), e + 2 * U * (m + np.abs(d_h[r]))
+                out["d_x"][r], err["d_x"][r] = i[r] * lam, i[r] * (lam_e + (d[r] + 2 * U) * lam_m)
+                rest, rest_m, rest_e = before[t], np.abs(before[t]), before_err[t]
+                by = np.ones(C)
+                if gate == SIGMOID:
+                    rest, rest_m, by = rest - x[r], rest_m + np.abs(x[r]), f[r] * i[r]
+                out["d_g"][r] = lam * rest * by
+                err["d_g"][r] = by * (lam_e * np.abs(rest) + lam_m * rest_e + (2 * d[r] + 8 * U) * lam_m * rest_m)
+                back, m, e = f[r] * lam, np.abs(f[r]) * lam_m, np.abs(f[r]) * lam_e + d[r] * np.abs(f[r]) * lam_m
+            out["d_h0"][s], err["d_h0"][s] = back, e
+        a += L
+    return out, err
+
+
+def check(got, want, err, dtype, n):
+    for k, v in got.items():
+        if k == "tape":
+            continue
+        g = host(v)
+        w, e = want[k], err[k]
+        if k in ("h", "d_g", "d_x"):
+            g = g[:n]
+            e = e + half_step(dtype, w) + half_step(dtype, e)
+        bad = np.abs(g - w) - (1.01 * e + 1e-37)
+        assert g.shape == w.shape and (bad <= 0).all(), (k, float(bad.max()), np.argwhere(bad > 0)[:4].tolist())
+
+
+def inputs(lengths, C, dtype, gate, seed=0, packed=False, first=True, behind=0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    n = sum(lengths) + behind
+    new = lambda *s, dt=dtype: torch.randn(s, generator=gen, device="cuda", dtype=dt)
+    if packed:
+        both = new(n, 2 * C + 3)
+        g, x = both[:, 1:1 + C], both[:, C + 2:2 * C + 2]
+    else:
+        g, x = new(n, C), new(n, C)
+    g.mul_(1.5).add_(1.0)
+    if gate == GIVEN:
+        g.tanh_()                               # of either sign
+    h0 = new(len(lengths), C, dt=torch.float32) if first else None
+    return g, x, h0, new(n, C), new(len(lengths), C, dt=torch.float32)
+
+
+RAGGED = [int(v) for v in np.random.default_rng(5).integers(0, 90, 40)]
+LENGTHS = {"one": [1], "none": [0], "short": [0, 1, 0, 2, 7, 8, 9, 0], "blocks": [63, 64, 65, 0, 1, 128, 129], "ragged": RAGGED, "tokens": [1] * 300,
+           "cut": [1500], "cut_ragged": [700, 0, 1, 650, 64, 0], "cut_far": [9000]}
+
+
+def run(lengths, C, dtype, gate, **kw):
+    g, x, h0, d_h, d_last = inputs(lengths, C, dtype, gate, **kw)
+    off = offsets(lengths)
+    out = binding.tl_recur(g, x, off, h0, gate, with_last=True, with_tape=True)
+    out.update(binding.tl_recur_backward(g, x, off, out["tape"], d_h, d_last, gate))
+    want, err = reference(host(g), host(x), lengths, None if h0 is None else host(h0), gate, host(d_h), host(d_last))
+    check(out, want, err, dtype, sum(lengths))
+    return out
+
+
+@pytest.mark.parametrize("lengths", LENGTHS)
+@pytest.mark.parametrize("gate", [SIGMOID, GIVEN], ids=["sigmoid", "given"])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_states_and_gradients(dtype, gate, lengths):
+    run(LENGTHS[lengths], 70 if dtype == "f32" else 150, TYPES[dtype], gate, packed=lengths in ("ragged", "cut"), first=lengths != "blocks")
+
+
+@pytest.mark.parametrize("C", [1, 2, 3, 4, 5, 63, 64, 65, 127, 128, 129, 255, 256, 257, 512, 515])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_channels(dtype, C):
+    run([3, 70, 0, 1, 130], C, TYPES[dtype], SIGMOID, packed=C % 2 == 1)
+    run([1] * 5, C, TYPES[dtype], GIVEN)
+
+
+def test_workspace_is_used_where_sentences_are_few_and_long():
+    for lengths, cut in ((LENGTHS["cut"], True), (LENGTHS["cut_ragged"], True), (LENGTHS["ragged"], False), (LENGTHS["tokens"], False)):
+        n = sum(lengths)
+        g = torch.zeros(n, 70, device="cuda")
+        r = binding._recurrence(g, g, offsets(lengths), SIGMOID, 0)
+        for back in (0, 1):
+            assert (binding._recur_workspace(r, back, g.device)[1] > 0) == cut
+
+
+@pytest.mark.parametrize("lengths", ["ragged", "cut"])
+def test_gradients_against_differences(lengths):
+    """Central differences of the loop in 64 bits: their own error is of third order, some 1e-8 for steps of 1e-4 on values near one."""
+    lengths, C = LENGTHS[lengths][:6], 6
+    g, x, h0, d_h, d_last = inputs(lengths, C, torch.float32, SIGMOID, seed=3)
+    off = offsets(lengths)
+    out = binding.tl_recur(g, x, off, h0, with_last=True, with_tape=True)
+    got = binding.tl_recur_backward(g, x, off, out["tape"], d_h, d_last)
+    G, X, S, D, E = host(g), host(x), host(h0), host(d_h), host(d_last)
+
+    def loss(G, X, S):
+        w, _ = reference(G, X, lengths, S, SIGMOID)
+        return (w["h"] * D).sum() + (w["h_last"] * E).sum()
+
+    rng = np.random.default_rng(0)
+    for name, k in (("d_g", 0), ("d_x", 1), ("d_h0", 2)):
+        for _ in range(4):
+            args = [G, X, S]
+            at = tuple(int(rng.integers(0, n)) for n in args[k].shape)
+            ends = []
+            for step in (1e-4, -1e-4):
+                moved = [v.copy() for v in args]
+                moved[k][at] += step
+                ends.append(loss(*moved))
+            assert abs(float(got[name][at]) - (ends[0] - ends[1]) / 2e-4) <= 1e-5 * max(1, abs(float(got[name][at]))), (name, at)
+
+
+def test_missing_gradients_are_zero():
+    for name in ("ragged", "cut"):
+        lengths = LENGTHS[name]
+        g, x, h0, d_h, d_last = inputs(lengths, 40, torch.float32, SIGMOID)
+        off = offsets(lengths)
+        tape = binding.tl_recur(g, x, off, h0, with_tape=True)["tape"]
+        call = lambda *a: binding.tl_recur_backward(g, x, off, tape, *a)
+        for got, want in ((call(None, d_last), call(torch.zeros_like(d_h), d_last)), (call(d_h), call(d_h, torch.zeros_like(d_last)))):
+            for k in want:
+                assert torch.equal(got[k], want[k])
+
+
+@pytest.mark.parametrize("lengths", [[5, 0, 70], [900, 300], [1] * 9])
+def test_rows_behind_the_last_sentence(lengths):
+    C, n = 37, sum(lengths)
+    g, x, h0, d_h, d_last = inputs(lengths, C, torch.float32, SIGMOID, behind=150)
+    g[n:], x[n:], d_h[n:] = float("nan"), float("nan"), float("nan")
+    off = offsets(lengths)
+    h = torch.full_like(g, 7.0)
+    out = binding.tl_recur(g, x, off, h0, h=h, with_last=True, with_tape=True)
+    assert (h[n:] == 7).all()
+    out.update(binding.tl_recur_backward(g, x, off, out["tape"], d_h, d_last))
+    for k in ("d_g", "d_x"):
+        assert (out[k][n:] == 0).all()
+    want, err = reference(host(g[:n]), host(x[:n]), lengths, host(h0), SIGMOID, host(d_h[:n]), host(d_last))
+    check(out, want, err, torch.float32, n)
+
+
+@pytest.mark.parametrize("lengths", ["tokens", "short", "ragged", "cut", "cut_ragged"])
+def test_states_updated_in_place(lengths):
+    g, x, h0, _, _ = inputs(LENGTHS[lengths], 131, torch.bfloat16, SIGMOID)
+    off = offsets(LENGTHS[lengths])
+    want = binding.tl_recur(g, x, off, h0, with_last=True)
+    state = h0.clone()
+    got = binding.tl_recur(g, x, off, state, h_last=state)
+    assert got["h_last"] is state and torch.equal(state, want["h_last"]) and torch.equal(got["h"], want["h"])
+
+
+def test_token_by_token_is_the_whole_sentence():
+    """A sentence read a word at a time through h_last in place: the same recurrence, joined in another order (bounds of both sides)."""
+    L, B, C = 40, 7, 96
+    g, x, h0, _, _ = inputs([L] * B, C, torch.float32, SIGMOID)
+    whole = binding.tl_recur(g, x, offsets([L] * B), h0, with_last=True)
+    _, err = reference(host(g), host(x), [L] * B, host(h0), SIGMOID)
+    one, state = offsets([1] * B), h0.clone()
+    G, X, H = (t.view(B, L, C) for t in (g, x, whole["h"]))
+    for t in range(L):
+        h = binding.tl_recur(G[:, t], X[:, t], one, state, h_last=state)["h"]
+        assert (np.abs(host(h) - host(H[:, t])) <= 2.02 * err["h"].reshape(B, L, C)[:, t]).all()
+        assert torch.equal(h, state)
+
+
+def loop32(g, x, h0, gate):
+    """One sentence word by word in fp32, on the host: where infinities and NaN have to be."""
+    g, x, h = g.float().cpu(), x.float().cpu(), h0.float().cpu().clone()
+    out = torch.empty_like(g)
+    for t in range(g.shape[0]):
+        f, i = (torch.sigmoid(g[t]), torch.sigmoid(-g[t])) if gate == SIGMOID else (g[t], torch.ones_like(g[t]))
+        h = f * h + i * x[t]
+        out[t] = h
+    return out
+
+
+@pytest.mark.parametrize("L", [1, 30, 64, 200, 1500])
+def test_infinities_and_nan_where_the_formula_has_them(L):
+    C = 12
+    g, x, h0, _, _ = inputs([L, L], C, torch.float32, SIGMOID, seed=L)
+    g, x, h0 = g.clone(), x.clone(), h0.clone()
+    t = L // 3
+    x[t, 1] = float("inf")
+    x[t, 2] = float("nan")
+    g[t, 3] = float("nan")
+    x[t, 4] = -float("inf")
+    x[min(t + 20, L - 1), 4] = float("inf")
+    h0[0, 5] = float("inf")
+    g[t, 6], x[t, 6] = 200.0, float("inf")             # a closed gate before an infinity: zero times it
+    g[t, 7] = float("inf")
+    g[t, 8] = -float("inf")
+    x[t, 9] = float("inf")
+    g[t + 1:, 9] = -60.0                               # products of gates that vanish, of states that are infinite
+    g[:, 10] = -100.0
+    off = offsets([L, L])
+    got = binding.tl_recur(g, x, off, h0, with_last=True)
+    for s in range(2):
+        want = loop32(g[s * L:(s + 1) * L], x[s * L:(s + 1) * L], h0[s], SIGMOID)
+        have = got["h"][s * L:(s + 1) * L].cpu()
+        assert torch.equal(torch.isnan(want), torch.isnan(have))
+        inf = torch.isinf(want)
+        assert torch.equal(inf, torch.isinf(have)) and torch.equal(want[inf], have[inf])
+        assert torch.equal(got["h_last"][s].cpu().nan_to_num(), have[-1].nan_to_num())
+        fine = torch.isfinite(want)
+        assert ((want - have)[fine].abs() <= 1e-4 * (1 + want[fine].abs())).all()      # (places, not digits, are what is tested here)
+
+
+@pytest.mark.parametrize("L", [30, 64, 300, 1500])
+def test_given_gates_whose_products_overflow(L):
+    """Words one by one stay finite, products of the gates alone do not."""
+    C = 8
+    g = torch.full((L, C), 0.5, device="cuda")
+    x = torch.ones(L, C, device="cuda")
+    h0 = torch.zeros(1, C, device="cuda")
+    g[:, 0], x[:, 0] = 1e20, 0.0                        # zero stays zero
+    g[:, 1], x[:, 1] = 1e20, 0.0
+    g[L // 2:, 1] = 0.0
+    g[::2, 2], g[1::2, 2] = 1e30, 1e-30                  # a product near one, taken in parts of 1e30^n
+    g[:, 3] = 2.0                                       # grows until it is infinite, as the loop does
+    g[:, 4], x[:, 4] = -1.0, 1.0
+    g[:, 5] = 0.0
+    g[0, 6] = 1e38
+    x[:, 7] = 3e38
+    got = binding.tl_recur(g, x, offsets([L]), h0, GIVEN)["h"].cpu()
+    want = loop32(g, x, h0[0], GIVEN)
+    assert torch.equal(torch.isfinite(got), torch.isfinite(want)) and torch.equal(torch.isnan(got), torch.isnan(want))
+    fine = torch.isfinite(want)
+    assert ((want - got)[fine].abs() <= 1e-5 * (1 + want[fine].abs())).all()
+    # ... and back: gradients of zero weights stay zero, others are those of the loop
+    tape = binding.tl_recur(g, x, offsets([L]), h0, GIVEN, with_tape=True)["tape"]
+    d_h = torch.zeros(L, C, device="cuda")
+    back = binding.tl_recur_backward(g, x, offsets([L]), tape, d_h, None, GIVEN)
+    assert (back["d_x"] == 0).all() and (back["d_h0"] == 0).all()
+    assert (back["d_g"][:, :3] == 0).all()
+
+
+@pytest.mark.parametrize("L", [64, 1500])
+def test_nan_stays_in_its_channel_and_sentence(L):
+    C, t = 70, L // 2
+    lengths = [L, L, L]
+    g, x, h0, d_h, d_last = inputs(lengths, C, torch.bfloat16, SIGMOID)
+    off = offsets(lengths)
+    def all_of(x, d_h):
+        out = binding.tl_recur(g, x, off, h0, with_last=True, with_tape=True)
+        out.update(binding.tl_recur_backward(g, x, off, out.pop("tape"), d_h, d_last))
+        return out
+    clean = all_of(x, d_h)
+    bad, bad_d = x.clone(), d_h.clone()
+    bad[L + t, 5] = float("nan")
+    bad_d[L + t, 9] = float("nan")
+    got = all_of(bad, bad_d)
+    for k, want in clean.items():
+        have = got[k]
+        touched = torch.zeros_like(want, dtype=torch.bool)
+        if k == "h":
+            touched[L + t:2 * L, 5] = True
+        elif k == "h_last":
+            touched[1, 5] = True
+        elif k == "d_g":
+            touched[L + t:2 * L, 5] = True                       # its state, of every later word
+            touched[L:L + t + 1, 9] = True                       # what comes back, to every earlier one
+        elif k == "d_x":
+            touched[L:L + t + 1, 9] = True
+        else:
+            touched[1, 9] = True
+        assert torch.isnan(have[touched]).all() and torch.equal(have[~touched], want[~touched]), k
+
+
+def test_bits_repeat_and_streams():
+    for name in ("ragged", "cut_far", "tokens"):
+        lengths = LENGTHS[name]
+        g, x, h0, d_h, d_last = inputs(lengths, 100, torch.bfloat16, SIGMOID)
+        off = offsets(lengths)
+        first = binding.tl_recur(g, x, off, h0, with_last=True, with_tape=True)
+        back = binding.tl_recur_backward(g, x, off, first["tape"], d_h, d_last)
+        other = torch.cuda.Stream()
+        other.wait_stream(torch.cuda.current_stream())
+        again = binding.tl_recur(g, x, off, h0, with_last=True, with_tape=True, stream=other)
+        with torch.cuda.stream(other):
+            back_again = binding.tl_recur_backward(g, x, off, again["tape"], d_h, d_last)
+        torch.cuda.synchronize()
+        for a, b in ((first, again), (back, back_again)):
+            for k in ("h", "h_last", "d_g", "d_x", "d_h0"):
+                if k in a:
+                    assert torch.equal(a[k], b[k])
+
+
+@pytest.mark.parametrize("lengths", ["ragged", "cut"])
+def test_captured_and_replayed(lengths):
+    """Forward and gradients in one graph, replayed with other values in place, eager calls between."""
+    lengths = LENGTHS[lengths]
+    g, x, h0, d_h, d_last = inputs(lengths, 90, torch.float32, SIGMOID)
+    off = offsets(lengths)
+
+    def both():
+        out = binding.tl_recur(g, x, off, h0, with_last=True, with_tape=True)
+        out.update(binding.tl_recur_backward(g, x, off, out["tape"], d_h, d_last))
+        return out
+
+    both()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        recorded = both()
+    for seed in range(3):
+        for t, new in zip((g, x, h0, d_h, d_last), inputs(lengths, 90, torch.float32, SIGMOID, seed=seed + 20)):
+            t.copy_(new)
+        graph.replay()
+        eager = both()
+        torch.cuda.synchronize()
+        for k in ("h", "h_last", "d_g", "d_x", "d_h0"):
+            assert torch.equal(recorded[k], eager[k]), k
+
+
+def test_repeated_rows():
+    """Gates of one row for all words: a stride of zero."""
+    lengths = [30, 5, 100]
+    g, x, h0, d_h, d_last = inputs(lengths, 50, torch.float32, SIGMOID)
+    one = g[:1].expand(g.shape)
+    off = offsets(lengths)
+    a = binding.tl_recur(one, x, off, h0, with_tape=True)
+    b = binding.tl_recur(one.contiguous(), x, off, h0, with_tape=True)
+    assert torch.equal(a["h"], b["h"])
+    a, b = (binding.tl_recur_backward(t, x, off, a["tape"], d_h, d_last) for t in (one, one.contiguous()))
+    assert all(torch.equal(a[k], b[k]) for k in b)
+
+
+def test_no_words_at_all():
+    h0 = torch.randn(3, 20, device="cuda")
+    empty = torch.empty(0, 20, device="cuda")
+    out = binding.tl_recur(empty, empty, offsets([0, 0, 0]), h0, with_last=True, with_tape=True)
+    assert torch.equal(out["h_last"], h0)
+    back = binding.tl_recur_backward(empty, empty, offsets([0, 0, 0]), out["tape"], empty, h0)
+    assert torch.equal(back["d_h0"], h0)
+    none = torch.empty(0, 20, device="cuda")
+    binding.tl_recur(none, none, offsets([]), None)

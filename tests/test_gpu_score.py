@@ -1,0 +1,267 @@
+"""Log probabilities, entropies, alternatives and their gradient against 64 bits.
+
+Tolerances, u = 2^-24, d = x - max x of a word: exp is met to (3 |d| + 3) u of itself (the difference, its product with a rounded constant, the
+exponential).  A row of V words is summed by at least 256 lanes, so that a word's share passes V / 256 + 20 additions, and twice that many rescalings
+at most: z to S u of itself with S = 3 V / 256 + 60 and the mean of 3 |d| over p added.  log z: that, and u of itself.  The sum of e d the same of its
+own magnitude.
+"""
+import numpy as np
+import pytest
+import torch
+
+from paper_1809_00832_amd import binding
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+INF, NAN = float("inf"), float("nan")
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def reference(x, word, n_top, dl=None, dh=None):
+    """Row by row in 64 bits, and bounds of the errors before anything is stored in 16 bits."""
+    n, V = x.shape
+    out = {"logprob": np.zeros(n), "entropy": np.zeros(n), "top_word": np.full((n, n_top), -1), "top_logprob": np.full((n, n_top), -np.inf), "d_logits": np.zeros((n, V))}
+    err = {k: np.zeros_like(v, dtype=float) for k, v in out.items()}
+    x = np.where(np.isnan(x), -np.inf, x)
+    for r in range(n):
+        row, m = x[r], x[r].max()
+        there = 0 <= word[r] < V
+        if m == -np.inf:
+            out["logprob"][r] = -np.inf if there else 0
+            continue
+        with np.errstate(invalid="ignore"):
+            d = np.where(row == m, 0.0, row - m)
+        e = np.exp(d)
+        z = e.sum()
+        p, logp = e / z, d - np.log(z)
+        far = np.where(p > 0, -d, 0.0)
+        far = np.where(np.isfinite(far), far, 0.0)
+        S = 3 * V / 256 + 60 + 3 * (p * far).sum()
+        spread = (p * far).sum()
+        out["entropy"][r] = np.log(z) + spread
+        err["entropy"][r] = U * (2 * S * (1 + spread) + 3 * np.log(z) + 3 * (p * far * far).sum())
+        step = U * (S + 2 * np.log(z) + 2 * np.abs(np.where(np.isfinite(d), d, 0.0)) + 2 * np.where(np.isfinite(logp), np.abs(logp), 0))
+        if there:
+            out["logprob"][r], err["logprob"][r] = logp[word[r]], step[word[r]]
+        order = [j for j in np.lexsort((np.arange(V), -row)) if row[j] > -np.inf][:n_top] if n_top else []
+        out["top_word"][r, :len(order)] = order
+        out["top_logprob"][r, :len(order)], err["top_logprob"][r, :len(order)] = logp[order], step[order]
+        if dl is not None:
+            a, b = (dl[r] if there else 0.0), dh[r]
+            with np.errstate(invalid="ignore"):
+                inner = np.where(p > 0, logp + out["entropy"][r], 0.0)
+            out["d_logits"][r] = -a * p - b * p * inner
+            if there:
+                out["d_logits"][r, word[r]] += a
+            rel = U * (S + 3 * far + 10)
+            err["d_logits"][r] = p * (rel * (np.abs(a) + np.abs(b) * np.abs(inner)) + np.abs(b) * (err["entropy"][r] + step + 4 * U * (np.abs(inner) + far + np.log(z) + out["entropy"][r])))
+            err["d_logits"][r] += 2 * U * np.abs(a) * (p + (np.arange(V) == word[r])) + (abs(a) + abs(b) * 100) * 2.0 ** -120
+    return out, err
+
+
+def half_step(dtype, value):
+    tiny = {torch.float32: 2.0 ** -150, torch.bfloat16: 2.0 ** -134, torch.float16: 2.0 ** -25}[dtype]
+    return np.abs(value) * torch.finfo(dtype).eps / 2 + tiny
+
+
+def check(x, word, n_top=0, back=True, **kw):
+    dtype, (n, V) = x.dtype, x.shape
+    rng = np.random.default_rng(V)
+    w = torch.tensor(word, dtype=torch.int32, device="cuda")
+    dl = torch.from_numpy(rng.normal(size=n).astype(np.float32)).cuda()
+    dh = torch.from_numpy(rng.normal(size=n).astype(np.float32)).cuda()
+    got = binding.tl_score(x, w, n_top)
+    if back:
+        got["d_logits"] = binding.tl_score_backward(x, w, got["stats"], dl, dh)
+    want, err = reference(x.double().cpu().numpy(), word, n_top, dl.double().cpu().numpy(), dh.double().cpu().numpy())
+    for k in want:
+        if k not in got or (n_top == 0 and k.startswith("top")):
+            continue
+        g, w64, e = got[k].cpu().double().numpy(), want[k], err[k]
+        w64 = np.where(np.abs(w64) >= 2.0 ** 128, np.copysign(np.inf, w64), w64)       # (beyond fp32: differences of large logits)
+        assert g.shape == w64.shape, k
+        if k == "top_word":
+            assert np.array_equal(g, w64), (k, np.argwhere(g != w64)[:4])
+            continue
+        if k == "d_logits":
+            e = e + half_step(dtype, w64) + half_step(dtype, e)
+        with np.errstate(invalid="ignore"):
+            same = (g == w64) | (np.isfinite(w64) & (np.abs(g - w64) <= 1.01 * e))
+        assert same.all(), (k, np.argwhere(~same)[:4].tolist(), g[~same][:4], w64[~same][:4], e[~same][:4])
+    return got
+
+
+def logits(n, V, dtype, seed=0, spread=2.5):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(n, V, generator=gen, device="cuda") * spread).to(dtype)
+
+
+def words(n, V, seed=0):
+    return [int(v) for v in np.random.default_rng(seed).integers(0, V, n)]
+
+
+@pytest.mark.parametrize("V", [1, 2, 3, 7, 8, 9, 15, 17, 63, 64, 65, 255, 256, 1000, 1023, 4097, 8192, 20000, 50001])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows(dtype, V):
+    n = 5 if V > 4000 else 33
+    for top in (0, 1, 5, 64):
+        check(logits(n, V, TYPES[dtype]), words(n, V), top, back=top == 0)
+
+
+@pytest.mark.parametrize("n,V", [(1, 8192), (1, 30000), (2, 100003), (100, 9000), (127, 20001), (300, 9000)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_few_rows_divided_among_workgroups(dtype, n, V):
+    check(logits(n, V, TYPES[dtype]), words(n, V), 20, back=False)
+
+
+@pytest.mark.parametrize("V", [100, 5000, 40000])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_equal_values_go_by_index(dtype, V):
+    dt = TYPES[dtype]
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    few = torch.randint(0, 3, (4, V), generator=gen, device="cuda").to(dt)
+    few[1] = 0
+    few[2] = torch.where(torch.arange(V, device="cuda") % 7 == 3, 1.0, -INF).to(dt)
+    few[3, ::2] = -0.0
+    few[3, 1::2] = 0.0
+    for top in (1, 20, 64):
+        check(few, words(4, V), top, back=False)
+
+
+@pytest.mark.parametrize("V", [3000, 40000])
+def test_rows_in_order(V):
+    """Ascending rows: every word is larger than all before it."""
+    up = torch.arange(V, device="cuda", dtype=torch.float32) * (10.0 / V)
+    check(torch.stack([up, up.flip(0), torch.sin(up * 50)]), words(3, V), 40, back=False)
+
+
+@pytest.mark.parametrize("n_top", [0, 10])
+@pytest.mark.parametrize("V", [5, 70, 3001, 20000])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_infinities_and_nan(dtype, V, n_top):
+    x = logits(12, V, TYPES[dtype]).clone()
+    word = words(12, V)
+    x[0] = -INF
+    x[1] = NAN
+    x[2, :] = -INF
+    x[2, V // 2] = 3.0
+    x[3, ::3] = -INF
+    x[4, ::3] = NAN
+    x[5, V // 3] = INF
+    x[6, ::2] = INF
+    word[6] = 0
+    x[7, 0], x[7, 1:] = INF, -INF
+    x[8] = NAN
+    x[8, V - 1] = INF
+    word[5], word[8] = V // 3, V - 1
+    word[9], word[10], word[11] = -1, V, 2 ** 31 - 1
+    check(x, word, n_top)
+
+
+@pytest.mark.parametrize("scale", [1e4, 1e30, 3.4e38])
+def test_large_values(scale):
+    x = torch.randn(6, 700, device="cuda", generator=torch.Generator(device="cuda").manual_seed(0))
+    x = (x / x.abs().max() * scale).clamp(-3.4e38, 3.4e38)
+    x[0, :] = scale
+    x[1, :] = -scale
+    x[2, ::2], x[2, 1::2] = scale, -scale
+    check(x, words(6, 700), 5)
+
+
+def test_peaked_and_flat_rows():
+    x = logits(4, 5000, torch.float32, spread=0.01)
+    x[1, 77] = 30.0
+    x[2, 77] = 200.0
+    x[3] = 0
+    got = check(x, [77, 77, 77, 77], 3)
+    assert float(got["entropy"].min()) >= 0
+
+
+def test_strides_and_addresses():
+    big = logits(9, 4100, torch.bfloat16)
+    for first in (0, 1, 3, 7):
+        x = big[:, first:first + 3001]
+        a, b = check(x, words(9, 3001), 7), check(x.contiguous(), words(9, 3001), 7)
+        assert torch.equal(a["top_word"], b["top_word"])
+    one = big[:1].expand(9, 4100)
+    check(one, words(9, 4100), 3)
+    out = torch.full((9, 3010), 5.0, device="cuda", dtype=torch.bfloat16)
+    w = torch.tensor(words(9, 3001), dtype=torch.int32, device="cuda")
+    x = big[:, 1:3002]
+    s = binding.tl_score(x, w)
+    dl = torch.ones(9, device="cuda")
+    binding.tl_score_backward(x, w, s["stats"], dl, d_logits=out[:, 3:3004])
+    assert torch.equal(out[:, 3:3004], binding.tl_score_backward(x, w, s["stats"], dl)) and (out[:, :3] == 5).all() and (out[:, 3004:] == 5).all()
+
+
+@pytest.mark.parametrize("V", [1, 1000, 4099])
+def test_gradient_in_place_and_missing_factors(V):
+    x = logits(20, V, torch.float32)
+    w = torch.tensor(words(20, V), dtype=torch.int32, device="cuda")
+    s = binding.tl_score(x, w)
+    dl, zero = torch.randn(20, device="cuda"), torch.zeros(20, device="cuda")
+    full = binding.tl_score_backward(x, w, s["stats"], dl, zero)
+    assert torch.equal(full, binding.tl_score_backward(x, w, s["stats"], dl))
+    only = binding.tl_score_backward(x, w, s["stats"], zero, dl)
+    assert torch.equal(only, binding.tl_score_backward(x, None, s["stats"], None, dl))
+    assert (binding.tl_score_backward(x, w, s["stats"]) == 0).all()
+    there = x.clone()
+    assert binding.tl_score_backward(there, w, s["stats"], dl, d_logits=there) is there and torch.equal(there, full)
+
+
+def test_gradient_against_differences():
+    """Central differences in 64 bits of a loss of log probabilities and entropies, steps of 1e-4: some 1e-8 off by themselves."""
+    x = logits(3, 40, torch.float32)
+    word = [3, 39, -1]
+    w = torch.tensor(word, dtype=torch.int32, device="cuda")
+    dl, dh = torch.tensor([1.0, -2.0, 3.0], device="cuda"), torch.tensor([0.5, 0.0, 1.0], device="cuda")
+    s = binding.tl_score(x, w)
+    got = binding.tl_score_backward(x, w, s["stats"], dl, dh).cpu()
+    X = x.double().cpu().numpy()
+
+    def loss(X):
+        r, _ = reference(X, word, 0)
+        return r["logprob"] @ dl.cpu().double().numpy() + r["entropy"] @ dh.cpu().double().numpy()
+
+    for r in range(3):
+        for j in (0, 3, 20, 39):
+            a, b = X.copy(), X.copy()
+            a[r, j] += 1e-4
+            b[r, j] -= 1e-4
+            assert abs(float(got[r, j]) - (loss(a) - loss(b)) / 2e-4) < 2e-6
+
+
+def test_without_words():
+    x = logits(6, 500, torch.float16)
+    a = binding.tl_score(x, None, 4)
+    b = binding.tl_score(x, torch.zeros(6, dtype=torch.int32, device="cuda"), 4)
+    assert "logprob" not in a and all(torch.equal(a[k], b[k]) for k in a)
+    assert binding.tl_score(x[:0], None, 4)["top_word"].shape == (0, 4)
+
+
+def test_bits_repeat_on_another_stream_and_in_a_graph():
+    for n, V in ((1, 60000), (40, 7000)):
+        x, w = logits(n, V, torch.float32), torch.tensor(words(n, V), dtype=torch.int32, device="cuda")
+        dl = torch.ones(n, device="cuda")
+
+        def both(stream=None):
+            out = binding.tl_score(x, w, 10, stream=stream)
+            out["d"] = binding.tl_score_backward(x, w, out["stats"], dl, dl, stream=stream)
+            return out
+
+        first = both()
+        other = torch.cuda.Stream()
+        other.wait_stream(torch.cuda.current_stream())
+        again = both(other)
+        torch.cuda.synchronize()
+        assert all(torch.equal(first[k], again[k]) for k in first)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            recorded = both()
+        for seed in range(3):
+            x.copy_(logits(n, V, torch.float32, seed=seed + 5))
+            graph.replay()
+            eager = both()
+            torch.cuda.synchronize()
+            assert all(torch.equal(recorded[k], eager[k]) for k in eager)
