@@ -6,12 +6,16 @@ using namespace tl;
 
 namespace {
 
-constexpr int WAVES = 8, ROWS = 8;              // of a block: 64 words
+// Waves of a workgroup, words that each takes at a time and bytes of a row that a lane has: of whole sentences, and of parts of cut ones.
+constexpr int F_WAVES = 4, F_WORDS = 8, F_BYTES = 4;
+constexpr int B_WAVES = 4, B_WORDS = 16, B_BYTES = 4;
+constexpr int FC_WAVES = 8, FC_WORDS = 32, FC_BYTES = 4;
+constexpr int BC_WAVES = 8, BC_WORDS = 16, BC_BYTES = 4;
+
 // (as many words as a state's place and the block behind the last word can be counted in 32 bits with)
 constexpr int MOST_ROWS = INT32_MAX - 65536;
 
-// Channels of a lane: 8 bytes of a row forwards, 4 or 8 backwards (four tensors' worth of registers).
-constexpr int lanes_channels(int size, bool back) { return back ? 2 : 8 / size; }
+constexpr int log_2(int n) { return n > 1 ? 1 + log_2(n / 2) : 0; }
 
 bool check(const tl_recurrence *r)
 {
@@ -23,30 +27,36 @@ bool check(const tl_recurrence *r)
 
 struct Plan {
     int V, slices, shift, slots;
-    bool single;                                // a wave per sentence
-    long long blocks;
+    bool single, cut;                           // a wave per sentence; parts
+    long long blocks, pairs, states, parts, copy;               // bytes of the workspace's parts
+    long long workspace() const { return pairs + states + parts + copy; }
 };
 
+// Whether sentences are cut into parts, by their words on average (the host does not know the lengths, and a batch with one sentence much longer than the
+// others waits for it).  A whole sentence is a chain of blocks, a part waits for others and needs a launch more.  Measured (us, whole / cut, states
+// alone; words x channels, bf16): 40 sentences of 100 x 512 12.1 / 13.0, 60 of 400 34.8 / 34.3, 60 of 1000 72 / 60, 100 of 400 44 / 47, 100 of 1000 98 / 88, 256 of 750 151 / 161,
+// 4 of 1500 x 256 116 / 17; with gradients 30 / 34, 85 / 82, 179 / 159, 112 / 119, 253 / 244, 409 / 449, 287 / 37.
 bool plan(const tl_recurrence *r, bool back, Plan *p)
 {
-    p->V = lanes_channels(element_size(r->dtype), back);
+    const long long rows = r->n_rows, trees = r->n_trees;
+    const int size = element_size(r->dtype);
+    const int whole_V = (back ? B_BYTES : F_BYTES) / size;
+    const long long workgroups = trees * ((r->channels + 64 * whole_V - 1) / (64 * whole_V));
+    p->cut = rows > 128 * trees && rows / trees > 2 * workgroups;
+    p->single = !back && !p->cut && rows <= 8 * trees;
+    p->V = p->cut ? (back ? BC_BYTES : FC_BYTES) / size : whole_V;
     if (r->channels < p->V) p->V = 1;
     p->slices = (r->channels + 64 * p->V - 1) / (64 * p->V);
-    const long long rows = r->n_rows, trees = r->n_trees;
-    p->single = !back && rows <= 8 * trees;
-    p->shift = REC_WHOLE;
-    const long long wanted = 2ll * compute_units();
-    if (trees * p->slices < wanted && rows > 128 * trees) {
-        p->shift = 6;
-        while (p->shift < 14 && (rows >> (p->shift + 1)) * p->slices >= 2 * wanted) ++p->shift;
-    }
+    p->shift = !p->cut ? REC_WHOLE : back ? log_2(BC_WAVES * BC_WORDS) : log_2(FC_WAVES * FC_WORDS);
     const long long slots = (rows >> p->shift) + trees;
     p->blocks = slots * p->slices;
     p->slots = (int)slots;
-    return p->blocks <= most_blocks(64 * WAVES);
+    p->pairs = p->cut ? round16(8 * slots * r->channels) : 0;
+    p->states = p->cut ? round16(4 * (slots / REC_GROUP + 1) * r->channels) : 0;
+    p->parts = p->cut ? 16 * slots : 0;
+    p->copy = p->cut && !back ? round16(4 * trees * r->channels) : 0;
+    return p->blocks <= most_blocks(64 * 16);
 }
-
-long long workspace(const tl_recurrence *r, const Plan &p) { return p.shift == REC_WHOLE ? 0 : round16(8ll * p.slots * r->channels); }
 
 RecurArgs arguments(const tl_recurrence *r, const Plan &p)
 {
@@ -65,34 +75,49 @@ RecurArgs arguments(const tl_recurrence *r, const Plan &p)
     return a;
 }
 
+void lay_out(const Plan &p, void *workspace, RecurArgs *a)
+{
+    if (!p.cut) return;
+    char *const base = static_cast<char *>(workspace);
+    a->pairs = reinterpret_cast<uint64_t *>(base);
+    a->states = reinterpret_cast<uint32_t *>(base + p.pairs);
+    a->parts = reinterpret_cast<int4 *>(base + p.pairs + p.states);
+    if (p.copy && a->h0) a->copy = reinterpret_cast<float *>(base + p.pairs + p.states + p.parts);
+}
+
+template <auto KERNEL> hipError_t start(const RecurArgs &a, const Plan &p, int waves, hipStream_t st)
+{
+    hipLaunchKernelGGL(KERNEL, dim3((unsigned)p.blocks), dim3(64 * waves), 0, st, a);
+    return hipGetLastError();
+}
+
 template <typename T, int V, int GATE> hipError_t forward_of(const RecurArgs &a, const Plan &p, hipStream_t st)
 {
-    if (p.shift != REC_WHOLE) {
-        hipLaunchKernelGGL((k_recur_pairs<T, V, WAVES, ROWS, GATE, false>), dim3((unsigned)p.blocks), dim3(64 * WAVES), 0, st, a);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    if (p.single) hipLaunchKernelGGL((k_recur<T, V, 1, ROWS, GATE>), dim3((unsigned)p.blocks), dim3(64), 0, st, a);
-    else hipLaunchKernelGGL((k_recur<T, V, WAVES, ROWS, GATE>), dim3((unsigned)p.blocks), dim3(64 * WAVES), 0, st, a);
-    return hipGetLastError();
+    if (p.cut && !a.tape) return start<k_recur<T, V, FC_WAVES, FC_WORDS, GATE, true, true>>(a, p, FC_WAVES, st);
+    if (p.cut) return start<k_recur<T, V, FC_WAVES, FC_WORDS, GATE, true>>(a, p, FC_WAVES, st);
+    if (p.single) return start<k_recur<T, V, 1, F_WORDS, GATE, false>>(a, p, 1, st);
+    return start<k_recur<T, V, F_WAVES, F_WORDS, GATE, false>>(a, p, F_WAVES, st);
 }
 
 template <typename T, int V, int GATE> hipError_t backward_of(const RecurArgs &a, const Plan &p, hipStream_t st)
 {
-    if (p.shift != REC_WHOLE) {
-        hipLaunchKernelGGL((k_recur_pairs<T, V, WAVES, ROWS, GATE, true>), dim3((unsigned)p.blocks), dim3(64 * WAVES), 0, st, a);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    hipLaunchKernelGGL((k_recur_back<T, V, WAVES, ROWS, GATE>), dim3((unsigned)p.blocks), dim3(64 * WAVES), 0, st, a);
-    return hipGetLastError();
+    if (p.cut) return start<k_recur_back<T, V, BC_WAVES, BC_WORDS, GATE, true>>(a, p, BC_WAVES, st);
+    return start<k_recur_back<T, V, B_WAVES, B_WORDS, GATE, false>>(a, p, B_WAVES, st);
 }
 
 template <typename T, int GATE> hipError_t launch_at(const RecurArgs &a, const Plan &p, bool back, hipStream_t st)
 {
-    constexpr int F = lanes_channels(sizeof(T), false), B = lanes_channels(sizeof(T), true);
-    if (back) return p.V == 1 ? backward_of<T, 1, GATE>(a, p, st) : backward_of<T, B, GATE>(a, p, st);
-    return p.V == 1 ? forward_of<T, 1, GATE>(a, p, st) : forward_of<T, F, GATE>(a, p, st);
+    constexpr int V = 4 / sizeof(T);
+    static_assert(F_BYTES == 4 && B_BYTES == 4 && FC_BYTES == 4 && BC_BYTES == 4, "a lane's channels");
+    if (p.cut) {
+        const long long words = (p.pairs + p.states) / 8, copies = (long long)a.n_trees * a.C, most = 4ll * compute_units();
+        const long long blocks = ((words > copies ? words : copies) + 255) / 256;
+        hipLaunchKernelGGL(k_recur_prepare, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, st, a, words, copies);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (back) return p.V == 1 ? backward_of<T, 1, GATE>(a, p, st) : backward_of<T, V, GATE>(a, p, st);
+    return p.V == 1 ? forward_of<T, 1, GATE>(a, p, st) : forward_of<T, V, GATE>(a, p, st);
 }
 
 template <typename T> hipError_t launch_for(const RecurArgs &a, int gate, const Plan &p, bool back, hipStream_t st)
@@ -122,7 +147,7 @@ int tl_recur_workspace(const tl_recurrence *r, int backward, int64_t *bytes)
     *bytes = 0;
     if (r->n_trees == 0) return TL_OK;
     if (!plan(r, backward != 0, &p)) return TL_EINVAL;
-    *bytes = workspace(r, p);
+    *bytes = p.workspace();
     return TL_OK;
 }
 
@@ -133,7 +158,7 @@ int tl_recur(const tl_recurrence *r, const float *h0, void *h, int64_t h_row, fl
     if (r->n_trees == 0) return TL_OK;
     Plan p;
     if (!plan(r, false, &p)) return TL_EINVAL;
-    const long long need = workspace(r, p);
+    const long long need = p.workspace();
     if (need > workspace_bytes) return TL_ELIMIT;
     if (need > 0 && (!workspace_p || ((uintptr_t)workspace_p & 15))) return TL_EINVAL;
     RecurArgs a = arguments(r, p);
@@ -142,7 +167,7 @@ int tl_recur(const tl_recurrence *r, const float *h0, void *h, int64_t h_row, fl
     a.h0 = h0;
     a.h_last = h_last;
     a.tape = tape;
-    a.pairs = static_cast<float *>(workspace_p);
+    lay_out(p, workspace_p, &a);
     return launch(r, a, p, false, hip_stream);
 }
 
@@ -155,7 +180,7 @@ int tl_recur_backward(const tl_recurrence *r, const float *tape, const void *d_h
     if (r->n_trees == 0) return TL_OK;
     Plan p;
     if (!plan(r, true, &p)) return TL_EINVAL;
-    const long long need = workspace(r, p);
+    const long long need = p.workspace();
     if (need > workspace_bytes) return TL_ELIMIT;
     if (need > 0 && (!workspace_p || ((uintptr_t)workspace_p & 15))) return TL_EINVAL;
     RecurArgs a = arguments(r, p);
@@ -168,7 +193,7 @@ int tl_recur_backward(const tl_recurrence *r, const float *tape, const void *d_h
     a.d_x = d_x;
     a.d_x_row = d_x_row;
     a.d_h0 = d_h0;
-    a.pairs = static_cast<float *>(workspace_p);
+    lay_out(p, workspace_p, &a);
     return launch(r, a, p, true, hip_stream);
 }
 

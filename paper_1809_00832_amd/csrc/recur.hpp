@@ -6,8 +6,9 @@
 //
 // Both are linear maps of a state, so that a run of words is one pair (A, B), state -> A state + B, and pairs of runs side by side join
 // to one.  A lane owns V channels; a wave takes R words, a workgroup W R words at a time: a wave forms the pair of its words from registers, the
-// pairs are exchanged through LDS, and each wave then steps through its words once more, from the state that is its own.  Sentences that are few
-// and long are cut into parts: a first launch writes the pair of every part, the second one starts each part from the pairs before it.
+// pairs are exchanged through LDS, and each wave then steps through its words once more, from the state that is its own.  A workgroup walks a
+// whole sentence so.  Sentences that are few and long are cut into parts of W R words, a workgroup each, which holds its words in registers: it publishes
+// its pair, takes the pairs of the parts before it, and goes on from the state that they give, so that every tensor is read once.
 //
 // The backward pass needs h_(t-1) in fp32 for every word.  It reads no h: the forward keeps the state of every 64th word (the tape, 1/64 of the
 // states in fp32), and a block of 64 words is stepped through again from there.  So five tensors move instead of six, and a 16-bit h's
@@ -31,7 +32,10 @@ struct RecurArgs {
     const int32_t *off;
     const float *h0, *d_last;
     float *h_last, *d_h0, *tape;
-    float *pairs;                               // of every part (see find_slot): A [channels], then B; a cut sentence's last part holds a copy of h0 instead
+    uint64_t *pairs;                            // of every part (see RecPart), a number per channel: A and B, all ones until it is published
+    uint32_t *states;                           // behind every 32nd part of a sentence
+    int4 *parts;                                // of every part: its sentence, that one's words, the slot of its first part
+    float *copy;                                // of h0, which h_last may be written over
     int n_trees, n_rows, C, slices, slots, shift;
 };
 
@@ -42,35 +46,41 @@ template <typename T, int V> struct __attribute__((packed, aligned(sizeof(T)))) 
 };
 
 // Channels base .. base + V - 1, moved back by `back` where they would pass the last one: such a lane reads what its neighbour reads too, and
-// writes only what is its own.
+// writes only what is its own.  Lanes behind the last channel do the same as the lane that has it.  A row's address is the same in all lanes, a lane's
+// place in it a 32-bit number of its own.
 template <int V> struct RecLane {
-    int base, back;
-    bool on;
+    uint32_t base;
+    int back;
+    bool even;                                  // no lane is moved back
     __device__ RecLane(int slice, int lane, int C)
     {
-        const int want = (slice * 64 + lane) * V;
-        on = want < C;
-        back = on ? max(want + V - C, 0) : 0;
-        base = on ? want - back : 0;
+        const int want = min((slice * 64 + lane) * V, (C - 1) / V * V);
+        back = max(want + V - C, 0);
+        base = want - back;
+        even = V == 1 || C % V == 0;
     }
-    template <typename T> __device__ void load(const T *p, float (&v)[V]) const
+    template <typename T> __device__ RecRaw<T, V> raw(const T *row) const
     {
-        const RecRaw<T, V> r = *reinterpret_cast<const RecRaw<T, V> *>(p + base);
+        return *reinterpret_cast<const RecRaw<T, V> *>(reinterpret_cast<const char *>(row) + base * (uint32_t)sizeof(T));
+    }
+    template <typename T> __device__ void load(const T *row, float (&v)[V]) const
+    {
+        const RecRaw<T, V> r = raw(row);
 #pragma unroll
         for (int j = 0; j < V; ++j) v[j] = (float)r.v[j];
     }
-    template <typename T> __device__ void store(T *p, const float (&v)[V]) const
+    template <typename T> __device__ void store(T *row, const float (&v)[V]) const
     {
-        if (!on) return;
-        if (back == 0) {
-            RecRaw<T, V> r;
+        char *const at = reinterpret_cast<char *>(row) + base * (uint32_t)sizeof(T);
+        RecRaw<T, V> r;
 #pragma unroll
-            for (int j = 0; j < V; ++j) r.v[j] = (T)v[j];
-            *reinterpret_cast<RecRaw<T, V> *>(p + base) = r;
+        for (int j = 0; j < V; ++j) r.v[j] = (T)v[j];
+        if (even) {
+            *reinterpret_cast<RecRaw<T, V> *>(at) = r;
         } else {
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                if (j >= back) p[base + j] = (T)v[j];
+                if (j >= back) reinterpret_cast<T *>(at)[j] = r.v[j];
         }
     }
 };
@@ -88,43 +98,38 @@ template <int GATE> __device__ inline void rec_gates(float g, float &f, float &i
     }
 }
 
-__device__ inline bool rec_finite(float x) { return fabsf(x) < INFINITY; }
-
-// Words [from, to) of one channel, one by one.
-template <typename T, int GATE> __device__ __noinline__ float rec_walk(const RecurArgs &a, int from, int to, int c, float s)
-{
-    for (int r = from; r < to && s == s; ++r) {
-        float f, i;
-        rec_gates<GATE>((float)static_cast<const T *>(a.g)[r * a.g_row + c], f, i);
-        s = f * s + i * (float)static_cast<const T *>(a.x)[r * a.x_row + c];
-    }
-    return s;
-}
-template <typename T, int GATE> __device__ __noinline__ float rec_walk_back(const RecurArgs &a, int from, int to, int c, float m)
-{
-    for (int r = to - 1; r >= from && m == m; --r) {
-        float f, i;
-        rec_gates<GATE>((float)static_cast<const T *>(a.g)[r * a.g_row + c], f, i);
-        m = f * (m + (a.d_h ? (float)static_cast<const T *>(a.d_h)[r * a.d_h_row + c] : 0.f));
-    }
-    return m;
-}
-
 // The state behind words [from, to), whose pair is A, B.
 template <typename T, int GATE, int V, bool BACK>
-__device__ inline void rec_join(const RecurArgs &a, const RecLane<V> &l, int from, int to, const float (&A)[V], const float (&B)[V], float (&s)[V])
+__device__ inline void rec_join(const RecurArgs &a, const RecLane<V> &l, int from, int to, const float (&A)[V], const float (&B)[V], float (&s)[V], bool all = false)
 {
     float t[V];
-    bool fine = true;
+    bool walk[V], any = false;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         t[j] = fmaf(A[j], s[j], B[j]);
-        fine = fine && rec_finite(t[j]);
+        walk[j] = all || (!(fabsf(t[j]) < INFINITY) && s[j] == s[j]);     // (a NaN stays one)
+        any = any || walk[j];
     }
-    if (!fine && l.on) {
+    if (__any(any)) {
+        float w[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-            if (!rec_finite(t[j])) t[j] = BACK ? rec_walk_back<T, GATE>(a, from, to, l.base + j, s[j]) : rec_walk<T, GATE>(a, from, to, l.base + j, s[j]);
+        for (int j = 0; j < V; ++j) w[j] = s[j];
+#pragma unroll 1
+        for (int n = 0; n < to - from; ++n) {
+            const long long r = BACK ? to - 1 - n : from + n;
+            float g[V], u[V] = {};
+            l.load(static_cast<const T *>(a.g) + r * a.g_row, g);
+            if (!BACK) l.load(static_cast<const T *>(a.x) + r * a.x_row, u);
+            else if (a.d_h) l.load(static_cast<const T *>(a.d_h) + r * a.d_h_row, u);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                float f, i;
+                rec_gates<GATE>(g[j], f, i);
+                w[j] = BACK ? f * (w[j] + u[j]) : fmaf(f, w[j], i * u[j]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) t[j] = walk[j] ? w[j] : t[j];
     }
 #pragma unroll
     for (int j = 0; j < V; ++j) s[j] = t[j];
@@ -132,231 +137,433 @@ __device__ inline void rec_join(const RecurArgs &a, const RecLane<V> &l, int fro
 
 // ---- which words a workgroup has -------------------------------------------------------------
 
+// A sentence has a slot for every part, and at most one more: slot off / words + sentence on.  (Offsets are kept inside the batch, whatever they hold.)
 struct RecPart {
     int tree, slot0;                            // the sentence, and the slot of its first part
     int lo, hi;                                 // its words
     int part, parts;
     int first, end;                             // the words of this part
     bool there;
-    __device__ RecPart(const RecurArgs &a, int slot)
+    template <bool CUT> __device__ static RecPart of(const RecurArgs &a, int slot)
     {
-        // (places as in find_slot, of offsets kept inside the batch: pairs are looked up by them)
-        auto base = [&](int t) { return (min(max(a.off[t], 0), a.n_rows) >> a.shift) + t; };
-        tree = a.shift == REC_WHOLE ? slot : find_last(a.n_trees, slot, base);
-        slot0 = a.shift == REC_WHOLE ? slot : __builtin_amdgcn_readfirstlane(base(tree));
-        tree_range(a.off, tree, a.n_rows, &lo, &hi);
-        const long long n = hi - lo, size = 1ll << a.shift;
-        parts = max((int)((n + size - 1) >> a.shift), 1);
-        part = slot - slot0;
-        there = part >= 0 && part < parts;
-        if (!there) part = 0;
-        first = (int)min(lo + part * size, (long long)hi);
-        end = (int)min(first + size, (long long)hi);
+        RecPart p;
+        if constexpr (CUT) {
+            const int4 r = a.parts[slot];
+            p.tree = __builtin_amdgcn_readfirstlane(r.x);
+            p.lo = __builtin_amdgcn_readfirstlane(r.y);
+            p.hi = __builtin_amdgcn_readfirstlane(r.z);
+            p.slot0 = __builtin_amdgcn_readfirstlane(r.w);
+            const int size = 1 << a.shift;
+            p.parts = max((int)(((long long)p.hi - p.lo + size - 1) >> a.shift), 1);
+            p.part = slot - p.slot0;
+            p.there = p.part >= 0 && p.part < p.parts;
+            p.first = (int)min(p.lo + (long long)p.part * size, (long long)p.hi);
+            p.end = (int)min((long long)p.first + size, (long long)p.hi);
+        } else {
+            p.tree = p.slot0 = slot;
+            tree_range(a.off, slot, a.n_rows, &p.lo, &p.hi);
+            p.part = 0;
+            p.parts = 1;
+            p.first = p.lo;
+            p.end = p.hi;
+            p.there = true;
+        }
+        return p;
     }
 };
 
-// R words from `row` on (as far as `end`; beyond it the last one again) of one tensor.
+// R words from `row` on (as far as `end`; beyond it the last one again) of one tensor, as they lie in memory; zeros where there is none.
 template <typename T, int V, int R> struct RecRows {
-    RecRaw<T, V> r[R];
-    __device__ void load(const void *p, long long stride, const RecLane<V> &l, int row, int end)
+    static constexpr bool PACKED = sizeof(T) == 2 && V == 2;    // two values in a register
+    typedef typename std::conditional<PACKED, uint32_t, RecRaw<T, V>>::type Row;
+    Row r[R];
+    __device__ void clear()
     {
-        const T *at = static_cast<const T *>(p) + l.base;
 #pragma unroll
-        for (int k = 0; k < R; ++k) r[k] = *reinterpret_cast<const RecRaw<T, V> *>(at + min(row + k, end - 1) * stride);
+        for (int k = 0; k < R; ++k) r[k] = {};
     }
-    __device__ float get(int k, int j) const { return (float)r[k].v[j]; }
+    // ONCE: nothing reads the rows again, so they need no place in the caches.
+    template <bool ONCE = false> __device__ void load(const void *p, long long stride, const RecLane<V> &l, int row, int end)
+    {
+        typedef uint32_t __attribute__((aligned(2))) Word;
+        const T *at = static_cast<const T *>(p) + row * stride;
+        const int more = end - 1 - row;
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            if constexpr (ONCE && sizeof(Row) == 4) {
+                const uint32_t v = __builtin_nontemporal_load(reinterpret_cast<const Word *>(reinterpret_cast<const char *>(at) + l.base * (uint32_t)sizeof(T)));
+                __builtin_memcpy(&r[k], &v, 4);
+            } else {
+                const RecRaw<T, V> v = l.raw(at);
+                __builtin_memcpy(&r[k], &v, sizeof(v));
+            }
+            at += k < more ? stride : 0;
+        }
+    }
+    __device__ float get(int k, int j) const
+    {
+        if constexpr (PACKED) {
+            if constexpr (std::is_same<T, bf16_t>::value) return __uint_as_float(j == 0 ? r[k] << 16 : r[k] & 0xffff0000u);
+            const uint16_t w = j == 0 ? (uint16_t)r[k] : (uint16_t)(r[k] >> 16);
+            T v;
+            __builtin_memcpy(&v, &w, 2);
+            return (float)v;
+        } else {
+            return (float)r[k].v[j];
+        }
+    }
+    // What is computed from the rows after this is computed anew: registers hold the rows, not the results.
+    __device__ void forget()
+    {
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            if constexpr (PACKED) asm volatile("" : "+v"(r[k]));
+            else if constexpr (sizeof(T) == 4)
+#pragma unroll
+                for (int j = 0; j < V; ++j) asm volatile("" : "+v"(r[k].v[j]));
+        }
+    }
 };
 
-// ---- pairs of parts ----------------------------------------------------------------------------
-
-// A part's waves take an even share of its words each, one after the other.
-template <typename T, int V, int W, int R, int GATE, bool BACK> __global__ __launch_bounds__(64 * W) void k_recur_pairs(RecurArgs a)
-{
-    __shared__ float lds[W][2][V][64];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int slot = blockIdx.x / a.slices, slice = blockIdx.x - slot * a.slices;
-    const RecPart p(a, slot);
-    if (!p.there || p.parts == 1) return;
-    const RecLane<V> l(slice, lane, a.C);
-    float *const out = a.pairs + 2ll * slot * a.C;
-    if (!BACK && p.part == p.parts - 1) {
-        float s[V] = {};
-        if (wave == 0 && a.h0) l.load(a.h0 + (long long)p.tree * a.C, s);
-        if (wave == 0) l.store(out, s);
-        return;
+// The gates of R words: held (KEEP), or made again from the words wherever they are needed.
+template <typename T, int V, int R, int GATE, bool KEEP> struct RecGates {
+    RecRows<T, V, R> g;
+    float f[KEEP ? R : 1][V], i[KEEP ? R : 1][V];
+    __device__ explicit RecGates(const RecRows<T, V, R> &rows) : g(rows)
+    {
+        if constexpr (KEEP)
+#pragma unroll
+            for (int k = 0; k < R; ++k)
+#pragma unroll
+                for (int j = 0; j < V; ++j) rec_gates<GATE>(g.get(k, j), f[k][j], i[k][j]);
     }
-    if (BACK && p.part == 0) return;
-    const int share = (1 << a.shift) / W;
-    const int from = min(p.first + wave * share, p.end), to = min(from + share, p.end);
-    float A[V], B[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) A[j] = 1.f, B[j] = 0.f;
-    const void *const second = BACK ? a.d_h : a.x;
-    const long long second_row = BACK ? a.d_h_row : a.x_row;
-    RecRows<T, V, R> g, u;
-    // (backwards: words are taken from the last run of R on)
-    const int runs = (to - from + R - 1) / R;
-    auto at = [&](int n) { return from + (BACK ? runs - 1 - n : n) * R; };
-    if (runs > 0) {
-        g.load(a.g, a.g_row, l, at(0), to);
-        if (second) u.load(second, second_row, l, at(0), to);
-    }
-    for (int n = 0; n < runs; ++n) {
-        const RecRows<T, V, R> G = g, U = u;
-        if (n + 1 < runs) {
-            g.load(a.g, a.g_row, l, at(n + 1), to);
-            if (second) u.load(second, second_row, l, at(n + 1), to);
-        }
-        const int row = at(n);
-#pragma unroll
-        for (int q = 0; q < R; ++q) {
-            const int k = BACK ? R - 1 - q : q;
-            if (row + k < to) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    float f, i;
-                    rec_gates<GATE>(G.get(k, j), f, i);
-                    A[j] *= f;
-                    B[j] = BACK ? f * (B[j] + (second ? U.get(k, j) : 0.f)) : fmaf(f, B[j], i * U.get(k, j));
-                }
-            }
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < V; ++j) lds[wave][0][j][lane] = A[j], lds[wave][1][j][lane] = B[j];
-    __syncthreads();
-    if (wave != 0) return;
-#pragma unroll
-    for (int j = 0; j < V; ++j) A[j] = 1.f, B[j] = 0.f;
-    for (int q = 0; q < W; ++q) {
-        const int w = BACK ? W - 1 - q : q;
+    __device__ __forceinline__ void at(int k, float (&F)[V], float (&I)[V]) const
+    {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const float c = lds[w][0][j][lane];
-            A[j] *= c;
-            B[j] = fmaf(c, B[j], lds[w][1][j][lane]);
+            if constexpr (KEEP) F[j] = f[k][j], I[j] = i[k][j];
+            else rec_gates<GATE>(g.get(k, j), F[j], I[j]);
         }
     }
-    l.store(out, A);
-    l.store(out + a.C, B);
+    __device__ void forget()
+    {
+        if constexpr (!KEEP) g.forget();
+    }
+};
+
+// ---- parts of a sentence -------------------------------------------------------------------------
+//
+// A part's pair needs nothing but the part's own words, so a workgroup that waits for pairs waits for workgroups that wait for nothing.  A state is
+// published behind every 32nd part: a part needs the state behind the last such part before it, and the pairs from there on, 31 at most.  Values are
+// published as they are, in words that were filled with ones before: a word that is no longer all ones is complete, and no fence is needed.
+// Parts are numbered in the order in which a state passes them, and workgroups are started in that order, so that what is waited for has been started.
+// Every wait ends all the same: after REC_POLLS polls the words in question are walked, from the start of the sentence.
+
+constexpr int REC_GROUP = 32, REC_POLLS = 1 << 16;
+constexpr uint32_t REC_NAN = 0x7fc00000u;       // published for a NaN that is all ones
+
+__device__ inline uint32_t rec_bits(float x)
+{
+    const uint32_t b = __float_as_uint(x);
+    return b == ~0u ? REC_NAN : b;
 }
 
-// The state at the start of a part, or (BACK) what comes back to its last word: pairs of the parts in between, joined one by one.
-template <typename T, int GATE, int V, bool BACK> __device__ inline void rec_enter(const RecurArgs &a, const RecPart &p, const RecLane<V> &l, float (&s)[V])
+template <int V> __device__ inline void rec_publish(uint64_t *at, const RecLane<V> &l, const float (&A)[V], const float (&B)[V])
 {
-    const float *const from = BACK ? a.d_last : a.h0;
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+        if (j >= l.back) __hip_atomic_store(at + l.base + j, (uint64_t)rec_bits(A[j]) << 32 | rec_bits(B[j]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <int V> __device__ inline void rec_publish(uint32_t *at, const RecLane<V> &l, const float (&s)[V])
+{
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+        if (j >= l.back) __hip_atomic_store(at + l.base + j, rec_bits(s[j]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Whether the words came.
+template <int V, int N, typename W> __device__ inline bool rec_wait(W *const (&at)[N], int n, const RecLane<V> &l, W (&v)[N][V])
+{
+#pragma unroll 1
+    for (int poll = 0; poll < REC_POLLS; ++poll) {
+        bool there = true;
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (k < n)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    v[k][j] = __hip_atomic_load(at[k] + l.base + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    there = there && v[k][j] != (W)~(W)0;
+                }
+        if (__all(there)) return true;
+        __builtin_amdgcn_s_sleep(1);
+    }
+    return false;
+}
+
+template <int V, int W> struct RecEnter {
+    float pair[W][2][V][64], state[V][64];
+    int late;
+};
+
+// The state in front of a part's first word, or (BACK) what comes back to its last one.  Every wave joins an even share of the pairs to one, all
+// join these.  `start`: the state at the sentence's own end.  (e.late is zero before the call's first barrier; the caller has a barrier between.)
+template <typename T, int GATE, int V, int W, bool BACK>
+__device__ inline void rec_enter(const RecurArgs &a, const RecPart &p, const RecLane<V> &l, int wave, RecEnter<V, W> &e, float (&s)[V])
+{
+    constexpr int SHARE = (REC_GROUP - 1 + W - 1) / W;
+    const int lane = threadIdx.x & 63, size = 1 << a.shift;
+    const int nth = BACK ? p.parts - 1 - p.part : p.part, group = nth & ~(REC_GROUP - 1), many = nth - group;
+    auto slot = [&](int n) { return p.slot0 + (BACK ? p.parts - 1 - n : n); };
+    bool fine = true;
+    if (wave == 0) {
+        if (group > 0) {
+            uint32_t *const at[1] = {a.states + (long long)(slot(group - 1) / REC_GROUP) * a.C};
+            uint32_t v[1][V];
+            fine = rec_wait<V, 1>(at, 1, l, v);
+#pragma unroll
+            for (int j = 0; j < V; ++j) s[j] = __uint_as_float(v[0][j]);
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) e.state[j][lane] = s[j];
+    }
+    const int first = wave * SHARE, n = min(SHARE, many - first);
+    if (n > 0) {
+        constexpr int N = SHARE < 4 ? SHARE : 4;
+        float A[V], B[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) A[j] = 1.f, B[j] = 0.f;
+#pragma unroll 1
+        for (int i = 0; i < n; i += N) {
+            uint64_t *at[N], v[N][V];
+#pragma unroll
+            for (int k = 0; k < N; ++k) at[k] = a.pairs + (long long)slot(group + first + min(i + k, n - 1)) * a.C;
+            fine = rec_wait<V, N>(at, n - i, l, v) && fine;
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (i + k < n)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const float c = __uint_as_float((uint32_t)(v[k][j] >> 32));
+                        A[j] *= c;
+                        B[j] = fmaf(c, B[j], __uint_as_float((uint32_t)v[k][j]));
+                    }
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) e.pair[wave][0][j][lane] = A[j], e.pair[wave][1][j][lane] = B[j];
+    }
+    if (!fine) e.late = 1;
+    __syncthreads();
+    const bool late = e.late != 0;
+    float t[V];
+    bool bad[V], any = false;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        s[j] = e.state[j][lane];
+        t[j] = s[j];
+        for (int w = 0; w * SHARE < many; ++w) t[j] = fmaf(e.pair[w][0][j][lane], t[j], e.pair[w][1][j][lane]);
+        bad[j] = late || (!(fabsf(t[j]) < INFINITY) && s[j] == s[j]);
+        any = any || bad[j];
+    }
+    if (__any(any)) {
+        // the words between the published state, or the sentence's own end, and this part
+        float w[V];
+        const float *const from = BACK ? a.d_last : a.copy;
+#pragma unroll
+        for (int j = 0; j < V; ++j) w[j] = late ? 0.f : s[j];
+        if (late && from) l.load(from + (long long)p.tree * a.C, w);
+        const int edge = late ? 0 : group;
+        const float none[V] = {};
+        if (BACK) rec_join<T, GATE, V, BACK>(a, l, p.end, (int)min(p.lo + (long long)(p.parts - edge) * size, (long long)p.hi), none, none, w, true);
+        else rec_join<T, GATE, V, BACK>(a, l, p.lo + edge * size, p.first, none, none, w, true);
+#pragma unroll
+        for (int j = 0; j < V; ++j) t[j] = bad[j] ? w[j] : t[j];
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) s[j] = t[j];
+}
+
+// What the parts need before they start: what each of them is, words of ones, and a copy of h0.
+__global__ __launch_bounds__(256) void k_recur_prepare(RecurArgs a, long long n_words, long long n_copy)
+{
+    const long long at = blockIdx.x * 256ll + threadIdx.x, step = (long long)gridDim.x * 256;
+    for (long long slot = at; slot < a.slots; slot += step) {
+        auto place = [&](int t) { return min(max(a.off[t], 0), a.n_rows); };
+        int t = 0, n = a.n_trees;               // the last sentence whose slots do not begin behind this one
+        while (n > 1) {
+            const int half = n >> 1, base = (place(t + half) >> a.shift) + t + half;
+            t = base <= slot ? t + half : t;
+            n -= half;
+        }
+        const int lo = place(t);
+        a.parts[slot] = int4{t, lo, max(place(t + 1), lo), (lo >> a.shift) + t};
+    }
+    for (long long i = at; i < n_words; i += step) a.pairs[i] = ~0ull;      // (pairs, and the states behind them)
+    if (a.copy)
+        for (long long i = at; i < n_copy; i += step) a.copy[i] = a.h0[i];
+}
+
+// Where a sentence's words begin: its row of h0, or (BACK) of what comes back from behind them.
+template <int V> __device__ inline void rec_start(const float *from, const RecPart &p, const RecLane<V> &l, int C, float (&s)[V])
+{
 #pragma unroll
     for (int j = 0; j < V; ++j) s[j] = 0.f;
-    if (!BACK && p.parts > 1) {
-        l.load(a.pairs + 2ll * (p.slot0 + p.parts - 1) * a.C, s);
-    } else if (from) {
-        l.load(from + (long long)p.tree * a.C, s);
-    }
-    const int size = 1 << (a.shift & 31);
-    const int many = BACK ? p.parts - 1 - p.part : p.part;
-    for (int n = 0; n < many; ++n) {
-        const int k = BACK ? p.parts - 1 - n : n;
-        const float *const at = a.pairs + 2ll * (p.slot0 + k) * a.C;
-        float A[V], B[V];
-        l.load(at, A);
-        l.load(at + a.C, B);
-        const int begin = p.lo + k * size;
-        rec_join<T, GATE, V, BACK>(a, l, begin, (int)min((long long)begin + size, (long long)p.hi), A, B, s);
-    }
+    if (from) l.load(from + (long long)p.tree * C, s);
+}
+
+__device__ inline float *rec_tape(const RecurArgs &a, const RecPart &p, int row)
+{
+    return a.tape + ((long long)(p.lo / REC_TAPE) + p.tree + (row - p.lo) / REC_TAPE) * a.C;
 }
 
 // ---- forward -----------------------------------------------------------------------------------
 
-template <typename T, int V, int W, int R, int GATE> __global__ __launch_bounds__(64 * W) void k_recur(RecurArgs a)
+// f(k) for the first `words` of R words, in order.
+template <int R, typename F> __device__ __forceinline__ void rec_each(int words, F f)
 {
-    static_assert(REC_TAPE % (W * R) == 0, "states of the tape lie at starts of blocks");
-    __shared__ float lds[W > 1 ? 2 : 1][W][2][V][64];
+    if (words >= R) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) f(k);
+    } else {
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+            if (k < words) f(k);
+    }
+}
+template <int R, typename F> __device__ __forceinline__ void rec_each_back(int words, F f)
+{
+    if (words >= R) {
+#pragma unroll
+        for (int k = R - 1; k >= 0; --k) f(k);
+    } else {
+#pragma unroll
+        for (int k = R - 1; k >= 0; --k)
+            if (k < words) f(k);
+    }
+}
+
+// CUT: a part of W R words, else a whole sentence, W R words at a time.  In a part the registers hold the words as they were read, which are put through
+// their gates twice, for the pair and for the states: that costs less than the registers of the results, which would halve the waves of a compute unit.
+// ONCE: nothing reads g and x again (there is no tape); a branch on the tape in the kernel would cost what the other loads gain.  Measured (us, two sentences of
+// 26 000 words in all, bf16 x 2048): 97 with ordinary loads, 91 so; a training step of eight of 1 800 words x 1024: 72.5 and 74.
+template <typename T, int V, int W, int R, int GATE, bool CUT, bool ONCE = false> __global__ __launch_bounds__(64 * W) void k_recur(RecurArgs a)
+{
+    static_assert(REC_TAPE % R == 0, "states of the tape lie where a wave's words begin");
+    constexpr bool KEEP = !CUT && W > 1;
+    __shared__ float lds[W > 1 && !CUT ? 2 : 1][W][2][V][64];
+    __shared__ RecEnter<V, W> enter[1];                         // (CUT only)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int slot = blockIdx.x / a.slices, slice = blockIdx.x - slot * a.slices;
-    const RecPart p(a, slot);
+    const RecPart p = RecPart::of<CUT>(a, slot);
     if (!p.there) return;
     const RecLane<V> l(slice, lane, a.C);
+    RecRows<T, V, R> g, x;
+    auto load = [&](int row) {
+        g.clear();                                              // (so that what was there ends here)
+        x.clear();
+        if (row >= p.end) return;
+        g.template load<ONCE>(a.g, a.g_row, l, row, p.end);
+        x.template load<ONCE>(a.x, a.x_row, l, row, p.end);
+    };
+    load(p.first + wave * R);
     float c[V];
-    rec_enter<T, GATE, V, false>(a, p, l, c);
+    rec_start(CUT ? a.copy : a.h0, p, l, a.C, c);
     if (p.lo == p.hi) {                                         // no words
         if (a.h_last && wave == 0) l.store(a.h_last + (long long)p.tree * a.C, c);
         return;
     }
-    RecRows<T, V, R> g, x;
-    auto load = [&](int row) {
-        if (row >= p.end) return;
-        g.load(a.g, a.g_row, l, row, p.end);
-        x.load(a.x, a.x_row, l, row, p.end);
-    };
-    load(p.first + wave * R);
+    if constexpr (CUT)
+        if (threadIdx.x == 0) enter[0].late = 0;
     int buf = 0;
-    for (int block = p.first; block < p.end; block += W * R, buf ^= 1) {
-        const int row = block + wave * R;
-        float f[R][V], u[R][V], s[V];
-#pragma unroll
-        for (int k = 0; k < R; ++k)
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                float i;
-                rec_gates<GATE>(g.get(k, j), f[k][j], i);
-                u[k][j] = i * x.get(k, j);
-                if (row + k >= p.end) f[k][j] = 1.f, u[k][j] = 0.f;         // leaves a state as it is
-            }
-        if (block + W * R < p.end) load(row + W * R);
-        if (a.tape && wave == 0 && ((block - p.lo) & (REC_TAPE - 1)) == 0)
-            l.store(a.tape + (((long long)p.lo / REC_TAPE) + p.tree + (block - p.lo) / REC_TAPE) * a.C, c);
+#pragma unroll 1
+    for (int block = p.first;; block += W * R) {
+        const int row = block + wave * R, words = p.end - row;
+        RecGates<T, V, R, GATE, KEEP> G(g);
+        RecRows<T, V, R> X = x;
+        const bool more = !CUT && block + W * R < p.end;
+        if (more) load(row + W * R);
+        float f[V], i[V], s[V];
         if constexpr (W > 1) {
             float A[V], B[V];
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                A[j] = 1.f, B[j] = 0.f;
+            for (int j = 0; j < V; ++j) A[j] = 1.f, B[j] = 0.f;
+            rec_each<R>(words, [&](int k) __attribute__((always_inline)) {
+                G.at(k, f, i);
 #pragma unroll
-                for (int k = 0; k < R; ++k) {
-                    A[j] *= f[k][j];
-                    B[j] = fmaf(f[k][j], B[j], u[k][j]);
+                for (int j = 0; j < V; ++j) {
+                    A[j] *= f[j];
+                    B[j] = fmaf(f[j], B[j], i[j] * X.get(k, j));
                 }
+            });
+            G.forget();
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
                 lds[buf][wave][0][j][lane] = A[j];
                 lds[buf][wave][1][j][lane] = B[j];
             }
             __syncthreads();                                    // (the other buffer is written only after the next one)
+            if constexpr (CUT)
+                if (p.parts > 1) {
+                    if (wave == 0 && p.part < p.parts - 1) {
 #pragma unroll
+                        for (int j = 0; j < V; ++j)
+#pragma unroll
+                            for (int w = 1; w < W; ++w) {
+                                A[j] *= lds[0][w][0][j][lane];
+                                B[j] = fmaf(lds[0][w][0][j][lane], B[j], lds[0][w][1][j][lane]);
+                            }
+                        rec_publish(a.pairs + (long long)slot * a.C, l, A, B);
+                    }
+                    rec_enter<T, GATE, V, W, false>(a, p, l, wave, enter[0], c);
+                }
+#pragma unroll 1
             for (int w = 0; w < W; ++w) {
-                if (w == wave)
+                if (w == wave) {
 #pragma unroll
                     for (int j = 0; j < V; ++j) s[j] = c[j];
+                    if (CUT) break;
+                }
                 const int begin = block + w * R;
                 if (begin >= p.end) continue;
 #pragma unroll
                 for (int j = 0; j < V; ++j) A[j] = lds[buf][w][0][j][lane], B[j] = lds[buf][w][1][j][lane];
                 rec_join<T, GATE, V, false>(a, l, begin, min(begin + R, p.end), A, B, c);
             }
+            if (!CUT) buf ^= 1;
         } else {
 #pragma unroll
             for (int j = 0; j < V; ++j) s[j] = c[j];
         }
+        if (a.tape && words > 0 && ((row - p.lo) & (REC_TAPE - 1)) == 0) l.store(rec_tape(a, p, row), s);
+        T *h = static_cast<T *>(a.h) + row * a.h_row;
+        rec_each<R>(words, [&](int k) __attribute__((always_inline)) {
+            G.at(k, f, i);
 #pragma unroll
-        for (int k = 0; k < R; ++k) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) s[j] = fmaf(f[k][j], s[j], u[k][j]);
-            if (row + k < p.end) {
-                l.store(static_cast<T *>(a.h) + (row + k) * a.h_row, s);
-                if (a.h_last && row + k == p.hi - 1) l.store(a.h_last + (long long)p.tree * a.C, s);
-            }
-        }
+            for (int j = 0; j < V; ++j) s[j] = fmaf(f[j], s[j], i[j] * X.get(k, j));
+            l.store(h, s);
+            h += a.h_row;
+        });
+        if (a.h_last && words > 0 && row + R >= p.hi) l.store(a.h_last + (long long)p.tree * a.C, s);
+        if constexpr (CUT)
+            if (wave == W - 1 && p.part < p.parts - 1 && p.part % REC_GROUP == REC_GROUP - 1) rec_publish(a.states + (long long)(slot / REC_GROUP) * a.C, l, s);
         if constexpr (W == 1)
 #pragma unroll
             for (int j = 0; j < V; ++j) c[j] = s[j];
+        if (!more) break;
     }
 }
 
 // ---- gradients -----------------------------------------------------------------------------------
 
-template <typename T, int V, int W, int R, int GATE> __global__ __launch_bounds__(64 * W) void k_recur_back(RecurArgs a)
+template <typename T, int V, int W, int R, int GATE, bool CUT> __global__ __launch_bounds__(64 * W) void k_recur_back(RecurArgs a)
 {
-    static_assert(REC_TAPE == W * R, "a block starts from a state of the tape");
-    __shared__ float lds[2][W][3][V][64];
+    static_assert((W * R) % REC_TAPE == 0, "a block starts from a state of the tape");
+    constexpr bool KEEP = !CUT;
+    __shared__ float lds[CUT ? 1 : 2][W][3][V][64];
+    __shared__ RecEnter<V, W> enter[1];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int slot = blockIdx.x / a.slices, slice = blockIdx.x - slot * a.slices;
+    // (parts in the order in which gradients pass them)
+    const int from_end = blockIdx.x / a.slices, slice = blockIdx.x - from_end * a.slices, slot = a.slots - 1 - from_end;
     const RecLane<V> l(slice, lane, a.C);
     {   // rows behind the last sentence
         const int tail = min(max(__builtin_amdgcn_readfirstlane(a.off[a.n_trees]), 0), a.n_rows);
@@ -366,10 +573,10 @@ template <typename T, int V, int W, int R, int GATE> __global__ __launch_bounds_
             l.store(static_cast<T *>(a.d_x) + r * a.d_x_row, none);
         }
     }
-    const RecPart p(a, slot);
+    const RecPart p = RecPart::of<CUT>(a, slot);
     if (!p.there) return;
     float c[V];
-    rec_enter<T, GATE, V, true>(a, p, l, c);
+    rec_start(a.d_last, p, l, a.C, c);
     if (p.lo == p.hi) {
         if (a.d_h0 && wave == 0) l.store(a.d_h0 + (long long)p.tree * a.C, c);
         return;
@@ -378,90 +585,119 @@ template <typename T, int V, int W, int R, int GATE> __global__ __launch_bounds_
     float s0[V];
     auto load = [&](int block) {
         const int row = block + wave * R;
-        l.load(a.tape + (((long long)p.lo / REC_TAPE) + p.tree + (block - p.lo) / REC_TAPE) * a.C, s0);
+        l.load(rec_tape(a, p, block), s0);
+        g.clear();
+        x.clear();
+        d.clear();
         if (row >= p.end) return;
         g.load(a.g, a.g_row, l, row, p.end);
         x.load(a.x, a.x_row, l, row, p.end);
-        if (a.d_h) d.load(a.d_h, a.d_h_row, l, row, p.end);
+        if (a.d_h) d.load(a.d_h, a.d_h_row, l, row, p.end);     // (zeros else)
     };
     const int blocks = (p.end - p.first + W * R - 1) / (W * R);
     load(p.first + (blocks - 1) * (W * R));
+    if constexpr (CUT)
+        if (threadIdx.x == 0) enter[0].late = 0;
     int buf = 0;
-    for (int n = blocks - 1; n >= 0; --n, buf ^= 1) {
-        const int block = p.first + n * (W * R), row = block + wave * R;
-        float f[R][V], i[R][V], q[R][V], e[R][V], s[V], m[V];
+#pragma unroll 1
+    for (int n = blocks - 1;; --n) {
+        const int block = p.first + n * (W * R), row = block + wave * R, words = p.end - row;
+        RecGates<T, V, R, GATE, KEEP> G(g);
+        RecRows<T, V, R> X = x, E = d;
+        float f[V], i[V], s[V], m[V], A[V], B[V], D[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) s[j] = s0[j];
-#pragma unroll
-        for (int k = 0; k < R; ++k)
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                rec_gates<GATE>(g.get(k, j), f[k][j], i[k][j]);
-                q[k][j] = x.get(k, j);
-                e[k][j] = a.d_h ? d.get(k, j) : 0.f;
-                if (row + k >= p.end) f[k][j] = 1.f, i[k][j] = q[k][j] = e[k][j] = 0.f;
-            }
-        if (n > 0) load(block - W * R);
-        {
-            float A[V], B[V], D[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                A[j] = 1.f, B[j] = D[j] = 0.f;
-#pragma unroll
-                for (int k = 0; k < R; ++k) {
-                    A[j] *= f[k][j];
-                    B[j] = fmaf(f[k][j], B[j], i[k][j] * q[k][j]);
-                }
-#pragma unroll
-                for (int k = R - 1; k >= 0; --k) D[j] = f[k][j] * (D[j] + e[k][j]);
-                lds[buf][wave][0][j][lane] = A[j];
-                lds[buf][wave][1][j][lane] = B[j];
-                lds[buf][wave][2][j][lane] = D[j];
-            }
-            __syncthreads();
-            for (int w = 0; w < wave; ++w) {
-                const int begin = block + w * R;
-#pragma unroll
-                for (int j = 0; j < V; ++j) A[j] = lds[buf][w][0][j][lane], B[j] = lds[buf][w][1][j][lane];
-                if (begin < p.end) rec_join<T, GATE, V, false>(a, l, begin, min(begin + R, p.end), A, B, s);
-            }
-#pragma unroll
-            for (int w = W - 1; w >= 0; --w) {
-                if (w == wave)
-#pragma unroll
-                    for (int j = 0; j < V; ++j) m[j] = c[j];
-                const int begin = block + w * R;
-                if (begin >= p.end) continue;
-#pragma unroll
-                for (int j = 0; j < V; ++j) A[j] = lds[buf][w][0][j][lane], D[j] = lds[buf][w][2][j][lane];
-                rec_join<T, GATE, V, true>(a, l, begin, min(begin + R, p.end), A, D, c);
-            }
+        for (int j = 0; j < V; ++j) {
+            s[j] = s0[j];
+            A[j] = 1.f, B[j] = D[j] = 0.f;
         }
-        // forwards: what a word's own lambda is multiplied by in the gradient of its gate
-#pragma unroll
-        for (int k = 0; k < R; ++k)
+        const bool more = !CUT && n > 0;
+        if (more) load(block - W * R);
+        rec_each<R>(words, [&](int k) __attribute__((always_inline)) {
+            G.at(k, f, i);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float before = s[j];
-                s[j] = fmaf(f[k][j], before, i[k][j] * q[k][j]);
-                q[k][j] = GATE == TL_GATE_SIGMOID ? (before - q[k][j]) * (f[k][j] * i[k][j]) : before;
+                A[j] *= f[j];
+                B[j] = fmaf(f[j], B[j], i[j] * X.get(k, j));
+                D[j] = fmaf(A[j], E.get(k, j), D[j]);           // (what comes back from word k passes the gates of words 0 .. k)
             }
+        });
+        G.forget();
 #pragma unroll
-        for (int k = R - 1; k >= 0; --k) {
+        for (int j = 0; j < V; ++j) {
+            lds[buf][wave][0][j][lane] = A[j];
+            lds[buf][wave][1][j][lane] = B[j];
+            lds[buf][wave][2][j][lane] = D[j];
+        }
+        __syncthreads();
+        if constexpr (CUT)
+            if (p.parts > 1) {
+                if (wave == W - 1 && p.part > 0) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+#pragma unroll
+                        for (int w = W - 2; w >= 0; --w) {
+                            A[j] *= lds[0][w][0][j][lane];
+                            D[j] = fmaf(lds[0][w][0][j][lane], D[j], lds[0][w][2][j][lane]);
+                        }
+                    rec_publish(a.pairs + (long long)slot * a.C, l, A, D);
+                }
+                rec_enter<T, GATE, V, W, true>(a, p, l, wave, enter[0], c);
+            }
+#pragma unroll 1
+        for (int w = 0; w < wave; ++w) {
+            const int begin = block + w * R;
+#pragma unroll
+            for (int j = 0; j < V; ++j) A[j] = lds[buf][w][0][j][lane], B[j] = lds[buf][w][1][j][lane];
+            if (begin < p.end) rec_join<T, GATE, V, false>(a, l, begin, min(begin + R, p.end), A, B, s);
+        }
+#pragma unroll 1
+        for (int w = W - 1; w >= 0; --w) {
+            if (w == wave) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) m[j] = c[j];
+                if (CUT) break;
+            }
+            const int begin = block + w * R;
+            if (begin >= p.end) continue;
+#pragma unroll
+            for (int j = 0; j < V; ++j) A[j] = lds[buf][w][0][j][lane], D[j] = lds[buf][w][2][j][lane];
+            rec_join<T, GATE, V, true>(a, l, begin, min(begin + R, p.end), A, D, c);
+        }
+        if (!CUT) buf ^= 1;
+        // forwards: what a word's own lambda is multiplied by in the gradient of its gate, but for f i
+        float q[R][V];
+        rec_each<R>(words, [&](int k) __attribute__((always_inline)) {
+            G.at(k, f, i);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float v = X.get(k, j);
+                q[k][j] = GATE == TL_GATE_SIGMOID ? s[j] - v : s[j];
+                s[j] = fmaf(f[j], s[j], i[j] * v);
+            }
+        });
+        G.forget();
+        const int top = min(words, R) - 1;
+        T *at_g = static_cast<T *>(a.d_g) + (row + top) * a.d_g_row, *at_x = static_cast<T *>(a.d_x) + (row + top) * a.d_x_row;
+        rec_each_back<R>(words, [&](int k) __attribute__((always_inline)) {
+            G.at(k, f, i);
             float dg[V], dx[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float lambda = e[k][j] + m[j];
-                dg[j] = lambda * q[k][j];
-                dx[j] = lambda * i[k][j];
-                m[j] = f[k][j] * lambda;
+                const float lambda = E.get(k, j) + m[j];
+                dx[j] = lambda * i[j];
+                m[j] = lambda * f[j];
+                dg[j] = (GATE == TL_GATE_SIGMOID ? m[j] * i[j] : lambda) * q[k][j];
             }
-            if (row + k < p.end) {
-                l.store(static_cast<T *>(a.d_g) + (row + k) * a.d_g_row, dg);
-                l.store(static_cast<T *>(a.d_x) + (row + k) * a.d_x_row, dx);
-            }
+            l.store(at_g, dg);
+            l.store(at_x, dx);
+            at_g -= a.d_g_row;
+            at_x -= a.d_x_row;
+        });
+        if (wave == 0) {
+            if (a.d_h0 && block == p.lo) l.store(a.d_h0 + (long long)p.tree * a.C, m);
+            if (CUT && p.part > 0 && (p.parts - 1 - p.part) % REC_GROUP == REC_GROUP - 1) rec_publish(a.states + (long long)(slot / REC_GROUP) * a.C, l, m);
         }
-        if (a.d_h0 && wave == 0 && block == p.lo) l.store(a.d_h0 + (long long)p.tree * a.C, m);
+        if (!more) break;
     }
 }
 
