@@ -6,7 +6,12 @@ using namespace tl;
 
 namespace {
 
-constexpr int WIDE = 1024, NARROW = 256;        // threads of a row's workgroup
+constexpr int WIDE = 512, NARROW = 256;         // threads of a row's workgroup
+
+// Logits that are read past the caches: those of a list of words, which nothing reads again, and those that are too many to be there when the gradient
+// reads them (256 MB hold them, and what it writes).  Measured (us, kept / past): 512 x 131072 bf16 with a list 55 / 48, with gradients 4096 x 50000 bf16 237 / 209, 813 x
+// 20000 fp32 36 / 40.
+bool once(const ScoreArgs &a, int size) { return a.top > 0 || (double)a.n_rows * a.vocab * size > 1.3e8; }
 
 bool check(int dtype, int n_rows, int vocab, const void *logits, long long row)
 {
@@ -15,27 +20,34 @@ bool check(int dtype, int n_rows, int vocab, const void *logits, long long row)
 
 bool word_pointer(const void *p) { return ((uintptr_t)p & 3) == 0; }
 
-// Parts that a row is cut into: few rows are divided among workgroups as long as a part keeps 4096 words.
+// Parts that a row is cut into: few rows are divided among workgroups where a row is long enough to pay for the second launch, which joins them.  Measured (us,
+// whole / in parts of 16384 words): 1 x 50000 bf16 with 5 words 11.0 / 12.6, 1 x 131072 fp32 18.0 / 15.0, 64 x 131072 bf16 18.7 / 17.4, without words 18.4 / 13.0, 128 x 131072
+// fp32 with 20 words 23 / 28; parts of 4096: 1 x 20000 fp32 8.3 / 10.6, 1 x 131072 22.0.
 int parts_of(long long rows, long long vocab)
 {
-    const long long wanted = compute_units();
-    if (rows == 0 || 2 * rows > wanted || vocab < 2 * 4096) return 1;
-    long long n = wanted / rows;
-    if (n > vocab / 4096) n = vocab / 4096;
+    const long long units = compute_units();
+    if (rows == 0 || 4 * rows > units || vocab < 4 * 16384) return 1;
+    const long long n = units / rows < vocab / 16384 ? units / rows : vocab / 16384;
     return (int)(n > 64 ? 64 : n);
 }
 
 long long workspace(long long rows, int parts, int top) { return parts == 1 ? 0 : round16(rows * parts * (16 + (top > 0 ? 8ll * SCO_TOP : 0))); }
 
+template <typename T, bool TOP, bool ONCE> void launch_rows(const ScoreArgs &a, unsigned blocks, bool wide, hipStream_t st)
+{
+    if (wide) hipLaunchKernelGGL((k_score<T, WIDE, TOP, ONCE>), dim3(blocks), dim3(WIDE), 0, st, a);
+    else hipLaunchKernelGGL((k_score<T, NARROW, TOP, ONCE>), dim3(blocks), dim3(NARROW), 0, st, a);
+}
+
 template <typename T, bool TOP> hipError_t forward_of(ScoreArgs a, hipStream_t st)
 {
-    // (a narrow workgroup's waves have a few thousand words each; wide ones hide the loads of long rows)
+    // (narrow workgroups for short rows and parts: their waves have more than a round of pieces each)
     const bool wide = a.parts == 1 && (long long)a.vocab * sizeof(T) >= 32768;
     const long long most = most_blocks(wide ? WIDE : NARROW) / a.parts;
     for (long long left = a.n_rows; left > 0; left -= most, a.first += most) {
         const unsigned n = (unsigned)((left < most ? left : most) * a.parts);
-        if (wide) hipLaunchKernelGGL((k_score<T, WIDE, TOP>), dim3(n), dim3(WIDE), 0, st, a);
-        else hipLaunchKernelGGL((k_score<T, NARROW, TOP>), dim3(n), dim3(NARROW), 0, st, a);
+        if (once(a, sizeof(T))) launch_rows<T, TOP, true>(a, n, wide, st);
+        else launch_rows<T, TOP, TOP>(a, n, wide, st);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -51,7 +63,9 @@ template <typename T> hipError_t backward(ScoreArgs a, hipStream_t st)
     a.parts = (a.vocab + WORDS - 1) / WORDS;
     const long long most = most_blocks(SCO_BACK_THREADS) / a.parts;
     for (long long left = a.n_rows; left > 0; left -= most, a.first += most) {
-        hipLaunchKernelGGL(k_score_back<T>, dim3((unsigned)((left < most ? left : most) * a.parts)), dim3(SCO_BACK_THREADS), 0, st, a);
+        const dim3 grid((unsigned)((left < most ? left : most) * a.parts));
+        if (once(a, sizeof(T))) hipLaunchKernelGGL((k_score_back<T, true>), grid, dim3(SCO_BACK_THREADS), 0, st, a);
+        else hipLaunchKernelGGL((k_score_back<T, false>), grid, dim3(SCO_BACK_THREADS), 0, st, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

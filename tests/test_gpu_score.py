@@ -109,7 +109,7 @@ def test_rows(dtype, V):
         check(logits(n, V, TYPES[dtype]), words(n, V), top, back=top == 0)
 
 
-@pytest.mark.parametrize("n,V", [(1, 8192), (1, 30000), (2, 100003), (100, 9000), (127, 20001), (300, 9000)])
+@pytest.mark.parametrize("n,V", [(1, 8192), (1, 65536), (1, 300001), (2, 100003), (64, 65539), (100, 9000), (300, 9000)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_few_rows_divided_among_workgroups(dtype, n, V):
     check(logits(n, V, TYPES[dtype]), words(n, V), 20, back=False)
@@ -241,7 +241,7 @@ def test_without_words():
 
 
 def test_bits_repeat_on_another_stream_and_in_a_graph():
-    for n, V in ((1, 60000), (40, 7000)):
+    for n, V in ((1, 70000), (40, 7000)):
         x, w = logits(n, V, torch.float32), torch.tensor(words(n, V), dtype=torch.int32, device="cuda")
         dl = torch.ones(n, device="cuda")
 
