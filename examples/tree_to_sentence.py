@@ -6,7 +6,12 @@ training step is given the sentences: one tl_attend reads for all their words, t
 those of the nodes' states go on through tl_backward into the encoder.  Parameters and sentences are random: there is no data set
 here, and what is written means nothing.
 
+With --recurrent the decoder's state runs along the words by a gated linear recurrence from the tree's root (tl_recur): a training step takes
+whole sentences at once, with dropout (tl_dropout) and the words' log probabilities as its loss (tl_score and its gradient); a word is written by the
+same calls on one row per tree, states updated in place.
+
     python examples/tree_to_sentence.py --tokens 20 --steps 5
+    python examples/tree_to_sentence.py --recurrent
 """
 import argparse
 import os
@@ -34,6 +39,54 @@ class Attend(torch.autograd.Function):
         q, k, v, o, lse, q_off, kv_off, kv_mask = ctx.saved_tensors
         g = binding.tl_attend_backward(q, k, v, o, lse, d_o.contiguous(), q_off, kv_off, kv_mask)
         return g["d_q"], g["d_k"], g["d_v"], None, None, None
+
+
+class Recur(torch.autograd.Function):
+    """tl_recur from first states h0, with its gradients."""
+
+    @staticmethod
+    def forward(ctx, g, x, h0, off):
+        out = binding.tl_recur(g, x, off, h0, with_tape=True)
+        ctx.save_for_backward(g, x, off, out["tape"])
+        return out["h"]
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_h):
+        g, x, off, tape = ctx.saved_tensors
+        d = binding.tl_recur_backward(g, x, off, tape, d_h.contiguous())
+        return d["d_g"], d["d_x"], d["d_h0"], None
+
+
+class Dropout(torch.autograd.Function):
+    """residual + dropout(x): no mask is kept, the backward pass draws the same numbers again."""
+
+    @staticmethod
+    def forward(ctx, x, residual, p, numbers):
+        ctx.p = p
+        ctx.save_for_backward(numbers.clone())                  # (the next step's are other ones)
+        return binding.tl_dropout(x, p, numbers, residual)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_y):
+        d_y = d_y.contiguous()
+        return binding.tl_dropout(d_y, ctx.p, *ctx.saved_tensors), d_y, None, None
+
+
+class LogProb(torch.autograd.Function):
+    """Log probabilities of given words, and the entropies."""
+
+    @staticmethod
+    def forward(ctx, logits, word):
+        out = binding.tl_score(logits, word)
+        ctx.save_for_backward(logits, word, out["stats"])
+        return out["logprob"], out["entropy"]
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_logprob, d_entropy):
+        return binding.tl_score_backward(*ctx.saved_tensors, d_logprob.contiguous(), d_entropy.contiguous()), None
 
 
 class Decoder:
@@ -64,6 +117,105 @@ class Decoder:
         o = read((x @ self.w_q).view(-1, self.heads, self.head_dim))
         y = torch.tanh(x + o.reshape(x.shape) @ self.w_o)
         return y, y @ self.words.t()
+
+
+class RecurrentDecoder(Decoder):
+    """A decoder whose state is a gated mean of what the words so far brought, from the root of its tree on."""
+
+    def __init__(self, hidden, vocab, **more):
+        super().__init__(hidden, vocab, **more)
+        self.w_state = self.w_state.detach().repeat(1, 2).requires_grad_()              # gates and inputs of the recurrence: halves of one projection's rows
+
+    def states(self, last, h0, off):
+        """State behind every word of `last` (sentences cut by off)."""
+        both = (self.words[last] @ self.w_state).view(-1, 2, h0.shape[1])
+        return Recur.apply(both[:, 0], both[:, 1], h0, off)
+
+    def logits(self, h, read, drop=None):
+        """drop: (share, numbers) in training."""
+        o = read((h @ self.w_q).view(-1, self.heads, self.head_dim)).reshape(h.shape) @ self.w_o
+        y = torch.tanh(Dropout.apply(o, h, *drop) if drop else h + o)
+        return y, y @ self.words.t()
+
+
+def previous_words(sentences, s_off):
+    """What every word follows: a sentence's first word follows word 0."""
+    last = torch.cat([sentences.new_zeros(1), sentences[:-1]])
+    last[s_off[:-1][s_off[:-1] < s_off[1:]].long()] = 0
+    return last
+
+
+def score(decoder, batch, sentences, s_off, n_top=0, kv_mask=None):
+    """tl_score of given sentences: log probability of every word, entropies, and the words that were more probable in its place."""
+    with torch.no_grad():
+        k, v = decoder.nodes(batch["h"])
+        h = decoder.states(previous_words(sentences, s_off), batch["h_root"], s_off)
+        _, logits = decoder.logits(h, lambda q: binding.tl_attend(q, k, v, s_off, batch["tree_off"], kv_mask))
+        return binding.tl_score(logits, sentences, n_top)
+
+
+def recurrent_loss(decoder, h, h_root, tree_off, sentences, s_off, drop=None, reward=0.0, kv_mask=None):
+    """Mean of the words' negative log probabilities, less `reward` times their distributions' entropies."""
+    k, v = decoder.nodes(h)
+    state = decoder.states(previous_words(sentences, s_off), h_root, s_off)
+    _, logits = decoder.logits(state, lambda q: Attend.apply(q, k, v, s_off, tree_off, kv_mask), drop)
+    logprob, entropy = LogProb.apply(logits, sentences)
+    return -(logprob + reward * entropy).mean()
+
+
+def recurrent_step(net, decoder, batch, embed_dim, sentences, s_off, lr, drop=None, reward=0.0, kv_mask=None):
+    """One step of gradient descent through decoder and encoder; drop: (share, numbers), whose step is counted on.  Returns the loss (a CUDA
+    scalar)."""
+    binding.tl_set_keep_gates(net.ctx, True)
+    net.forward()
+    h = batch["h"].detach().requires_grad_()
+    h_root = h[batch["root"].long()]
+    loss = recurrent_loss(decoder, h, h_root, batch["tree_off"], sentences, s_off, drop, reward, kv_mask)
+    params = decoder.parameters()
+    *grads, d_h = torch.autograd.grad(loss, params + [h])
+    encoder = binding.tl_backward(net.ctx, batch, d_h.contiguous(), embed_dim)
+    binding.tl_sgd_update(net.ctx, lr, batch, encoder)
+    with torch.no_grad():
+        for p, g in zip(params, grads):
+            p.sub_(lr * g)
+        if drop:
+            drop[1][1:].add_(1)
+    return loss.detach()
+
+
+def write_recurrent(decoder, batch, n_tokens, u, kv_mask=None, temperature=1.0):
+    """n_tokens words for every tree, as write does it, recorded once and replayed: the recurrence takes a row per tree and updates its states in place."""
+    trees, dev = batch["B"], u.device
+    hidden = batch["h_root"].shape[1]
+    one_each = torch.arange(trees + 1, dtype=torch.int32, device=dev)
+    warmth = torch.full((trees,), temperature, device=dev)
+    state, word, number = batch["h_root"].clone(), torch.zeros(trees, dtype=torch.int32, device=dev), u[0].clone()
+
+    @torch.no_grad()
+    def token():
+        both = (decoder.words[word] @ decoder.w_state).view(-1, 2, hidden)
+        h = binding.tl_recur(both[:, 0], both[:, 1], one_each, state, h_last=state)["h"]
+        _, logits = decoder.logits(h, lambda q: binding.tl_attend(q, k, v, one_each, batch["tree_off"], kv_mask))
+        out = binding.tl_sample(logits, number, warmth)
+        word.copy_(out["token"])
+        return out
+
+    with torch.no_grad():
+        k, v = decoder.nodes(batch["h"])
+    token()                                     # (libraries set themselves up outside the recording)
+    state.copy_(batch["h_root"])
+    word.zero_()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = token()
+    tokens = torch.empty(n_tokens, trees, dtype=torch.int32, device=dev)
+    logprob = torch.empty(n_tokens, trees, device=dev)
+    for i in range(n_tokens):
+        number.copy_(u[i])
+        graph.replay()
+        tokens[i].copy_(out["token"])
+        logprob[i].copy_(out["logprob"])
+    return tokens, logprob
 
 
 def write(decoder, batch, n_tokens, u, kv_mask=None, temperature=0.8, top_k=0, top_p=0.9, min_p=0.0):
@@ -138,6 +290,8 @@ def main(argv=None):
     ap.add_argument("--tokens", type=int, default=20)
     ap.add_argument("--steps", type=int, default=5, help="training steps before the sentences are written")
     ap.add_argument("--lr", type=float, default=0.5)
+    ap.add_argument("--recurrent", action="store_true", help="a state that runs along the words, dropout, the entropy's reward")
+    ap.add_argument("--dropout", type=float, default=0.1)
     ap.add_argument("--leaves-only", action="store_true", help="read the leaves' states alone")
     ap.add_argument("--seed", type=int, default=0)
     args = ap.parse_args(argv)
@@ -145,15 +299,22 @@ def main(argv=None):
     net = binding.TreeNet(w.params, scheduler="level_device")
     batch = net.load(w.trees)
     mask = (batch["left"] < 0) if args.leaves_only else None
-    decoder = Decoder(w.params.hidden, w.params.vocab, seed=args.seed)
+    decoder = (RecurrentDecoder if args.recurrent else Decoder)(w.params.hidden, w.params.vocab, seed=args.seed)
+    numbers = torch.tensor([args.seed, 0], device="cuda")
     sentences, s_off = random_sentences(batch["B"], w.params.vocab, 5, 60, args.seed)
     for step in range(args.steps):
-        loss = train_step(net, decoder, batch, w.params.embed_dim, sentences, s_off, args.lr, mask)
+        if args.recurrent:
+            loss = recurrent_step(net, decoder, batch, w.params.embed_dim, sentences, s_off, args.lr, (args.dropout, numbers), 0.01, mask)
+        else:
+            loss = train_step(net, decoder, batch, w.params.embed_dim, sentences, s_off, args.lr, mask)
         print("step %d: loss %.4f" % (step, loss.item()))
     net.forward()
     gen = torch.Generator(device="cuda").manual_seed(args.seed)
     u = torch.rand(args.tokens, batch["B"], generator=gen, device="cuda")
-    tokens, logprob = write(decoder, batch, args.tokens, u, mask)
+    tokens, logprob = (write_recurrent if args.recurrent else write)(decoder, batch, args.tokens, u, mask)
+    if args.recurrent:
+        told = score(decoder, batch, sentences, s_off, 3, mask)
+        print("given sentences: log probability of a word %.2f, entropy %.2f" % (told["logprob"].mean().item(), told["entropy"].mean().item()))
     for tree in range(min(3, batch["B"])):
         print("tree %d (log probability %.2f):" % (tree, logprob[:, tree].sum().item()), *tokens[:, tree].tolist())
     net.close()

@@ -474,13 +474,15 @@ assert struct.calcsize("5i4x3Q2q") == ctypes.sizeof(tl_recurrence)
 def _recurrence(g, x, off, gate, index) -> bytes:
     import torch
     n, channels = g.shape
+    dtype = g.dtype
     assert index == x.get_device() == off.get_device(), "tensors of one device"
-    assert x.dtype == g.dtype and x.shape == g.shape
+    assert x.dtype is dtype and x.shape == g.shape
     g_row, g_c = g.stride()
     x_row, x_c = x.stride()
     assert channels == 1 or g_c == x_c == 1, "channels must be contiguous"
-    assert off.dtype == torch.int32 and off.is_contiguous() and off.numel() >= 1
-    return _PACK_RECURRENCE(_dtype(g), gate, off.numel() - 1, n, channels, off.data_ptr(), g.data_ptr(), x.data_ptr(), g_row, x_row)
+    n_off = off.numel()
+    assert off.dtype is torch.int32 and off.is_contiguous() and n_off >= 1
+    return _PACK_RECURRENCE(_dtype(g), gate, n_off - 1, n, channels, off.data_ptr(), g.data_ptr(), x.data_ptr(), g_row, x_row)
 
 
 def _recur_workspace(r, backward, device):
@@ -493,14 +495,23 @@ def _recur_workspace(r, backward, device):
 
 def _states(t, index, shape):
     import torch
-    assert t is None or (t.get_device() == index and t.dtype == torch.float32 and t.is_contiguous() and tuple(t.shape) == shape)
-    return _ptr(t)
+    if t is None:
+        return None
+    assert t.get_device() == index and t.dtype is torch.float32 and t.is_contiguous() and t.shape == shape
+    return t.data_ptr()
 
 
 def _like(t, like, index):
     """Rows of the type and shape of `like`: address and stride."""
-    assert t.get_device() == index and t.dtype == like.dtype and t.shape == like.shape and (t.shape[1] == 1 or t.stride(1) == 1)
-    return t.data_ptr(), t.stride(0)
+    row, c = t.stride()
+    assert t.get_device() == index and t.dtype is like.dtype and t.shape == like.shape and (c == 1 or t.shape[1] == 1)
+    return t.data_ptr(), row
+
+
+def _new_like(t, shape):
+    """A new contiguous tensor of the type of t."""
+    import torch
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(shape)
 
 
 def tl_recur(g, x, off, h0=None, gate=TL_GATE_SIGMOID, h=None, h_last=None, with_last=False, with_tape=False, stream=None):
@@ -518,16 +529,23 @@ def tl_recur(g, x, off, h0=None, gate=TL_GATE_SIGMOID, h=None, h_last=None, with
     trees, device = off.numel() - 1, g.device
     state = (trees, channels)
     if h is None:
-        h = torch.empty((n, channels), dtype=g.dtype, device=device)
+        h = _new_like(g, (n, channels))
+        at, row = h.data_ptr(), channels
+    else:
+        at, row = _like(h, g, index)
     out = {"h": h}
-    if h_last is None and with_last:
-        h_last = torch.empty(state, dtype=torch.float32, device=device)
+    first, last, tape = _states(h0, index, state), None, None
     if h_last is not None:
+        last = _states(h_last, index, state)
+    elif with_last:
+        h_last = torch.empty_like(h0) if h0 is not None else torch.empty(state, dtype=torch.float32, device=device)
+        last = h_last.data_ptr()
+    if last is not None:
         out["h_last"] = h_last
     if with_tape:
-        out["tape"] = torch.empty((n // 64 + trees, channels), dtype=torch.float32, device=device)
-    at, row = _like(h, g, index)
-    call, first, last, tape, st = lib().tl_recur, _states(h0, index, state), _states(h_last, index, state), _ptr(out.get("tape")), _raw_stream(index)
+        out["tape"] = t = torch.empty((n // 64 + trees, channels), dtype=torch.float32, device=device)
+        tape = t.data_ptr()
+    call, st = lib().tl_recur, _raw_stream(index)
     code = call(r, first, at, row, last, tape, None, 0, st)
     if code == TL_ELIMIT:
         ws, size = _recur_workspace(r, 0, device)
@@ -548,8 +566,9 @@ def tl_recur_backward(g, x, off, tape, d_h=None, d_last=None, gate=TL_GATE_SIGMO
     n, channels = g.shape
     trees, device = off.numel() - 1, g.device
     state = (trees, channels)
-    d_g, d_x = (torch.empty((n, channels), dtype=g.dtype, device=device) for _ in range(2))
-    d_h0 = torch.empty(state, dtype=torch.float32, device=device)
+    d_g = _new_like(g, (n, channels))
+    d_x = torch.empty_like(d_g)
+    d_h0 = torch.empty_like(d_last) if d_last is not None else torch.empty(state, dtype=torch.float32, device=device)
     at, row = _like(d_h, g, index) if d_h is not None else (None, 0)
     call, kept, last, st = lib().tl_recur_backward, _states(tape, index, (n // 64 + trees, channels)), _states(d_last, index, state), _raw_stream(index)
     rest = (d_g.data_ptr(), channels, d_x.data_ptr(), channels, d_h0.data_ptr())
@@ -563,14 +582,17 @@ def tl_recur_backward(g, x, off, tape, d_h=None, d_last=None, gate=TL_GATE_SIGMO
 
 def _words(t, n, index):
     import torch
-    assert t is None or (t.get_device() == index and t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n)
-    return _ptr(t)
+    if t is None:
+        return None
+    assert t.get_device() == index and t.dtype is torch.int32 and t.is_contiguous() and t.numel() == n
+    return t.data_ptr()
 
 
 def tl_score(logits, word=None, n_top=0, stream=None):
     """Log probabilities of given words, entropies, and the n_top (up to 64) most probable words of rows of logits [n, vocab] (float32, bfloat16 or
     float16; rows any stride apart); word [n] int32, outside [0, vocab) where a row has none.  Returns dict(entropy [n], stats [3, n] for
-    tl_score_backward, logprob [n] with words, top_word [n, n_top] int32 and top_logprob [n, n_top] with n_top > 0) of new tensors."""
+    tl_score_backward, logprob [n] with words, top_word [n, n_top] int32 and top_logprob [n, n_top] with n_top > 0) of new tensors; entropy is a row
+    of stats."""
     import torch
     index = logits.get_device()
     if stream is not None or torch._C._cuda_getDevice() != index:
@@ -578,18 +600,22 @@ def tl_score(logits, word=None, n_top=0, stream=None):
             return tl_score(logits, word, n_top)
     n, vocab = logits.shape
     device, dtype = logits.device, _dtype(logits)
-    assert vocab == 1 or logits.stride(1) == 1
+    row, c = logits.stride()
+    assert vocab == 1 or c == 1
     words = _words(word, n, index)
     stats = torch.empty((3, n), dtype=torch.float32, device=device)
+    at = stats.data_ptr()
     out = {"entropy": stats[2], "stats": stats}
-    if word is not None:
-        out["logprob"] = torch.empty(n, dtype=torch.float32, device=device)
+    log_at = top_at = top_log_at = None
+    if words is not None:
+        out["logprob"] = t = torch.empty(n, dtype=torch.float32, device=device)
+        log_at = t.data_ptr()
     if n_top > 0:
-        out["top_word"] = torch.empty((n, n_top), dtype=torch.int32, device=device)
-        out["top_logprob"] = torch.empty((n, n_top), dtype=torch.float32, device=device)
+        out["top_word"] = t = torch.empty((n, n_top), dtype=torch.int32, device=device)
+        out["top_logprob"] = p = torch.empty((n, n_top), dtype=torch.float32, device=device)
+        top_at, top_log_at = t.data_ptr(), p.data_ptr()
     call, st = lib().tl_score, _raw_stream(index)
-    args = (dtype, n, vocab, logits.data_ptr(), logits.stride(0), words, n_top, _ptr(out.get("logprob")), stats.data_ptr(), _ptr(out.get("top_word")),
-            _ptr(out.get("top_logprob")))
+    args = (dtype, n, vocab, logits.data_ptr(), row, words, n_top, log_at, at, top_at, top_log_at)
     code = call(*args, None, 0, st)
     if code == TL_ELIMIT:
         size = ctypes.c_int64()
@@ -609,11 +635,14 @@ def tl_score_backward(logits, word, stats, d_logprob=None, d_entropy=None, d_log
         with _elsewhere(index, stream):
             return tl_score_backward(logits, word, stats, d_logprob, d_entropy, d_logits)
     n, vocab = logits.shape
-    assert vocab == 1 or logits.stride(1) == 1
+    x_row, c = logits.stride()
+    assert vocab == 1 or c == 1
     if d_logits is None:
-        d_logits = torch.empty((n, vocab), dtype=logits.dtype, device=logits.device)
-    at, row = _like(d_logits, logits, index)
-    _check(lib().tl_score_backward(_dtype(logits), n, vocab, logits.data_ptr(), logits.stride(0), _words(word, n, index), _states(stats, index, (3, n)),
+        d_logits = _new_like(logits, (n, vocab))
+        at, row = d_logits.data_ptr(), vocab
+    else:
+        at, row = _like(d_logits, logits, index)
+    _check(lib().tl_score_backward(_dtype(logits), n, vocab, logits.data_ptr(), x_row, _words(word, n, index), _states(stats, index, (3, n)),
                                    _states(d_logprob, index, (n,)), _states(d_entropy, index, (n,)), at, row, _raw_stream(index)), "tl_score_backward")
     return d_logits
 
@@ -629,12 +658,15 @@ def tl_dropout(x, p, numbers, residual=None, y=None, stream=None):
             return tl_dropout(x, p, numbers, residual, y)
     n, cols = x.shape
     assert numbers.get_device() == index and numbers.dtype in (torch.int64, torch.uint64) and numbers.is_contiguous() and numbers.numel() == 2
-    if y is None:
-        y = torch.empty((n, cols), dtype=x.dtype, device=x.device)
-    x_at, x_row = _like(x, x, index)
+    x_row, c = x.stride()
+    assert cols == 1 or c == 1
     r_at, r_row = _like(residual, x, index) if residual is not None else (None, 0)
-    y_at, y_row = _like(y, x, index)
-    _check(lib().tl_dropout(_dtype(x), n, cols, x_at, x_row, r_at, r_row, y_at, y_row, p, numbers.data_ptr(), _raw_stream(index)), "tl_dropout")
+    if y is None:
+        y = _new_like(x, (n, cols))
+        y_at, y_row = y.data_ptr(), cols
+    else:
+        y_at, y_row = _like(y, x, index)
+    _check(lib().tl_dropout(_dtype(x), n, cols, x.data_ptr(), x_row, r_at, r_row, y_at, y_row, p, numbers.data_ptr(), _raw_stream(index)), "tl_dropout")
     return y
 
 

@@ -233,10 +233,6 @@ template <typename T> __device__ inline void sco_answer(const ScoreArgs &a, long
 
 // ---- one row, or one part of it, per workgroup ------------------------------------------------------
 
-template <typename T> struct __attribute__((packed, aligned(16))) ScoPiece {
-    T v[16 / sizeof(T)];
-};
-
 // 16 bytes at any address of the type.  ONCE: they need no place in the caches.
 template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) ScoAny {
     T v[16 / sizeof(T)];
@@ -278,8 +274,7 @@ template <typename T, int NT, bool TOP, bool ONCE> __global__ __launch_bounds__(
     const int size = (((a.vocab + a.parts - 1) / a.parts) + E - 1) / E * E;
     const int begin = (int)min((long long)part * size, (long long)a.vocab), n = min(size, a.vocab - begin);
     const T *const p = static_cast<const T *>(a.logits) + row * a.row + begin;
-    const int head = min(n, (int)((16 - ((uintptr_t)p & 15)) & 15) / (int)sizeof(T));
-    const int pieces = (n - head) / E, edge = n - pieces * E;       // words in front of the first whole piece and behind the last one
+    const int pieces = n / E, edge = n - pieces * E;            // (16 bytes at any address: what a row gives does not depend on where it lies)
     ScoSums s = {-SCO_LARGE * SCO_LOG2_E, 0.f, 0.f};
     float m = -INFINITY;
     ScoList top;
@@ -326,18 +321,18 @@ template <typename T, int NT, bool TOP, bool ONCE> __global__ __launch_bounds__(
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int e = 0; e < E; ++e) v[u][e] = -INFINITY;
-        at[0] = tid < head ? tid : tid + pieces * E;
+        at[0] = pieces * E + tid;
 #pragma unroll
         for (int u = 1; u < U; ++u) at[u] = 0;
         if (tid < edge) v[0][0] = (float)p[at[0]];
         at[0] += begin;
         take(v, at);
     }
-    ScoPiece<T> next[U];
+    ScoAny<T> next[U];
     auto load = [&](int i) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (i + u * NT < pieces) sco_load<ONCE>(next[u], p + head + (i + u * NT) * E);
+            if (i + u * NT < pieces) sco_load<ONCE>(next[u], p + (i + u * NT) * E);
     };
     load(tid);
     for (int g = wave * 64; g < pieces; g += U * NT) {          // (the same in all lanes of a wave)
@@ -351,7 +346,7 @@ template <typename T, int NT, bool TOP, bool ONCE> __global__ __launch_bounds__(
         for (int u = 0; u < U; ++u) {
 #pragma unroll
             for (int e = 0; e < E; ++e) v[u][e] = (float)next[u].v[e];
-            at[u] = begin + head + (i + u * NT) * E;
+            at[u] = begin + (i + u * NT) * E;
         }
         load(i + U * NT);
         // (once a first round of pieces is there, and once a fourth is: rounds that all lanes take part in)
