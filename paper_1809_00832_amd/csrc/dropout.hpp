@@ -7,7 +7,7 @@
 // call at 16-bit types; the share of dropped values is then a multiple of 2^-16, and the factor is that share's own, so that the expectation is exact.
 #pragma once
 
-#include "attend.hpp"
+#include "stream.hpp"
 
 namespace tl {
 
@@ -37,7 +37,7 @@ __device__ inline u32x4 dro_philox(u32x4 c, uint32_t k0, uint32_t k1)
 }
 
 // A thread: eight columns of a row.
-template <typename T, bool RESIDUAL> __global__ __launch_bounds__(DRO_THREADS) void k_dropout(DropArgs a)
+template <typename T, bool RESIDUAL, bool ONCE> __global__ __launch_bounds__(DRO_THREADS) void k_dropout(DropArgs a)
 {
     struct __attribute__((packed, aligned(sizeof(T)))) Eight {
         T v[8];
@@ -54,22 +54,30 @@ template <typename T, bool RESIDUAL> __global__ __launch_bounds__(DRO_THREADS) v
     const T *const x = static_cast<const T *>(a.x) + row * a.x_row + col;
     const T *const r = RESIDUAL ? static_cast<const T *>(a.residual) + row * a.r_row + col : nullptr;
     T *const y = static_cast<T *>(a.y) + row * a.y_row + col;
-    const u32x4 w = dro_philox(u32x4{block, (uint32_t)row, (uint32_t)step, (uint32_t)(step >> 32)}, (uint32_t)seed, (uint32_t)(seed >> 32));
-    auto value = [&](T v, T old, int j) {
-        const uint32_t piece = j & 1 ? w[j >> 1] >> 16 : w[j >> 1] & 0xffffu;
-        const float s = piece < a.t ? 0.f : (float)v * a.scale;
-        return (T)(RESIDUAL ? (float)old + s : s);
-    };
+    Eight v, old = {};                                          // (read before the numbers are made: the rounds run while the values come)
     if (n == 8) {
-        Eight v = *reinterpret_cast<const Eight *>(x), old = {};
-        if (RESIDUAL) old = *reinterpret_cast<const Eight *>(r);
+        stream_load<ONCE>(v, x);
+        if (RESIDUAL) stream_load<ONCE>(old, r);
+    } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v.v[j] = value(v.v[j], old.v[j], j);
+        for (int j = 0; j < 8; ++j) {
+            v.v[j] = j < n ? x[j] : (T)0.f;
+            if (RESIDUAL) old.v[j] = j < n ? r[j] : (T)0.f;
+        }
+    }
+    const u32x4 w = dro_philox(u32x4{block, (uint32_t)row, (uint32_t)step, (uint32_t)(step >> 32)}, (uint32_t)seed, (uint32_t)(seed >> 32));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t piece = j & 1 ? w[j >> 1] >> 16 : w[j >> 1] & 0xffffu;
+        const float s = piece < a.t ? 0.f : (float)v.v[j] * a.scale;
+        v.v[j] = (T)(RESIDUAL ? (float)old.v[j] + s : s);
+    }
+    if (n == 8) {
         *reinterpret_cast<Eight *>(y) = v;
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (j < n) y[j] = value(x[j], RESIDUAL ? r[j] : (T)0.f, j);
+            if (j < n) y[j] = v.v[j];
     }
 }
 

@@ -29,7 +29,7 @@ struct Plan {
     int V, slices, shift, slots;
     bool single, cut;                           // a wave per sentence; parts
     long long blocks, pairs, states, parts, copy;               // bytes of the workspace's parts
-    long long workspace() const { return pairs + states + parts + copy; }
+    long long workspace() const { return pairs + states + parts + copy + (cut ? 16 : 0); }
 };
 
 // Whether sentences are cut into parts, by their words on average (the host does not know the lengths, and a batch with one sentence much longer than the
@@ -82,6 +82,7 @@ void lay_out(const Plan &p, void *workspace, RecurArgs *a)
     a->pairs = reinterpret_cast<uint64_t *>(base);
     a->states = reinterpret_cast<uint32_t *>(base + p.pairs);
     a->parts = reinterpret_cast<int4 *>(base + p.pairs + p.states);
+    a->broken = reinterpret_cast<uint32_t *>(base + p.pairs + p.states + p.parts + p.copy);
     if (p.copy && a->h0) a->copy = reinterpret_cast<float *>(base + p.pairs + p.states + p.parts);
 }
 

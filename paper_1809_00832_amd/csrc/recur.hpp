@@ -36,6 +36,7 @@ struct RecurArgs {
     uint32_t *states;                           // behind every 32nd part of a sentence
     int4 *parts;                                // of every part: its sentence, that one's words, the slot of its first part
     float *copy;                                // of h0, which h_last may be written over
+    uint32_t *broken;                           // not 0 once a wait has run out: no other waits as long again
     int n_trees, n_rows, C, slices, slots, shift;
 };
 
@@ -257,7 +258,7 @@ template <typename T, int V, int R, int GATE, bool KEEP> struct RecGates {
 // published behind every 32nd part: a part needs the state behind the last such part before it, and the pairs from there on, 31 at most.  Values are
 // published as they are, in words that were filled with ones before: a word that is no longer all ones is complete, and no fence is needed.
 // Parts are numbered in the order in which a state passes them, and workgroups are started in that order, so that what is waited for has been started.
-// Every wait ends all the same: after REC_POLLS polls the words in question are walked, from the start of the sentence.
+// Every wait ends all the same: after REC_POLLS polls (tenths of a second) the words in question are walked, from the start of the sentence.
 
 constexpr int REC_GROUP = 32, REC_POLLS = 1 << 16;
 constexpr uint32_t REC_NAN = 0x7fc00000u;       // published for a NaN that is all ones
@@ -282,7 +283,7 @@ template <int V> __device__ inline void rec_publish(uint32_t *at, const RecLane<
 }
 
 // Whether the words came.
-template <int V, int N, typename W> __device__ inline bool rec_wait(W *const (&at)[N], int n, const RecLane<V> &l, W (&v)[N][V])
+template <int V, int N, typename W> __device__ inline bool rec_wait(const RecurArgs &a, W *const (&at)[N], int n, const RecLane<V> &l, W (&v)[N][V])
 {
 #pragma unroll 1
     for (int poll = 0; poll < REC_POLLS; ++poll) {
@@ -296,8 +297,10 @@ template <int V, int N, typename W> __device__ inline bool rec_wait(W *const (&a
                     there = there && v[k][j] != (W)~(W)0;
                 }
         if (__all(there)) return true;
+        if ((poll & 255) == 255 && __hip_atomic_load(a.broken, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != 0) return false;
         __builtin_amdgcn_s_sleep(1);
     }
+    __hip_atomic_store(a.broken, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     return false;
 }
 
@@ -320,7 +323,7 @@ __device__ inline void rec_enter(const RecurArgs &a, const RecPart &p, const Rec
         if (group > 0) {
             uint32_t *const at[1] = {a.states + (long long)(slot(group - 1) / REC_GROUP) * a.C};
             uint32_t v[1][V];
-            fine = rec_wait<V, 1>(at, 1, l, v);
+            fine = rec_wait<V, 1>(a, at, 1, l, v);
 #pragma unroll
             for (int j = 0; j < V; ++j) s[j] = __uint_as_float(v[0][j]);
         }
@@ -338,7 +341,7 @@ __device__ inline void rec_enter(const RecurArgs &a, const RecPart &p, const Rec
             uint64_t *at[N], v[N][V];
 #pragma unroll
             for (int k = 0; k < N; ++k) at[k] = a.pairs + (long long)slot(group + first + min(i + k, n - 1)) * a.C;
-            fine = rec_wait<V, N>(at, n - i, l, v) && fine;
+            fine = rec_wait<V, N>(a, at, n - i, l, v) && fine;
 #pragma unroll
             for (int k = 0; k < N; ++k)
                 if (i + k < n)
@@ -398,6 +401,7 @@ __global__ __launch_bounds__(256) void k_recur_prepare(RecurArgs a, long long n_
         const int lo = place(t);
         a.parts[slot] = int4{t, lo, max(place(t + 1), lo), (lo >> a.shift) + t};
     }
+    if (at == 0) *a.broken = 0;
     for (long long i = at; i < n_words; i += step) a.pairs[i] = ~0ull;      // (pairs, and the states behind them)
     if (a.copy)
         for (long long i = at; i < n_copy; i += step) a.copy[i] = a.h0[i];
@@ -452,6 +456,7 @@ template <typename T, int V, int W, int R, int GATE, bool CUT, bool ONCE = false
     constexpr bool KEEP = !CUT && W > 1;
     __shared__ float lds[W > 1 && !CUT ? 2 : 1][W][2][V][64];
     __shared__ RecEnter<V, W> enter[1];                         // (CUT only)
+    __shared__ float begin_state[V][64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int slot = blockIdx.x / a.slices, slice = blockIdx.x - slot * a.slices;
     const RecPart p = RecPart::of<CUT>(a, slot);
@@ -466,8 +471,13 @@ template <typename T, int V, int W, int R, int GATE, bool CUT, bool ONCE = false
         x.template load<ONCE>(a.x, a.x_row, l, row, p.end);
     };
     load(p.first + wave * R);
-    float c[V];
-    rec_start(CUT ? a.copy : a.h0, p, l, a.C, c);
+    // (one wave reads h0 and hands it on: h_last may lie in the same place, and must not be written before it has been read)
+    float c[V] = {};
+    if (wave == 0) {
+        rec_start(CUT ? a.copy : a.h0, p, l, a.C, c);
+#pragma unroll
+        for (int j = 0; j < V; ++j) begin_state[j][lane] = c[j];
+    }
     if (p.lo == p.hi) {                                         // no words
         if (a.h_last && wave == 0) l.store(a.h_last + (long long)p.tree * a.C, c);
         return;
@@ -502,6 +512,9 @@ template <typename T, int V, int W, int R, int GATE, bool CUT, bool ONCE = false
                 lds[buf][wave][1][j][lane] = B[j];
             }
             __syncthreads();                                    // (the other buffer is written only after the next one)
+            if (block == p.first)
+#pragma unroll
+                for (int j = 0; j < V; ++j) c[j] = begin_state[j][lane];
             if constexpr (CUT)
                 if (p.parts > 1) {
                     if (wave == 0 && p.part < p.parts - 1) {

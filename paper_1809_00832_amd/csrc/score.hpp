@@ -12,6 +12,7 @@
 
 #include "attend.hpp"
 #include "sample.hpp"
+#include "stream.hpp"
 
 namespace tl {
 
@@ -233,31 +234,9 @@ template <typename T> __device__ inline void sco_answer(const ScoreArgs &a, long
 
 // ---- one row, or one part of it, per workgroup ------------------------------------------------------
 
-// 16 bytes at any address of the type.  ONCE: they need no place in the caches.
 template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) ScoAny {
     T v[16 / sizeof(T)];
 };
-template <bool ONCE, typename T, typename P> __device__ inline void sco_load(P &to, const T *from)
-{
-    typedef u32x4 __attribute__((aligned(2))) Words;
-    if constexpr (ONCE) {
-        const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const Words *>(from));
-        __builtin_memcpy(&to, &w, 16);
-    } else {
-        __builtin_memcpy(&to, reinterpret_cast<const P *>(from), 16);
-    }
-}
-template <bool ONCE, typename T, typename P> __device__ inline void sco_store(T *to, const P &from)
-{
-    typedef u32x4 __attribute__((aligned(2))) Words;
-    if constexpr (ONCE) {
-        u32x4 w;
-        __builtin_memcpy(&w, &from, 16);
-        __builtin_nontemporal_store(w, reinterpret_cast<Words *>(to));
-    } else {
-        __builtin_memcpy(reinterpret_cast<P *>(to), &from, 16);
-    }
-}
 
 template <typename T, int NT, bool TOP, bool ONCE> __global__ __launch_bounds__(NT) void k_score(ScoreArgs a)
 {
@@ -332,7 +311,7 @@ template <typename T, int NT, bool TOP, bool ONCE> __global__ __launch_bounds__(
     auto load = [&](int i) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (i + u * NT < pieces) sco_load<ONCE>(next[u], p + (i + u * NT) * E);
+            if (i + u * NT < pieces) stream_load<ONCE>(next[u], p + (i + u * NT) * E);
     };
     load(tid);
     for (int g = wave * 64; g < pieces; g += U * NT) {          // (the same in all lanes of a wave)
@@ -464,7 +443,7 @@ template <typename T, bool ONCE> __global__ __launch_bounds__(SCO_BACK_THREADS) 
     const float dl = there && a.d_logprob ? a.d_logprob[row] : 0.f, dh = a.d_entropy && some ? a.d_entropy[row] : 0.f;
     const int pieces = n / E;
     if (dl == 0.f && dh == 0.f) {                               // (a row without a word costs no reads)
-        for (int i = tid; i < pieces; i += NT) sco_store<ONCE>(out + i * E, Any{});
+        for (int i = tid; i < pieces; i += NT) stream_store<ONCE>(out + i * E, Any{});
         if (pieces * E + tid < n) out[pieces * E + tid] = (T)0.f;
         return;
     }
@@ -488,7 +467,7 @@ template <typename T, bool ONCE> __global__ __launch_bounds__(SCO_BACK_THREADS) 
     Any v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-        if (tid + u * NT < pieces) sco_load<ONCE>(v[u], x + (tid + u * NT) * E);
+        if (tid + u * NT < pieces) stream_load<ONCE>(v[u], x + (tid + u * NT) * E);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int i = tid + u * NT;
@@ -500,7 +479,7 @@ template <typename T, bool ONCE> __global__ __launch_bounds__(SCO_BACK_THREADS) 
 #pragma unroll
                 for (int e = 0; e < E; ++e)
                     if (w == i * E + e) o.v[e] = (T)(gradient((float)v[u].v[e]) + dl);
-            sco_store<ONCE>(out + i * E, o);
+            stream_store<ONCE>(out + i * E, o);
         }
     }
     const int j = pieces * E + tid;

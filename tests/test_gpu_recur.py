@@ -395,3 +395,22 @@ def test_no_words_at_all():
     assert torch.equal(back["d_h0"], h0)
     none = torch.empty(0, 20, device="cuda")
     binding.tl_recur(none, none, offsets([]), None)
+
+
+@pytest.mark.parametrize("n,scale", [(300, 1), (3000, 10)])
+def test_offsets_that_are_not_offsets(n, scale):
+    """Results are unspecified, but nothing outside the arrays is written: rows and states stand between others that keep their values.  (Parts that wait for
+    words that nobody publishes give up.)"""
+    C, trees = 20, 6
+    off = torch.tensor([-7, 250 * scale, 20, 2 ** 31 - 1, -2 ** 31, 100 * scale, n], dtype=torch.int32, device="cuda")
+    outer = torch.full((n + 200, 3 * C), 3.0, device="cuda")
+    states = torch.full((3 * trees, C), 4.0, device="cuda")
+    g, x, _, d_h, _ = inputs([n], C, torch.float32, SIGMOID)
+    h = outer[100:100 + n, C:2 * C]
+    last = states[trees:2 * trees]
+    tape = binding.tl_recur(g, x, off, last, h=h, h_last=last, with_tape=True)["tape"]
+    binding.tl_recur_backward(g, x, off, tape, d_h, last)
+    torch.cuda.synchronize()
+    inside = torch.zeros_like(outer, dtype=torch.bool)
+    inside[100:100 + n, C:2 * C] = True
+    assert (outer[~inside] == 3).all() and (states[:trees] == 4).all() and (states[2 * trees:] == 4).all()
