@@ -9,6 +9,7 @@ namespace {
 // Waves of a workgroup, words that each takes at a time and bytes of a row that a lane has: of whole sentences, and of parts of cut ones.
 constexpr int F_WAVES = 4, F_WORDS = 8, F_BYTES = 4;
 constexpr int B_WAVES = 4, B_WORDS = 16, B_BYTES = 4;
+constexpr int FB_WAVES = 4, FB_WORDS = 8, BB_WAVES = 4, BB_WORDS = 16;
 constexpr int FC_WAVES = 8, FC_WORDS = 32, FC_BYTES = 4;
 constexpr int BC_WAVES = 8, BC_WORDS = 16, BC_BYTES = 4;
 
@@ -27,7 +28,7 @@ bool check(const tl_recurrence *r)
 
 struct Plan {
     int V, slices, shift, slots;
-    bool single, cut;                           // a wave per sentence; parts
+    bool single, brief, cut;                    // a wave per sentence; sentences of a block or two; parts
     long long blocks, pairs, states, parts, copy;               // bytes of the workspace's parts
     long long workspace() const { return pairs + states + parts + copy + (cut ? 16 : 0); }
 };
@@ -36,6 +37,8 @@ struct Plan {
 // others waits for it).  A whole sentence is a chain of blocks, a part waits for others and needs a launch more.  Measured (us, whole / cut, states
 // alone; words x channels, bf16): 40 sentences of 100 x 512 12.1 / 13.0, 60 of 400 34.8 / 34.3, 60 of 1000 72 / 60, 100 of 400 44 / 47, 100 of 1000 98 / 88, 256 of 750 151 / 161,
 // 4 of 1500 x 256 116 / 17; with gradients 30 / 34, 85 / 82, 179 / 159, 112 / 119, 253 / 244, 409 / 449, 287 / 37.
+// Sentences that end within a block, more of them than the chip holds at once, need no registers for the block after it (brief).  Measured (us, with gradients, with
+// those registers / without): 2000 sentences of 15 words x 256 bf16 71 / 49, 1024 of 15 x 256 fp32 42 / 38, 256 of 27 x 512 bf16 29.5 / 30.2.
 bool plan(const tl_recurrence *r, bool back, Plan *p)
 {
     const long long rows = r->n_rows, trees = r->n_trees;
@@ -44,6 +47,7 @@ bool plan(const tl_recurrence *r, bool back, Plan *p)
     const long long workgroups = trees * ((r->channels + 64 * whole_V - 1) / (64 * whole_V));
     p->cut = rows > 128 * trees && rows / trees > 2 * workgroups;
     p->single = !back && !p->cut && rows <= 8 * trees;
+    p->brief = !p->cut && rows <= 32 * trees && workgroups >= 8 * compute_units();
     p->V = p->cut ? (back ? BC_BYTES : FC_BYTES) / size : whole_V;
     if (r->channels < p->V) p->V = 1;
     p->slices = (r->channels + 64 * p->V - 1) / (64 * p->V);
@@ -94,16 +98,19 @@ template <auto KERNEL> hipError_t start(const RecurArgs &a, const Plan &p, int w
 
 template <typename T, int V, int GATE> hipError_t forward_of(const RecurArgs &a, const Plan &p, hipStream_t st)
 {
-    if (p.cut && !a.tape) return start<k_recur<T, V, FC_WAVES, FC_WORDS, GATE, true, true>>(a, p, FC_WAVES, st);
-    if (p.cut) return start<k_recur<T, V, FC_WAVES, FC_WORDS, GATE, true>>(a, p, FC_WAVES, st);
-    if (p.single) return start<k_recur<T, V, 1, F_WORDS, GATE, false>>(a, p, 1, st);
-    return start<k_recur<T, V, F_WAVES, F_WORDS, GATE, false>>(a, p, F_WAVES, st);
+    if (p.cut && !a.tape) return start<k_recur<T, V, FC_WAVES, FC_WORDS, GATE, true, true, false>>(a, p, FC_WAVES, st);
+    if (p.cut) return start<k_recur<T, V, FC_WAVES, FC_WORDS, GATE, true, false, false>>(a, p, FC_WAVES, st);
+    if (p.single) return start<k_recur<T, V, 1, F_WORDS, GATE, false, false, true>>(a, p, 1, st);
+    if (p.brief) return start<k_recur<T, V, FB_WAVES, FB_WORDS, GATE, false, false, false>>(a, p, FB_WAVES, st);
+    if (!a.tape) return start<k_recur<T, V, F_WAVES, F_WORDS, GATE, false, true, true>>(a, p, F_WAVES, st);
+    return start<k_recur<T, V, F_WAVES, F_WORDS, GATE, false, false, true>>(a, p, F_WAVES, st);
 }
 
 template <typename T, int V, int GATE> hipError_t backward_of(const RecurArgs &a, const Plan &p, hipStream_t st)
 {
-    if (p.cut) return start<k_recur_back<T, V, BC_WAVES, BC_WORDS, GATE, true>>(a, p, BC_WAVES, st);
-    return start<k_recur_back<T, V, B_WAVES, B_WORDS, GATE, false>>(a, p, B_WAVES, st);
+    if (p.cut) return start<k_recur_back<T, V, BC_WAVES, BC_WORDS, GATE, true, false>>(a, p, BC_WAVES, st);
+    if (p.brief) return start<k_recur_back<T, V, BB_WAVES, BB_WORDS, GATE, false, false>>(a, p, BB_WAVES, st);
+    return start<k_recur_back<T, V, B_WAVES, B_WORDS, GATE, false, true>>(a, p, B_WAVES, st);
 }
 
 template <typename T, int GATE> hipError_t launch_at(const RecurArgs &a, const Plan &p, bool back, hipStream_t st)

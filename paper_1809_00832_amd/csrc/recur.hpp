@@ -450,10 +450,11 @@ template <int R, typename F> __device__ __forceinline__ void rec_each_back(int w
 // their gates twice, for the pair and for the states: that costs less than the registers of the results, which would halve the waves of a compute unit.
 // ONCE: nothing reads g and x again (there is no tape); a branch on the tape in the kernel would cost what the other loads gain.  Measured (us, two sentences of
 // 26 000 words in all, bf16 x 2048): 97 with ordinary loads, 91 so; a training step of eight of 1 800 words x 1024: 72.5 and 74.
-template <typename T, int V, int W, int R, int GATE, bool CUT, bool ONCE = false> __global__ __launch_bounds__(64 * W) void k_recur(RecurArgs a)
+template <typename T, int V, int W, int R, int GATE, bool CUT, bool ONCE, bool AHEAD> __global__ __launch_bounds__(64 * W) void k_recur(RecurArgs a)
 {
     static_assert(REC_TAPE % R == 0, "states of the tape lie where a wave's words begin");
-    constexpr bool KEEP = !CUT && W > 1;
+    static_assert(!(CUT && AHEAD), "a part is one block");
+    constexpr bool KEEP = AHEAD && W > 1;
     __shared__ float lds[W > 1 && !CUT ? 2 : 1][W][2][V][64];
     __shared__ RecEnter<V, W> enter[1];                         // (CUT only)
     __shared__ float begin_state[V][64];
@@ -491,7 +492,7 @@ template <typename T, int V, int W, int R, int GATE, bool CUT, bool ONCE = false
         RecGates<T, V, R, GATE, KEEP> G(g);
         RecRows<T, V, R> X = x;
         const bool more = !CUT && block + W * R < p.end;
-        if (more) load(row + W * R);
+        if (AHEAD && more) load(row + W * R);
         float f[V], i[V], s[V];
         if constexpr (W > 1) {
             float A[V], B[V];
@@ -563,15 +564,17 @@ template <typename T, int V, int W, int R, int GATE, bool CUT, bool ONCE = false
 #pragma unroll
             for (int j = 0; j < V; ++j) c[j] = s[j];
         if (!more) break;
+        if (!AHEAD) load(row + W * R);
     }
 }
 
 // ---- gradients -----------------------------------------------------------------------------------
 
-template <typename T, int V, int W, int R, int GATE, bool CUT> __global__ __launch_bounds__(64 * W) void k_recur_back(RecurArgs a)
+template <typename T, int V, int W, int R, int GATE, bool CUT, bool AHEAD> __global__ __launch_bounds__(64 * W) void k_recur_back(RecurArgs a)
 {
     static_assert((W * R) % REC_TAPE == 0, "a block starts from a state of the tape");
-    constexpr bool KEEP = !CUT;
+    static_assert(!(CUT && AHEAD), "a part is one block");
+    constexpr bool KEEP = AHEAD;
     __shared__ float lds[CUT ? 1 : 2][W][3][V][64];
     __shared__ RecEnter<V, W> enter[1];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -624,7 +627,7 @@ template <typename T, int V, int W, int R, int GATE, bool CUT> __global__ __laun
             A[j] = 1.f, B[j] = D[j] = 0.f;
         }
         const bool more = !CUT && n > 0;
-        if (more) load(block - W * R);
+        if (AHEAD && more) load(block - W * R);
         rec_each<R>(words, [&](int k) __attribute__((always_inline)) {
             G.at(k, f, i);
 #pragma unroll
@@ -711,6 +714,7 @@ template <typename T, int V, int W, int R, int GATE, bool CUT> __global__ __laun
             if (CUT && p.part > 0 && (p.parts - 1 - p.part) % REC_GROUP == REC_GROUP - 1) rec_publish(a.states + (long long)(slot / REC_GROUP) * a.C, l, m);
         }
         if (!more) break;
+        if (!AHEAD) load(block - W * R);
     }
 }
 
