@@ -557,9 +557,13 @@ int tl_sample(int dtype, int n_rows, int vocab, const void *logits, int64_t row,
  * A gated linear recurrence along sentences.  Rows are all sentences' words one after the other, cut by off; per channel
  *     h_t = f_t h_(t-1) + i_t x_t          h before a sentence's first word: its row of h0
  *     TL_GATE_SIGMOID  f = 1 / (1 + exp(-g)),  i = 1 - f        TL_GATE_GIVEN  f = g,  i = 1
- * States and sums are fp32 whatever the type; h is rounded once, when it is stored.  Words that are far apart are joined as runs, so the last
- * bits differ from those of a loop over words, but infinities and NaN appear where the formula has them and reach only later words of
- * their channel and sentence.  Results repeat bit for bit.
+ * States and sums are fp32 whatever the type; h is rounded once, when it is stored.  Words are joined as runs, so the last bits differ from
+ * those of a loop over words, but infinities and NaN appear where the formula has them and reach only later words of
+ * their channel and sentence (a channel where joining runs gives an infinity is walked word by word, which takes long).  Results repeat bit for bit.
+ * Few long sentences are divided among workgroups that wait for one another's results, each only for such as have been started before it; every
+ * wait is bounded (some tenths of a second), and a workgroup whose wait runs out computes what it waited for: such a result is right, but
+ * its last bits may differ.  How sentences are divided goes by their words on average: a batch with one sentence much longer than the others waits for it.
+ * TL_EINVAL also where a launch would be too large: from n_trees * channels = 2^28 on (fp32; 16-bit types 2^29), fewer where channels < 64 (n_trees 2^22).
  */
 enum tl_gate { TL_GATE_SIGMOID = 0, TL_GATE_GIVEN = 1 };
 

@@ -508,6 +508,12 @@ def _like(t, like, index):
     return t.data_ptr(), row
 
 
+def _floats(t, shape):
+    """A new float32 tensor on the device of t.  (new_empty of t's own type takes a quarter less than torch.empty with a type and a device.)"""
+    import torch
+    return t.new_empty(shape) if t.dtype is torch.float32 else t.new_empty(shape, dtype=torch.float32)
+
+
 def _new_like(t, shape):
     """A new contiguous tensor of the type of t."""
     import torch
@@ -538,12 +544,12 @@ def tl_recur(g, x, off, h0=None, gate=TL_GATE_SIGMOID, h=None, h_last=None, with
     if h_last is not None:
         last = _states(h_last, index, state)
     elif with_last:
-        h_last = torch.empty_like(h0) if h0 is not None else torch.empty(state, dtype=torch.float32, device=device)
+        h_last = torch.empty_like(h0) if h0 is not None else _floats(g, state)
         last = h_last.data_ptr()
     if last is not None:
         out["h_last"] = h_last
     if with_tape:
-        out["tape"] = t = torch.empty((n // 64 + trees, channels), dtype=torch.float32, device=device)
+        out["tape"] = t = _floats(g, (n // 64 + trees, channels))
         tape = t.data_ptr()
     call, st = lib().tl_recur, _raw_stream(index)
     code = call(r, first, at, row, last, tape, None, 0, st)
@@ -568,7 +574,7 @@ def tl_recur_backward(g, x, off, tape, d_h=None, d_last=None, gate=TL_GATE_SIGMO
     state = (trees, channels)
     d_g = _new_like(g, (n, channels))
     d_x = torch.empty_like(d_g)
-    d_h0 = torch.empty_like(d_last) if d_last is not None else torch.empty(state, dtype=torch.float32, device=device)
+    d_h0 = torch.empty_like(d_last) if d_last is not None else _floats(g, state)
     at, row = _like(d_h, g, index) if d_h is not None else (None, 0)
     call, kept, last, st = lib().tl_recur_backward, _states(tape, index, (n // 64 + trees, channels)), _states(d_last, index, state), _raw_stream(index)
     rest = (d_g.data_ptr(), channels, d_x.data_ptr(), channels, d_h0.data_ptr())
@@ -603,16 +609,17 @@ def tl_score(logits, word=None, n_top=0, stream=None):
     row, c = logits.stride()
     assert vocab == 1 or c == 1
     words = _words(word, n, index)
-    stats = torch.empty((3, n), dtype=torch.float32, device=device)
+    stats = _floats(logits, (3, n))
     at = stats.data_ptr()
     out = {"entropy": stats[2], "stats": stats}
     log_at = top_at = top_log_at = None
     if words is not None:
-        out["logprob"] = t = torch.empty(n, dtype=torch.float32, device=device)
+        out["logprob"] = t = _floats(stats, (n,))
         log_at = t.data_ptr()
     if n_top > 0:
-        out["top_word"] = t = torch.empty((n, n_top), dtype=torch.int32, device=device)
-        out["top_logprob"] = p = torch.empty((n, n_top), dtype=torch.float32, device=device)
+        shape = (n, n_top)
+        out["top_word"] = t = word.new_empty(shape) if word is not None else torch.empty(shape, dtype=torch.int32, device=device)
+        out["top_logprob"] = p = _floats(stats, shape)
         top_at, top_log_at = t.data_ptr(), p.data_ptr()
     call, st = lib().tl_score, _raw_stream(index)
     args = (dtype, n, vocab, logits.data_ptr(), row, words, n_top, log_at, at, top_at, top_log_at)

@@ -47,7 +47,7 @@ bool plan(const tl_recurrence *r, bool back, Plan *p)
     const long long workgroups = trees * ((r->channels + 64 * whole_V - 1) / (64 * whole_V));
     p->cut = rows > 128 * trees && rows / trees > 2 * workgroups;
     p->single = !back && !p->cut && rows <= 8 * trees;
-    p->brief = !p->cut && rows <= 32 * trees && workgroups >= 8 * compute_units();
+    p->brief = !p->cut && rows <= 32 * trees && workgroups >= 1024 && workgroups >= 8 * compute_units();      // (asking for the units takes more than a microsecond)
     p->V = p->cut ? (back ? BC_BYTES : FC_BYTES) / size : whole_V;
     if (r->channels < p->V) p->V = 1;
     p->slices = (r->channels + 64 * p->V - 1) / (64 * p->V);

@@ -25,8 +25,9 @@ bool word_pointer(const void *p) { return ((uintptr_t)p & 3) == 0; }
 // fp32 with 20 words 23 / 28; parts of 4096: 1 x 20000 fp32 8.3 / 10.6, 1 x 131072 22.0.
 int parts_of(long long rows, long long vocab)
 {
+    if (rows == 0 || rows > 1024 || vocab < 4 * 16384) return 1;        // (asking for the units takes more than a microsecond)
     const long long units = compute_units();
-    if (rows == 0 || 4 * rows > units || vocab < 4 * 16384) return 1;
+    if (4 * rows > units) return 1;
     const long long n = units / rows < vocab / 16384 ? units / rows : vocab / 16384;
     return (int)(n > 64 ? 64 : n);
 }

@@ -414,3 +414,21 @@ def test_offsets_that_are_not_offsets(n, scale):
     inside = torch.zeros_like(outer, dtype=torch.bool)
     inside[100:100 + n, C:2 * C] = True
     assert (outer[~inside] == 3).all() and (states[:trees] == 4).all() and (states[2 * trees:] == 4).all()
+
+
+def test_four_million_sentences_of_a_word():
+    n = 4_000_000
+    g, x, h0 = (torch.randn(n, 3, device="cuda", generator=torch.Generator(device="cuda").manual_seed(k)) for k in range(3))
+    off = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    got = binding.tl_recur(g, x, off, h0, with_last=True, with_tape=True)
+    f = torch.sigmoid(g.double())
+    want = f * h0 + torch.sigmoid(-g.double()) * x
+    d = (2 * g.abs().double() + 12) * U * (f * h0.abs() + torch.sigmoid(-g.double()) * x.abs()) + 1e-37
+    assert ((got["h"] - want).abs() <= d + want.abs() * 2.0 ** -24).all() and torch.equal(got["h"], got["h_last"])
+    back = binding.tl_recur_backward(g, x, off, got["tape"], x)
+    assert ((back["d_h0"] - f * x).abs() <= (2 * g.abs().double() + 14) * U * (f * x).abs() + 1e-37).all()
+
+
+def test_one_sentence_of_many_parts():
+    """200 000 words of four channels: states behind every 32nd part are handed on fifty times."""
+    run([200_000], 4, torch.float32, SIGMOID)

@@ -265,3 +265,17 @@ def test_bits_repeat_on_another_stream_and_in_a_graph():
             eager = both()
             torch.cuda.synchronize()
             assert all(torch.equal(recorded[k], eager[k]) for k in eager)
+
+
+def test_more_rows_than_a_launch_has_workgroups():
+    n = (1 << 24) + 3
+    x = torch.randn(n, 2, device="cuda", generator=torch.Generator(device="cuda").manual_seed(0)).to(torch.bfloat16)
+    w = (torch.arange(n, device="cuda") % 3).int()              # (every third row has no word)
+    got = binding.tl_score(x, w)
+    logp = torch.log_softmax(x.float(), 1)
+    want = torch.where(w < 2, logp.gather(1, w.long().clamp(max=1)[:, None])[:, 0], 0.0)
+    assert (got["logprob"] - want).abs().max() <= 64 * U * 8    # (logits up to 6: differences up to 12, a few roundings each, on both sides)
+    dl = torch.ones(n, device="cuda")
+    d = binding.tl_score_backward(x, w, got["stats"], dl)
+    want = torch.where(w[:, None] < 2, (torch.arange(2, device="cuda") == w[:, None]).float() - logp.exp(), 0.0)
+    assert ((d - want).abs() <= want.abs() * 2.0 ** -8 + 64 * U).all()

@@ -65,6 +65,17 @@ def test_recurrence_workspace():
         assert workspace(recurrence(), back) == (OK, 0)
 
 
+def test_recurrences_that_would_be_too_large():
+    """2^22 workgroups, of which a sentence has one for every 64 (fp32) or 128 channels."""
+    for change, code in ((dict(n_trees=(1 << 22) - 1, channels=1), OK), (dict(n_trees=1 << 22, channels=1), EINVAL), (dict(n_trees=1 << 16, channels=4096), EINVAL),
+                         (dict(n_trees=(1 << 16) - 1, channels=4096), OK), (dict(n_trees=1 << 16, channels=4096, dtype=binding.TL_DT_F16), OK),
+                         (dict(n_trees=1 << 17, channels=4096, dtype=binding.TL_DT_BF16), EINVAL)):
+        r = recurrence(**change)
+        assert workspace(r)[0] == workspace(r, 1)[0] == code, change
+        if code == EINVAL:
+            assert forward(r, h_row=4096) == EINVAL and backward(r, d_h_row=4096, d_g_row=4096, d_x_row=4096) == EINVAL
+
+
 def test_recurrence_with_nothing_to_do():
     r = recurrence(n_trees=0, n_rows=0, off=None, g=None, x=None)
     assert workspace(r) == (OK, 0) and forward(r, h=None) == OK and backward(r, tape=None, d_g=None, d_x=None) == OK
