@@ -359,13 +359,15 @@ template <typename T, int NT, bool TOP, bool ONCE> __global__ __launch_bounds__(
     ScoSums x = sums[lane < WAVES ? lane : 0];
     ScoRow of = {m, 0.f, 0.f};
     if (fabsf(m) <= SCO_LARGE) {
-        const float r = sco_max(x.r);
-        x.scale(r);
-        const float z = sco_sum(lane < WAVES ? x.z : 0.f), t = sco_sum(lane < WAVES ? x.t : 0.f);
-        // ... and relative to m itself
-        const float lag = fmaf(m, SCO_LOG2_E, -r), c = __builtin_amdgcn_exp2f(-lag);
-        of.t = c * fmaf(-lag, z, t);
-        of.z = c * z;
+        if (wave == 0) {                                        // (which alone answers)
+            const float r = sco_max(x.r);
+            x.scale(r);
+            const float z = sco_sum(lane < WAVES ? x.z : 0.f), t = sco_sum(lane < WAVES ? x.t : 0.f);
+            // ... and relative to m itself
+            const float lag = fmaf(m, SCO_LOG2_E, -r), c = __builtin_amdgcn_exp2f(-lag);
+            of.t = c * fmaf(-lag, z, t);
+            of.z = c * z;
+        }
     } else if (m > -INFINITY) {                                 // (words at infinity share the mass)
         x = {0.f, 0.f, 0.f};
         for (int j = tid; j < n; j += NT) x.add_far((float)p[j], m);
