@@ -550,7 +550,7 @@ int tl_sample(int dtype, int n_rows, int vocab, const void *logits, int64_t row,
  *
  * What carries a state from word to word, regularises a training step, and says how probable words are.  As above: no context; the
  * current HIP device and hip_stream; nothing is allocated, nothing waits, and every call may be captured in a HIP graph.  Outputs must not overlap
- * inputs unless it is said below that they may.
+ * inputs unless it is said below that they may (an output at an input's address with another stride is refused).
  */
 
 /*

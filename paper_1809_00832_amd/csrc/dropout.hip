@@ -44,6 +44,7 @@ int tl_dropout(int dtype, int n_rows, int n_cols, const void *x, int64_t x_row, 
     if (!check_matrix(x, x_row, dtype, n_rows, n_cols, false) || !check_matrix(y, y_row, dtype, n_rows, n_cols, true)) return TL_EINVAL;
     if (residual && !check_matrix(residual, residual_row, dtype, n_rows, n_cols, false)) return TL_EINVAL;
     if (!numbers || ((uintptr_t)numbers & 7)) return TL_EINVAL;
+    if (n_rows > 1 && ((y == x && y_row != x_row) || (y == residual && y_row != residual_row))) return TL_EINVAL;
     DropArgs a = {};
     a.x = x;
     a.x_row = x_row;

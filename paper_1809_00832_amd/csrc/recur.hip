@@ -164,6 +164,7 @@ int tl_recur(const tl_recurrence *r, const float *h0, void *h, int64_t h_row, fl
     if (!check(r) || !check_matrix(h, h_row, r->dtype, r->n_rows, r->channels, true)) return TL_EINVAL;
     if (!float_pointer(h0) || !float_pointer(h_last) || !float_pointer(tape)) return TL_EINVAL;
     if (r->n_trees == 0) return TL_OK;
+    if (r->n_rows > 0 && (h == r->g || h == r->x)) return TL_EINVAL;         // (words that have to be walked are read a second time)
     Plan p;
     if (!plan(r, false, &p)) return TL_EINVAL;
     const long long need = p.workspace();
@@ -186,6 +187,10 @@ int tl_recur_backward(const tl_recurrence *r, const float *tape, const void *d_h
     if (!check_matrix(d_g, d_g_row, r->dtype, r->n_rows, r->channels, true) || !check_matrix(d_x, d_x_row, r->dtype, r->n_rows, r->channels, true)) return TL_EINVAL;
     if (!float_pointer(tape) || !float_pointer(d_last) || !float_pointer(d_h0) || (r->n_rows > 0 && !tape)) return TL_EINVAL;
     if (r->n_trees == 0) return TL_OK;
+    if (d_h0 && d_h0 == d_last) return TL_EINVAL;
+    for (const void *out : {d_g, d_x})
+        if (r->n_rows > 0 && (out == r->g || out == r->x || out == d_h)) return TL_EINVAL;
+    if (r->n_rows > 0 && d_g == d_x) return TL_EINVAL;
     Plan p;
     if (!plan(r, true, &p)) return TL_EINVAL;
     const long long need = p.workspace();

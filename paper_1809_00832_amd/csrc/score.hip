@@ -118,7 +118,7 @@ int tl_score_backward(int dtype, int n_rows, int vocab, const void *logits, int6
 {
     if (!check(dtype, n_rows, vocab, logits, row) || !check_matrix(d_logits, d_row, dtype, n_rows, vocab, true)) return TL_EINVAL;
     if (n_rows == 0) return TL_OK;
-    if (!stats || (d_logprob && !word)) return TL_EINVAL;
+    if (!stats || (d_logprob && !word) || (d_logits == logits && d_row != row && n_rows > 1)) return TL_EINVAL;
     for (const void *p : {(const void *)word, (const void *)stats, (const void *)d_logprob, (const void *)d_entropy})
         if (!word_pointer(p)) return TL_EINVAL;
     ScoreArgs a = {};

@@ -21,11 +21,14 @@ def workspace(r, backward=0):
     return binding.lib().tl_recur_workspace(ctypes.byref(r) if r else None, backward, ctypes.byref(n)), n.value
 
 
-def forward(r, h0=P, h=P, h_row=70, h_last=P, tape=P, ws=P, size=1 << 40):
+Q = P + (1 << 28)           # ... and for others
+
+
+def forward(r, h0=P, h=Q, h_row=70, h_last=P, tape=P, ws=P, size=1 << 40):
     return binding.lib().tl_recur(ctypes.byref(r) if r else None, h0, h, h_row, h_last, tape, ws, size, None)
 
 
-def backward(r, tape=P, d_h=P, d_h_row=70, d_last=P, d_g=P, d_g_row=70, d_x=P, d_x_row=70, d_h0=P, ws=P, size=1 << 40):
+def backward(r, tape=P, d_h=P, d_h_row=70, d_last=P, d_g=Q, d_g_row=70, d_x=Q + 4096, d_x_row=70, d_h0=Q, ws=P, size=1 << 40):
     return binding.lib().tl_recur_backward(ctypes.byref(r) if r else None, tape, d_h, d_h_row, d_last, d_g, d_g_row, d_x, d_x_row, d_h0, ws, size, None)
 
 
@@ -40,13 +43,15 @@ def test_recurrence_refuses(change):
     assert forward(r, h_row=row) == EINVAL and backward(r, d_h_row=row, d_g_row=row, d_x_row=row) == EINVAL
 
 
-@pytest.mark.parametrize("change", [dict(h=None), dict(h=P + 2), dict(h_row=69), dict(h_row=0), dict(h_row=-70), dict(h0=P + 2), dict(h_last=P + 1), dict(tape=P + 2)])
+@pytest.mark.parametrize("change", [dict(h=None), dict(h=P + 2), dict(h_row=69), dict(h_row=0), dict(h_row=-70), dict(h0=P + 2), dict(h_last=P + 1), dict(tape=P + 2),
+                                    dict(h=P)])
 def test_recurrence_outputs(change):
     assert forward(recurrence(), **change) == EINVAL
 
 
 @pytest.mark.parametrize("change", [dict(tape=None), dict(tape=P + 2), dict(d_h=P + 1), dict(d_h_row=-1), dict(d_last=P + 2), dict(d_g=None), dict(d_x=None), dict(d_g=P + 2),
-                                    dict(d_g_row=69), dict(d_x_row=0), dict(d_h0=P + 3)])
+                                    dict(d_g_row=69), dict(d_x_row=0), dict(d_h0=P + 3),
+                                    dict(d_g=P), dict(d_x=P), dict(d_g=Q + 4096), dict(d_h=Q), dict(d_last=Q)])
 def test_recurrence_gradients(change):
     assert backward(recurrence(), **change) == EINVAL
 
@@ -102,7 +107,7 @@ def score_backward(**change):
 
 @pytest.mark.parametrize("change", [dict(dtype=-1), dict(dtype=3), dict(n_rows=-1), dict(vocab=0), dict(vocab=(1 << 30) + 1), dict(logits=None), dict(logits=P + 2), dict(row=-1),
                                     dict(word=None), dict(word=P + 2), dict(stats=None), dict(stats=P + 1), dict(d_logprob=P + 2), dict(d_entropy=P + 1), dict(d_logits=None),
-                                    dict(d_logits=P + 2), dict(d_row=99), dict(d_row=0), dict(d_row=-100)])
+                                    dict(d_logits=P + 2), dict(d_row=99), dict(d_row=0), dict(d_row=-100), dict(d_row=200)])
 def test_gradient_of_scores_refuses(change):
     assert score_backward(**change) == EINVAL
 
@@ -129,14 +134,14 @@ def test_scores_of_no_rows():
 
 
 def dropout(**change):
-    v = dict(dtype=binding.TL_DT_F32, n_rows=3, n_cols=100, x=P, x_row=100, residual=P, residual_row=100, y=P, y_row=100, p=0.1, numbers=P, stream=None)
+    v = dict(dtype=binding.TL_DT_F32, n_rows=3, n_cols=100, x=P, x_row=100, residual=Q, residual_row=100, y=P, y_row=100, p=0.1, numbers=P, stream=None)
     v.update(change)
     return binding.lib().tl_dropout(*v.values())
 
 
 @pytest.mark.parametrize("change", [dict(dtype=-1), dict(dtype=3), dict(n_rows=-1), dict(n_cols=0), dict(n_cols=(1 << 30) + 1), dict(x=None), dict(x=P + 2), dict(x_row=-1),
                                     dict(residual=P + 1), dict(residual_row=-5), dict(y=None), dict(y=P + 2), dict(y_row=99), dict(y_row=0), dict(p=-0.1), dict(p=1.1),
-                                    dict(p=math.nan), dict(numbers=None), dict(numbers=P + 4), dict(dtype=binding.TL_DT_BF16, y=P + 1)])
+                                    dict(p=math.nan), dict(y_row=200), dict(x_row=0), dict(y=Q, residual_row=0), dict(numbers=None), dict(numbers=P + 4), dict(dtype=binding.TL_DT_BF16, y=P + 1)])
 def test_dropout_refuses(change):
     assert dropout(**change) == EINVAL
 
