@@ -6,12 +6,14 @@ using namespace tl;
 
 namespace {
 
-// Waves of a workgroup, words that each takes at a time and bytes of a row that a lane has: of whole sentences, and of parts of cut ones.
-constexpr int F_WAVES = 4, F_WORDS = 8, F_BYTES = 4;
-constexpr int B_WAVES = 4, B_WORDS = 16, B_BYTES = 4;
+// Waves of a workgroup and words that each takes at a time: whole sentences forwards (F) and backwards (B), many brief ones (FB, BB), parts (FC, BC) and large
+// parts (FL, BL) of cut ones.  A lane has 4 bytes of a row.
+constexpr int F_WAVES = 4, F_WORDS = 8;
+constexpr int B_WAVES = 4, B_WORDS = 16;
 constexpr int FB_WAVES = 4, FB_WORDS = 8, BB_WAVES = 4, BB_WORDS = 16;
-constexpr int FC_WAVES = 8, FC_WORDS = 32, FC_BYTES = 4;
-constexpr int BC_WAVES = 8, BC_WORDS = 16, BC_BYTES = 4;
+constexpr int FC_WAVES = 8, FC_WORDS = 16, FL_WAVES = 8, FL_WORDS = 32;
+constexpr int BC_WAVES = 8, BC_WORDS = 8, BL_WAVES = 8, BL_WORDS = 16;
+constexpr int LANE_BYTES = 4;
 
 // (as many words as a state's place and the block behind the last word can be counted in 32 bits with)
 constexpr int MOST_ROWS = INT32_MAX - 65536;
@@ -28,7 +30,7 @@ bool check(const tl_recurrence *r)
 
 struct Plan {
     int V, slices, shift, slots;
-    bool single, brief, cut;                    // a wave per sentence; sentences of a block or two; parts
+    bool narrow, single, brief, cut, large;                  // a wave per sentence; sentences of a block or two; parts
     long long blocks, pairs, states, parts, copy;               // bytes of the workspace's parts
     long long workspace() const { return pairs + states + parts + copy + (cut ? 16 : 0); }
 };
@@ -39,19 +41,28 @@ struct Plan {
 // 4 of 1500 x 256 116 / 17; with gradients 30 / 34, 85 / 82, 179 / 159, 112 / 119, 253 / 244, 409 / 449, 287 / 37.
 // Sentences that end within a block, more of them than the chip holds at once, need no registers for the block after it (brief).  Measured (us, with gradients, with
 // those registers / without): 2000 sentences of 15 words x 256 bf16 71 / 49, 1024 of 15 x 256 fp32 42 / 38, 256 of 27 x 512 bf16 29.5 / 30.2.
+// Large parts have half as many pairs to be taken, small ones fill the chip with fewer words and waste less of a sentence's last part.  Measured (us, large / small, bf16): states
+// of 2 sentences of 13 000 words x 2048 90 / 96, 8 of 1800 x 1024 32 / 35, 2 of 5000 x 2048 44 / 42, 60 of 1000 x 512 62 / 55, 4 of 1500 x 256 17.8 / 13.0; gradients
+// (less the states): 8 of 1800 x 1024 42 / 52, one of 8000 x 1024 32 / 42, one of 4000 x 1024 23 / 26, 4 of 1500 x 256 19 / 16.
 bool plan(const tl_recurrence *r, bool back, Plan *p)
 {
     const long long rows = r->n_rows, trees = r->n_trees;
-    const int size = element_size(r->dtype);
-    const int whole_V = (back ? B_BYTES : F_BYTES) / size;
-    const long long workgroups = trees * ((r->channels + 64 * whole_V - 1) / (64 * whole_V));
+    p->V = LANE_BYTES / element_size(r->dtype);
+    p->narrow = r->channels < p->V;             // fewer channels than a lane would have: one each
+    if (p->narrow) p->V = 1;
+    p->slices = (r->channels + 64 * p->V - 1) / (64 * p->V);
+    const long long workgroups = trees * p->slices;
     p->cut = rows > 128 * trees && rows / trees > 2 * workgroups;
     p->single = !back && !p->cut && rows <= 8 * trees;
     p->brief = !p->cut && rows <= 32 * trees && workgroups >= 1024 && workgroups >= 8 * compute_units();      // (asking for the units takes more than a microsecond)
-    p->V = p->cut ? (back ? BC_BYTES : FC_BYTES) / size : whole_V;
-    if (r->channels < p->V) p->V = 1;
-    p->slices = (r->channels + 64 * p->V - 1) / (64 * p->V);
-    p->shift = !p->cut ? REC_WHOLE : back ? log_2(BC_WAVES * BC_WORDS) : log_2(FC_WAVES * FC_WORDS);
+    p->large = false;
+    p->shift = REC_WHOLE;
+    if (p->cut) {
+        const int words = log_2(back ? BL_WAVES * BL_WORDS : FL_WAVES * FL_WORDS);
+        const long long blocks = ((rows >> words) + trees) * p->slices, units = compute_units();
+        p->large = back ? blocks >= units - units / 8 : 2 * blocks >= 3 * units && rows >= 1500 * trees;
+        p->shift = p->large ? words : log_2(back ? BC_WAVES * BC_WORDS : FC_WAVES * FC_WORDS);
+    }
     const long long slots = (rows >> p->shift) + trees;
     p->blocks = slots * p->slices;
     p->slots = (int)slots;
@@ -96,10 +107,15 @@ template <auto KERNEL> hipError_t start(const RecurArgs &a, const Plan &p, int w
     return hipGetLastError();
 }
 
+template <typename T, int V, int GATE, bool ONCE> hipError_t cut_of(const RecurArgs &a, const Plan &p, hipStream_t st)
+{
+    return p.large ? start<k_recur<T, V, FL_WAVES, FL_WORDS, GATE, true, ONCE, false>>(a, p, FL_WAVES, st)
+                   : start<k_recur<T, V, FC_WAVES, FC_WORDS, GATE, true, ONCE, false>>(a, p, FC_WAVES, st);
+}
+
 template <typename T, int V, int GATE> hipError_t forward_of(const RecurArgs &a, const Plan &p, hipStream_t st)
 {
-    if (p.cut && !a.tape) return start<k_recur<T, V, FC_WAVES, FC_WORDS, GATE, true, true, false>>(a, p, FC_WAVES, st);
-    if (p.cut) return start<k_recur<T, V, FC_WAVES, FC_WORDS, GATE, true, false, false>>(a, p, FC_WAVES, st);
+    if (p.cut) return a.tape ? cut_of<T, V, GATE, false>(a, p, st) : cut_of<T, V, GATE, true>(a, p, st);
     if (p.single) return start<k_recur<T, V, 1, F_WORDS, GATE, false, false, true>>(a, p, 1, st);
     if (p.brief) return start<k_recur<T, V, FB_WAVES, FB_WORDS, GATE, false, false, false>>(a, p, FB_WAVES, st);
     if (!a.tape) return start<k_recur<T, V, F_WAVES, F_WORDS, GATE, false, true, true>>(a, p, F_WAVES, st);
@@ -108,15 +124,19 @@ template <typename T, int V, int GATE> hipError_t forward_of(const RecurArgs &a,
 
 template <typename T, int V, int GATE> hipError_t backward_of(const RecurArgs &a, const Plan &p, hipStream_t st)
 {
+    if (p.cut && p.large) return start<k_recur_back<T, V, BL_WAVES, BL_WORDS, GATE, true, false>>(a, p, BL_WAVES, st);
     if (p.cut) return start<k_recur_back<T, V, BC_WAVES, BC_WORDS, GATE, true, false>>(a, p, BC_WAVES, st);
     if (p.brief) return start<k_recur_back<T, V, BB_WAVES, BB_WORDS, GATE, false, false>>(a, p, BB_WAVES, st);
     return start<k_recur_back<T, V, B_WAVES, B_WORDS, GATE, false, true>>(a, p, B_WAVES, st);
 }
 
+template <typename T, int V, int GATE> hipError_t launch_of(const RecurArgs &a, const Plan &p, bool back, hipStream_t st)
+{
+    return back ? backward_of<T, V, GATE>(a, p, st) : forward_of<T, V, GATE>(a, p, st);
+}
+
 template <typename T, int GATE> hipError_t launch_at(const RecurArgs &a, const Plan &p, bool back, hipStream_t st)
 {
-    constexpr int V = 4 / sizeof(T);
-    static_assert(F_BYTES == 4 && B_BYTES == 4 && FC_BYTES == 4 && BC_BYTES == 4, "a lane's channels");
     if (p.cut) {
         const long long words = (p.pairs + p.states) / 8, copies = (long long)a.n_trees * a.C, most = 4ll * compute_units();
         const long long blocks = ((words > copies ? words : copies) + 255) / 256;
@@ -124,8 +144,9 @@ template <typename T, int GATE> hipError_t launch_at(const RecurArgs &a, const P
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (back) return p.V == 1 ? backward_of<T, 1, GATE>(a, p, st) : backward_of<T, V, GATE>(a, p, st);
-    return p.V == 1 ? forward_of<T, 1, GATE>(a, p, st) : forward_of<T, V, GATE>(a, p, st);
+    if constexpr (sizeof(T) < LANE_BYTES)
+        if (p.narrow) return launch_of<T, 1, GATE>(a, p, back, st);
+    return launch_of<T, LANE_BYTES / sizeof(T), GATE>(a, p, back, st);
 }
 
 template <typename T> hipError_t launch_for(const RecurArgs &a, int gate, const Plan &p, bool back, hipStream_t st)

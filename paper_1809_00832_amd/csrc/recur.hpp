@@ -175,8 +175,10 @@ struct RecPart {
 
 // R words from `row` on (as far as `end`; beyond it the last one again) of one tensor, as they lie in memory; zeros where there is none.
 template <typename T, int V, int R> struct RecRows {
-    static constexpr bool PACKED = sizeof(T) == 2 && V == 2;    // two values in a register
-    typedef typename std::conditional<PACKED, uint32_t, RecRaw<T, V>>::type Row;
+    static constexpr int WORDS = V * (int)sizeof(T) / 4;        // registers of a row; 0: a single 16-bit value
+    struct Row {
+        uint32_t w[WORDS > 0 ? WORDS : 1];
+    };
     Row r[R];
     __device__ void clear()
     {
@@ -186,14 +188,19 @@ template <typename T, int V, int R> struct RecRows {
     // ONCE: nothing reads the rows again, so they need no place in the caches.
     template <bool ONCE = false> __device__ void load(const void *p, long long stride, const RecLane<V> &l, int row, int end)
     {
-        typedef uint32_t __attribute__((aligned(2))) Word;
+        typedef uint32_t Vec __attribute__((ext_vector_type(WORDS > 1 ? WORDS : 2)));
+        typedef Vec __attribute__((aligned(2))) Many;
+        typedef uint32_t __attribute__((aligned(2))) One;
         const T *at = static_cast<const T *>(p) + row * stride;
         const int more = end - 1 - row;
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            if constexpr (ONCE && sizeof(Row) == 4) {
-                const uint32_t v = __builtin_nontemporal_load(reinterpret_cast<const Word *>(reinterpret_cast<const char *>(at) + l.base * (uint32_t)sizeof(T)));
-                __builtin_memcpy(&r[k], &v, 4);
+            const char *const here = reinterpret_cast<const char *>(at) + l.base * (uint32_t)sizeof(T);
+            if constexpr (ONCE && WORDS == 1) {
+                r[k].w[0] = __builtin_nontemporal_load(reinterpret_cast<const One *>(here));
+            } else if constexpr (ONCE && WORDS > 1) {
+                const Vec v = __builtin_nontemporal_load(reinterpret_cast<const Many *>(here));
+                __builtin_memcpy(&r[k], &v, sizeof(v));
             } else {
                 const RecRaw<T, V> v = l.raw(at);
                 __builtin_memcpy(&r[k], &v, sizeof(v));
@@ -203,26 +210,21 @@ template <typename T, int V, int R> struct RecRows {
     }
     __device__ float get(int k, int j) const
     {
-        if constexpr (PACKED) {
-            if constexpr (std::is_same<T, bf16_t>::value) return __uint_as_float(j == 0 ? r[k] << 16 : r[k] & 0xffff0000u);
-            const uint16_t w = j == 0 ? (uint16_t)r[k] : (uint16_t)(r[k] >> 16);
-            T v;
-            __builtin_memcpy(&v, &w, 2);
-            return (float)v;
-        } else {
-            return (float)r[k].v[j];
-        }
+        if constexpr (sizeof(T) == 4) return __uint_as_float(r[k].w[j]);
+        const uint32_t w = r[k].w[j / 2];
+        if constexpr (std::is_same<T, bf16_t>::value) return __uint_as_float(j % 2 ? w & 0xffff0000u : w << 16);
+        const uint16_t half = (uint16_t)(j % 2 ? w >> 16 : w);
+        f16_t v;
+        __builtin_memcpy(&v, &half, 2);
+        return (float)v;
     }
     // What is computed from the rows after this is computed anew: registers hold the rows, not the results.
     __device__ void forget()
     {
 #pragma unroll
-        for (int k = 0; k < R; ++k) {
-            if constexpr (PACKED) asm volatile("" : "+v"(r[k]));
-            else if constexpr (sizeof(T) == 4)
+        for (int k = 0; k < R; ++k)
 #pragma unroll
-                for (int j = 0; j < V; ++j) asm volatile("" : "+v"(r[k].v[j]));
-        }
+            for (int n = 0; n < (WORDS > 0 ? WORDS : 1); ++n) asm volatile("" : "+v"(r[k].w[n]));
     }
 };
 
