@@ -37,8 +37,8 @@ struct Plan {
 
 // Whether sentences are cut into parts, by their words on average (the host does not know the lengths, and a batch with one sentence much longer than the
 // others waits for it).  A whole sentence is a chain of blocks, a part waits for others and needs a launch more.  Measured (us, whole / cut, states
-// alone; words x channels, bf16): 40 sentences of 100 x 512 12.1 / 13.0, 60 of 400 34.8 / 34.3, 60 of 1000 72 / 60, 100 of 400 44 / 47, 100 of 1000 98 / 88, 256 of 750 151 / 161,
-// 4 of 1500 x 256 116 / 17; with gradients 30 / 34, 85 / 82, 179 / 159, 112 / 119, 253 / 244, 409 / 449, 287 / 37.
+// alone; words x channels, bf16): 25 sentences of 125 x 150 fp32 9.7 / 9.0, 40 of 100 x 512 12.3 / 13.1, 40 of 165 17.5 / 15.3, 60 of 165 18.3 / 19.4, 60 of 400 37 / 29, 100 of 400 46 / 41, 200 of 650
+// 107 / 104, 256 of 750 139 / 150; with gradients 23 / 19, 30.5 / 34.8, 42 / 38, 43 / 44, 86 / 75, 112 / 111, 311 / 305, 409 / 449.
 // Sentences that end within a block, more of them than the chip holds at once, need no registers for the block after it (brief).  Measured (us, with gradients, with
 // those registers / without): 2000 sentences of 15 words x 256 bf16 71 / 49, 1024 of 15 x 256 fp32 42 / 38, 256 of 27 x 512 bf16 29.5 / 30.2.
 // Large parts have half as many pairs to be taken, small ones fill the chip with fewer words and waste less of a sentence's last part.  Measured (us, large / small, bf16): states
@@ -52,7 +52,7 @@ bool plan(const tl_recurrence *r, bool back, Plan *p)
     if (p->narrow) p->V = 1;
     p->slices = (r->channels + 64 * p->V - 1) / (64 * p->V);
     const long long workgroups = trees * p->slices;
-    p->cut = rows > 128 * trees && rows / trees > 2 * workgroups;
+    p->cut = rows > 96 * trees && 4 * (rows / trees) > 3 * workgroups;
     p->single = !back && !p->cut && rows <= 8 * trees;
     p->brief = !p->cut && rows <= 32 * trees && workgroups >= 1024 && workgroups >= 8 * compute_units();      // (asking for the units takes more than a microsecond)
     p->large = false;
