@@ -562,7 +562,8 @@ int tl_sample(int dtype, int n_rows, int vocab, const void *logits, int64_t row,
  * their channel and sentence (a channel where joining runs gives an infinity is walked word by word, which takes long).  Results repeat bit for bit.
  * Few long sentences are divided among workgroups that wait for one another's results, each only for such as have been started before it; every
  * wait is bounded (some tenths of a second), and a workgroup whose wait runs out computes what it waited for: such a result is right, but
- * its last bits may differ.  How sentences are divided goes by their words on average: a batch with one sentence much longer than the others waits for it.
+ * its last bits may differ.  How sentences are divided goes by the batch, by words on average: a sentence's last bits do too, and a batch of short sentences
+ * with one much longer than the others waits for that one.
  * TL_EINVAL also where a launch would be too large: from n_trees * channels = 2^28 on (fp32; 16-bit types 2^29), fewer where channels < 64 (n_trees 2^22).
  */
 enum tl_gate { TL_GATE_SIGMOID = 0, TL_GATE_GIVEN = 1 };
@@ -612,7 +613,8 @@ int tl_recur_backward(const tl_recurrence *r, const float *tape, const void *d_h
  *     entropy  - sum_j p_j log p_j
  *     top      the n_top words of largest x, equal ones by index, and their log p; behind the last word above -infinity: -1 and -infinity
  * Words at -infinity have log p = -infinity.  A row without a value above -infinity: every log p -infinity, entropy 0.  +infinity: the words that have it
- * share the mass.  Weights are exp(x - max x), summed in fp32 by a fixed scheme: results repeat bit for bit.
+ * share the mass.  Weights are exp(x - max x), summed in fp32 by a fixed scheme: results repeat bit for bit, and depend on a row's own values alone, but in
+ * their last bits also on n_rows where a row has 2^16 words or more (few such rows are divided among workgroups).
  *   logits [n_rows x vocab] of dtype, `row` elements (>= 0) from one row to the next; 1 <= vocab <= 2^30     DEVICE, read-only
  *   word   [n_rows] int32, may be NULL if logprob is                                       DEVICE, read-only
  *   n_top  0 .. 64

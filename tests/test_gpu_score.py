@@ -279,3 +279,16 @@ def test_more_rows_than_a_launch_has_workgroups():
     d = binding.tl_score_backward(x, w, got["stats"], dl)
     want = torch.where(w[:, None] < 2, (torch.arange(2, device="cuda") == w[:, None]).float() - logp.exp(), 0.0)
     assert ((d - want).abs() <= want.abs() * 2.0 ** -8 + 64 * U).all()
+
+
+@pytest.mark.parametrize("dtype,V", [("f32", 20000), ("bf16", 50001), ("f16", 333)])
+def test_a_row_does_not_depend_on_its_batch(dtype, V):
+    x = logits(7, V, TYPES[dtype])
+    w = torch.tensor(words(7, V), dtype=torch.int32, device="cuda")
+    got = binding.tl_score(x, w, 9)
+    d = torch.randn(7, device="cuda")
+    grad = binding.tl_score_backward(x, w, got["stats"], d, d)
+    for r in (0, 3, 6):
+        one = binding.tl_score(x[r:r + 1], w[r:r + 1], 9)
+        assert all(torch.equal(one[k][0], got[k][r]) for k in ("logprob", "entropy", "top_word", "top_logprob"))
+        assert torch.equal(binding.tl_score_backward(x[r:r + 1], w[r:r + 1], one["stats"], d[r:r + 1], d[r:r + 1])[0], grad[r])
