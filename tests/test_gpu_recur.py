@@ -432,3 +432,28 @@ def test_four_million_sentences_of_a_word():
 def test_one_sentence_of_many_parts():
     """200 000 words of four channels: states behind every 32nd part are handed on fifty times."""
     run([200_000], 4, torch.float32, SIGMOID)
+
+
+def test_two_calls_at_once():
+    """Divided sentences on two streams, each call larger than the chip holds at a time: workgroups of both wait side by side, and neither result changes."""
+    lengths, C = [6000, 9000], 1600
+    off = offsets(lengths)
+    sides = []
+    for seed in range(2):
+        g, x, h0, d_h, d_last = inputs(lengths, C, torch.bfloat16, SIGMOID, seed=seed)
+
+        def both(g=g, x=x, h0=h0, d_h=d_h, d_last=d_last):
+            out = binding.tl_recur(g, x, off, h0, with_last=True, with_tape=True)
+            return dict(out, **binding.tl_recur_backward(g, x, off, out["tape"], d_h, d_last))
+
+        sides.append((both, both(), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(4):
+        for both, _, stream in sides:
+            with torch.cuda.stream(stream):
+                got.append(both())
+    torch.cuda.synchronize()
+    for i, out in enumerate(got):
+        want = sides[i % 2][1]
+        assert all(torch.equal(out[k], want[k]) for k in ("h", "h_last", "d_g", "d_x", "d_h0"))
