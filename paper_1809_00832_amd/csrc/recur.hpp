@@ -19,6 +19,7 @@
 #pragma once
 
 #include "attend.hpp"
+#include "recur_rows.hpp"
 
 namespace tl {
 
@@ -590,7 +591,7 @@ template <typename T, int V, int W, int R, int GATE, bool CUT, bool AHEAD> __glo
     {   // rows behind the last sentence
         const int tail = min(max(__builtin_amdgcn_readfirstlane(a.off[a.n_trees]), 0), a.n_rows);
         const float none[V] = {};
-        for (long long r = tail + slot + (long long)wave * a.slots; r < a.n_rows; r += (long long)W * a.slots) {
+        for (long long r = rec_behind(tail, slot, wave, a.slots); r < a.n_rows; r += (long long)W * a.slots) {
             l.store(static_cast<T *>(a.d_g) + r * a.d_g_row, none);
             l.store(static_cast<T *>(a.d_x) + r * a.d_x_row, none);
         }

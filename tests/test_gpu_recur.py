@@ -457,3 +457,24 @@ def test_two_calls_at_once():
     for i, out in enumerate(got):
         want = sides[i % 2][1]
         assert all(torch.equal(out[k], want[k]) for k in ("h", "h_last", "d_g", "d_x", "d_h0"))
+
+
+def test_gradients_of_nearly_two_to_the_31_rows():
+    """More than 2^16 sentences and as many rows as are accepted, none behind the last sentence.  Two bytes a row: in front of d_g lie as many bytes as a row number
+    that came out negative would reach, and d_g lies in front of d_x.  Gates are zero, so that every state is the x before it (2, as on the tape)."""
+    n, trees = 2 ** 31 - 2 ** 16 - 1, 70_000
+    if torch.cuda.mem_get_info()[0] < 10 * n:
+        pytest.skip("needs 21 GB")
+    off = (torch.arange(trees + 1, device="cuda", dtype=torch.float64) * (n / trees)).floor().int()
+    off[-1] = n
+    one = lambda v: torch.full((1, 1), v, device="cuda", dtype=torch.bfloat16).expand(n, 1)
+    g, x, d_h = one(0.0), one(2.0), one(1.0)
+    tape = torch.full((n // 64 + trees, 1), 2.0, device="cuda")
+    held = torch.full((3, n), 7.0, device="cuda", dtype=torch.bfloat16)
+    d_h0 = torch.full((trees, 1), 7.0, device="cuda")
+    r = binding._recurrence(g, x, off, GIVEN, 0)
+    assert binding._recur_workspace(r, 1, g.device)[1] == 0
+    code = binding.lib().tl_recur_backward(r, tape.data_ptr(), d_h.data_ptr(), 0, None, held[1].data_ptr(), 1, held[2].data_ptr(), 1, d_h0.data_ptr(), None, 0,
+                                           binding._raw_stream(0))
+    assert code == binding.TL_OK
+    assert (held[0] == 7).all() and (held[1] == 2).all() and (held[2] == 1).all() and (d_h0 == 0).all()
