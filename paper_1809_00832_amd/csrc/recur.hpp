@@ -14,8 +14,9 @@
 // states in fp32), and a block of 64 words is stepped through again from there.  So five tensors move instead of six, and a 16-bit h's
 // rounding is in no gradient.
 //
-// A pair can overflow, or multiply an infinity by a zero, where the words one after the other do neither.  So where joining gives
-// something that is not finite, the words in question are walked one by one for that channel: infinities and NaN come out as the formula has them.
+// A pair can overflow, vanish or multiply an infinity by a zero where the words one after the other do not, and words can overflow where the pair does
+// not.  So a pair is made such that it says what may be taken from it (below), and where that is too little the words in question are walked one by one
+// for that channel: infinities and NaN come out as the loop has them.
 #pragma once
 
 #include "attend.hpp"
@@ -87,6 +88,8 @@ template <int V> struct RecLane {
     }
 };
 
+// (A gate's exponent is a rounded product, off by 2 |g| 2^-24 of the gate, and the exponential gives no subnormal numbers: a gate below 2^-126 is zero.  What would mend both
+// is four instructions more for each of a part's gates, made twice.)
 template <int GATE> __device__ inline void rec_gates(float g, float &f, float &i)
 {
     if constexpr (GATE == TL_GATE_SIGMOID) {
@@ -100,6 +103,102 @@ template <int GATE> __device__ inline void rec_gates(float g, float &f, float &i
     }
 }
 
+// ---- what pairs may be trusted with --------------------------------------------------------------
+//
+// A state s goes through a run of n words as A s + B.  That is the loop's result, but for last bits, if nothing overflows between and the product A has its bits.  A product that
+// vanishes, or is subnormal, is off by n 2^-149, and the state by that times s: below 2^-80 for n up to 2^13, states up to REC_LARGE and products of the runs before up to
+// REC_PREFIX.  That much is let go (the loop itself rounds states to 2^-149, and what is lost goes on through the same gates).  Larger states: sigmoid gates enlarge nothing, so that it is
+// in a result's last bits unless the result is 2^-116 of the state; gates of the caller's may, and such a state's words are walked.  A pair says what else it cannot be trusted with:
+//   A is NaN        gates above one enlarge something by more than REC_GROW or REC_PREFIX on the way, or what had vanished (the product is taken in one order, gradients pass in the other)
+//   B is NaN        inputs above REC_INPUT or sums above REC_LARGE
+// and then the words are walked whatever the state.  So no state overflows between unless it is told: 2^40 2^16 2^32 at most, and 2^80 2^32 n from the inputs.
+// Chains of runs are joined first and asked about once, by the largest state on the way, and again run by run where that fails.  (Asked about at every joining, two
+// sentences of 26 000 words in all took 101 us; now 91, and 90 without any of this.)
+
+constexpr float REC_LEAST = 0x1p-126f, REC_GROW = 0x1p32f, REC_PREFIX = 0x1p16f, REC_LARGE = 0x1p40f, REC_INPUT = 0x1p80f, REC_RATIO = 0x1p116f;
+
+// The larger of m and |x|, and of m, |x| and |y|, NaN left out (of which products and sums tell).  By hand: a number as it was read would first be made quiet, an instruction more.
+__device__ inline void rec_largest(float &m, float x) { asm("v_max_f32 %0, |%1|, %0" : "+v"(m) : "v"(x)); }
+__device__ inline void rec_largest(float &m, float x, float y) { asm("v_max3_f32 %0, |%1|, |%2|, %0" : "+v"(m) : "v"(x), "v"(y)); }
+
+// Whether t, which came from states up to `most`, may be something else than what the loop has.
+template <int GATE> __device__ inline bool rec_doubt(float most, float t)
+{
+    return !(fabsf(t) < INFINITY && most <= (GATE == TL_GATE_SIGMOID ? fmaxf(fabsf(t) * REC_RATIO, REC_LARGE) : REC_LARGE));
+}
+
+// A chain of runs, a channel: a state B on its way, or the pair A, B of all.
+template <int GATE> struct RecChain {
+    float A = 1.f, B = 0.f, most = 0.f, above = 0.f;            // the largest state before a run, the largest product so far
+    __device__ void state(float P, float Q)
+    {
+        rec_largest(most, B);
+        B = fmaf(P, B, Q);
+    }
+    __device__ void pair(float P, float Q)
+    {
+        state(P, Q);
+        A *= P;
+        if constexpr (GATE == TL_GATE_GIVEN) rec_largest(above, A);
+    }
+    __device__ bool doubt() const { return rec_doubt<GATE>(most, B); }
+    __device__ void settle()
+    {
+        if (doubt()) B = NAN;
+        if (GATE == TL_GATE_GIVEN && above > REC_PREFIX) A = NAN;
+    }
+};
+
+// The pair of a run that a wave has in registers, once A and B are the products and sums, and D (D_TOO) the sum that comes back: what it says for itself.  f_most, u_most, d_most: the
+// largest gate, input and gradient (0 where they do not matter).  gate(k, f): gates of word k; grad(k, j): what comes back to it.
+template <int GATE, int V, int R, bool D_TOO, typename F, typename E>
+__device__ __forceinline__ void rec_sound(int words, const float (&f_most)[V], const float (&u_most)[V], const float (&d_most)[V], float (&A)[V], float (&B)[V], float (&D)[V], F gate, E grad)
+{
+    if constexpr (GATE == TL_GATE_GIVEN) {
+        bool any = false;
+#pragma unroll
+        for (int j = 0; j < V; ++j) any = any || f_most[j] > 1.f;
+        if (__any(any)) {
+            float p[V], least[V], grow[V], m[V], f[V];
+            bool closed[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) p[j] = least[j] = grow[j] = 1.f, m[j] = 0.f, closed[j] = false;
+#pragma unroll
+            for (int k = 0; k < R; ++k)
+                if (k < words) {
+                    gate(k, f);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        closed[j] = closed[j] || f[j] == 0.f;
+                        p[j] *= f[j];
+                        least[j] = closed[j] ? least[j] : fminf(least[j], fabsf(p[j]));
+                        grow[j] *= fmaxf(1.f, fabsf(f[j]));
+                    }
+                }
+            // what comes back in its own order, as the loop takes it
+            if constexpr (D_TOO) {
+#pragma unroll
+                for (int k = R - 1; k >= 0; --k)
+                    if (k < words) {
+                        gate(k, f);
+#pragma unroll
+                        for (int j = 0; j < V; ++j) m[j] = f[j] * (grad(k, j) + m[j]);
+                    }
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                if (f_most[j] > 1.f && (!(grow[j] <= REC_GROW) || least[j] < REC_LEAST)) A[j] = NAN;
+                if constexpr (D_TOO) D[j] = m[j];
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        if (GATE == TL_GATE_GIVEN && u_most[j] > REC_INPUT) B[j] = NAN;
+        if (D_TOO && (rec_doubt<GATE>(d_most[j], D[j]) || d_most[j] > REC_INPUT)) D[j] = NAN;
+    }
+}
+
 // The state behind words [from, to), whose pair is A, B.
 template <typename T, int GATE, int V, bool BACK>
 __device__ inline void rec_join(const RecurArgs &a, const RecLane<V> &l, int from, int to, const float (&A)[V], const float (&B)[V], float (&s)[V], bool all = false)
@@ -109,7 +208,7 @@ __device__ inline void rec_join(const RecurArgs &a, const RecLane<V> &l, int fro
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         t[j] = fmaf(A[j], s[j], B[j]);
-        walk[j] = all || (!(fabsf(t[j]) < INFINITY) && s[j] == s[j]);     // (a NaN stays one)
+        walk[j] = all || (rec_doubt<GATE>(fabsf(s[j]), t[j]) && s[j] == s[j]);      // (a NaN stays one)
         any = any || walk[j];
     }
     if (__any(any)) {
@@ -135,6 +234,65 @@ __device__ inline void rec_join(const RecurArgs &a, const RecLane<V> &l, int fro
     }
 #pragma unroll
     for (int j = 0; j < V; ++j) s[j] = t[j];
+}
+
+// c through the runs of the waves from `first` on, of R words from `block` on each (BACK: of those before it), as far as `wave`, in front of whose run it is s; unless that ends
+// it, on behind the last one.  pair(w, 0, j), pair(w, 1, j): what wave w found.  Whether a channel has to be joined run by run, from where it began.
+template <int GATE, int V, int W, int R, bool BACK, typename F>
+__device__ __forceinline__ bool rec_steps(int block, int end, int first, int wave, bool ends, float (&c)[V], float (&s)[V], bool (&bad)[V], F pair)
+{
+    RecChain<GATE> t[V];
+    bool any = false;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        t[j].B = c[j];
+        bad[j] = false;
+    }
+#pragma unroll 1
+    for (int w = first; BACK ? w >= 0 : w < W; w += BACK ? -1 : 1) {
+        if (w == wave) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                s[j] = t[j].B;
+                bad[j] = t[j].doubt();
+            }
+            if (ends) break;
+        }
+        if (block + w * R >= end) continue;
+#pragma unroll
+        for (int j = 0; j < V; ++j) t[j].state(pair(w, 0, j), pair(w, 1, j));
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        c[j] = t[j].B;
+        bad[j] = bad[j] || (!ends && t[j].doubt());
+        any = any || bad[j];
+    }
+    return any;
+}
+// The same run by run from `from` on, for channels that have to be.
+template <typename T, int GATE, int V, int W, int R, bool BACK, typename F>
+__device__ __forceinline__ void rec_steps_again(const RecurArgs &a, const RecLane<V> &l, int block, int end, int first, int wave, bool ends, const float (&from)[V], const bool (&bad)[V],
+                                                float (&c)[V], float (&s)[V], F pair)
+{
+    float r[V], A[V], B[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) r[j] = from[j];
+#pragma unroll 1
+    for (int w = first; BACK ? w >= 0 : w < W; w += BACK ? -1 : 1) {
+        if (w == wave) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) s[j] = bad[j] ? r[j] : s[j];
+            if (ends) break;
+        }
+        const int begin = block + w * R;
+        if (begin >= end) continue;
+#pragma unroll
+        for (int j = 0; j < V; ++j) A[j] = pair(w, 0, j), B[j] = pair(w, 1, j);
+        rec_join<T, GATE, V, BACK>(a, l, begin, min(begin + R, end), A, B, r);
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) c[j] = bad[j] ? r[j] : c[j];
 }
 
 // ---- which words a workgroup has -------------------------------------------------------------
@@ -307,6 +465,17 @@ template <int V, int N, typename W> __device__ inline bool rec_wait(const RecurA
     return false;
 }
 
+// A pair that is there.
+template <int V> __device__ inline void rec_taken(const RecurArgs &a, int slot, const RecLane<V> &l, float (&A)[V], float (&B)[V])
+{
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const uint64_t v = __hip_atomic_load(a.pairs + (long long)slot * a.C + l.base + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        A[j] = __uint_as_float((uint32_t)(v >> 32));
+        B[j] = __uint_as_float((uint32_t)v);
+    }
+}
+
 template <int V, int W> struct RecEnter {
     float pair[W][2][V][64], state[V][64];
     int late;
@@ -336,9 +505,7 @@ __device__ inline void rec_enter(const RecurArgs &a, const RecPart &p, const Rec
     const int first = wave * SHARE, n = min(SHARE, many - first);
     if (n > 0) {
         constexpr int N = SHARE < 4 ? SHARE : 4;
-        float A[V], B[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) A[j] = 1.f, B[j] = 0.f;
+        RecChain<GATE> c[V];
 #pragma unroll 1
         for (int i = 0; i < n; i += N) {
             uint64_t *at[N], v[N][V];
@@ -349,14 +516,13 @@ __device__ inline void rec_enter(const RecurArgs &a, const RecPart &p, const Rec
             for (int k = 0; k < N; ++k)
                 if (i + k < n)
 #pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        const float c = __uint_as_float((uint32_t)(v[k][j] >> 32));
-                        A[j] *= c;
-                        B[j] = fmaf(c, B[j], __uint_as_float((uint32_t)v[k][j]));
-                    }
+                    for (int j = 0; j < V; ++j) c[j].pair(__uint_as_float((uint32_t)(v[k][j] >> 32)), __uint_as_float((uint32_t)v[k][j]));
         }
 #pragma unroll
-        for (int j = 0; j < V; ++j) e.pair[wave][0][j][lane] = A[j], e.pair[wave][1][j][lane] = B[j];
+        for (int j = 0; j < V; ++j) {
+            c[j].settle();
+            e.pair[wave][0][j][lane] = c[j].A, e.pair[wave][1][j][lane] = c[j].B;
+        }
     }
     if (!fine) e.late = 1;
     __syncthreads();
@@ -365,23 +531,27 @@ __device__ inline void rec_enter(const RecurArgs &a, const RecPart &p, const Rec
     bool bad[V], any = false;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        s[j] = e.state[j][lane];
-        t[j] = s[j];
-        for (int w = 0; w * SHARE < many; ++w) t[j] = fmaf(e.pair[w][0][j][lane], t[j], e.pair[w][1][j][lane]);
-        bad[j] = late || (!(fabsf(t[j]) < INFINITY) && s[j] == s[j]);
+        RecChain<GATE> c;
+        c.B = s[j] = e.state[j][lane];
+        for (int w = 0; w * SHARE < many; ++w) c.state(e.pair[w][0][j][lane], e.pair[w][1][j][lane]);
+        t[j] = c.B;
+        bad[j] = late || c.doubt();
         any = any || bad[j];
     }
     if (__any(any)) {
-        // the words between the published state, or the sentence's own end, and this part
+        // part by part from the published state, of pairs that are all there; or from the sentence's own end, every word
         float w[V];
         const float *const from = BACK ? a.d_last : a.copy;
 #pragma unroll
         for (int j = 0; j < V; ++j) w[j] = late ? 0.f : s[j];
         if (late && from) l.load(from + (long long)p.tree * a.C, w);
-        const int edge = late ? 0 : group;
-        const float none[V] = {};
-        if (BACK) rec_join<T, GATE, V, BACK>(a, l, p.end, (int)min(p.lo + (long long)(p.parts - edge) * size, (long long)p.hi), none, none, w, true);
-        else rec_join<T, GATE, V, BACK>(a, l, p.lo + edge * size, p.first, none, none, w, true);
+#pragma unroll 1
+        for (int n = late ? 0 : group; n < nth; ++n) {
+            const int at = slot(n) - p.slot0;
+            float A[V], B[V];
+            rec_taken<V>(a, slot(n), l, A, B);                          // (whatever it is, where all words are walked)
+            rec_join<T, GATE, V, BACK>(a, l, p.lo + at * size, (int)min(p.lo + (at + 1ll) * size, (long long)p.hi), A, B, w, late);
+        }
 #pragma unroll
         for (int j = 0; j < V; ++j) t[j] = bad[j] ? w[j] : t[j];
     }
@@ -459,7 +629,7 @@ template <typename T, int V, int W, int R, int GATE, bool CUT, bool ONCE, bool A
 {
     static_assert(REC_TAPE % R == 0, "states of the tape lie where a wave's words begin");
     static_assert(!(CUT && AHEAD), "a part is one block");
-    constexpr bool KEEP = AHEAD && W > 1;
+    constexpr bool KEEP = AHEAD && W > 1, WIDE = sizeof(T) == 4 || std::is_same<T, bf16_t>::value;      // (no fp16 number is above REC_INPUT)
     __shared__ float lds[W > 1 && !CUT ? 2 : 1][W][2][V][64];
     __shared__ RecEnter<V, W> enter[1];                         // (CUT only)
     __shared__ float begin_state[V][64];
@@ -500,17 +670,25 @@ template <typename T, int V, int W, int R, int GATE, bool CUT, bool ONCE, bool A
         if (AHEAD && more) load(row + W * R);
         float f[V], i[V], s[V];
         if constexpr (W > 1) {
-            float A[V], B[V];
+            float A[V], B[V], D[V], f_most[V], u_most[V], d_most[V];
 #pragma unroll
-            for (int j = 0; j < V; ++j) A[j] = 1.f, B[j] = 0.f;
+            for (int j = 0; j < V; ++j) A[j] = 1.f, B[j] = D[j] = f_most[j] = u_most[j] = d_most[j] = 0.f;
             rec_each<R>(words, [&](int k) __attribute__((always_inline)) {
                 G.at(k, f, i);
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
                     A[j] *= f[j];
                     B[j] = fmaf(f[j], B[j], i[j] * X.get(k, j));
+                    if constexpr (GATE == TL_GATE_GIVEN) {
+                        if (k % 2 == 0) {                       // (behind the last word it is there again)
+                            rec_largest(f_most[j], G.g.get(k, j), G.g.get(k + 1, j));
+                            if constexpr (WIDE) rec_largest(u_most[j], X.get(k, j), X.get(k + 1, j));
+                        }
+                    }
                 }
             });
+            rec_sound<GATE, V, R, false>(words, f_most, u_most, d_most, A, B, D, [&](int k, float (&F)[V]) __attribute__((always_inline)) { float I[V]; G.at(k, F, I); },
+                                         [](int, int) { return 0.f; });
             G.forget();
 #pragma unroll
             for (int j = 0; j < V; ++j) {
@@ -524,30 +702,27 @@ template <typename T, int V, int W, int R, int GATE, bool CUT, bool ONCE, bool A
             if constexpr (CUT)
                 if (p.parts > 1) {
                     if (wave == 0 && p.part < p.parts - 1) {
+                        RecChain<GATE> t[V];
 #pragma unroll
-                        for (int j = 0; j < V; ++j)
+                        for (int w = 0; w < W; ++w)
 #pragma unroll
-                            for (int w = 1; w < W; ++w) {
-                                A[j] *= lds[0][w][0][j][lane];
-                                B[j] = fmaf(lds[0][w][0][j][lane], B[j], lds[0][w][1][j][lane]);
-                            }
+                            for (int j = 0; j < V; ++j) t[j].pair(lds[0][w][0][j][lane], lds[0][w][1][j][lane]);
+#pragma unroll
+                        for (int j = 0; j < V; ++j) {
+                            t[j].settle();
+                            A[j] = t[j].A, B[j] = t[j].B;
+                        }
                         rec_publish(a.pairs + (long long)slot * a.C, l, A, B);
                     }
                     rec_enter<T, GATE, V, W, false>(a, p, l, wave, enter[0], c);
                 }
-#pragma unroll 1
-            for (int w = 0; w < W; ++w) {
-                if (w == wave) {
+            float from[V];
+            bool bad[V];
+            auto pair = [&](int w, int n, int j) __attribute__((always_inline)) { return lds[buf][w][n][j][lane]; };
 #pragma unroll
-                    for (int j = 0; j < V; ++j) s[j] = c[j];
-                    if (CUT) break;
-                }
-                const int begin = block + w * R;
-                if (begin >= p.end) continue;
-#pragma unroll
-                for (int j = 0; j < V; ++j) A[j] = lds[buf][w][0][j][lane], B[j] = lds[buf][w][1][j][lane];
-                rec_join<T, GATE, V, false>(a, l, begin, min(begin + R, p.end), A, B, c);
-            }
+            for (int j = 0; j < V; ++j) from[j] = c[j];
+            if (__any(rec_steps<GATE, V, W, R, false>(block, p.end, 0, wave, CUT, c, s, bad, pair)))
+                rec_steps_again<T, GATE, V, W, R, false>(a, l, block, p.end, 0, wave, CUT, from, bad, c, s, pair);
             if (!CUT) buf ^= 1;
         } else {
 #pragma unroll
@@ -577,11 +752,13 @@ template <typename T, int V, int W, int R, int GATE, bool CUT, bool ONCE, bool A
 
 // Blocks from the last one to the first.  A block's words are stepped through from the tape's state first, for what each gate's gradient needs, then backwards.  Bound by memory:
 // 256 sentences of 33 words x 512 fp32 21 us for 85 MB, eight of 1 800 x 1024 bf16 40 for 146 MB (one and a half rounds of workgroups).
-template <typename T, int V, int W, int R, int GATE, bool CUT, bool AHEAD> __global__ __launch_bounds__(64 * W) void k_recur_back(RecurArgs a)
+// (Registers: as many as leave a SIMD the waves that it has without the code for what is walked, whose registers would take one of them; fp32 256 x 33 x 512 39 us then for 34.)
+template <typename T, int V, int W, int R, int GATE, bool CUT, bool AHEAD>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(!AHEAD ? 4 : V == 1 ? 3 : 2))) void k_recur_back(RecurArgs a)
 {
     static_assert((W * R) % REC_TAPE == 0, "a block starts from a state of the tape");
     static_assert(!(CUT && AHEAD), "a part is one block");
-    constexpr bool KEEP = AHEAD;
+    constexpr bool KEEP = AHEAD, WIDE = sizeof(T) == 4 || std::is_same<T, bf16_t>::value;
     __shared__ float lds[CUT ? 1 : 2][W][3][V][64];
     __shared__ RecEnter<V, W> enter[1];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -627,11 +804,11 @@ template <typename T, int V, int W, int R, int GATE, bool CUT, bool AHEAD> __glo
         const int block = p.first + n * (W * R), row = block + wave * R, words = p.end - row;
         RecGates<T, V, R, GATE, KEEP> G(g);
         RecRows<T, V, R> X = x, E = d;
-        float f[V], i[V], s[V], m[V], A[V], B[V], D[V];
+        float f[V], i[V], s[V], m[V], A[V], B[V], D[V], f_most[V], u_most[V], d_most[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             s[j] = s0[j];
-            A[j] = 1.f, B[j] = D[j] = 0.f;
+            A[j] = 1.f, B[j] = D[j] = f_most[j] = u_most[j] = d_most[j] = 0.f;
         }
         const bool more = !CUT && n > 0;
         if (AHEAD && more) load(block - W * R);
@@ -642,8 +819,17 @@ template <typename T, int V, int W, int R, int GATE, bool CUT, bool AHEAD> __glo
                 A[j] *= f[j];
                 B[j] = fmaf(f[j], B[j], i[j] * X.get(k, j));
                 D[j] = fmaf(A[j], E.get(k, j), D[j]);           // (what comes back from word k passes the gates of words 0 .. k)
+                if (k % 2 == 0) {                               // (behind the last word it is there again)
+                    if constexpr (GATE == TL_GATE_GIVEN) {
+                        rec_largest(f_most[j], G.g.get(k, j), G.g.get(k + 1, j));
+                        if constexpr (WIDE) rec_largest(u_most[j], X.get(k, j), X.get(k + 1, j));
+                    }
+                    if constexpr (WIDE) rec_largest(d_most[j], E.get(k, j), E.get(k + 1, j));
+                }
             }
         });
+        rec_sound<GATE, V, R, true>(words, f_most, u_most, d_most, A, B, D, [&](int k, float (&F)[V]) __attribute__((always_inline)) { float I[V]; G.at(k, F, I); },
+                                    [&](int k, int j) __attribute__((always_inline)) { return E.get(k, j); });
         G.forget();
 #pragma unroll
         for (int j = 0; j < V; ++j) {
@@ -655,36 +841,33 @@ template <typename T, int V, int W, int R, int GATE, bool CUT, bool AHEAD> __glo
         if constexpr (CUT)
             if (p.parts > 1) {
                 if (wave == W - 1 && p.part > 0) {
+                    RecChain<GATE> t[V];
+#pragma unroll 4
+                    for (int w = W - 1; w >= 0; --w)
 #pragma unroll
-                    for (int j = 0; j < V; ++j)
+                        for (int j = 0; j < V; ++j) t[j].pair(lds[0][w][0][j][lane], lds[0][w][2][j][lane]);
 #pragma unroll
-                        for (int w = W - 2; w >= 0; --w) {
-                            A[j] *= lds[0][w][0][j][lane];
-                            D[j] = fmaf(lds[0][w][0][j][lane], D[j], lds[0][w][2][j][lane]);
-                        }
+                    for (int j = 0; j < V; ++j) {
+                        t[j].settle();
+                        A[j] = t[j].A, D[j] = t[j].B;
+                    }
                     rec_publish(a.pairs + (long long)slot * a.C, l, A, D);
                 }
                 rec_enter<T, GATE, V, W, true>(a, p, l, wave, enter[0], c);
             }
-#pragma unroll 1
-        for (int w = 0; w < wave; ++w) {
-            const int begin = block + w * R;
+        {
+            float from[V], from_back[V], here[V];
+            bool bad[V], bad_back[V];
+            auto pair = [&](int w, int n, int j) __attribute__((always_inline)) { return lds[buf][w][n][j][lane]; };
+            auto pair_back = [&](int w, int n, int j) __attribute__((always_inline)) { return lds[buf][w][2 * n][j][lane]; };
 #pragma unroll
-            for (int j = 0; j < V; ++j) A[j] = lds[buf][w][0][j][lane], B[j] = lds[buf][w][1][j][lane];
-            if (begin < p.end) rec_join<T, GATE, V, false>(a, l, begin, min(begin + R, p.end), A, B, s);
-        }
-#pragma unroll 1
-        for (int w = W - 1; w >= 0; --w) {
-            if (w == wave) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) m[j] = c[j];
-                if (CUT) break;
+            for (int j = 0; j < V; ++j) from[j] = s[j], from_back[j] = c[j];
+            const bool any = rec_steps<GATE, V, W, R, false>(block, p.end, 0, wave, true, s, here, bad, pair);
+            const bool any_back = rec_steps<GATE, V, W, R, true>(block, p.end, W - 1, wave, CUT, c, m, bad_back, pair_back);
+            if (__any(any || any_back)) {
+                rec_steps_again<T, GATE, V, W, R, false>(a, l, block, p.end, 0, wave, true, from, bad, s, here, pair);
+                rec_steps_again<T, GATE, V, W, R, true>(a, l, block, p.end, W - 1, wave, CUT, from_back, bad_back, c, m, pair_back);
             }
-            const int begin = block + w * R;
-            if (begin >= p.end) continue;
-#pragma unroll
-            for (int j = 0; j < V; ++j) A[j] = lds[buf][w][0][j][lane], D[j] = lds[buf][w][2][j][lane];
-            rec_join<T, GATE, V, true>(a, l, begin, min(begin + R, p.end), A, D, c);
         }
         if (!CUT) buf ^= 1;
         // forwards: what a word's own lambda is multiplied by in the gradient of its gate, but for f i
