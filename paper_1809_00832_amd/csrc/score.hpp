@@ -192,11 +192,12 @@ template <int D = 32> __device__ inline float sco_max(float x)
     return x;
 }
 
-// The largest of three numbers, NaN left out.  (fmaxf of a number that was just read would first be made quiet, an instruction each.)
+// The largest of three numbers, NaN if one of them is, whichever kind of NaN.  (The other maximum leaves a quiet NaN out, but of a signalling one and a number makes a NaN, which hides the
+// number from the next step; and fmaxf of a number that was just read would first be made quiet, an instruction each.)
 __device__ inline float sco_max3(float a, float b, float c)
 {
     float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    asm("v_maximum3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
     return r;
 }
 
@@ -258,17 +259,29 @@ template <typename T, int NT, bool TOP, bool ONCE> __global__ __launch_bounds__(
     float m = -INFINITY;
     ScoList top;
     if (TOP) top.init(wait[TOP ? wave : 0], a.top);
-    auto take = [&](const float (&v)[U][E], const int (&at)[U]) {   // at: index of each piece's first word
-        float most[U], all = -INFINITY;
+    auto take = [&](float (&v)[U][E], const int (&at)[U]) {         // at: index of each piece's first word
+        float most[U], all;
+        auto largest_of = [&]() {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            most[u] = v[u][0];
+            for (int u = 0; u < U; ++u) {
+                most[u] = v[u][0];
 #pragma unroll
-            for (int e = 1; e < E; e += 2) most[u] = sco_max3(most[u], v[u][e], v[u][e + 1 < E ? e + 1 : e]);
-            all = fmaxf(all, most[u]);
+                for (int e = 1; e < E; e += 2) most[u] = sco_max3(most[u], v[u][e], v[u][e + 1 < E ? e + 1 : e]);
+                all = u ? sco_max3(all, most[u], most[u]) : most[u];
+            }
+        };
+        largest_of();
+        if (__any(!(fmaf(all, SCO_LOG2_E, -s.r) <= SCO_LAG))) {
+            if (__any(all != all)) {                            // (NaN as -infinity)
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) v[u][e] = v[u][e] == v[u][e] ? v[u][e] : -INFINITY;
+                largest_of();
+            }
+            if (__any(fmaf(all, SCO_LOG2_E, -s.r) > SCO_LAG)) s.scale(fmaxf(s.r, all * SCO_LOG2_E));
         }
         m = fmaxf(m, all);
-        if (__any(fmaf(all, SCO_LOG2_E, -s.r) > SCO_LAG)) s.scale(fmaxf(s.r, all * SCO_LOG2_E));
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll

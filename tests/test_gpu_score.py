@@ -292,3 +292,27 @@ def test_a_row_does_not_depend_on_its_batch(dtype, V):
         one = binding.tl_score(x[r:r + 1], w[r:r + 1], 9)
         assert all(torch.equal(one[k][0], got[k][r]) for k in ("logprob", "entropy", "top_word", "top_logprob"))
         assert torch.equal(binding.tl_score_backward(x[r:r + 1], w[r:r + 1], one["stats"], d[r:r + 1], d[r:r + 1])[0], grad[r])
+
+
+SIGNALLING = {"f32": (torch.int32, 0x7F800001), "bf16": (torch.int16, 0x7F81), "f16": (torch.int16, 0x7C01)}
+
+
+@pytest.mark.parametrize("n_top", [0, 10, 64])
+@pytest.mark.parametrize("V", [9, 70, 3001, 20000, 70001])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_signalling_nan(dtype, V, n_top):
+    """NaN whose first bit of the fraction is not set, of either sign, around the largest words and anywhere: they count as -infinity like others."""
+    x = logits(6, V, TYPES[dtype]).clone()
+    whole, bits = SIGNALLING[dtype]
+    sign = -2 ** (31 if dtype == "f32" else 15)
+    raw = x.view(whole)
+    at = torch.arange(V, device="cuda")
+    for r in range(6):
+        peak = int(x[r].float().argmax())
+        for step in ((1, -1), (1, 2, 3), (-1, -2, -3), (4, -4))[r % 4]:
+            if 0 <= peak + step < V:
+                raw[r, peak + step] = bits if step % 2 else bits + sign
+    raw[4, at % 5 == 2] = bits
+    raw[5, at % 2 == 0] = bits
+    assert int(torch.isnan(x).sum()) > V // 2
+    check(x, words(6, V), n_top)
