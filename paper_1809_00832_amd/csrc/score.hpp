@@ -379,7 +379,7 @@ template <typename T, int NT, bool TOP, bool ONCE> __global__ __launch_bounds__(
             // ... and relative to m itself
             const float lag = fmaf(m, SCO_LOG2_E, -r), c = __builtin_amdgcn_exp2f(-lag);
             of.t = c * fmaf(-lag, z, t);
-            of.z = c * z;
+            of.z = fmaxf(c * z, 1.f);                           // (m's own weight is one; c is rounded, and no log probability may come out above zero)
         }
     } else if (m > -INFINITY) {                                 // (words at infinity share the mass)
         x = {0.f, 0.f, 0.f};

@@ -316,3 +316,18 @@ def test_signalling_nan(dtype, V, n_top):
     raw[5, at % 2 == 0] = bits
     assert int(torch.isnan(x).sum()) > V // 2
     check(x, words(6, V), n_top)
+
+
+@pytest.mark.parametrize("n,V", [(4096, 40), (64, 9000), (3, 70001)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_no_log_probability_is_above_zero(dtype, n, V):
+    """All but certain words, of logits of any size: sums of weights relative to the largest logit are one at least, whatever their rounding."""
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    peak = (torch.rand(n, 1, generator=gen, device="cuda") * 200 - 100).to(TYPES[dtype])
+    x = (peak.float() - 25 - torch.rand(n, V, generator=gen, device="cuda") * 40).to(TYPES[dtype])
+    word = torch.randint(0, V, (n,), generator=gen, device="cuda", dtype=torch.int32)
+    x.scatter_(1, word.long()[:, None], peak)
+    got = check(x[:8], word[:8].tolist(), 3) if n > 3 else check(x, word.tolist(), 3)
+    got = binding.tl_score(x, word, 3)
+    assert (got["logprob"] <= 0).all() and (got["top_logprob"] <= 0).all() and (got["entropy"] >= 0).all() and (got["stats"][1] >= 1).all()
+    assert torch.equal(got["top_word"][:, 0], word) and torch.equal(got["top_logprob"][:, 0], got["logprob"])
