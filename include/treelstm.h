@@ -562,7 +562,7 @@ int tl_sample(int dtype, int n_rows, int vocab, const void *logits, int64_t row,
  * overflows on the way, and reach only later words (gradients: earlier ones) of their channel and sentence.  A sigmoid gate below 2^-126 is zero.  What joining cannot tell is walked word by
  * word, which takes long: channels whose states or incoming gradients are infinite, sigmoid: fade by 2^-116 from above 2^40; TL_GATE_GIVEN: are above 2^40, or have gates
  * above one whose products grow beyond 2^16 over some hundred words, or pass through the smallest numbers.  Results repeat bit for bit.
- * Few long sentences are divided among workgroups that wait for one another's results, each only for such as have been started before it; every
+ * Few long sentences are divided among workgroups that wait for one another's results, each only for such as have been started before it, whatever else runs; every
  * wait is bounded (some tenths of a second), and a workgroup whose wait runs out computes what it waited for: such a result is right, but
  * its last bits may differ.  How sentences are divided goes by the batch, by words on average: a sentence's last bits do too, and a batch of short sentences
  * with one much longer than the others waits for that one.

@@ -67,7 +67,7 @@ bool plan(const tl_recurrence *r, bool back, Plan *p)
     p->blocks = slots * p->slices;
     p->slots = (int)slots;
     p->pairs = p->cut ? round16(8 * slots * r->channels) : 0;
-    p->states = p->cut ? round16(4 * (slots / REC_GROUP + 1) * r->channels) : 0;
+    p->states = p->cut ? round16(4 * ((slots / REC_GROUP + 1) * r->channels + REC_LINE * p->slices)) : 0;
     p->parts = p->cut ? 16 * slots : 0;
     p->copy = p->cut && !back ? round16(4 * trees * r->channels) : 0;
     return p->blocks <= most_blocks(64 * 16);
@@ -96,6 +96,7 @@ void lay_out(const Plan &p, void *workspace, RecurArgs *a)
     char *const base = static_cast<char *>(workspace);
     a->pairs = reinterpret_cast<uint64_t *>(base);
     a->states = reinterpret_cast<uint32_t *>(base + p.pairs);
+    a->taken = a->states + (p.slots / REC_GROUP + 1ll) * a->C;
     a->parts = reinterpret_cast<int4 *>(base + p.pairs + p.states);
     a->broken = reinterpret_cast<uint32_t *>(base + p.pairs + p.states + p.parts + p.copy);
     if (p.copy && a->h0) a->copy = reinterpret_cast<float *>(base + p.pairs + p.states + p.parts);

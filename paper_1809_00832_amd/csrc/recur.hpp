@@ -36,6 +36,7 @@ struct RecurArgs {
     float *h_last, *d_h0, *tape;
     uint64_t *pairs;                            // of every part (see RecPart), a number per channel: A and B, all ones until it is published
     uint32_t *states;                           // behind every 32nd part of a sentence
+    uint32_t *taken;                            // of every slice, a cache line each: how many of its parts have been started, less one
     int4 *parts;                                // of every part: its sentence, that one's words, the slot of its first part
     float *copy;                                // of h0, which h_last may be written over
     uint32_t *broken;                           // not 0 once a wait has run out: no other waits as long again
@@ -304,6 +305,12 @@ struct RecPart {
     int part, parts;
     int first, end;                             // the words of this part
     bool there;
+    __device__ void take(int n, int size)
+    {
+        part = n;
+        first = (int)min(lo + (long long)n * size, (long long)hi);
+        end = (int)min((long long)first + size, (long long)hi);
+    }
     template <bool CUT> __device__ static RecPart of(const RecurArgs &a, int slot)
     {
         RecPart p;
@@ -315,10 +322,8 @@ struct RecPart {
             p.slot0 = __builtin_amdgcn_readfirstlane(r.w);
             const int size = 1 << a.shift;
             p.parts = max((int)(((long long)p.hi - p.lo + size - 1) >> a.shift), 1);
-            p.part = slot - p.slot0;
-            p.there = p.part >= 0 && p.part < p.parts;
-            p.first = (int)min(p.lo + (long long)p.part * size, (long long)p.hi);
-            p.end = (int)min((long long)p.first + size, (long long)p.hi);
+            p.there = slot - p.slot0 >= 0 && slot - p.slot0 < p.parts;
+            p.take(slot - p.slot0, size);
         } else {
             p.tree = p.slot0 = slot;
             tree_range(a.off, slot, a.n_rows, &p.lo, &p.hi);
@@ -418,10 +423,11 @@ template <typename T, int V, int R, int GATE, bool KEEP> struct RecGates {
 // A part's pair needs nothing but the part's own words, so a workgroup that waits for pairs waits for workgroups that wait for nothing.  A state is
 // published behind every 32nd part: a part needs the state behind the last such part before it, and the pairs from there on, 31 at most.  Values are
 // published as they are, in words that were filled with ones before: a word that is no longer all ones is complete, and no fence is needed.
-// Parts are numbered in the order in which a state passes them, and workgroups are started in that order, so that what is waited for has been started.
-// Every wait ends all the same: after REC_POLLS polls (tenths of a second) the words in question are walked, from the start of the sentence.
+// Parts are numbered in the order in which a state passes them.  A workgroup takes the next number of its slice when it starts: the hardware starts them in order within an XCD only, and two
+// launches side by side could else fill one another's units with workgroups that wait for such as find no place.  So what is waited for has been started (a lane that is moved back
+// waits for its own channels alone).  It costs an atomic add's way a workgroup: two sentences of 26 000 words in all 94 us, 91 without.  Every wait ends all the same: after REC_POLLS polls (tenths of a second) the words in question are walked, from the start of the sentence.
 
-constexpr int REC_GROUP = 32, REC_POLLS = 1 << 16;
+constexpr int REC_GROUP = 32, REC_POLLS = 1 << 16, REC_LINE = 32;
 constexpr uint32_t REC_NAN = 0x7fc00000u;       // published for a NaN that is all ones
 
 __device__ inline uint32_t rec_bits(float x)
@@ -455,6 +461,7 @@ template <int V, int N, typename W> __device__ inline bool rec_wait(const RecurA
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
                     v[k][j] = __hip_atomic_load(at[k] + l.base + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    if (V > 1 && j < l.back) v[k][j] = 0;
                     there = there && v[k][j] != (W)~(W)0;
                 }
         if (__all(there)) return true;
@@ -470,7 +477,7 @@ template <int V> __device__ inline void rec_taken(const RecurArgs &a, int slot, 
 {
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        const uint64_t v = __hip_atomic_load(a.pairs + (long long)slot * a.C + l.base + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const uint64_t v = V > 1 && j < l.back ? 0 : __hip_atomic_load(a.pairs + (long long)slot * a.C + l.base + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         A[j] = __uint_as_float((uint32_t)(v >> 32));
         B[j] = __uint_as_float((uint32_t)v);
     }
@@ -575,9 +582,18 @@ __global__ __launch_bounds__(256) void k_recur_prepare(RecurArgs a, long long n_
         a.parts[slot] = int4{t, lo, max(place(t + 1), lo), (lo >> a.shift) + t};
     }
     if (at == 0) *a.broken = 0;
-    for (long long i = at; i < n_words; i += step) a.pairs[i] = ~0ull;      // (pairs, and the states behind them)
+    for (long long i = at; i < n_words; i += step) a.pairs[i] = ~0ull;      // (pairs, and behind them states and numbers of parts)
     if (a.copy)
         for (long long i = at; i < n_copy; i += step) a.copy[i] = a.h0[i];
+}
+
+// Which part a workgroup takes: as many as workgroups of its slice have started before it.
+__device__ inline int rec_take(const RecurArgs &a, int slice)
+{
+    __shared__ uint32_t number;
+    if (threadIdx.x == 0) number = __hip_atomic_fetch_add(a.taken + slice * REC_LINE, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u;
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(number);
 }
 
 // Where a sentence's words begin: its row of h0, or (BACK) of what comes back from behind them.
@@ -634,7 +650,7 @@ template <typename T, int V, int W, int R, int GATE, bool CUT, bool ONCE, bool A
     __shared__ RecEnter<V, W> enter[1];                         // (CUT only)
     __shared__ float begin_state[V][64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int slot = blockIdx.x / a.slices, slice = blockIdx.x - slot * a.slices;
+    const int nth = blockIdx.x / a.slices, slice = blockIdx.x - nth * a.slices, slot = CUT ? rec_take(a, slice) : nth;
     const RecPart p = RecPart::of<CUT>(a, slot);
     if (!p.there) return;
     const RecLane<V> l(slice, lane, a.C);
@@ -762,8 +778,8 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(!AHEAD ?
     __shared__ float lds[CUT ? 1 : 2][W][3][V][64];
     __shared__ RecEnter<V, W> enter[1];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    // (parts in the order in which gradients pass them)
-    const int from_end = blockIdx.x / a.slices, slice = blockIdx.x - from_end * a.slices, slot = a.slots - 1 - from_end;
+    // (from behind, as gradients pass them)
+    const int nth = blockIdx.x / a.slices, slice = blockIdx.x - nth * a.slices, slot = a.slots - 1 - (CUT ? rec_take(a, slice) : nth);
     const RecLane<V> l(slice, lane, a.C);
     {   // rows behind the last sentence
         const int tail = min(max(__builtin_amdgcn_readfirstlane(a.off[a.n_trees]), 0), a.n_rows);
