@@ -563,8 +563,8 @@ int tl_sample(int dtype, int n_rows, int vocab, const void *logits, int64_t row,
  * word, which takes long: channels whose states or incoming gradients are infinite, sigmoid: fade by 2^-116 from above 2^40; TL_GATE_GIVEN: are above 2^40, or have gates
  * above one whose products grow beyond 2^16 over some hundred words, or pass through the smallest numbers.  Results repeat bit for bit.
  * Few long sentences are divided among workgroups that wait for one another's results, each only for such as have been started before it, whatever else runs; every
- * wait is bounded (some tenths of a second), and a workgroup whose wait runs out computes what it waited for: such a result is right, but
- * its last bits may differ.  How sentences are divided goes by the batch, by words on average: a sentence's last bits do too, and a batch of short sentences
+ * wait is bounded (spin_limit; by default some tenths of a second), and a workgroup whose wait runs out computes what it waited for, word by word: such a
+ * result is right, but its last bits may differ.  How sentences are divided goes by the batch, by words on average: a sentence's last bits do too, and a batch of short sentences
  * with one much longer than the others waits for that one.
  * TL_EINVAL also where a launch would be too large: from n_trees * channels = 2^28 on (fp32; 16-bit types 2^29), fewer where channels < 64 (n_trees 2^22).
  */
@@ -575,6 +575,7 @@ typedef struct {
     int gate;                /* enum tl_gate                                                                              */
     int n_trees, n_rows;     /* sentences and rows, >= 0; n_rows below 2^31 - 2^16                                        */
     int channels;            /* 1 .. 2^20                                                                                 */
+    int spin_limit;          /* 0 = default.  Upper bound of the polls of a wait between workgroups (the default at most); below 0: none  */
     const int32_t *off;      /* [n_trees+1], from 0 to at most n_rows, ascending (equal ones: no words)       DEVICE
                                 Offsets outside these bounds: results are unspecified, nothing outside the arrays is accessed.  */
     const void *g, *x;       /* rows of `channels` values, `g_row` and `x_row` elements apart (>= 0)         DEVICE, read-only */

@@ -52,7 +52,7 @@ class tl_attention(ctypes.Structure):
 
 class tl_recurrence(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int), ("gate", ctypes.c_int), ("n_trees", ctypes.c_int), ("n_rows", ctypes.c_int), ("channels", ctypes.c_int),
-                ("off", ctypes.c_void_p), ("g", ctypes.c_void_p), ("x", ctypes.c_void_p), ("g_row", ctypes.c_int64), ("x_row", ctypes.c_int64)]
+                ("spin_limit", ctypes.c_int), ("off", ctypes.c_void_p), ("g", ctypes.c_void_p), ("x", ctypes.c_void_p), ("g_row", ctypes.c_int64), ("x_row", ctypes.c_int64)]
 
 
 _lib = None
@@ -467,11 +467,11 @@ def tl_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, s
     return out
 
 
-_PACK_RECURRENCE = struct.Struct("5i4x3Q2q").pack
-assert struct.calcsize("5i4x3Q2q") == ctypes.sizeof(tl_recurrence)
+_PACK_RECURRENCE = struct.Struct("6i3Q2q").pack
+assert struct.calcsize("6i3Q2q") == ctypes.sizeof(tl_recurrence)
 
 
-def _recurrence(g, x, off, gate, index) -> bytes:
+def _recurrence(g, x, off, gate, index, spin_limit=0) -> bytes:
     import torch
     n, channels = g.shape
     dtype = g.dtype
@@ -482,7 +482,7 @@ def _recurrence(g, x, off, gate, index) -> bytes:
     assert channels == 1 or g_c == x_c == 1, "channels must be contiguous"
     n_off = off.numel()
     assert off.dtype is torch.int32 and off.is_contiguous() and n_off >= 1
-    return _PACK_RECURRENCE(_dtype(g), gate, n_off - 1, n, channels, off.data_ptr(), g.data_ptr(), x.data_ptr(), g_row, x_row)
+    return _PACK_RECURRENCE(_dtype(g), gate, n_off - 1, n, channels, spin_limit, off.data_ptr(), g.data_ptr(), x.data_ptr(), g_row, x_row)
 
 
 def _recur_workspace(r, backward, device):
@@ -520,17 +520,18 @@ def _new_like(t, shape):
     return torch.empty_like(t) if t.is_contiguous() else t.new_empty(shape)
 
 
-def tl_recur(g, x, off, h0=None, gate=TL_GATE_SIGMOID, h=None, h_last=None, with_last=False, with_tape=False, stream=None):
+def tl_recur(g, x, off, h0=None, gate=TL_GATE_SIGMOID, h=None, h_last=None, with_last=False, with_tape=False, stream=None, spin_limit=0):
     """h_t = f_t h_(t-1) + i_t x_t along the rows of every sentence.  g, x [n, channels]: CUDA tensors of one type (float32, bfloat16, float16)
     with rows any stride apart; off [sentences + 1] int32, from 0 to at most n; h0 [sentences, channels] float32, None: zero.  Returns dict(h,
     h_last with with_last or where one is given, tape with with_tape): h is new unless given (its rows behind the last sentence are left
-    as they were, of a new one undefined), h_last [sentences, channels] float32 may be h0 itself, the tape is for tl_recur_backward."""
+    as they were, of a new one undefined), h_last [sentences, channels] float32 may be h0 itself, the tape is for tl_recur_backward.  spin_limit: most polls of
+    a wait between workgroups (0: default, below 0: none)."""
     import torch
     index = g.get_device()
     if stream is not None or torch._C._cuda_getDevice() != index:
         with _elsewhere(index, stream):
-            return tl_recur(g, x, off, h0, gate, h, h_last, with_last, with_tape)
-    r = _recurrence(g, x, off, gate, index)
+            return tl_recur(g, x, off, h0, gate, h, h_last, with_last, with_tape, None, spin_limit)
+    r = _recurrence(g, x, off, gate, index, spin_limit)
     n, channels = g.shape
     trees, device = off.numel() - 1, g.device
     state = (trees, channels)
@@ -560,15 +561,15 @@ def tl_recur(g, x, off, h0=None, gate=TL_GATE_SIGMOID, h=None, h_last=None, with
     return out
 
 
-def tl_recur_backward(g, x, off, tape, d_h=None, d_last=None, gate=TL_GATE_SIGMOID, stream=None):
+def tl_recur_backward(g, x, off, tape, d_h=None, d_last=None, gate=TL_GATE_SIGMOID, stream=None, spin_limit=0):
     """Gradients of tl_recur for its arguments and its tape: d_h [n, channels] of the type of g, d_last [sentences, channels] float32, None: zero.
     Returns dict(d_g, d_x, d_h0) of new tensors; rows of d_g and d_x behind the last sentence are zero."""
     import torch
     index = g.get_device()
     if stream is not None or torch._C._cuda_getDevice() != index:
         with _elsewhere(index, stream):
-            return tl_recur_backward(g, x, off, tape, d_h, d_last, gate)
-    r = _recurrence(g, x, off, gate, index)
+            return tl_recur_backward(g, x, off, tape, d_h, d_last, gate, None, spin_limit)
+    r = _recurrence(g, x, off, gate, index, spin_limit)
     n, channels = g.shape
     trees, device = off.numel() - 1, g.device
     state = (trees, channels)

@@ -87,6 +87,7 @@ RecurArgs arguments(const tl_recurrence *r, const Plan &p)
     a.slices = p.slices;
     a.slots = p.slots;
     a.shift = p.shift;
+    a.polls = r->spin_limit == 0 || r->spin_limit > REC_POLLS ? REC_POLLS : r->spin_limit > 0 ? r->spin_limit : 0;
     return a;
 }
 

@@ -40,7 +40,7 @@ struct RecurArgs {
     int4 *parts;                                // of every part: its sentence, that one's words, the slot of its first part
     float *copy;                                // of h0, which h_last may be written over
     uint32_t *broken;                           // not 0 once a wait has run out: no other waits as long again
-    int n_trees, n_rows, C, slices, slots, shift;
+    int n_trees, n_rows, C, slices, slots, shift, polls;
 };
 
 // ---- channels of a lane ----------------------------------------------------------------------
@@ -425,7 +425,8 @@ template <typename T, int V, int R, int GATE, bool KEEP> struct RecGates {
 // published as they are, in words that were filled with ones before: a word that is no longer all ones is complete, and no fence is needed.
 // Parts are numbered in the order in which a state passes them.  A workgroup takes the next number of its slice when it starts: the hardware starts them in order within an XCD only, and two
 // launches side by side could else fill one another's units with workgroups that wait for such as find no place.  So what is waited for has been started (a lane that is moved back
-// waits for its own channels alone).  It costs an atomic add's way a workgroup: two sentences of 26 000 words in all 94 us, 91 without.  Every wait ends all the same: after REC_POLLS polls (tenths of a second) the words in question are walked, from the start of the sentence.
+// waits for its own channels alone).  It costs an atomic add's way a workgroup: two sentences of 26 000 words in all 94 us, 91 without.  Every wait ends all the same: after REC_POLLS polls (tenths of a second), or as
+// many as the caller allows, the words in question are walked, from the start of the sentence.
 
 constexpr int REC_GROUP = 32, REC_POLLS = 1 << 16, REC_LINE = 32;
 constexpr uint32_t REC_NAN = 0x7fc00000u;       // published for a NaN that is all ones
@@ -452,8 +453,12 @@ template <int V> __device__ inline void rec_publish(uint32_t *at, const RecLane<
 // Whether the words came.
 template <int V, int N, typename W> __device__ inline bool rec_wait(const RecurArgs &a, W *const (&at)[N], int n, const RecLane<V> &l, W (&v)[N][V])
 {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[k][j] = 0;
 #pragma unroll 1
-    for (int poll = 0; poll < REC_POLLS; ++poll) {
+    for (int poll = 0; poll < a.polls; ++poll) {
         bool there = true;
 #pragma unroll
         for (int k = 0; k < N; ++k)
