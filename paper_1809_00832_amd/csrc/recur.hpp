@@ -39,7 +39,7 @@ struct RecurArgs {
     uint32_t *taken;                            // of every slice, a cache line each: how many of its parts have been started, less one
     int4 *parts;                                // of every part: its sentence, that one's words, the slot of its first part
     float *copy;                                // of h0, which h_last may be written over
-    uint32_t *broken;                           // not 0 once a wait has run out: no other waits as long again
+    uint32_t *broken;                           // not 0 once a wait has run out: no other waits as long again; behind it the polls of a wait (read with them: a scalar register less)
     int n_trees, n_rows, C, slices, slots, shift, polls;
 };
 
@@ -453,13 +453,10 @@ template <int V> __device__ inline void rec_publish(uint32_t *at, const RecLane<
 // Whether the words came.
 template <int V, int N, typename W> __device__ inline bool rec_wait(const RecurArgs &a, W *const (&at)[N], int n, const RecLane<V> &l, W (&v)[N][V])
 {
-#pragma unroll
-    for (int k = 0; k < N; ++k)
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[k][j] = 0;
 #pragma unroll 1
-    for (int poll = 0; poll < a.polls; ++poll) {
+    for (int poll = 1;; ++poll) {
         bool there = true;
+        const uint64_t how = __hip_atomic_load(reinterpret_cast<uint64_t *>(a.broken), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 #pragma unroll
         for (int k = 0; k < N; ++k)
             if (k < n)
@@ -469,8 +466,10 @@ template <int V, int N, typename W> __device__ inline bool rec_wait(const RecurA
                     if (V > 1 && j < l.back) v[k][j] = 0;
                     there = there && v[k][j] != (W)~(W)0;
                 }
-        if (__all(there)) return true;
-        if ((poll & 255) == 255 && __hip_atomic_load(a.broken, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != 0) return false;
+        const int polls = (int)(how >> 32);
+        if (__all(there) && polls > 0) return true;
+        if (poll >= polls) break;
+        if ((poll & 255) == 0 && (uint32_t)how != 0) return false;
         __builtin_amdgcn_s_sleep(1);
     }
     __hip_atomic_store(a.broken, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -586,7 +585,7 @@ __global__ __launch_bounds__(256) void k_recur_prepare(RecurArgs a, long long n_
         const int lo = place(t);
         a.parts[slot] = int4{t, lo, max(place(t + 1), lo), (lo >> a.shift) + t};
     }
-    if (at == 0) *a.broken = 0;
+    if (at < 2) a.broken[at] = at ? (uint32_t)a.polls : 0;
     for (long long i = at; i < n_words; i += step) a.pairs[i] = ~0ull;      // (pairs, and behind them states and numbers of parts)
     if (a.copy)
         for (long long i = at; i < n_copy; i += step) a.copy[i] = a.h0[i];
