@@ -573,7 +573,7 @@ enum tl_gate { TL_GATE_SIGMOID = 0, TL_GATE_GIVEN = 1 };
 typedef struct {
     int dtype;               /* enum tl_dtype: of g, x, h and their gradients                                             */
     int gate;                /* enum tl_gate                                                                              */
-    int n_trees, n_rows;     /* sentences and rows, >= 0; n_rows below 2^31 - 2^16                                        */
+    int n_trees, n_rows;     /* sentences and rows, >= 0; n_rows below 2^31 - 2^16, and 0 where n_trees is                */
     int channels;            /* 1 .. 2^20                                                                                 */
     int spin_limit;          /* 0 = default.  Upper bound of the polls of a wait between workgroups (the default at most); below 0: none  */
     const int32_t *off;      /* [n_trees+1], from 0 to at most n_rows, ascending (equal ones: no words)       DEVICE
