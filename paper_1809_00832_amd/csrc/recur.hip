@@ -35,15 +35,16 @@ struct Plan {
     long long workspace() const { return pairs + states + parts + copy + (cut ? 16 : 0); }
 };
 
-// Whether sentences are cut into parts, by their words on average (the host does not know the lengths, and a batch with one sentence much longer than the
-// others waits for it).  A whole sentence is a chain of blocks, a part waits for others and needs a launch more.  Measured (us, whole / cut, states
-// alone; words x channels, bf16): 25 sentences of 125 x 150 fp32 9.7 / 9.0, 40 of 100 x 512 12.3 / 13.1, 40 of 165 17.5 / 15.3, 60 of 165 18.3 / 19.4, 60 of 400 37 / 29, 100 of 400 46 / 41, 200 of 650
-// 107 / 104, 256 of 750 139 / 150; with gradients 23 / 19, 30.5 / 34.8, 42 / 38, 43 / 44, 86 / 75, 112 / 111, 311 / 305, 409 / 449.
-// Sentences that end within a block, more of them than the chip holds at once, need no registers for the block after it (brief).  Measured (us, with gradients, with
-// those registers / without): 2000 sentences of 15 words x 256 bf16 71 / 49, 1024 of 15 x 256 fp32 42 / 38, 256 of 27 x 512 bf16 29.5 / 30.2.
+// Whether sentences are cut into parts, by their words on average (the host sees no lengths, and a batch with one sentence much longer than the
+// others waits for it).  A whole sentence is a chain of blocks, a part waits for others, for its number, and needs a launch more.  Measured (us, whole / cut, states alone, then gradients
+// less the states; words x channels, bf16): 20 sentences of 165 x 512 15.4 / 12.5, 20.7 / 17.0; 25 of 200 x 150 fp32 13.1 / 10.8, 17.8 / 13.7, of 125 8.8 / 9.6, 10.7 / 11.4; 40 of 165 16.0 / 16.4,
+// 21.9 / 25.6; 40 of 400 32.2 / 24.6, 45.7 / 38.3; 60 of 400 32.6 / 32.9, 46.7 / 48.8; 100 of 400 41.5 / 46.1, 62.0 / 70.1, of 900 88.0 / 84.6, 144 / 151; 200 of 650 107 / 117, 201 / 215.
+// Sentences that end within a block, more of them than the chip holds at once, need no registers for the block after it (brief).  Measured (us, states, then gradients, with
+// those registers / without): 2000 sentences of 15 words x 256 bf16 20.1 / 16.4, 63 / 36; 1024 of 15 x 256 fp32 14.3 / 13.0, 32.6 / 28.0; 256 of 27 x 512 bf16 7.4 / 8.1, 18.4 / 15.4.
 // Large parts have half as many pairs to be taken, small ones fill the chip with fewer words and waste less of a sentence's last part.  Measured (us, large / small, bf16): states
-// of 2 sentences of 13 000 words x 2048 90 / 96, 8 of 1800 x 1024 32 / 35, 2 of 5000 x 2048 44 / 42, 60 of 1000 x 512 62 / 55, 4 of 1500 x 256 17.8 / 13.0; gradients
-// (less the states): 8 of 1800 x 1024 42 / 52, one of 8000 x 1024 32 / 42, one of 4000 x 1024 23 / 26, 4 of 1500 x 256 19 / 16.
+// of 2 sentences of 13 000 words x 2048 99 / 107, 8 of 1800 x 1024 34.5 / 37.0, 2 of 5000 x 2048 47.0 / 48.2, 60 of 1000 x 512 65 / 59, 4 of 1500 x 256 18.2 / 13.7; gradients
+// (less the states): 8 of 1800 x 1024 52 / 57, one of 8000 x 1024 42 / 50, one of 4000 x 1024 25 / 30, 4 of 1500 x 256 20 / 17.
+// (All as graphs of ten calls.)
 bool plan(const tl_recurrence *r, bool back, Plan *p)
 {
     const long long rows = r->n_rows, trees = r->n_trees;
@@ -52,7 +53,7 @@ bool plan(const tl_recurrence *r, bool back, Plan *p)
     if (p->narrow) p->V = 1;
     p->slices = (r->channels + 64 * p->V - 1) / (64 * p->V);
     const long long workgroups = trees * p->slices;
-    p->cut = rows > 96 * trees && 4 * (rows / trees) > 3 * workgroups;
+    p->cut = rows > 96 * trees && rows / trees > 2 * workgroups;
     p->single = !back && !p->cut && rows <= 8 * trees;
     p->brief = !p->cut && rows <= 32 * trees && workgroups >= 1024 && workgroups >= 8 * compute_units();      // (asking for the units takes more than a microsecond)
     p->large = false;
