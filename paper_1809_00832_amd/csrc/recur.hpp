@@ -89,8 +89,8 @@ template <int V> struct RecLane {
     }
 };
 
-// (A gate's exponent is a rounded product, off by 2 |g| 2^-24 of the gate, and the exponential gives no subnormal numbers: a gate below 2^-126 is zero.  What would mend both
-// is four instructions more for each of a part's gates, made twice.)
+// (A gate's exponent is a rounded product, so that the gate is off by 2 |g| 2^-24 of itself, and the exponential gives no subnormal numbers: a gate below 2^-126 is zero.  More of either
+// would take instructions for every gate, which are made twice in parts.)
 template <int GATE> __device__ inline void rec_gates(float g, float &f, float &i)
 {
     if constexpr (GATE == TL_GATE_SIGMOID) {
@@ -114,7 +114,7 @@ template <int GATE> __device__ inline void rec_gates(float g, float &f, float &i
 //   B is NaN        inputs above REC_INPUT or sums above REC_LARGE
 // and then the words are walked whatever the state.  So no state overflows between unless it is told: 2^40 2^16 2^32 at most, and 2^80 2^32 n from the inputs.
 // Chains of runs are joined first and asked about once, by the largest state on the way, and again run by run where that fails.  (Asked about at every joining, two
-// sentences of 26 000 words in all took 101 us; now 91, and 90 without any of this.)
+// sentences of 26 000 words in all took 101 us; 91 so, and 90 without any of this.)
 
 constexpr float REC_LEAST = 0x1p-126f, REC_GROW = 0x1p32f, REC_PREFIX = 0x1p16f, REC_LARGE = 0x1p40f, REC_INPUT = 0x1p80f, REC_RATIO = 0x1p116f;
 
@@ -640,11 +640,11 @@ template <int R, typename F> __device__ __forceinline__ void rec_each_back(int w
 }
 
 // CUT: a part of W R words, else a whole sentence, W R words at a time; AHEAD: the next block's rows are on their way while one is worked on.  Memory bounds long batches
-// (256 sentences of 750 words x 512 bf16: 139 us, 4.2 TB/s; two of 13 000 x 2048: 87, 3.7, the vector unit 53 % busy), a block's chain of offsets, rows, pairs and
+// (256 sentences of 750 words x 512 bf16: 139 us, 4.2 TB/s; two of 13 000 x 2048: 92, 3.5, the vector unit 52 % busy), a block's chain of offsets, rows, pairs and
 // states short ones (256 of 33 x 512 bf16: 10, of which bytes are 5).  A row is read in 4 bytes a lane: 8 take twice the registers and were slower (13 for 11).  In a part the registers hold the words as they were read, which are put through
 // their gates twice, for the pair and for the states: that costs less than the registers of the results, which would halve the waves of a compute unit.
 // ONCE: nothing reads g and x again (there is no tape); a branch on the tape in the kernel would cost what the other loads gain.  Measured (us, two sentences of
-// 26 000 words in all, bf16 x 2048): 97 with ordinary loads, 91 so; a training step of eight of 1 800 words x 1024: 72.5 and 74.
+// 26 000 words in all, bf16 x 2048): 100 with ordinary loads, 94 so; a training step of eight of 1 800 words x 1024: 81.6 and 83.0.
 template <typename T, int V, int W, int R, int GATE, bool CUT, bool ONCE, bool AHEAD> __global__ __launch_bounds__(64 * W) void k_recur(RecurArgs a)
 {
     static_assert(REC_TAPE % R == 0, "states of the tape lie where a wave's words begin");
@@ -771,8 +771,8 @@ template <typename T, int V, int W, int R, int GATE, bool CUT, bool ONCE, bool A
 // ---- gradients -----------------------------------------------------------------------------------
 
 // Blocks from the last one to the first.  A block's words are stepped through from the tape's state first, for what each gate's gradient needs, then backwards.  Bound by memory:
-// 256 sentences of 33 words x 512 fp32 21 us for 85 MB, eight of 1 800 x 1024 bf16 40 for 146 MB (one and a half rounds of workgroups).
-// (Registers: as many as leave a SIMD the waves that it has without the code for what is walked, whose registers would take one of them; fp32 256 x 33 x 512 39 us then for 34.)
+// 256 sentences of 33 words x 512 fp32 21 to 22 us for 85 MB, eight of 1 800 x 1024 bf16 43 for 146 MB (one and a half rounds of workgroups).
+// Registers: as many as leave a SIMD the waves that it would have without the code for words that are walked, which would take one wave's (fp32 256 x 33 x 512, with states: 39 us for 34).
 template <typename T, int V, int W, int R, int GATE, bool CUT, bool AHEAD>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(!AHEAD ? 4 : V == 1 ? 3 : 2))) void k_recur_back(RecurArgs a)
 {
