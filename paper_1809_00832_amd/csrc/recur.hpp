@@ -189,7 +189,7 @@ __device__ __forceinline__ void rec_sound(int words, const float (&f_most)[V], c
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 if (f_most[j] > 1.f && (!(grow[j] <= REC_GROW) || least[j] < REC_LEAST)) A[j] = NAN;
-                if constexpr (D_TOO) D[j] = m[j];
+                if constexpr (D_TOO) D[j] = f_most[j] > 1.f ? m[j] : D[j];
             }
         }
     }

@@ -185,3 +185,28 @@ def test_open_and_closed_gates_of_ordinary_words(L):
     g = torch.rand(L, C, generator=gen, device="cuda") ** 8
     g[torch.rand(L, C, generator=gen, device="cuda") < 0.05] = 0.0
     check(g, x, h0, GIVEN, d_h, d_last)
+
+
+@pytest.mark.parametrize("lengths", [[40] * 30, [700, 900]], ids=["whole", "parts"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_channels_do_not_depend_on_one_another(dtype, lengths):
+    """Gates above one, infinite ones, large states and gradients in some channels: the others keep their bits."""
+    n, C = sum(lengths), 131
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    new = lambda *s, dt=dtype: torch.randn(s, generator=gen, device="cuda", dtype=dt)
+    g, x, d_h = new(n, C).tanh(), new(n, C), new(n, C)
+    h0, d_last = new(len(lengths), C, dt=torch.float32), new(len(lengths), C, dt=torch.float32)
+    off = torch.tensor([0] + lengths, device="cuda").cumsum(0).int()
+
+    def run():
+        out = binding.tl_recur(g, x, off, h0, GIVEN, with_last=True, with_tape=True)
+        return dict(out, **binding.tl_recur_backward(g, x, off, out.pop("tape"), d_h, d_last, GIVEN))
+
+    before = run()
+    g[::3, 4], g[7, 20], g[9, 130], h0[:, 37], d_h[:, 60], x[5, 90] = 1.5, float("inf"), -1e30, 1e20, 1e15, float("nan")
+    after = run()
+    own = torch.ones(C, dtype=torch.bool, device="cuda")
+    own[[4, 20, 130, 37, 60, 90]] = False
+    for k in before:
+        assert torch.equal(before[k][:, own], after[k][:, own]), k
+        assert not torch.equal(before[k][:, 4], after[k][:, 4]), k
