@@ -466,10 +466,10 @@ template <int V, int N, typename W> __device__ inline bool rec_wait(const RecurA
                     if (V > 1 && j < l.back) v[k][j] = 0;
                     there = there && v[k][j] != (W)~(W)0;
                 }
-        const int polls = (int)(how >> 32);
+        const int polls = __builtin_amdgcn_readfirstlane((int)(how >> 32));
         if (__all(there) && polls > 0) return true;
         if (poll >= polls) break;
-        if ((poll & 255) == 0 && (uint32_t)how != 0) return false;
+        if ((poll & 255) == 0 && __builtin_amdgcn_readfirstlane((uint32_t)how) != 0) return false;
         __builtin_amdgcn_s_sleep(1);
     }
     __hip_atomic_store(a.broken, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
