@@ -558,9 +558,9 @@ int tl_sample(int dtype, int n_rows, int vocab, const void *logits, int64_t row,
  *     h_t = f_t h_(t-1) + i_t x_t          h before a sentence's first word: its row of h0
  *     TL_GATE_SIGMOID  f = 1 / (1 + exp(-g)),  i = 1 - f        TL_GATE_GIVEN  f = g,  i = 1
  * States and sums are fp32 whatever the type; h is rounded once, when it is stored.  Words are joined as runs, so that results differ from
- * those of a loop over words in fp32: in their last bits, and by up to 2^-80, which goes on through the gates that follow.  Infinities and NaN appear where that loop has them, also where it
+ * those of a loop over words in fp32: in their last bits, and by up to 2^-120 of the largest state before them, which goes on through the gates that follow.  Infinities and NaN appear where that loop has them, also where it
  * overflows on the way, and reach only later words (gradients: earlier ones) of their channel and sentence.  A sigmoid gate below 2^-126 is zero.  What joining cannot tell is walked word by
- * word, which takes long: channels whose states or incoming gradients are infinite, sigmoid: fade by 2^-116 from above 2^40; TL_GATE_GIVEN: are above 2^40, or have gates
+ * word, which takes long: channels whose states or incoming gradients are infinite, sigmoid: fade by 2^-116 from above 2^60; TL_GATE_GIVEN: are above 2^60, or have gates
  * above one whose products grow beyond 2^16 over some hundred words, or pass through the smallest numbers.  Results repeat bit for bit.
  * Few long sentences are divided among workgroups that wait for one another's results, each only for such as have been started before it, whatever else runs; every
  * wait is bounded (spin_limit; by default some tenths of a second), and a workgroup whose wait runs out computes what it waited for, word by word: such a

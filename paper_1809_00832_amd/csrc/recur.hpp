@@ -107,16 +107,16 @@ template <int GATE> __device__ inline void rec_gates(float g, float &f, float &i
 // ---- what pairs may be trusted with --------------------------------------------------------------
 //
 // A state s goes through a run of n words as A s + B.  That is the loop's result, but for last bits, if nothing overflows between and the product A has its bits.  A product that
-// vanishes, or is subnormal, is off by n 2^-149, and the state by that times s: below 2^-80 for n up to 2^13, states up to REC_LARGE and products of the runs before up to
-// REC_PREFIX.  That much is let go (the loop itself rounds states to 2^-149, and what is lost goes on through the same gates).  Larger states: sigmoid gates enlarge nothing, so that it is
+// vanishes, or is subnormal, is off by n 2^-149, and the state by that times s: 2^-120 of it at most, for n up to 2^13 and products of the runs before up to
+// REC_PREFIX.  That much is let go (what is lost goes on through the same gates) of states up to REC_LARGE.  Larger ones: sigmoid gates enlarge nothing, so that it is
 // in a result's last bits unless the result is 2^-116 of the state; gates of the caller's may, and such a state's words are walked.  A pair says what else it cannot be trusted with:
 //   A is NaN        gates above one enlarge something by more than REC_GROW or REC_PREFIX on the way, or what had vanished (the product is taken in one order, gradients pass in the other)
 //   B is NaN        inputs above REC_INPUT or sums above REC_LARGE
-// and then the words are walked whatever the state.  So no state overflows between unless it is told: 2^40 2^16 2^32 at most, and 2^80 2^32 n from the inputs.
+// and then the words are walked whatever the state.  So no state overflows between unless it is told: 2^60 2^16 2^32 at most, and 2^80 2^32 n from the inputs.
 // Chains of runs are joined first and asked about once, by the largest state on the way, and again run by run where that fails.  (Asked about at every joining, two
 // sentences of 26 000 words in all took 101 us; 91 so, and 90 without any of this.)
 
-constexpr float REC_LEAST = 0x1p-126f, REC_GROW = 0x1p32f, REC_PREFIX = 0x1p16f, REC_LARGE = 0x1p40f, REC_INPUT = 0x1p80f, REC_RATIO = 0x1p116f;
+constexpr float REC_LEAST = 0x1p-126f, REC_GROW = 0x1p32f, REC_PREFIX = 0x1p16f, REC_LARGE = 0x1p60f, REC_INPUT = 0x1p80f, REC_RATIO = 0x1p116f;
 
 // The larger of m and |x|, and of m, |x| and |y|, NaN left out (of which products and sums tell).  By hand: a number as it was read would first be made quiet, an instruction more.
 __device__ inline void rec_largest(float &m, float x) { asm("v_max_f32 %0, |%1|, %0" : "+v"(m) : "v"(x)); }

@@ -1,9 +1,9 @@
 """The recurrence where products of gates leave the range of fp32, or states do on the way: outputs are those of the loop over the words.
 
 The reference is that loop: every word's value is taken in 64 bits (products of fp32 numbers are exact there) and rounded to fp32, subnormal numbers kept, overflow to
-infinity.  Bounds, u = 2^-24: a word is met to 4 u of its magnitude M_t = |f_t| M_(t-1) + |i_t x_t| (sigmoid gates: (2 |g| + 12) u), and to 2^-80: the product of n gates is
-rounded to multiples of 2^-149 where it is subnormal, so that a state s is met to n 2^-149 |s| behind them, with n up to 2^10 gates of parts joined at once, states up to 2^40 and products up to 2^16
-of what was joined before: 2^-83, twice where a wave's own run follows.  So E_t = |f_t| E_(t-1) + d_t M_t + 2^-80.  What goes back likewise.  fp32 throughout, so nothing is rounded to fewer bits.
+infinity.  Bounds, u = 2^-24: a word is met to 4 u of its magnitude M_t = |f_t| M_(t-1) + |i_t x_t| (sigmoid gates: (2 |g| + 12) u), and to 2^-120 of the largest magnitude S_t so far: the
+product of n gates is rounded to multiples of 2^-149 where it is subnormal, so that a state s is met to n 2^-149 |s| behind them, with n up to 2^10 gates of parts joined at once and products up to
+2^16 of what was joined before: 2^-123, and again where a wave's own run follows.  So E_t = |f_t| E_(t-1) + d_t M_t + 2^-120 S_t, and a step of 2^-149 for what is subnormal itself.  What goes back likewise.  fp32 throughout, so nothing is rounded to fewer bits.
 A sigmoid gate below 2^-126 is zero.
 """
 import numpy as np
@@ -16,7 +16,7 @@ pytestmark = pytest.mark.gpu
 
 U = 2.0 ** -24
 SIGMOID, GIVEN = binding.TL_GATE_SIGMOID, binding.TL_GATE_GIVEN
-STEP = 2.0 ** -80
+STEP, LEAST = 2.0 ** -120, 2.0 ** -149
 
 
 def f32(v):
@@ -35,6 +35,7 @@ def loop(g, x, h0, gate, d_h, d_last):
     out = {k: np.zeros((L, C)) for k in ("h", "d_g", "d_x")}
     err, near = {k: np.zeros((L, C)) for k in out}, np.zeros((L, C), dtype=bool)
     h, m, e = h0.copy(), np.abs(h0), np.zeros(C)
+    top = m.copy()
     before, before_m, before_e = np.zeros((L, C)), np.zeros((L, C)), np.zeros((L, C))
     edge = lambda v: (np.abs(v) > 2.0 ** 127.99) & (np.abs(v) < 2.0 ** 128.01)
     for t in range(L):
@@ -43,15 +44,17 @@ def loop(g, x, h0, gate, d_h, d_last):
         near[t] |= edge(wide)
         h = f32(wide)
         m = np.abs(f[t]) * m + np.abs(i[t] * x[t])
-        e = np.abs(f[t]) * e + d[t] * m + STEP
+        top = np.maximum(top, m)
+        e = np.abs(f[t]) * e + d[t] * m + STEP * top + LEAST
         out["h"][t], err["h"][t] = h, e
     back, m, e = d_last.copy(), np.abs(d_last), np.zeros(C)
+    top = m.copy()
     for t in range(L - 1, -1, -1):
         wide = back + d_h[t]
         near[t] |= edge(wide)
         lam, lam_m = f32(wide), m + np.abs(d_h[t])
         lam_e = e + 2 * U * lam_m
-        out["d_x"][t], err["d_x"][t] = f32(lam * i[t]), i[t] * lam_e + (d[t] + 2 * U) * np.abs(i[t]) * lam_m + STEP
+        out["d_x"][t], err["d_x"][t] = f32(lam * i[t]), i[t] * lam_e + (d[t] + 2 * U) * np.abs(i[t]) * lam_m + LEAST
         near[t] |= edge(lam * i[t])
         back = f32(lam * f[t])
         near[t] |= edge(lam * f[t])
@@ -62,8 +65,9 @@ def loop(g, x, h0, gate, d_h, d_last):
             rest, by, own, rest_m = before[t], np.ones(C), lam, before_m[t]
         out["d_g"][t] = f32(own * rest)
         near[t] |= edge(own * rest)
-        err["d_g"][t] = by * (lam_e * np.abs(rest) + lam_m * before_e[t] + (2 * d[t] + 8 * U) * lam_m * rest_m) + STEP * (2 + np.abs(rest) + rest_m)
-        m, e = np.abs(f[t]) * lam_m, np.abs(f[t]) * lam_e + d[t] * np.abs(f[t]) * lam_m + STEP
+        err["d_g"][t] = by * (lam_e * np.abs(rest) + lam_m * before_e[t] + (2 * d[t] + 8 * U) * lam_m * rest_m) + LEAST * (2 + np.abs(rest) + rest_m)
+        top = np.maximum(top, lam_m)
+        m, e = np.abs(f[t]) * lam_m, np.abs(f[t]) * lam_e + d[t] * np.abs(f[t]) * lam_m + STEP * top + LEAST
     out["h_last"], err["h_last"], out["d_h0"], err["d_h0"] = h[None], err["h"][-1:], back[None], e[None]
     near_back = np.flip(np.maximum.accumulate(np.flip(near, 0), 0), 0) | np.maximum.accumulate(near, 0)
     return out, err, near_back
@@ -210,3 +214,18 @@ def test_channels_do_not_depend_on_one_another(dtype, lengths):
     for k in before:
         assert torch.equal(before[k][:, own], after[k][:, own]), k
         assert not torch.equal(before[k][:, 4], after[k][:, 4]), k
+
+
+@pytest.mark.parametrize("L", [100, 900, 5000])
+def test_large_states_and_gradients_of_gates_up_to_one(L):
+    """Sums along the sentence, of numbers far above 2^40, and states that fade from there to ordinary numbers and on."""
+    C = 40
+    gen = torch.Generator(device="cuda").manual_seed(L)
+    new = lambda *s: torch.randn(s, generator=gen, device="cuda")
+    g, x, h0, d_h, d_last = torch.ones(L, C, device="cuda"), new(L, C) * 1e20, new(1, C) * 1e25, new(L, C) * 1e18, new(1, C) * 1e22
+    g[:, 10:20] = 1 - torch.rand(L, 10, generator=gen, device="cuda") ** 3
+    g[:, 20:30] *= -1
+    x[:, 25:], d_h[:, 25:] = 0.0, 0.0
+    g[:, 30:35] = 10.0 ** (-70 / L)
+    g[:, 35:] = torch.rand(L, 5, generator=gen, device="cuda") ** 4
+    check(g, x, h0, GIVEN, d_h, d_last)
